@@ -118,8 +118,8 @@ SQ_API int sq_seq_new(sq_cache *cache, sq_seq *out);
 /* Append n_tokens K/V rows to the end of `seq` (Algorithm 1: C <- C + R,
  * C <- C + O; the aux thread's C_aux <- C + p).
  *   k, v: device, bf16, contiguous [num_layers][n_tokens][num_kv_heads][head_dim]
- *         (keys already rotated: the library never applies positional
- *         encodings).
+ *         (keys already rotated: this call stores what it is given;
+ *         sq_qk_norm_rope_store rotates).
  * If the sequence's last page is partial and shared with another sequence it
  * is first copied (copy-on-write); then fresh pages are taken, lowest free id
  * first, in increasing logical order.  n_tokens == 0 is a no-op.
@@ -352,6 +352,140 @@ SQ_API int sq_stats(sq_cache *cache, sq_stats_t *out);
 SQ_API int sq_decode_attention_noalloc(sq_cache *cache, const sq_seq *seqs, int32_t n_seqs,
                                        int32_t layer, const void *q, void *out,
                                        int32_t out_dtype, float sm_scale, void *stream);
+
+/* ---- norms and rotation of queries and keys; rows stored layer by layer ---- */
+
+/* The norm of every query and key head and the position rotation after it.  For
+ * a row x of head_dim elements with the weights w of its kind,
+ *     y = w * x / sqrt(mean(x^2) + eps),
+ * and each of the rot_dim / 2 pairs (a, b) of y's first rot_dim elements turns:
+ * (a c - b s, b c + a s), c and s = rope[position][pair]. */
+typedef struct {
+    const void *q_weight;    /* device [head_dim], 16-byte aligned; NULL: ones */
+    const void *k_weight;    /* device [head_dim], 16-byte aligned; NULL: ones */
+    const float *rope;       /* device [max_pos][rot_dim / 2][2] (cosine, sine),
+                                16-byte aligned; may be NULL when rot_dim is 0 */
+    int32_t weight_dtype;    /* SQ_OUT_BF16 or SQ_OUT_F32, of both weights */
+    int32_t rot_dim;         /* 0 .. head_dim, a multiple of 16 */
+    int32_t interleaved;     /* 0: pairs (e, e + rot_dim / 2); 1: (2e, 2e + 1) */
+    int32_t max_pos;         /* rows of the table, >= 1 when rot_dim > 0 */
+    float eps;               /* finite, >= 0 */
+} sq_norm_rope;
+
+/* Lengthen n_seqs sequences by n_new[i] rows each (n_new NULL: by one), whose
+ * keys and values come later, layer by layer: a model has a layer's K/V only
+ * when it reaches that layer.  Page rules as sq_append_kv, sequence by sequence
+ * in the order given (a shared partial last page is copied, then fresh pages are
+ * taken); all or nothing.  The new rows hold whatever their slots held until
+ * sq_qk_norm_rope_store (or the caller, through sq_pool_ptr) writes them.
+ *   seqs: host, distinct live handles; n_new: host, >= 0
+ * Errors: BAD_HANDLE, INVALID_ARG, NO_PAGES, CAPACITY, CUDA. */
+SQ_API int sq_extend(sq_cache *cache, const sq_seq *seqs, int32_t n_seqs, const int32_t *n_new,
+                     void *stream);
+
+/* Norm and rotate the queries and keys of the newest n_new[i] rows (NULL: one)
+ * of each sequence at one layer, and store the keys, with the values as they
+ * are, into the cache: row j of the call is the j-th of the sequences' newest
+ * rows, sequence after sequence.  The rows are there already (sq_extend); a
+ * second store overwrites the first.
+ *   q, k, v: device bf16, rows [num_q_heads][head_dim] and [num_kv_heads][head_dim],
+ *            16-byte aligned, q_stride .. v_stride elements from token to token
+ *            (multiples of 8, at least a row): parts of one fused projection do
+ *   positions: device int32 [rows], 4-byte aligned; NULL: the sequence's own
+ *            (sq_seq_next_pos less its distance from the end).  One outside the
+ *            table is a device-side error (SQ_ERR_DEVICE at sq_sync_status; the
+ *            row is written as if at position 0)
+ *   q_out:   device bf16 [rows][num_q_heads][head_dim], 16-byte aligned, as the
+ *            attention calls take it; overlaps none of q, k, v (INVALID_ARG)
+ * Sums are fp32; outputs are rounded once, to nearest even.  Rows in a page that
+ * another sequence holds too are INVALID_ARG (its rows would change with them).
+ * Errors: BAD_HANDLE, INVALID_ARG, UNSUPPORTED, NO_MEMORY, CUDA. */
+SQ_API int sq_qk_norm_rope_store(sq_cache *cache, const sq_seq *seqs, int32_t n_seqs,
+                                 const int32_t *n_new, int32_t layer, const void *q,
+                                 int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                                 int64_t v_stride, const int32_t *positions,
+                                 const sq_norm_rope *params, void *q_out, void *stream);
+
+/* The same norms and rotation of n_tokens tokens, into tensors: q_out [n_tokens]
+ * [num_q_heads][head_dim], k_out [n_tokens][num_kv_heads][head_dim] (bf16, 16-byte
+ * aligned, overlapping neither each other nor q or k).  positions may be NULL
+ * only when rot_dim is 0.  The cache lends its geometry and error word; its
+ * sequences are not touched.  n_tokens == 0 is a no-op.
+ * Errors: BAD_HANDLE, INVALID_ARG, UNSUPPORTED, CUDA. */
+SQ_API int sq_qk_norm_rope(sq_cache *cache, int32_t n_tokens, const void *q, int64_t q_stride,
+                           const void *k, int64_t k_stride, const int32_t *positions,
+                           const sq_norm_rope *params, void *q_out, void *k_out, void *stream);
+
+/* Its gradients: from dq_out and dk_out (of the outputs; bf16, contiguous) those
+ * of the inputs, dq and dk (bf16, rows dq_stride and dk_stride elements apart,
+ * rounded once), and of the weights, dq_weight and dk_weight (fp32 [head_dim],
+ * 4-byte aligned, sums over tokens and heads in a fixed order; NULL: not
+ * wanted).  The gradients overlap no input and not each other (INVALID_ARG).
+ * n_tokens == 0 zeroes the weights' gradients.
+ * Errors: BAD_HANDLE, INVALID_ARG, UNSUPPORTED, NO_MEMORY, CUDA. */
+SQ_API int sq_qk_norm_rope_backward(sq_cache *cache, int32_t n_tokens, const void *q,
+                                    int64_t q_stride, const void *k, int64_t k_stride,
+                                    const int32_t *positions, const sq_norm_rope *params,
+                                    const void *dq_out, const void *dk_out, void *dq,
+                                    int64_t dq_stride, void *dk, int64_t dk_stride,
+                                    float *dq_weight, float *dk_weight, void *stream);
+
+/* ---- attention of query blocks: sliding windows, sinks, drafted trees ---- */
+
+/* Attention of the newest n_q[i] tokens (NULL: one) of each of n_seqs sequences
+ * at one layer, each query at most `window` tokens wide: the query of row p (of
+ * the rows that the sequence holds now, 0 first) sees the rows j <= p with
+ *     j > p - window  (itself and the window - 1 before it), or
+ *     j < n_sink      (the first rows: sinks, which stay visible).
+ * window 0: no limit (plain causal attention).  With GQA as in
+ * sq_prefill_attention; one call serves single tokens of a batch, whole prompts,
+ * and both together.
+ *   seqs: host, distinct live handles; n_q: host, 0 .. the sequence's rows
+ *   q:    device bf16 [sum of n_q][num_q_heads][head_dim], 16-byte aligned: the
+ *         queries of one sequence after the other's
+ *   out:  device, like q, bf16 or fp32 (out_dtype); lse: NULL or device float
+ *         [sum of n_q][num_q_heads], as in sq_prefill_attention; q, out and lse
+ *         overlap nowhere (INVALID_ARG)
+ *   sm_scale: finite, >= 0; window, n_sink >= 0
+ * Rows of partial pages (sq_evict_spans_ragged) are counted as the rows they are.
+ * Only the 64-row runs of pages that some query sees a row of are read; the rows
+ * in those that a query does not see must be finite, as rows stored once are
+ * (their weights are zero), while slots past a sequence's end may hold anything.
+ * Weights and normaliser are rounded as in sq_prefill_attention, whose limits on
+ * library memory for partial results hold too.  A plan of more than 2^24 key
+ * tiles (all queries of the call together) is refused.
+ * Errors: BAD_HANDLE, INVALID_ARG, CAPACITY, UNSUPPORTED, NO_MEMORY, CUDA. */
+SQ_API int sq_window_attention(sq_cache *cache, const sq_seq *seqs, int32_t n_seqs,
+                               const int32_t *n_q, int32_t layer, const void *q, void *out,
+                               int32_t out_dtype, float *lse, float sm_scale, int32_t window,
+                               int32_t n_sink, void *stream);
+
+/* Drafted tokens one sequence may have in a sq_tree_attention call. */
+#define SQ_MAX_DRAFT 256
+
+/* Attention of trees of drafted tokens (verification of speculative decoding):
+ * the newest n_draft[i] rows of sequence i are a tree over the rows before them,
+ * its context.  A drafted token sees the context, its ancestors and itself.
+ *   parents: host int32 [sum of n_draft]: the index in its sequence's tree of
+ *            each token's parent, less than its own; -1: the context's last row
+ * The token's position is the context's length plus its number of ancestors;
+ * with window > 0 it sees, of those rows, the ones whose positions are above its
+ * own less the window, or below n_sink.  n_draft[i] is 0 .. SQ_MAX_DRAFT.  The
+ * drafted rows lie in consecutive slots (true for rows added after the last
+ * ragged eviction), else UNSUPPORTED.  Everything else as sq_window_attention.
+ * Errors: BAD_HANDLE, INVALID_ARG, CAPACITY, UNSUPPORTED, NO_MEMORY, CUDA. */
+SQ_API int sq_tree_attention(sq_cache *cache, const sq_seq *seqs, int32_t n_seqs,
+                             const int32_t *n_draft, const int32_t *parents, int32_t layer,
+                             const void *q, void *out, int32_t out_dtype, float *lse,
+                             float sm_scale, int32_t window, int32_t n_sink, void *stream);
+
+/* After verification: of the newest n_draft rows of `seq` those with the indices
+ * path[0] < path[1] < ... (a path of the tree from its root, n_path of them, 0:
+ * none) stay, in order, and the others leave, as by sq_evict_spans_ragged, but
+ * sq_seq_next_pos goes back by as many: their positions are handed out again.
+ * Errors: BAD_HANDLE, INVALID_ARG, NO_PAGES, NO_MEMORY, CUDA. */
+SQ_API int sq_accept_draft(sq_cache *cache, sq_seq seq, int32_t n_draft, const int32_t *path,
+                           int32_t n_path, void *stream);
 
 /* Measurement helper: streams `bytes` (a multiple of 16, 16-byte aligned)
  * of device memory at `buf` once with plain loads and no writes, so that the

@@ -34,6 +34,7 @@ SQ_ERR_NO_MEMORY = -9
 SQ_OUT_BF16 = 0
 SQ_OUT_F32 = 1
 SQ_DEBUG_DROP_DECODE_STAGE = 1
+SQ_MAX_DRAFT = 256
 
 
 class sq_config(ctypes.Structure):
@@ -53,6 +54,19 @@ class sq_config(ctypes.Structure):
 
 class sq_span(ctypes.Structure):
     _fields_ = [("start", ctypes.c_int32), ("end", ctypes.c_int32)]
+
+
+class sq_norm_rope(ctypes.Structure):
+    _fields_ = [
+        ("q_weight", ctypes.c_void_p),
+        ("k_weight", ctypes.c_void_p),
+        ("rope", ctypes.c_void_p),
+        ("weight_dtype", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("max_pos", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+    ]
 
 
 class sq_stats_t(ctypes.Structure):
@@ -77,7 +91,9 @@ _lock = threading.Lock()
 
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
+_I64 = ctypes.c_int64
 _I32P = ctypes.POINTER(ctypes.c_int32)
+_F32 = ctypes.c_float
 _SIGS = {
     "sq_pool_bytes": (ctypes.c_size_t, [ctypes.POINTER(sq_config)]),
     "sq_cache_create": (ctypes.c_int, [ctypes.POINTER(sq_config), ctypes.POINTER(_P)]),
@@ -106,6 +122,17 @@ _SIGS = {
     "sq_debug_set": (ctypes.c_int, [_P, _I32]),
     "sq_decode_attention_noalloc": (ctypes.c_int, [_P, _I32P, _I32, _I32, _P, _P, _I32,
                                                    ctypes.c_float, _P]),
+    "sq_extend": (ctypes.c_int, [_P, _P, _I32, _P, _P]),
+    "sq_qk_norm_rope_store": (ctypes.c_int, [_P, _P, _I32, _P, _I32, _P, _I64, _P, _I64, _P, _I64,
+                                             _P, _P, _P, _P]),
+    "sq_qk_norm_rope": (ctypes.c_int, [_P, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _P]),
+    "sq_qk_norm_rope_backward": (ctypes.c_int, [_P, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _P,
+                                                _I64, _P, _I64, _P, _P, _P]),
+    "sq_window_attention": (ctypes.c_int, [_P, _P, _I32, _P, _I32, _P, _P, _I32, _P, _F32, _I32,
+                                           _I32, _P]),
+    "sq_tree_attention": (ctypes.c_int, [_P, _P, _I32, _P, _P, _I32, _P, _P, _I32, _P, _F32, _I32,
+                                         _I32, _P]),
+    "sq_accept_draft": (ctypes.c_int, [_P, _I32, _I32, _P, _I32, _P]),
 }
 
 
@@ -193,6 +220,83 @@ def _spans(spans):
     return buf.buffer_info()[0], buf
 
 
+def _ints(x):
+    """(address, what keeps it alive) of host int32 values: a sequence of them,
+    an int32 buffer (array.array, numpy) or a ctypes array; None stays None."""
+    if x is None:
+        return None, None
+    if isinstance(x, ctypes.Array):
+        return ctypes.addressof(x), x
+    if not (isinstance(x, array.array) and x.itemsize == 4):
+        x = array.array("i", x)
+    return x.buffer_info()[0], x
+
+
+def _rows(x, heads, dim, name):
+    """(address, elements between tokens) of a [tokens, heads, dim] tensor whose
+    rows are contiguous; an address alone stands for a contiguous one."""
+    if isinstance(x, int):
+        return x, heads * dim
+    if x.dim() != 3 or x.shape[1:] != (heads, dim):
+        raise ValueError(f"{name}: [tokens, {heads}, {dim}] expected, not {list(x.shape)}")
+    if x.stride(2) != 1 or x.stride(1) != dim:
+        raise ValueError(f"{name}: the rows of a token must be contiguous")
+    _dtype(x, "bfloat16", name)
+    # (one token has no distance to the next)
+    return int(x.data_ptr()), max(x.stride(0), heads * dim) if x.shape[0] > 1 else heads * dim
+
+
+def _dtype(x, want, name):
+    got = str(x.dtype).rpartition(".")[2]
+    if got != want:
+        raise ValueError(f"{name}: {want} expected, not {got}")
+
+
+def _flat(x, want, count, name):
+    """Address of a contiguous tensor of `count` elements (None and addresses as
+    they are)."""
+    if x is None or isinstance(x, int):
+        return x
+    _dtype(x, want, name)
+    if not x.is_contiguous() or x.numel() != count:
+        raise ValueError(f"{name}: {count} contiguous elements expected, not {list(x.shape)}")
+    return int(x.data_ptr())
+
+
+def norm_rope(rope=None, rot_dim=0, eps=1e-6, q_weight=None, k_weight=None,
+              interleaved=False) -> sq_norm_rope:
+    """The parameters of the norms and the rotation: `rope` a float32 CUDA tensor
+    [max_pos, rot_dim / 2, 2] of cosines and sines (rope_table makes one),
+    weights bfloat16 or float32 tensors [head_dim] of one type, or None (ones)."""
+    weights = [w for w in (q_weight, k_weight) if w is not None]
+    f32 = [str(w.dtype).endswith("float32") for w in weights]
+    for w, single in zip(weights, f32):
+        if not single:
+            _dtype(w, "bfloat16", "weight")
+        if not w.is_contiguous():
+            raise ValueError("weight: not contiguous")
+    if len(set(f32)) > 1:
+        raise ValueError("weights: both bfloat16 or both float32")
+    max_pos = 0
+    if rope is not None and rot_dim:
+        max_pos = rope.shape[0]
+        _flat(rope, "float32", max_pos * rot_dim, "rope")
+    p = sq_norm_rope(_ptr(q_weight), _ptr(k_weight), _ptr(rope) if max_pos else None,
+                     SQ_OUT_F32 if f32 and f32[0] else SQ_OUT_BF16, rot_dim, int(interleaved),
+                     max_pos, eps)
+    p._keep = (rope, q_weight, k_weight)
+    return p
+
+
+def rope_table(max_pos, rot_dim, theta=10000.0, device="cuda"):
+    """Cosines and sines of position x theta^(-2 i / rot_dim), float32 [max_pos,
+    rot_dim / 2, 2] (angles in 64 bits)."""
+    import torch
+    inv = theta ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64, device=device) / rot_dim)
+    angle = torch.arange(max_pos, dtype=torch.float64, device=device)[:, None] * inv
+    return torch.stack([angle.cos(), angle.sin()], -1).float().contiguous()
+
+
 # ---- the C calls ------------------------------------------------------------
 def make_config(num_layers, num_q_heads, num_kv_heads, head_dim, page_size, num_pages,
                 max_seqs=64, max_pages_per_seq=None, kv_pool=None, decode_ctas=0) -> sq_config:
@@ -277,6 +381,68 @@ def sq_prefill_attention(cache: int, seq: int, layer: int, n_q: int, q, out,
                                       _ptr(lse), float(sm_scale), arr, len(spans),
                                       _stream(stream)),
            "sq_prefill_attention")
+
+
+def sq_extend(cache: int, seqs, n_new=None, stream=None) -> None:
+    """Lengthen sequences by n_new[i] rows (None: one each) stored later."""
+    arr, _keep = _ints(seqs)
+    cnt, _keep2 = _ints(n_new)
+    _check(lib().sq_extend(cache, arr, len(seqs), cnt, _stream(stream)), "sq_extend")
+
+
+def sq_qk_norm_rope_store(cache: int, seqs, n_new, layer: int, q, q_stride, k, k_stride, v, v_stride,
+                          positions, params: sq_norm_rope, q_out, stream=None) -> None:
+    arr, _keep = _ints(seqs)
+    cnt, _keep2 = _ints(n_new)
+    _check(lib().sq_qk_norm_rope_store(cache, arr, len(seqs), cnt, layer, _ptr(q), q_stride, _ptr(k),
+                                       k_stride, _ptr(v), v_stride, _ptr(positions),
+                                       ctypes.addressof(params), _ptr(q_out), _stream(stream)),
+           "sq_qk_norm_rope_store")
+
+
+def sq_qk_norm_rope(cache: int, n_tokens: int, q, q_stride, k, k_stride, positions,
+                    params: sq_norm_rope, q_out, k_out, stream=None) -> None:
+    _check(lib().sq_qk_norm_rope(cache, n_tokens, _ptr(q), q_stride, _ptr(k), k_stride,
+                                 _ptr(positions), ctypes.addressof(params), _ptr(q_out), _ptr(k_out),
+                                 _stream(stream)), "sq_qk_norm_rope")
+
+
+def sq_qk_norm_rope_backward(cache: int, n_tokens: int, q, q_stride, k, k_stride, positions,
+                             params: sq_norm_rope, dq_out, dk_out, dq, dq_stride, dk, dk_stride,
+                             dq_weight=None, dk_weight=None, stream=None) -> None:
+    _check(lib().sq_qk_norm_rope_backward(cache, n_tokens, _ptr(q), q_stride, _ptr(k), k_stride,
+                                          _ptr(positions), ctypes.addressof(params), _ptr(dq_out),
+                                          _ptr(dk_out), _ptr(dq), dq_stride, _ptr(dk), dk_stride,
+                                          _ptr(dq_weight), _ptr(dk_weight), _stream(stream)),
+           "sq_qk_norm_rope_backward")
+
+
+def sq_window_attention(cache: int, seqs, n_q, layer: int, q, out, window: int, n_sink: int = 0,
+                        out_dtype: int = SQ_OUT_BF16, lse=None, sm_scale: float = 1.0,
+                        stream=None) -> None:
+    arr, _keep = _ints(seqs)
+    cnt, _keep2 = _ints(n_q)
+    _check(lib().sq_window_attention(cache, arr, len(seqs), cnt, layer, _ptr(q), _ptr(out), out_dtype,
+                                     _ptr(lse), float(sm_scale), window, n_sink, _stream(stream)),
+           "sq_window_attention")
+
+
+def sq_tree_attention(cache: int, seqs, n_draft, parents, layer: int, q, out, window: int = 0,
+                      n_sink: int = 0, out_dtype: int = SQ_OUT_BF16, lse=None, sm_scale: float = 1.0,
+                      stream=None) -> None:
+    arr, _keep = _ints(seqs)
+    cnt, _keep2 = _ints(n_draft)
+    par, _keep3 = _ints(parents)
+    _check(lib().sq_tree_attention(cache, arr, len(seqs), cnt, par, layer, _ptr(q), _ptr(out),
+                                   out_dtype, _ptr(lse), float(sm_scale), window, n_sink,
+                                   _stream(stream)),
+           "sq_tree_attention")
+
+
+def sq_accept_draft(cache: int, seq: int, n_draft: int, path, stream=None) -> None:
+    arr, _keep = _ints(path)
+    _check(lib().sq_accept_draft(cache, seq, n_draft, arr, len(path), _stream(stream)),
+           "sq_accept_draft")
 
 
 def sq_release(cache: int, seq: int, stream=None) -> None:
@@ -403,6 +569,80 @@ class Cache:
                          sm_scale=1.0, spans=(), stream=None:
                          sq_prefill_attention(self.handle, seq, layer, n_q, q, out, out_dtype, lse,
                                               sm_scale, spans, stream))
+    def _counted(self, seqs, counts, n, what):
+        """The call's rows per sequence add up to the tensors' tokens."""
+        total = len(seqs) if counts is None else sum(counts)
+        if counts is not None and len(counts) != len(seqs):
+            raise ValueError(f"{what}: {len(counts)} counts for {len(seqs)} sequences")
+        if n is not None and n != total:
+            raise ValueError(f"{what}: {n} tokens given, {total} counted")
+        return total
+
+    extend = lambda self, seqs, n_new=None, stream=None: sq_extend(self.handle, seqs, n_new, stream)
+
+    def qk_norm_rope_store(self, seqs, n_new, layer, q, k, v, positions, params, q_out, stream=None):
+        """q [tokens, Hq, D], k and v [tokens, Hkv, D] (parts of a fused projection
+        do) of the sequences' newest rows: queries normed and rotated into q_out,
+        keys into the cache with the values."""
+        n = self._counted(seqs, n_new, getattr(q, "shape", (None,))[0], "qk_norm_rope_store")
+        q, qs = _rows(q, self.Hq, self.D, "q")
+        k, ks = self._kv(k, n, "k")
+        v, vs = self._kv(v, n, "v")
+        sq_qk_norm_rope_store(self.handle, seqs, n_new, layer, q, qs, k, ks, v, vs,
+                              _flat(positions, "int32", n, "positions"), params,
+                              _flat(q_out, "bfloat16", n * self.Hq * self.D, "q_out"), stream)
+
+    def _kv(self, x, n, name):
+        if not isinstance(x, int) and x.shape[0] != n:
+            raise ValueError(f"{name}: {n} tokens expected, not {x.shape[0]}")
+        return _rows(x, self.Hkv, self.D, name)
+
+    def qk_norm_rope(self, q, k, positions, params, q_out, k_out, stream=None):
+        """Norms and rotation of q [tokens, Hq, D] and k [tokens, Hkv, D] into tensors."""
+        n = q.shape[0]
+        q, qs = _rows(q, self.Hq, self.D, "q")
+        k, ks = self._kv(k, n, "k")
+        sq_qk_norm_rope(self.handle, n, q, qs, k, ks, _flat(positions, "int32", n, "positions"), params,
+                        _flat(q_out, "bfloat16", n * self.Hq * self.D, "q_out"),
+                        _flat(k_out, "bfloat16", n * self.Hkv * self.D, "k_out"), stream)
+
+    def qk_norm_rope_backward(self, q, k, positions, params, dq_out, dk_out, dq, dk, dq_weight=None,
+                              dk_weight=None, stream=None):
+        """Gradients of qk_norm_rope: dq and dk (rows apart as they are) and, where
+        wanted, the weights' (float32)."""
+        n = q.shape[0]
+        q, qs = _rows(q, self.Hq, self.D, "q")
+        k, ks = self._kv(k, n, "k")
+        if not isinstance(dq, int) and dq.shape[0] != n:
+            raise ValueError(f"dq: {n} tokens expected, not {dq.shape[0]}")
+        dq, dqs = _rows(dq, self.Hq, self.D, "dq")
+        dk, dks = self._kv(dk, n, "dk")
+        sq_qk_norm_rope_backward(self.handle, n, q, qs, k, ks, _flat(positions, "int32", n, "positions"),
+                                 params, _flat(dq_out, "bfloat16", n * self.Hq * self.D, "dq_out"),
+                                 _flat(dk_out, "bfloat16", n * self.Hkv * self.D, "dk_out"), dq, dqs,
+                                 dk, dks, _flat(dq_weight, "float32", self.D, "dq_weight"),
+                                 _flat(dk_weight, "float32", self.D, "dk_weight"), stream)
+
+    def window_attention(self, seqs, n_q, layer, q, out, window, n_sink=0, out_dtype=SQ_OUT_BF16,
+                         lse=None, sm_scale=1.0, stream=None):
+        """Attention of the newest n_q[i] tokens (None: one) of each sequence, each
+        seeing its last `window` tokens and the first n_sink."""
+        self._counted(seqs, n_q, getattr(q, "shape", (None,))[0], "window_attention")
+        sq_window_attention(self.handle, seqs, n_q, layer, q, out, window, n_sink, out_dtype, lse,
+                            sm_scale, stream)
+
+    def tree_attention(self, seqs, n_draft, parents, layer, q, out, window=0, n_sink=0,
+                       out_dtype=SQ_OUT_BF16, lse=None, sm_scale=1.0, stream=None):
+        """Attention of trees of drafted tokens, each sequence's newest n_draft[i]
+        rows; parents: every drafted token's parent in its tree, -1 the context."""
+        n = self._counted(seqs, n_draft, getattr(q, "shape", (None,))[0], "tree_attention")
+        if len(parents) != n:
+            raise ValueError(f"tree_attention: {len(parents)} parents of {n} drafted tokens")
+        sq_tree_attention(self.handle, seqs, n_draft, parents, layer, q, out, window, n_sink, out_dtype,
+                          lse, sm_scale, stream)
+
+    accept_draft = (lambda self, seq, n_draft, path, stream=None:
+                    sq_accept_draft(self.handle, seq, n_draft, path, stream))
     release = lambda self, seq, stream=None: sq_release(self.handle, seq, stream)
     seq_info = lambda self, seq: sq_seq_info(self.handle, seq)
     next_pos = lambda self, seq: sq_seq_next_pos(self.handle, seq)

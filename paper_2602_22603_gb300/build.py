@@ -23,15 +23,17 @@ NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-use_fast_math", "-Xcompiler", 
               "-Xcompiler", "-fvisibility=hidden", "-I" + INCLUDE]
 
 LIBSQ_SOURCES = [
+    "kernels/blocks.cu",
     "kernels/decode.cu",
     "kernels/kv.cu",
     "kernels/noalloc_scratch.cu",
+    "kernels/norm_rope.cu",
     "kernels/prefill.cu",
     "kernels/probe.cu",
     "host/core.cpp",
     "api/sq_api.cpp",
 ]
-HOST_SOURCES = ["host/core.cpp", "api/host_test_api.cpp"]
+HOST_SOURCES = ["host/core.cpp", "api/host_test_api.cpp", "api/host_test_operators.cpp"]
 
 LIBSQ = os.path.join(OUT, "libsq.so")
 LIBSQ_HOST = os.path.join(OUT, "libsq_host.so")
@@ -48,7 +50,7 @@ def _all_sources():
     out = []
     for d, _, files in os.walk(CSRC):
         for f in files:
-            if f.endswith((".cu", ".cuh", ".cpp", ".hpp", ".h")):
+            if f.endswith((".cu", ".cuh", ".cpp", ".hpp", ".h", ".inl")):
                 out.append(os.path.join(d, f))
     out.append(os.path.join(INCLUDE, "sq.h"))
     return out

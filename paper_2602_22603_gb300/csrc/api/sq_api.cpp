@@ -14,12 +14,15 @@
 #include <deque>
 #include <memory>
 #include <new>
+#include <stdexcept>
 #include <unordered_map>
 #include <vector>
 
+#include "../host/blocks.hpp"
 #include "../host/core.hpp"
 #include "../kernels/launch.hpp"
 #include "../kernels/noalloc.hpp"
+#include "../kernels/operators.hpp"
 
 using namespace sq;
 
@@ -91,6 +94,39 @@ struct PrefillPlanEntry {
     uint64_t last_use = 0;
 };
 
+// Plans of attention for query blocks, reused while the sequences' versions, the
+// query counts, the trees and the window stay the same: the layers of one kind
+// share one plan (a model with windowed and full layers has two).
+constexpr int kBlockPlanEntries = 4;
+struct BlockPlanEntry : PrefillPlanEntry {
+    bool tree = false;
+    std::vector<int32_t> call;   // window, sinks, query counts, parents
+    std::vector<int32_t> handles;
+    std::vector<uint64_t> versions;
+    size_t o_rows = 0, o_bits = 0;  // (o_rows 0: no table)
+    int32_t n_words = 0, unit_rows = 0;
+    bool one = false;
+};
+
+// A device buffer that calls on any stream take turns with.
+struct TurnBuffer {
+    uint8_t* d = nullptr;
+    size_t cap = 0;
+    cudaEvent_t ev = nullptr;   // recorded after the last work that used it
+    bool ev_recorded = false;
+    cudaStream_t ev_stream = nullptr;
+};
+
+// The places of a store's rows, kept for the same rows at the next layer.
+constexpr int kStorePlanEntries = 2;
+struct StorePlanEntry {
+    bool valid = false;
+    std::vector<int32_t> handles, counts;
+    std::vector<uint64_t> versions;
+    TurnBuffer buf;
+    uint64_t last_use = 0;
+};
+
 struct UploadSlot {
     uint8_t* d = nullptr;
     size_t cap = 0;
@@ -149,6 +185,9 @@ struct sq_cache {
     PrefillPlanEntry* pre_last = nullptr;
     PlanEntry plans[kPlanCacheEntries];
     PrefillPlanEntry pre_plans[kPrefillPlanEntries];
+    BlockPlanEntry block_plans[kBlockPlanEntries];
+    StorePlanEntry store_plans[kStorePlanEntries];
+    TurnBuffer norm_part;  // partial gradients of the norms' weights
     uint64_t use_clock = 0;
     UploadSlot slots[kUploadSlots];
     int next_slot = 0;
@@ -175,6 +214,11 @@ struct sq_cache {
     // is known complete.
     uint64_t write_seq = 0, write_done = 0;
     bool early_ok = true;
+    // the newest store of rows already counted (sq_qk_norm_rope_store), which
+    // changes no version: its pages and ticket, and the newest ticket of the
+    // stores before it to other pages
+    std::vector<int32_t> store_pages;
+    uint64_t store_ticket = 0, store_rest = 0;
     std::vector<uint64_t> page_ticket;
     std::deque<std::pair<uint64_t, cudaEvent_t>> write_pending;
     std::vector<cudaEvent_t> write_events;  // recycled
@@ -231,6 +275,20 @@ int make_tensor_map(sq_cache* c) {
                         estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? SQ_OK : SQ_ERR_UNSUPPORTED;
+}
+
+// Queries {D, Hq, n_q}: one box is the G heads of a KV head x BP positions.
+int make_query_map(sq_cache* c, const void* q, int32_t n_q, int32_t BP, CUtensorMap* qmap) {
+    const Geometry& g = c->g;
+    auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(c->encode_fn);
+    cuuint64_t dims[3] = {(cuuint64_t)g.D, (cuuint64_t)g.Hq, (cuuint64_t)n_q};
+    cuuint64_t strides[2] = {(cuuint64_t)g.D * 2, (cuuint64_t)g.Hq * g.D * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)g.G(), (cuuint32_t)BP};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = encode(qmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box,
+                        estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SQ_OK : SQ_ERR_INVALID_ARG;
 }
 
 // Before `stream` writes pages taken from the free list, wait for the work
@@ -348,7 +406,11 @@ bool early_writes(sq_cache* c, const WriteTickets& w, int32_t* unsafe, int32_t* 
     *n_unsafe = 0;
     if (!c->early_ok) return false;
     poll_writes(c);
-    if (w.rest > c->write_done) return false;
+    if (w.rest > c->write_done || c->store_rest > c->write_done) return false;
+    if (c->store_ticket > c->write_done) {
+        if (c->store_pages.size() + w.top.size() > (size_t)kMaxUnsafe) return false;
+        for (int32_t p : c->store_pages) unsafe[(*n_unsafe)++] = p;
+    }
     for (const auto& tp : w.top)
         if (tp.first > c->write_done) unsafe[(*n_unsafe)++] = tp.second;
     return true;
@@ -440,6 +502,8 @@ int reserve_parts(sq_cache* c, size_t need) {
         c->pre_part = nullptr;
         for (auto& p : c->pre_plans)
             if (p.n_parts > 0) p.valid = false;
+        for (auto& p : c->block_plans)
+            if (p.n_parts > 0) p.valid = false;
         return cuda_status(e);
     }
     c->pre_part_cap = cap;
@@ -518,6 +582,10 @@ int sq_cache_create(const sq_config* cfg, sq_cache** out) {
     if (e != cudaSuccess) return cuda_status(e);
     e = prefill_prepare(g.D);
     if (e != cudaSuccess) return cuda_status(e);
+    if (blocks_prepare) {
+        e = blocks_prepare(g.D);
+        if (e != cudaSuccess) return cuda_status(e);
+    }
     choose_evict_shape(c.get());
     c->pool_bytes = pool_bytes_of(g);
     if (cfg->kv_pool) {
@@ -604,6 +672,16 @@ int sq_cache_destroy(sq_cache* c) {
         if (p.d) cudaFree(p.d);
         if (p.ev) cudaEventDestroy(p.ev);
     }
+    for (auto& p : c->block_plans) {
+        if (p.d) cudaFree(p.d);
+        if (p.ev) cudaEventDestroy(p.ev);
+    }
+    for (auto& p : c->store_plans) {
+        if (p.buf.d) cudaFree(p.buf.d);
+        if (p.buf.ev) cudaEventDestroy(p.buf.ev);
+    }
+    if (c->norm_part.d) cudaFree(c->norm_part.d);
+    if (c->norm_part.ev) cudaEventDestroy(c->norm_part.ev);
     for (auto& s : c->slots) {
         if (s.d) cudaFree(s.d);
         if (s.ev) cudaEventDestroy(s.ev);
@@ -1325,19 +1403,10 @@ int sq_prefill_attention(sq_cache* c, sq_seq seq, int32_t layer, int32_t n_q, co
         }
         c->pre_last = hit;  // (its event is recorded whatever becomes of the call)
     }
-    // queries: {D, Hq, n_q}, one box = the G heads of a KV head x BP positions
     CUtensorMap qmap;
     {
-        auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(c->encode_fn);
-        cuuint64_t dims[3] = {(cuuint64_t)g.D, (cuuint64_t)g.Hq, (cuuint64_t)n_q};
-        cuuint64_t strides[2] = {(cuuint64_t)g.D * 2, (cuuint64_t)g.Hq * g.D * 2};
-        cuuint32_t box[3] = {64, (cuuint32_t)g.G(), (cuuint32_t)plan.BP};
-        cuuint32_t estr[3] = {1, 1, 1};
-        CUresult r = encode(&qmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims,
-                            strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-        if (r != CUDA_SUCCESS) return drop_plan(*hit, st, SQ_ERR_INVALID_ARG);
+        const int qrc = make_query_map(c, q, n_q, plan.BP, &qmap);
+        if (qrc != SQ_OK) return drop_plan(*hit, st, qrc);
     }
     PrefillShortArgs a;
     a.tiles = reinterpret_cast<const PrefillTile*>(plan.d);
@@ -1627,3 +1696,5 @@ int sq_decode_attention_noalloc(sq_cache* c, const sq_seq* seqs, int32_t n_seqs,
 }
 
 }  // extern "C"
+
+#include "operators.inl"

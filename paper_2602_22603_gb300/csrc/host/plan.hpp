@@ -154,6 +154,38 @@ constexpr int64_t prefill_part_bytes(int32_t D) {
 }
 constexpr int64_t kPrefillPartLimit = int64_t(128) << 20;
 
+// Attention of query blocks (windows, sinks, drafted trees over a batch of
+// sequences).  A unit is up to kPrefillQTiles query tiles of one sequence at one
+// KV head; its key tiles (PrefillTile, two 64-key boxes each, increasing) are its
+// block's own: the boxes in which some query of the block sees a key.  An item is
+// a unit, or a piece of its key tiles.  Positions are slots.
+constexpr int32_t kBlockTwoTiles = 1 << 30;
+struct BlockItem {
+    int32_t head;      // KV head, and kBlockTwoTiles if the queries need both tiles
+    int32_t t0;        // its key tiles [t0, t0 + n_tiles)
+    int32_t n_tiles;
+    int32_t part;      // partial result, -1: the unit's only item
+    int32_t q_row;     // row of its first query among the call's
+    int32_t n_q;       // queries
+    int32_t n;         // slot-space end of the sequence
+    int32_t pos0;      // slot of the first query (a call without a row table)
+    int32_t low0;      // first slot in the first query's window (likewise)
+    int32_t sink_end;  // slots below it are visible whatever the window
+    int32_t base;      // first slot that the drafted tree's bitmaps rule, a multiple
+                       // of 32; kBlockNoTree: none
+    int32_t pad;
+};
+constexpr int32_t kBlockNoTree = 0x7fffffff;
+// A unit whose items' partial results [part0, part0 + n) are merged.
+struct BlockMerge {
+    int32_t g, part0, n, q_row;
+    int32_t n_q, pad[3];
+};
+// Drafted rows of one sequence at most, and the words of a row's bitmap then.
+constexpr int32_t kMaxDraft = 256;
+// Key tiles a plan may have.
+constexpr int64_t kMaxBlockTiles = int64_t(1) << 24;
+
 // Byte offsets of the arrays of a decode plan inside one upload buffer.
 // Byte offsets of the serialised decode plan.  `arrive` holds one 32-bit
 // arrival count per (sequence, KV head), zero in the serialised plan; the

@@ -161,7 +161,8 @@ __global__ void __launch_bounds__(kAppendThreads)
     grid_launch_dependents();
     write_lens(a.lens);
     if (blockIdx.x >= (unsigned)a.n_blocks) {
-        cow_rows(a.pool, a.num_pages, a.L, a.Hkv, a.P, a.D, a.cow, blockIdx.x - a.n_blocks, a.err);
+        if (a.n_cow > 0)
+            cow_rows(a.pool, a.num_pages, a.L, a.Hkv, a.P, a.D, a.cow, blockIdx.x - a.n_blocks, a.err);
         return;
     }
     const int chunk = append_chunk_tokens(a.Hkv, a.D);
@@ -352,7 +353,9 @@ template <typename Args>
 static cudaError_t launch_append_kernel(void (*kernel)(Args), Args& a, int n, int n_cow,
                                         cudaStream_t st) {
     const int64_t rows = append_blocks(a.L, a.Hkv, a.D, n);
-    const int64_t blocks = rows + (int64_t)n_cow * a.L * 2 * a.Hkv;
+    // (one block at least: sequences may get longer without a row or a copy, and
+    // block 0 writes their lengths)
+    const int64_t blocks = std::max<int64_t>(1, rows + (int64_t)n_cow * a.L * 2 * a.Hkv);
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
     a.n_blocks = (int32_t)rows;
     cudaLaunchAttribute at;
@@ -373,7 +376,7 @@ cudaError_t launch_append(AppendArgs& a, cudaStream_t st) {
 }
 
 cudaError_t launch_append_batch(AppendBatchArgs& a, cudaStream_t st) {
-    if (a.n <= 0) return cudaSuccess;
+    if (a.n <= 0 && a.n_cow <= 0 && a.lens.n <= 0) return cudaSuccess;
     return launch_append_kernel(sq_append_kv_batch_kernel, a, a.n, a.n_cow, st);
 }
 
