@@ -10,7 +10,7 @@ extern "C" {
 
 // Plans a call over the sequences of a host cache.  info: tiles, items, merges,
 // rows (0 or queries), n_words, n_pieces, BP, n_parts, one, unit_rows,
-// max_splits.  Arrays of the plan are copied to the non-null buffers (which the
+// max_splits, n_ctas.  Arrays of the plan are copied to the non-null buffers (which the
 // caller sizes by a first call without them).
 int sqh_plan_blocks(void* c, const int32_t* handles, int32_t n_seqs, const int32_t* n_q,
                     const int32_t* parents, int32_t window, int32_t n_sink, int32_t ctas,
@@ -25,7 +25,7 @@ int sqh_plan_blocks(void* c, const int32_t* handles, int32_t n_seqs, const int32
     if (rc != kOk) return rc;
     const int64_t v[] = {(int64_t)p.tiles.size(), (int64_t)p.items.size(), (int64_t)p.merges.size(),
                          (int64_t)p.rows.size() / 2, p.n_words, p.n_pieces, p.BP, p.n_parts, p.one,
-                         p.unit_rows, p.max_splits};
+                         p.unit_rows, p.max_splits, p.n_ctas};
     std::memcpy(info, v, sizeof v);
     auto put = [](void* to, const void* from, size_t n) {
         if (to && n) std::memcpy(to, from, n);

@@ -444,7 +444,7 @@ int norm_backward_impl(sq_cache* c, int32_t n_tokens, const void* q, int64_t q_s
     a.dq_weight = dq_weight;
     a.dk_weight = dk_weight;
     a.n = n_tokens;
-    a.ctas = norm_rope_grad_ctas(n_tokens, g.Hq + g.Hkv, g.D, c->num_sms);
+    a.ctas = norm_rope_grad_ctas(n_tokens, g.Hq, g.Hkv, g.D, c->num_sms);
     fill_params(c, params, &a);
     if (!weights) return cuda_status(launch_norm_rope_grad(a, g.D, st));
     rc = take_buffer(c->norm_part, (size_t)a.ctas * 2 * g.D * sizeof(float), st);
@@ -584,6 +584,7 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
         victim->max_splits = plan.max_splits;
         victim->unit_rows = plan.unit_rows;
         victim->one = plan.one;
+        victim->n_ctas = plan.n_ctas;
         std::vector<int32_t> read;
         for (int32_t p : plan.tile_pages)
             if (p >= 0 && (read.empty() || read.back() != p)) read.push_back(p);
@@ -622,6 +623,7 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
     a.rows = plan.o_rows ? reinterpret_cast<const int2*>(plan.d + plan.o_rows) : nullptr;
     a.bits = reinterpret_cast<const uint32_t*>(plan.d + plan.o_bits);
     a.n_words = plan.n_words;
+    a.n_ctas = plan.n_ctas;
     a.n_pieces = plan.n_pieces;
     a.n_tiles = a.n = a.n_q = 0;  // (the items')
     a.layer = layer;

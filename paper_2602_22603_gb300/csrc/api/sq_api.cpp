@@ -104,7 +104,7 @@ struct BlockPlanEntry : PrefillPlanEntry {
     std::vector<int32_t> handles;
     std::vector<uint64_t> versions;
     size_t o_rows = 0, o_bits = 0;  // (o_rows 0: no table)
-    int32_t n_words = 0, unit_rows = 0;
+    int32_t n_words = 0, unit_rows = 0, n_ctas = 0;
     bool one = false;
 };
 

@@ -4,11 +4,12 @@
 // Every sequence's queries are cut into blocks of up to kPrefillQTiles query
 // tiles.  A block lists the 64-slot boxes in which some query of it sees a row,
 // two to a key tile; each block is a unit at every KV head, and units are cut
-// into items where there are too few of them for the CTAs.
+// into items that give the CTAs even work.
 #pragma once
 
 #include <algorithm>
 #include <cstring>
+#include <functional>
 
 #include "core.hpp"
 
@@ -16,14 +17,14 @@ namespace sq {
 
 struct BlockPlanHost {
     std::vector<PrefillTile> tiles;
-    std::vector<BlockItem> items;      // longest first
+    std::vector<BlockItem> items;      // one: by CTA (see BlockItem::next); else longest first
     std::vector<BlockMerge> merges;    // units of more than one item
     std::vector<int32_t> tile_pages;   // [tiles][n_pieces] page of each piece, -1: none
     std::vector<int32_t> rows;         // [queries][2] first and last slot of each one's
                                        // window; empty: low0 + i, pos0 + i of the items
     std::vector<uint32_t> bits;        // [queries][n_words], drafted trees only
     int32_t n_words = 0, n_pieces = 0, BP = 0, n_parts = 0, max_splits = 0;
-    int32_t n_queries = 0;
+    int32_t n_queries = 0, n_ctas = 0;
     int32_t unit_rows = 0;             // rows of a tile pair that can hold queries
     bool one = true;                   // every item's queries fit in one query tile
 };
@@ -72,9 +73,15 @@ struct Unit {
     int32_t t0, T, q_row, n_q, n, pos0, low0, sink_end, base;
 };
 
-// Pieces that each unit's key tiles are cut into.  The estimate of a cut: items
-// run `ctas` at a time, longest first; each costs its key tiles and a fixed part,
-// and where units are cut at all the merge's launch comes on top.
+// A piece of a unit's key tiles.
+struct Piece {
+    int32_t unit, head, t0, n_tiles;
+};
+
+// Two-tile units are handed out item by item (longest first, to whichever CTA is
+// free), so only their lengths matter: into how many pieces is each cut?  The
+// estimate of a cut plays the hand-out through; an item costs its key tiles and a
+// fixed part, and where units are cut at all the merge's launch comes on top.
 inline void cut_units(const std::vector<Unit>& units, int32_t heads, int32_t ctas, int64_t max_parts,
                       int32_t D, std::vector<int32_t>* pieces) {
     const double item = D == 128 ? 3.0 : 6.0, merge = D == 128 ? 2.5 : 5.0;  // in key tiles
@@ -85,41 +92,110 @@ inline void cut_units(const std::vector<Unit>& units, int32_t heads, int32_t cta
         T_max = std::max(T_max, u.T);
         total += u.T;
     }
-    if (T_max < 2) return;
+    // (many items each: they even out)
+    if (T_max < 2 || (int64_t)units.size() * heads > 8 * (int64_t)ctas) return;
     double best = 0;
     int32_t best_len = T_max;
-    static const int32_t cuts[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 19, 24, 32, 48, 64};
+    static const int32_t cuts[] = {1, 2, 3, 4, 5, 6, 8, 11, 16, 24, 40, 64};
+    std::vector<int32_t> count(T_max + 1);  // items of each length
+    std::vector<double> load;
     for (int32_t k : cuts) {
         if (k > T_max) break;
         const int32_t len = ceil_div(T_max, k);
-        int64_t count = 0, parts = 0, longest = 0, shortest = T_max;
+        std::fill(count.begin(), count.end(), 0);
+        int64_t parts = 0, items = 0;
         for (const Unit& u : units) {
-            const int64_t c = std::max(1, ceil_div(u.T, len));
-            const int64_t piece = ceil_div(u.T, c);
-            count += c;
-            if (c > 1) parts += c;
-            longest = std::max(longest, piece);
-            shortest = std::min(shortest, piece);
+            const int32_t c = std::max(1, ceil_div(u.T, len));
+            count[ceil_div(u.T, c)] += c * heads;
+            items += (int64_t)c * heads;
+            if (c > 1) parts += (int64_t)c * heads;
         }
-        count *= heads;
-        parts *= heads;
-        if (parts > max_parts) break;
-        const double sum = (double)total * heads + item * count;
-        double cost = longest + item;
-        if (count > ctas) {
-            // alike items run in rounds; others fill the CTAs to within one of them
-            const double even = sum / ctas;
-            cost = longest <= shortest + 1 ? ceil_div(count, ctas) * (longest + item)
-                                           : std::max(cost, even + 0.5 * (sum / count));
-        }
-        if (parts > 0) cost += merge + 0.02 * parts;
+        if (parts > max_parts || items > 16 * (int64_t)ctas) break;
+        load.assign(ctas, 0.0);  // a heap, the least loaded CTA in front
+        double most = 0;
+        for (int32_t t = T_max; t > 0; --t)
+            for (int32_t x = 0; x < count[t]; ++x) {
+                std::pop_heap(load.begin(), load.end(), std::greater<double>());
+                load.back() += t + item;
+                most = std::max(most, load.back());
+                std::push_heap(load.begin(), load.end(), std::greater<double>());
+            }
+        const double cost = most + (parts > 0 ? merge + 0.02 * parts : 0.0);
         if (k == 1 || cost < 0.97 * best) {
             best = cost;
             best_len = len;
         }
+        if (cost > 1.3 * best) break;
     }
     for (size_t i = 0; i < units.size(); ++i)
         (*pieces)[i] = std::max(1, std::min(kPrefillMaxSplit, ceil_div(units[i].T, best_len)));
+}
+
+// One-tile units are bound by HBM, so every CTA gets an even share of the key
+// tiles: the units' heads in a line, cut into stretches of equal cost (key tiles
+// and a fixed part for each piece).  A cut is moved to a unit's end when it would
+// leave a sliver on either side.  Short units are left whole while that leaves no
+// CTA with a second one: a merge would cost more than it saves.
+// pieces[c]: those of CTA c, in order.
+inline void deal_units(const std::vector<Unit>& units, int32_t heads, int32_t ctas, int64_t max_parts,
+                       int32_t D, std::vector<std::vector<Piece>>* out) {
+    const double fixed = D == 128 ? 2.0 : 4.0;  // in key tiles
+    const int32_t sliver = D == 128 ? 2 : 3, short_unit = D == 128 ? 6 : 12;
+    out->clear();
+    int64_t total = 0;
+    int32_t T_max = 0;
+    for (const Unit& u : units) {
+        total += (int64_t)u.T * heads;
+        T_max = std::max(T_max, u.T);
+    }
+    const int64_t n = (int64_t)units.size() * heads;
+    const bool whole = max_parts < 2 || (n <= ctas && T_max <= short_unit);
+    // (a cut at the end of each share adds a piece)
+    // and a unit has at most kPrefillMaxSplit pieces
+    const double share = std::max({2.0 * sliver, (total + fixed * n) / ctas + fixed,
+                                   (double)T_max / (kPrefillMaxSplit - 1) + fixed});
+    out->emplace_back();
+    double room = share;  // what the last CTA may still take; the next begins with the rest
+
+    int64_t parts = 0;
+    for (int32_t u = 0; u < (int32_t)units.size(); ++u)
+        for (int32_t h = 0; h < heads; ++h) {
+            const int32_t T = units[u].T;
+            int32_t at = 0, cut = 0;  // tiles dealt, pieces so far
+            while (at < T) {
+                const int32_t left = T - at;
+                int32_t take = left;
+                const bool may = (int32_t)out->size() < ctas;
+                if (whole) {
+                    if (may && !out->back().empty() && n <= ctas) {
+                        out->emplace_back();
+                        room += share;
+                    }
+                } else if (may && left + fixed > room + sliver) {
+                    take = (int32_t)(room - fixed);
+                    // too little room for a piece worth its start
+                    if (take < sliver) {
+                        if (!out->back().empty()) {
+                            out->emplace_back();
+                            room += share;
+                            continue;
+                        }
+                        take = std::min(left, sliver);
+                    }
+                    if (left - take < sliver || cut + 1 >= kPrefillMaxSplit || parts + 2 > max_parts) take = left;
+                }
+                if (take < left || cut > 0) ++parts;
+                out->back().push_back({u, h, at, take});
+                room -= take + fixed;
+                at += take;
+                ++cut;
+                if (!whole && may && room < sliver + fixed) {
+                    out->emplace_back();
+                    room += share;
+                }
+            }
+        }
+    if (out->back().empty()) out->pop_back();
 }
 
 }  // namespace blocks_detail
@@ -252,8 +328,41 @@ inline int plan_blocks(const Geometry& g, const std::vector<BlockSeq>& seqs, int
         }
         q_row += m;
     }
+    const int64_t max_parts = part_limit / prefill_part_bytes(g.D);
+    auto item_of = [&](const Piece& p, int32_t part) {
+        const Unit& u = units[p.unit];
+        return BlockItem{p.head | (u.n_q > BP ? kBlockTwoTiles : 0), u.t0 + p.t0, p.n_tiles, part, u.q_row, u.n_q,
+                         u.n, u.pos0, u.low0, u.sink_end, u.base, -1};
+    };
+    if (out->one) {
+        std::vector<std::vector<Piece>> dealt;
+        deal_units(units, g.Hkv, std::max(1, ctas), max_parts, g.D, &dealt);
+        // pieces of a unit follow one another over the CTAs: number them as they come
+        out->n_ctas = (int32_t)dealt.size();
+        std::vector<BlockItem> rest;
+        out->items.reserve(dealt.size());
+        for (size_t c = 0; c < dealt.size(); ++c)
+            for (size_t x = 0; x < dealt[c].size(); ++x) {
+                const Piece& p = dealt[c][x];
+                int32_t part = -1;
+                if (p.n_tiles < units[p.unit].T) {
+                    if (p.t0 == 0)
+                        out->merges.push_back({p.head, out->n_parts, 0, units[p.unit].q_row, units[p.unit].n_q,
+                                               {0, 0, 0}});
+                    out->max_splits = std::max(out->max_splits, ++out->merges.back().n);
+                    part = out->n_parts++;
+                }
+                BlockItem it = item_of(p, part);
+                if (x + 1 < dealt[c].size())  // (its place once the first ones are in)
+                    it.next = (int32_t)(dealt.size() + rest.size()) + (x == 0 ? 0 : 1);
+                if (x == 0) out->items.push_back(it);
+                else rest.push_back(it);
+            }
+        out->items.insert(out->items.end(), rest.begin(), rest.end());
+        return kOk;
+    }
     std::vector<int32_t> pieces;
-    cut_units(units, g.Hkv, std::max(1, ctas), part_limit / prefill_part_bytes(g.D), g.D, &pieces);
+    cut_units(units, g.Hkv, std::max(1, ctas), max_parts, g.D, &pieces);
     // items, longest first; the heads of one block side by side (their queries and
     // pages are neighbours)
     std::vector<std::pair<int32_t, int32_t>> order;  // (longest piece, unit)
@@ -270,9 +379,7 @@ inline int plan_blocks(const Geometry& g, const std::vector<BlockSeq>& seqs, int
     out->items.reserve(n_items);
     for (const auto& o : order) {
         const Unit& u = units[o.second];
-        const int32_t k = pieces[o.second];
-        const int32_t two = u.n_q > BP ? kBlockTwoTiles : 0;
-        const int32_t part0 = out->n_parts;
+        const int32_t k = pieces[o.second], part0 = out->n_parts;
         if (k > 1) {
             for (int32_t h = 0; h < g.Hkv; ++h)
                 out->merges.push_back({h, part0 + h * k, k, u.q_row, u.n_q, {0, 0, 0}});
@@ -282,10 +389,10 @@ inline int plan_blocks(const Geometry& g, const std::vector<BlockSeq>& seqs, int
         for (int32_t x = 0; x < k; ++x)
             for (int32_t h = 0; h < g.Hkv; ++h) {
                 const int32_t a = (int32_t)((int64_t)u.T * x / k), b = (int32_t)((int64_t)u.T * (x + 1) / k);
-                out->items.push_back({h | two, u.t0 + a, b - a, k > 1 ? part0 + h * k + x : -1, u.q_row, u.n_q,
-                                      u.n, u.pos0, u.low0, u.sink_end, u.base, 0});
+                out->items.push_back(item_of({o.second, h, a, b - a}, k > 1 ? part0 + h * k + x : -1));
             }
     }
+    out->n_ctas = (int32_t)out->items.size();
     return kOk;
 }
 

@@ -173,7 +173,8 @@ struct BlockItem {
     int32_t sink_end;  // slots below it are visible whatever the window
     int32_t base;      // first slot that the drafted tree's bitmaps rule, a multiple
                        // of 32; kBlockNoTree: none
-    int32_t pad;
+    int32_t next;      // plans of one-tile blocks: the item that follows on the same
+                       // CTA (CTA c starts with item c), -1: none
 };
 constexpr int32_t kBlockNoTree = 0x7fffffff;
 // A unit whose items' partial results [part0, part0 + n) are merged.

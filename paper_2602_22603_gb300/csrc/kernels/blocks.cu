@@ -47,7 +47,7 @@ cudaError_t launch_after(void (*kernel)(P...), unsigned grid, unsigned block, in
 template <int D, typename Args>
 cudaError_t launch_one(const CUtensorMap& pool_map, const CUtensorMap& qmap, const Args& a, cudaStream_t st) {
     using C = dev::PreCfg<D, dev::ModeOf<Args>::value>;
-    return launch_after(dev::sq_prefill_kernel<D, Args>, (unsigned)a.n_items, C::kThreads, C::kSmemBytes, st,
+    return launch_after(dev::sq_prefill_kernel<D, Args>, (unsigned)a.n_ctas, C::kThreads, C::kSmemBytes, st,
                         pool_map, qmap, a);
 }
 

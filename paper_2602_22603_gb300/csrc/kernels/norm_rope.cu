@@ -14,11 +14,13 @@
 // and heads of dy * x r.
 //
 // What bounds it: HBM.  Every row is read once and written once, 2 D bytes each
-// way, and the arithmetic per row (~10 fp32 operations an element) is a third of
-// what the SMs do meanwhile.  A row takes D / 8 lanes with a 16-byte vector each,
-// so its sum of squares is 3 or 4 shuffles and a half-pair's partner one shuffle
-// an element; a warp has one token's table rows in registers and kUnroll rows of
-// each lane group in flight.
+// way.  To keep the SMs' issue slots out of the way a lane holds both halves of
+// its pairs: D / 8 lanes take a row, each four elements f .. f + 3 and the four
+// g .. g + 3 they turn with, so that the rotation needs no shuffle; the weight and
+// the cosine are one factor of each element, made once for a warp's rows; and the
+// products go two at a time (fma.rn.f32x2).  A warp's task is up to kUnroll rows
+// of each of its lane groups, all query, all key or all value heads of one token:
+// its loads are all issued before the first is used.
 #include <algorithm>
 #include <type_traits>
 
@@ -30,32 +32,57 @@ namespace {
 
 using namespace dev;
 
-constexpr int kNormThreads = 256;
-constexpr int kUnroll = 4;  // rows of a lane group in flight
+constexpr int kNormThreads = 128;
+constexpr int kUnroll = 8;      // rows of a lane group in flight
+constexpr int kGradThreads = 256;
+constexpr int kGradUnroll = 4;  // ... backwards, of two tensors
 
 template <int D>
 struct NormCfg {
-    static constexpr int kLanes = D / 8;                 // lanes of a row
-    static constexpr int kGroups = 32 / kLanes;          // rows a warp holds at once
-    static constexpr int kTaskRows = kGroups * kUnroll;  // rows of a warp's task
+    static constexpr int kLanes = D / 8;     // lanes of a row
+    static constexpr int kGroups = 32 / kLanes;  // rows a warp holds at once
 };
 
-__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+typedef uint64_t f32x2;  // two floats, the first in the low half
+__device__ __forceinline__ f32x2 f2(float a, float b) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 un2(f32x2 v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ f32x2 swap2(f32x2 v) {
+    const float2 x = un2(v);
+    return f2(x.y, x.x);
+}
+__device__ __forceinline__ f32x2 unpack2(uint32_t w) {
+    return f2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ uint32_t pack2(f32x2 v) {
+    const float2 x = un2(v);
+    return pack_bf16x2(x.x, x.y);
 }
 
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-    return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                      pack_bf16x2(x[6], x[7]));
+// Streaming loads (read once).
+__device__ __forceinline__ uint2 ld_half_row(const __nv_bfloat16* p) {
+    uint2 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
 }
-
-// Streaming 16-byte load (read once).
-__device__ __forceinline__ uint4 ld_row(const void* p) {
+__device__ __forceinline__ uint4 ld_row(const __nv_bfloat16* p) {
     uint4 v;
     asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
@@ -63,87 +90,97 @@ __device__ __forceinline__ uint4 ld_row(const void* p) {
     return v;
 }
 
-// The norm's weights of elements e0 .. e0 + 7 (ones where there are none).
-__device__ __forceinline__ void load_weights(const void* w, int f32, int e0, float (&x)[8]) {
-    if (!w) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 1.f;
-    } else if (f32) {
-        const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(w) + e0);
-        const float4 a = __ldg(p), b = __ldg(p + 1);
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    } else {
-        unpack8(__ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(w) + e0)), x);
+// The eight elements a lane has of every row: f .. f + 3 and g .. g + 3.
+struct Lane {
+    int f, g;
+    int pair;   // first of its four pairs in the table
+    bool on;    // its elements turn
+    template <bool kPairs>
+    __device__ __forceinline__ void init(int l, int rot) {
+        on = 8 * l < rot;  // (rot is a multiple of 16)
+        pair = 4 * l;
+        f = !kPairs && on ? 4 * l : 8 * l;
+        g = !kPairs && on ? rot / 2 + 4 * l : 8 * l + 4;
     }
-}
-
-// A lane's part of the rotation at one position: the cosine and sine of each of
-// its elements (of pairs of neighbours: of elements 2 i and 2 i + 1), the sine
-// negative where the element is its pair's first, and the lane holding the other
-// halves.
-struct Turn {
-    float c[8], s[8];
-    int partner;
-    bool on;  // this lane's elements turn
 };
 
-// `pos` is inside the table.  `group0`: the row's first lane.
-__device__ __forceinline__ void load_turn(Turn& t, const float2* rope, int pos, int rot, int interleaved,
-                                          int e0, int group0) {
-    t.on = e0 < rot;
-    t.partner = group0 + e0 / 8;
-    if (!t.on) return;
-    const int half = rot >> 1;  // a multiple of 8
-    const float2* row = rope + (int64_t)pos * half;
-    if (interleaved) {
-        const float4* p = reinterpret_cast<const float4*>(row + e0 / 2);
+// Eight values of a lane as pairs: f's, then g's.
+struct Eight {
+    f32x2 v[4];
+    __device__ __forceinline__ void set(uint2 a, uint2 b) {
+        v[0] = unpack2(a.x);
+        v[1] = unpack2(a.y);
+        v[2] = unpack2(b.x);
+        v[3] = unpack2(b.y);
+    }
+    // what each element turns with
+    template <bool kPairs>
+    __device__ __forceinline__ f32x2 other(int i) const {
+        return kPairs ? swap2(v[i]) : v[i ^ 2];
+    }
+};
+
+// Four weights of an element type (ones where there are none).
+__device__ __forceinline__ void load_weights4(const void* w, int f32, int e, f32x2& a, f32x2& b) {
+    if (!w) {
+        a = b = f2(1.f, 1.f);
+    } else if (f32) {
+        const float4 x = __ldg(reinterpret_cast<const float4*>(reinterpret_cast<const float*>(w) + e));
+        a = f2(x.x, x.y);
+        b = f2(x.z, x.w);
+    } else {
+        const uint2 x = __ldg(reinterpret_cast<const uint2*>(reinterpret_cast<const __nv_bfloat16*>(w) + e));
+        a = unpack2(x.x);
+        b = unpack2(x.y);
+    }
+}
+__device__ __forceinline__ void load_weights(const void* w, int f32, const Lane& ln, Eight& x) {
+    load_weights4(w, f32, ln.f, x.v[0], x.v[1]);
+    load_weights4(w, f32, ln.g, x.v[2], x.v[3]);
+}
+
+// Cosines and sines of a lane's elements at one position (the sine negative where
+// an element is its pair's first), 1 and 0 for those that do not turn.
+struct Turn {
+    f32x2 c[4], s[4];
+};
+// `pos` is inside the table.
+template <bool kPairs>
+__device__ __forceinline__ void load_turn(Turn& t, const float2* rope, int pos, int rot, const Lane& ln) {
+    if (!ln.on) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float4 v = __ldg(p + i);
-            t.c[4 * i] = t.c[4 * i + 1] = v.x;
-            t.s[4 * i] = -v.y;
-            t.s[4 * i + 1] = v.y;
-            t.c[4 * i + 2] = t.c[4 * i + 3] = v.z;
-            t.s[4 * i + 2] = -v.w;
-            t.s[4 * i + 3] = v.w;
+        for (int i = 0; i < 4; ++i) {
+            t.c[i] = f2(1.f, 1.f);
+            t.s[i] = f2(0.f, 0.f);
         }
         return;
     }
-    const bool first = e0 < half;
-    t.partner = group0 + (first ? e0 + half : e0 - half) / 8;
-    const float4* p = reinterpret_cast<const float4*>(row + (first ? e0 : e0 - half));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float4 v = __ldg(p + i);
-        t.c[2 * i] = v.x;
-        t.s[2 * i] = first ? -v.y : v.y;
-        t.c[2 * i + 1] = v.z;
-        t.s[2 * i + 1] = first ? -v.w : v.w;
-    }
-}
-
-// y turned by the position (kBack: turned back, the transpose).  Every lane of
-// the warp calls it.
-template <bool kBack>
-__device__ __forceinline__ void turn(const Turn& t, int interleaved, float (&y)[8]) {
-    float o[8];
-    if (interleaved) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = y[i ^ 1];
+    const float4* p = reinterpret_cast<const float4*>(rope + (int64_t)pos * (rot >> 1) + ln.pair);
+    const float4 a = __ldg(p), b = __ldg(p + 1);  // c0 s0 c1 s1, c2 s2 c3 s3
+    if (kPairs) {
+        t.c[0] = f2(a.x, a.x);
+        t.c[1] = f2(a.z, a.z);
+        t.c[2] = f2(b.x, b.x);
+        t.c[3] = f2(b.z, b.z);
+        t.s[0] = f2(-a.y, a.y);
+        t.s[1] = f2(-a.w, a.w);
+        t.s[2] = f2(-b.y, b.y);
+        t.s[3] = f2(-b.w, b.w);
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = __shfl_sync(0xffffffffu, y[i], t.partner);
-    }
-    if (t.on) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = kBack ? y[i] * t.c[i] - o[i] * t.s[i] : y[i] * t.c[i] + o[i] * t.s[i];
+        t.c[0] = t.c[2] = f2(a.x, a.z);
+        t.c[1] = t.c[3] = f2(b.x, b.z);
+        t.s[2] = f2(a.y, a.w);
+        t.s[3] = f2(b.y, b.w);
+        t.s[0] = f2(-a.y, -a.w);
+        t.s[1] = f2(-b.y, -b.w);
     }
 }
 
 // Sum over the lanes of a row.
 template <int D>
-__device__ __forceinline__ float row_sum(float x) {
+__device__ __forceinline__ float row_sum(f32x2 v) {
+    const float2 p = un2(v);
+    float x = p.x + p.y;
 #pragma unroll
     for (int o = NormCfg<D>::kLanes / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
@@ -156,9 +193,19 @@ __device__ __forceinline__ int checked_pos(int pos, int max_pos, int* err) {
     return 0;
 }
 
-// One warp: kTaskRows of a token's rows (its query heads, its key heads, and
-// with kStore its value heads, which are copied).
-template <int D, bool kStore, typename Args>
+// Tasks of a token: its query heads, its key heads, its value heads (kStore).
+template <int D, int kRows>
+struct Tasks {
+    int q, k, total;
+    __host__ __device__ Tasks(int Hq, int Hkv, bool store) {
+        constexpr int n = NormCfg<D>::kGroups * kRows;
+        q = (Hq + n - 1) / n;
+        k = (Hkv + n - 1) / n;
+        total = q + k + (store ? k : 0);
+    }
+};
+
+template <int D, bool kStore, bool kPairs, typename Args>
 __global__ void __launch_bounds__(kNormThreads)
     sq_norm_rope_kernel(const __grid_constant__ Args a) {
     using C = NormCfg<D>;
@@ -166,163 +213,210 @@ __global__ void __launch_bounds__(kNormThreads)
     grid_dependency_wait();
     grid_launch_dependents();
     const int lane = threadIdx.x & 31;
-    const int n_rows = a.Hq + (kStore ? 2 : 1) * a.Hkv;
-    const unsigned chunks = (unsigned)(n_rows + C::kTaskRows - 1) / C::kTaskRows;
-    // (n x chunks fits: the rows of as many tokens would not fit the device)
+    const Tasks<D, kUnroll> per(a.Hq, a.Hkv, kStore);
+    // (n x tasks fits: the rows of as many tokens would not fit the device)
     const unsigned task = blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
-    const unsigned t = task / chunks;
+    const unsigned t = task / (unsigned)per.total;
     if (t >= (unsigned)a.n) return;
-    const int sub = lane / C::kLanes, e0 = (lane % C::kLanes) * 8;
-    const int row0 = (int)(task - t * chunks) * C::kTaskRows + sub;
-    uint4 raw[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const int h = row0 + u * C::kGroups;
-        const __nv_bfloat16* p = h < a.Hq ? a.q + t * a.q_stride + (int64_t)h * D
-                                 : h < a.Hq + a.Hkv
-                                     ? a.k + t * a.k_stride + (int64_t)(h - a.Hq) * D
-                                     : a.v + t * a.v_stride + (int64_t)(h - a.Hq - a.Hkv) * D;
-        raw[u] = h < n_rows ? ld_row(p + e0) : make_uint4(0, 0, 0, 0);
-    }
+    int part = (int)(task - t * per.total);
+    const bool is_v = part >= per.q + per.k, is_k = part >= per.q;
+    if (is_k) part -= per.q;
+    if (is_v) part -= per.k;
+    const int sub = lane / C::kLanes, l = lane % C::kLanes;
+    const int heads = is_k ? a.Hkv : a.Hq;
+    const int h0 = part * C::kGroups * kUnroll;   // first head of the warp's
+    const int n_pass = min(kUnroll, (heads - h0 + C::kGroups - 1) / C::kGroups);
+    const int h = h0 + sub;
+    const __nv_bfloat16* src = (is_v ? a.v + t * a.v_stride : is_k ? a.k + t * a.k_stride : a.q + t * a.q_stride) +
+                               (int64_t)h * D;
     RowPlace place = {0, 0};
     if constexpr (kStore) {
         if constexpr (kInline) place = a.inline_place[t];
         else place = a.places[t];
     }
-    Turn tn;
-    {
-        int pos = a.positions ? __ldg(&a.positions[t]) : place.pos;
-        if (a.rot > 0) pos = checked_pos(pos, a.max_pos, a.err);
-        load_turn(tn, a.rope, pos, a.rot, a.interleaved, e0, sub * C::kLanes);
-    }
-    float wq[8], wk[8];
-    load_weights(a.q_weight, a.weight_f32, e0, wq);
-    load_weights(a.k_weight, a.weight_f32, e0, wk);
-    __nv_bfloat16* kv_row = nullptr;  // the token's row of head 0 of K in the pool
-    if constexpr (kStore) {
+    // where head h goes, and the elements from head to head
+    __nv_bfloat16* dst = nullptr;
+    int64_t step = D;
+    if (!is_k) {
+        dst = a.q_out + ((int64_t)t * a.Hq + h) * D;
+    } else if constexpr (kStore) {
         const int lp = __ffs(a.P) - 1;
         const int64_t page = place.row >> lp;
+        step = (int64_t)a.P * D;
         if (place.row >= 0 && page < a.num_pages)
-            kv_row = a.pool + (((int64_t)a.layer * a.num_pages + page) * 2 * a.Hkv * a.P +
-                               (place.row & (a.P - 1))) * D;
+            dst = a.pool + ((((int64_t)a.layer * a.num_pages + page) * 2 + (is_v ? 1 : 0)) * a.Hkv + h) * step +
+                  (int64_t)(place.row & (a.P - 1)) * D;
         else set_error(a.err, kErrBounds);
+    } else {
+        dst = a.k_out + ((int64_t)t * a.Hkv + h) * D;
+    }
+    if (kStore && is_v) {
+        uint4 raw[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (h + u * C::kGroups < heads) raw[u] = ld_row(src + u * C::kGroups * D + 8 * l);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (h + u * C::kGroups < heads && dst)
+                *reinterpret_cast<uint4*>(dst + u * C::kGroups * step + 8 * l) = raw[u];
+        return;
+    }
+    Lane ln;
+    ln.init<kPairs>(l, a.rot);
+    uint2 rf[kUnroll], rg[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        rf[u] = rg[u] = make_uint2(0, 0);
+        if (h + u * C::kGroups < heads) {
+            rf[u] = ld_half_row(src + u * C::kGroups * D + ln.f);
+            rg[u] = ld_half_row(src + u * C::kGroups * D + ln.g);
+        }
+    }
+    // out = r (x A + other B): A the weight times the cosine, B the other's weight
+    // times the sine
+    f32x2 A[4], B[4];
+    {
+        Turn tn;
+        int pos = a.positions ? __ldg(&a.positions[t]) : place.pos;
+        if (a.rot > 0) pos = checked_pos(pos, a.max_pos, a.err);
+        load_turn<kPairs>(tn, a.rope, pos, a.rot, ln);
+        Eight w;
+        load_weights(is_k ? a.k_weight : a.q_weight, a.weight_f32, ln, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            A[i] = mul2(w.v[i], tn.c[i]);
+            B[i] = mul2(w.other<kPairs>(i), tn.s[i]);
+        }
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-        const int h = row0 + u * C::kGroups;
-        if (row0 - sub + u * C::kGroups >= n_rows) break;  // (warp-uniform)
-        const bool is_k = h >= a.Hq, is_v = kStore && h >= a.Hq + a.Hkv;
-        float y[8];
-        unpack8(raw[u], y);
-        float ss = 0.f;
+        if (u >= n_pass) break;  // (warp-uniform)
+        Eight x;
+        x.set(rf[u], rg[u]);
+        f32x2 ss = mul2(x.v[0], x.v[0]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss += y[i] * y[i];
+        for (int i = 1; i < 4; ++i) ss = fma2(x.v[i], x.v[i], ss);
         const float r = rsqrtf(row_sum<D>(ss) * (1.f / D) + a.eps);
+        const f32x2 rr = f2(r, r);
+        uint32_t o[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = y[i] * r * (is_k ? wk[i] : wq[i]);
-        turn<false>(tn, a.interleaved, y);
-        if (h >= n_rows) continue;
-        __nv_bfloat16* to;
-        if (!is_k) to = a.q_out + ((int64_t)t * a.Hq + h) * D;
-        else if constexpr (kStore) to = kv_row ? kv_row + (int64_t)(h - a.Hq) * a.P * D : nullptr;
-        else to = a.k_out + ((int64_t)t * a.Hkv + h - a.Hq) * D;
-        if (to) *reinterpret_cast<uint4*>(to + e0) = is_v ? raw[u] : pack8(y);
+        for (int i = 0; i < 4; ++i)
+            o[i] = pack2(mul2(fma2(x.v[i], A[i], mul2(x.other<kPairs>(i), B[i])), rr));
+        if (h + u * C::kGroups < heads && dst) {
+            __nv_bfloat16* to = dst + u * C::kGroups * step;
+            *reinterpret_cast<uint2*>(to + ln.f) = make_uint2(o[0], o[1]);
+            *reinterpret_cast<uint2*>(to + ln.g) = make_uint2(o[2], o[3]);
+        }
     }
 }
 
-// Backwards.  A CTA's warps take tasks (a token's kTaskRows query or key rows) in
-// turn and add up the weights' gradients of their lanes' elements; the CTA's sums
-// go to one partial row, added by a second kernel in a fixed order.
-template <int D>
-__global__ void __launch_bounds__(kNormThreads)
+// Backwards.  A CTA's warps take tasks (query or key heads of a token) in turn and
+// add up the weights' gradients of their lanes' elements; the CTA's sums go to one
+// partial row, added by a second kernel in a fixed order.
+template <int D, bool kPairs>
+__global__ void __launch_bounds__(kGradThreads)
     sq_norm_rope_grad_kernel(const __grid_constant__ NormRopeGradArgs a) {
     using C = NormCfg<D>;
     grid_dependency_wait();
     grid_launch_dependents();
-    constexpr int kWarps = kNormThreads / 32;
+    constexpr int kWarps = kGradThreads / 32;
     __shared__ float red[kWarps][2][D];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int sub = lane / C::kLanes, e0 = (lane % C::kLanes) * 8;
-    const int n_rows = a.Hq + a.Hkv;
-    const unsigned chunks = (unsigned)(n_rows + C::kTaskRows - 1) / C::kTaskRows;
-    const unsigned tasks = (unsigned)a.n * chunks;
-    float wq[8], wk[8], gq[8], gk[8];
-    load_weights(a.q_weight, a.weight_f32, e0, wq);
-    load_weights(a.k_weight, a.weight_f32, e0, wk);
+    const int sub = lane / C::kLanes;
+    const Tasks<D, kGradUnroll> per(a.Hq, a.Hkv, false);
+    const unsigned tasks = (unsigned)a.n * per.total;
+    Lane ln;
+    ln.init<kPairs>(lane % C::kLanes, a.rot);
+    Eight wq, wk;
+    load_weights(a.q_weight, a.weight_f32, ln, wq);
+    load_weights(a.k_weight, a.weight_f32, ln, wk);
+    f32x2 gq[4], gk[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) gq[i] = gk[i] = 0.f;
+    for (int i = 0; i < 4; ++i) gq[i] = gk[i] = f2(0.f, 0.f);
     for (unsigned task = blockIdx.x * kWarps + warp; task < tasks; task += gridDim.x * kWarps) {
-        const unsigned t = task / chunks;
-        const int row0 = (int)(task - t * chunks) * C::kTaskRows + sub;
-        uint4 rx[kUnroll], rz[kUnroll];
+        const unsigned t = task / (unsigned)per.total;
+        int part = (int)(task - t * per.total);
+        const bool is_k = part >= per.q;
+        if (is_k) part -= per.q;
+        const int heads = is_k ? a.Hkv : a.Hq;
+        const int h0 = part * C::kGroups * kGradUnroll, h = h0 + sub;
+        const int n_pass = min(kGradUnroll, (heads - h0 + C::kGroups - 1) / C::kGroups);
+        const __nv_bfloat16* xs = (is_k ? a.k + t * a.k_stride : a.q + t * a.q_stride) + (int64_t)h * D;
+        const __nv_bfloat16* zs = (is_k ? a.dk_out : a.dq_out) + ((int64_t)t * heads + h) * D;
+        __nv_bfloat16* dst = (is_k ? a.dk + t * a.dk_stride : a.dq + t * a.dq_stride) + (int64_t)h * D;
+        uint2 xf[kGradUnroll], xg[kGradUnroll], zf[kGradUnroll], zg[kGradUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int h = row0 + u * C::kGroups;
-            const bool is_k = h >= a.Hq;
-            rx[u] = rz[u] = make_uint4(0, 0, 0, 0);
-            if (h < n_rows) {
-                rx[u] = ld_row((is_k ? a.k + t * a.k_stride + (int64_t)(h - a.Hq) * D
-                                     : a.q + t * a.q_stride + (int64_t)h * D) + e0);
-                rz[u] = ld_row((is_k ? a.dk_out + ((int64_t)t * a.Hkv + h - a.Hq) * D
-                                     : a.dq_out + ((int64_t)t * a.Hq + h) * D) + e0);
+        for (int u = 0; u < kGradUnroll; ++u) {
+            xf[u] = xg[u] = zf[u] = zg[u] = make_uint2(0, 0);
+            if (h + u * C::kGroups < heads) {
+                xf[u] = ld_half_row(xs + u * C::kGroups * D + ln.f);
+                xg[u] = ld_half_row(xs + u * C::kGroups * D + ln.g);
+                zf[u] = ld_half_row(zs + u * C::kGroups * D + ln.f);
+                zg[u] = ld_half_row(zs + u * C::kGroups * D + ln.g);
             }
         }
         Turn tn;
         int pos = a.positions ? __ldg(&a.positions[t]) : 0;
         if (a.rot > 0) pos = checked_pos(pos, a.max_pos, a.err);
-        load_turn(tn, a.rope, pos, a.rot, a.interleaved, e0, sub * C::kLanes);
+        load_turn<kPairs>(tn, a.rope, pos, a.rot, ln);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int h = row0 + u * C::kGroups;
-            if (row0 - sub + u * C::kGroups >= n_rows) break;  // (warp-uniform)
-            const bool is_k = h >= a.Hq;
-            float x[8], dy[8];
-            unpack8(rx[u], x);
-            unpack8(rz[u], dy);
-            turn<true>(tn, a.interleaved, dy);
-            float ss = 0.f;
+        for (int u = 0; u < kGradUnroll; ++u) {
+            if (u >= n_pass) break;  // (warp-uniform)
+            Eight x, z;
+            x.set(xf[u], xg[u]);
+            z.set(zf[u], zg[u]);
+            f32x2 ss = mul2(x.v[0], x.v[0]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
-            // (rows past the token's heads add nothing)
+            for (int i = 1; i < 4; ++i) ss = fma2(x.v[i], x.v[i], ss);
             const float rs = rsqrtf(row_sum<D>(ss) * (1.f / D) + a.eps);
-            const float r = h < n_rows ? rs : 0.f;
-            float dot = 0.f;
+            // (rows past the token's heads add nothing)
+            const float r = h + u * C::kGroups < heads ? rs : 0.f;
+            const f32x2 rr = f2(r, r), back = f2(-1.f, -1.f);
+            f32x2 dn[4], dot = f2(0.f, 0.f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] *= r;
-                const float g = dy[i] * x[i];
-                if (is_k) gk[i] += g;
-                else gq[i] += g;
-                dy[i] *= is_k ? wk[i] : wq[i];
-                dot += dy[i] * x[i];
+            for (int i = 0; i < 4; ++i) {
+                // dy: dz turned back
+                const f32x2 dy = fma2(z.v[i], tn.c[i], mul2(mul2(z.other<kPairs>(i), tn.s[i]), back));
+                x.v[i] = mul2(x.v[i], rr);
+                if (is_k) gk[i] = fma2(dy, x.v[i], gk[i]);
+                else gq[i] = fma2(dy, x.v[i], gq[i]);
+                dn[i] = mul2(dy, is_k ? wk.v[i] : wq.v[i]);
+                dot = fma2(dn[i], x.v[i], dot);
             }
-            dot = row_sum<D>(dot) * (1.f / D);
+            const float m = row_sum<D>(dot) * (-1.f / D);
+            const f32x2 mm = f2(m, m);
+            uint32_t o[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dy[i] = r * (dy[i] - x[i] * dot);
-            if (h < n_rows)
-                *reinterpret_cast<uint4*>((is_k ? a.dk + t * a.dk_stride + (int64_t)(h - a.Hq) * D
-                                                : a.dq + t * a.dq_stride + (int64_t)h * D) + e0) =
-                    pack8(dy);
+            for (int i = 0; i < 4; ++i) o[i] = pack2(mul2(fma2(x.v[i], mm, dn[i]), rr));
+            if (h + u * C::kGroups < heads) {
+                __nv_bfloat16* to = dst + u * C::kGroups * D;
+                *reinterpret_cast<uint2*>(to + ln.f) = make_uint2(o[0], o[1]);
+                *reinterpret_cast<uint2*>(to + ln.g) = make_uint2(o[2], o[3]);
+            }
         }
     }
     if (!a.part) return;
     // the lane groups of the warp, then the warps
 #pragma unroll
-    for (int o = C::kLanes; o < 32; o <<= 1)
+    for (int i = 0; i < 4; ++i) {
+        float2 q = un2(gq[i]), k = un2(gk[i]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            gq[i] += __shfl_xor_sync(0xffffffffu, gq[i], o);
-            gk[i] += __shfl_xor_sync(0xffffffffu, gk[i], o);
+        for (int o = C::kLanes; o < 32; o <<= 1) {
+            q.x += __shfl_xor_sync(0xffffffffu, q.x, o);
+            q.y += __shfl_xor_sync(0xffffffffu, q.y, o);
+            k.x += __shfl_xor_sync(0xffffffffu, k.x, o);
+            k.y += __shfl_xor_sync(0xffffffffu, k.y, o);
         }
-    if (sub == 0) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            red[warp][0][e0 + i] = gq[i];
-            red[warp][1][e0 + i] = gk[i];
+        if (sub == 0) {
+            const int e = (i < 2 ? ln.f : ln.g) + 2 * (i & 1);
+            red[warp][0][e] = q.x;
+            red[warp][0][e + 1] = q.y;
+            red[warp][1][e] = k.x;
+            red[warp][1][e + 1] = k.y;
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * D; i += kNormThreads) {
+    for (int i = threadIdx.x; i < 2 * D; i += kGradThreads) {
         float s = 0.f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) s += (&red[w][0][0])[i];
@@ -368,20 +462,29 @@ cudaError_t launch_after(void (*kernel)(P...), unsigned grid, unsigned block, cu
 
 template <int D, bool kStore, typename Args>
 cudaError_t launch_rows(const Args& a, cudaStream_t st) {
-    const int rows = a.Hq + (kStore ? 2 : 1) * a.Hkv;
-    const int64_t warps = (int64_t)a.n * ((rows + NormCfg<D>::kTaskRows - 1) / NormCfg<D>::kTaskRows);
+    const int64_t warps = (int64_t)a.n * Tasks<D, kUnroll>(a.Hq, a.Hkv, kStore).total;
     if (warps == 0) return cudaSuccess;
     constexpr int per = kNormThreads / 32;
-    return launch_after(sq_norm_rope_kernel<D, kStore, Args>, (unsigned)((warps + per - 1) / per),
-                        kNormThreads, st, a);
+    const unsigned grid = (unsigned)((warps + per - 1) / per);
+    return a.interleaved ? launch_after(sq_norm_rope_kernel<D, kStore, true, Args>, grid, kNormThreads, st, a)
+                         : launch_after(sq_norm_rope_kernel<D, kStore, false, Args>, grid, kNormThreads, st, a);
 }
 
 template <int D>
 cudaError_t launch_grad(const NormRopeGradArgs& a, cudaStream_t st) {
-    cudaError_t e = launch_after(sq_norm_rope_grad_kernel<D>, (unsigned)a.ctas, kNormThreads, st, a);
+    const cudaError_t e =
+        a.interleaved ? launch_after(sq_norm_rope_grad_kernel<D, true>, (unsigned)a.ctas, kGradThreads, st, a)
+                      : launch_after(sq_norm_rope_grad_kernel<D, false>, (unsigned)a.ctas, kGradThreads, st, a);
     if (e != cudaSuccess || !a.part) return e;
     return launch_after(sq_norm_rope_grad_sum_kernel<D>, 2 * D / 32, 1024, st, (const float*)a.part,
                         (int)a.ctas, a.dq_weight, a.dk_weight);
+}
+
+template <int D>
+int grad_ctas(int32_t n, int32_t Hq, int32_t Hkv, int num_sms) {
+    const int64_t tasks = (int64_t)n * Tasks<D, kGradUnroll>(Hq, Hkv, false).total;
+    constexpr int per = kGradThreads / 32;
+    return (int)std::max<int64_t>(1, std::min<int64_t>((tasks + per - 1) / per, 2 * (int64_t)num_sms));
 }
 
 }  // namespace
@@ -395,11 +498,8 @@ cudaError_t launch_norm_rope_inline(const NormRopeInlineArgs& a, int D, cudaStre
     return D == 128 ? launch_rows<128, true>(a, st) : launch_rows<64, true>(a, st);
 }
 
-int norm_rope_grad_ctas(int32_t n, int32_t heads, int D, int num_sms) {
-    const int task = D == 128 ? NormCfg<128>::kTaskRows : NormCfg<64>::kTaskRows;
-    const int64_t tasks = (int64_t)n * ((heads + task - 1) / task);
-    constexpr int per = kNormThreads / 32;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((tasks + per - 1) / per, 3 * (int64_t)num_sms));
+int norm_rope_grad_ctas(int32_t n, int32_t Hq, int32_t Hkv, int D, int num_sms) {
+    return D == 128 ? grad_ctas<128>(n, Hq, Hkv, num_sms) : grad_ctas<64>(n, Hq, Hkv, num_sms);
 }
 
 cudaError_t launch_norm_rope_grad(const NormRopeGradArgs& a, int D, cudaStream_t st) {

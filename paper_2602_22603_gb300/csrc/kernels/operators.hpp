@@ -60,7 +60,7 @@ struct NormRopeGradArgs {
 SQ_OPTIONAL cudaError_t launch_norm_rope(const NormRopeArgs& a, int D, bool store, cudaStream_t st);
 SQ_OPTIONAL cudaError_t launch_norm_rope_inline(const NormRopeInlineArgs& a, int D, cudaStream_t st);
 // CTAs of the backward kernel for n tokens of a geometry on a device of num_sms.
-SQ_OPTIONAL int norm_rope_grad_ctas(int32_t n, int32_t heads, int D, int num_sms);
+SQ_OPTIONAL int norm_rope_grad_ctas(int32_t n, int32_t Hq, int32_t Hkv, int D, int num_sms);
 SQ_OPTIONAL cudaError_t launch_norm_rope_grad(const NormRopeGradArgs& a, int D, cudaStream_t st);
 
 // ---- attention of query blocks ---------------------------------------------------
@@ -72,6 +72,8 @@ struct BlockArgs : PrefillArgs {
     const uint32_t* bits;   // [queries][n_words] drafted trees' visibility from the
                             // item's base on
     int32_t n_words;
+    int32_t n_ctas;         // CTAs launched (one-tile blocks are dealt out to them;
+                            // otherwise one for each item)
 };
 // Calls whose items' queries all fit in one query tile.
 struct BlockShortArgs : BlockArgs {

@@ -300,6 +300,8 @@ struct ItemRecord {
             p[2] = more[1];
         }
     }
+    // the CTA's next item (blocks of one query tile, dealt out beforehand)
+    __device__ __forceinline__ int next() const { return more[of_blocks<M> ? 1 : 0].w; }
     // slots of the item's sequence, and the row of its first query
     __device__ __forceinline__ int n(const PrefillArgs& a) const { return of_blocks<M> ? more[0].z : a.n; }
     __device__ __forceinline__ int q_row(const Item& it) const { return of_blocks<M> ? more[0].x : it.pos_lo; }
@@ -435,7 +437,15 @@ __device__ void prefill_produce(const CUtensorMap* pool_map, const CUtensorMap* 
     // queries over 33,001 tokens 841 -> 835 us); taken in with the last loads.
     ItemRecord<M> next = item;
     next.raw = make_int4(0, 0, -1, 0);
+    // (query blocks of one tile are dealt out to the CTAs beforehand: HBM bounds
+    // them, and an even share of the bytes beats handing out whole items)
+    constexpr bool kDealt = of_blocks<M> && one_tile<M>;
     auto request = [&]() {
+        if constexpr (kDealt) {
+            next.raw = make_int4(0, 0, -1, 0);
+            if (item.next() >= 0) next.read(a, item.next());
+            return;
+        }
         if (lane == 0) {
             mbar_arrive_expect_tx(sm.bar<D, M>(C::kBarClc), 16);
             clc_request(sm.base + C::kOffClc, sm.bar<D, M>(C::kBarClc));
@@ -443,6 +453,10 @@ __device__ void prefill_produce(const CUtensorMap* pool_map, const CUtensorMap* 
         asked = true;
     };
     auto take_next = [&](uint32_t parity) {
+        if constexpr (kDealt) {
+            first = load_rec(next.raw.y, next.raw.z, 0);
+            return;
+        }
         ok = __all_sync(0xffffffffu, mbar_wait(sm.bar<D, M>(C::kBarClc), parity, abort_flag));
         if (!ok) return;
         asked = false;
@@ -470,6 +484,19 @@ __device__ void prefill_produce(const CUtensorMap* pool_map, const CUtensorMap* 
             request();
             take_next(clc_parity);
         }
+        // pages of fewer than 64 tokens: a lane issues one box of one of the two
+        // loads; its page is read a step ahead
+        auto piece_page = [&](int u) -> int32_t {
+            int j, kv;
+            load_of(u + (lane >> 4), T, it.dual, j, kv);
+            return (lane & 15) < n_pieces && j < T
+                       ? __ldg(&a.tile_pages[(size_t)(it.t0 + j) * n_pieces + (lane & 15)])
+                       : -1;
+        };
+        int32_t piece = -1;
+        if constexpr (of_blocks<M>) {
+            if (n_pieces > 2 && T > 0) piece = piece_page(u_early);
+        }
         int fill_b = 1;    // the next batch to read
         int merge_b = -1;  // the batch read into `pend`, not yet in place
         // only the sequence's last key tile has rows past its end
@@ -486,6 +513,10 @@ __device__ void prefill_produce(const CUtensorMap* pool_map, const CUtensorMap* 
             if (merge_b < 0 && fill_b * kBatch < T && jmax + 10 >= kBatch * fill_b) {
                 if ((lane >> 4) == (fill_b & 1)) pend = load_rec(it.t0, T, fill_b * kBatch);
                 merge_b = fill_b++;
+            }
+            const int32_t my_piece = piece;
+            if constexpr (of_blocks<M>) {
+                if (n_pieces > 2 && u0 + 2 < n_units) piece = piece_page(u0 + 2);
             }
             const uint32_t U0 = ub + u0;
             const uint32_t slot1 = slot0 + 1 == C::kSlots ? 0 : slot0 + 1;
@@ -542,34 +573,71 @@ __device__ void prefill_produce(const CUtensorMap* pool_map, const CUtensorMap* 
             } else {
                 // rows of the tile inside the sequence: the lower half's, then
                 // the upper half's
-                const int rows_b = key0b < n ? min(64, n - key0b) : 0;
-                const int rows = rows_b > 0 ? 64 + rows_b : min(64, n - key0);
-                const bool vfix = lane < 2 && kv == 1 && rows < kPrefillKeys;
-                if (lane < 2) {
-                    const int nv = (rows + br - 1) / br;  // boxes inside the sequence (a prefix)
-                    const uint32_t fb = vfix ? sm.bar<D, M>(C::kBarVfix) : sm.bar<D, M>(C::kBarFull + slot);
-                    mbar_arrive_expect_tx(fb, (uint32_t)nv * br * 128 * C::kColBlocks);
+                auto rows_of = [&](int k0, int k0b) {
+                    const int rows_b = k0b < n ? min(64, n - k0b) : 0;
+                    return rows_b > 0 ? 64 + rows_b : min(64, n - k0);
+                };
+                // lanes that issue a load whose V has rows past the end, the load
+                // (0 or 1) such a lane issues, its slot and its rows
+                uint32_t fix = 0;
+                int fslot = slot, r0 = 0, per_load = 1;
+                bool spread = false;
+                if constexpr (of_blocks<M>) spread = n_pieces > 2;
+                if (spread) {
+                    const int i = lane & 15, sl = lane < 16 ? slot0 : slot1;
+                    const int jx = lane < 16 ? j0 : j1, kvx = lane < 16 ? kv0 : kv1;
+                    const int k0 = __shfl_sync(0xffffffffu, rec.x, jx & 31);
+                    const int k0b = __shfl_sync(0xffffffffu, rec.w, jx & 31);
                     const int half = n_pieces / 2;
-#pragma unroll 1
-                    for (int i = 0; i < nv; ++i) {
-                        const int32_t page =
-                            i == 0
-                                ? pg0
-                                : (i == 1 ? pg1
-                                          : __ldg(&a.tile_pages[(size_t)(it.t0 + j) * n_pieces + i]));
-                        load_box(fb, i, i < half ? key0 + i * br : key0b + (i - half) * br,
-                                 checked(page));
+                    const int key = i < half ? k0 + i * br : k0b + (i - half) * br;
+                    r0 = rows_of(k0, k0b);
+                    fslot = sl;
+                    per_load = 16;
+                    const bool box = my_piece >= 0, vfix = kvx == 1 && r0 < kPrefillKeys;
+                    const uint32_t boxes = __ballot_sync(0xffffffffu, box) >> (lane & 16) & 0xffffu;
+                    const uint32_t fb = vfix ? sm.bar<D, M>(C::kBarVfix) : sm.bar<D, M>(C::kBarFull + sl);
+                    if (i == 0)
+                        mbar_arrive_expect_tx(fb, (uint32_t)__popc(boxes) * br * 128 * C::kColBlocks);
+                    __syncwarp();
+                    if (box) {
+                        const int row = (kvx ? a.Hkv + it.g : it.g) * a.P + (key & (a.P - 1));
+                        const int32_t page = checked(my_piece);
+#pragma unroll
+                        for (int cb = 0; cb < C::kColBlocks; ++cb)
+                            tma_load_4d(sm.base + C::kOffRing + sl * C::kSlotBytes + cb * C::kBlockBytes +
+                                            i * br * 128,
+                                        pool_map, fb, cb * 64, row, page, a.layer);
                     }
+                    fix = __ballot_sync(0xffffffffu, vfix && i == 0);
+                } else {
+                    r0 = rows_of(key0, key0b);
+                    const bool vfix = lane < 2 && kv == 1 && r0 < kPrefillKeys;
+                    if (lane < 2) {
+                        const int nv = (r0 + br - 1) / br;  // boxes inside the sequence (a prefix)
+                        const uint32_t fb = vfix ? sm.bar<D, M>(C::kBarVfix) : sm.bar<D, M>(C::kBarFull + slot);
+                        mbar_arrive_expect_tx(fb, (uint32_t)nv * br * 128 * C::kColBlocks);
+                        const int half = n_pieces / 2;
+#pragma unroll 1
+                        for (int i = 0; i < nv; ++i) {
+                            const int32_t page =
+                                i == 0
+                                    ? pg0
+                                    : (i == 1 ? pg1
+                                              : __ldg(&a.tile_pages[(size_t)(it.t0 + j) * n_pieces + i]));
+                            load_box(fb, i, i < half ? key0 + i * br : key0b + (i - half) * br,
+                                     checked(page));
+                        }
+                    }
+                    fix = __ballot_sync(0xffffffffu, vfix);
                 }
-                const uint32_t fix = __ballot_sync(0xffffffffu, vfix);
                 if (fix) {
                     // V of the last key tile: its rows past the sequence's end hold
                     // stale or never-written data.  Their weights are zero, but
                     // 0 * NaN is not, so zero those rows before the MMAs read the slot.
                     const int src = __ffs(fix) - 1;
-                    const int fslot = __shfl_sync(0xffffffffu, slot, src);
-                    const int r0 = __shfl_sync(0xffffffffu, rows, src);  // 1 .. 127
-                    tail_u = U0 + src;
+                    fslot = __shfl_sync(0xffffffffu, fslot, src);
+                    r0 = __shfl_sync(0xffffffffu, r0, src);  // 1 .. 127
+                    tail_u = U0 + src / per_load;
                     tail_open = true;
                     issued = U0 + 2;
                     if (lane == 0) ok = mbar_wait(sm.bar<D, M>(C::kBarVfix), n_fix & 1, abort_flag);
@@ -1248,11 +1316,11 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
         ph.par ^= kParX;
         tc_fence_after();
         const float mb = xchg[2 * row], lb = xchg[2 * row + 1];
-        const float M = fmaxf(m_run, mb);
-        wa = m_run == -INFINITY ? 0.f : exp2f(m_run - M);
-        wb = mb == -INFINITY ? 0.f : exp2f(mb - M);
+        const float m_top = fmaxf(m_run, mb);
+        wa = m_run == -INFINITY ? 0.f : exp2f(m_run - m_top);
+        wb = mb == -INFINITY ? 0.f : exp2f(mb - m_top);
         l = l * wa + lb * wb;
-        m_run = M;
+        m_run = m_top;
     }
     // the item again, from its slot
     const Item end = make_item<M>(a, item_read<D, M>(sm, k));

@@ -16,7 +16,7 @@ KEYS, ROWS, NO_KEYS, TWO, NO_TREE = 128, 128, 0x7fffffc0, 1 << 30, 0x7fffffff
 def plan(c, handles, n_q, parents=None, window=0, sinks=0, ctas=152, part_limit=1 << 27):
     L = hostlib.lib()
     arr = lambda x: (ctypes.c_int32 * max(1, len(x)))(*x)  # noqa: E731
-    info = (ctypes.c_int64 * 11)()
+    info = (ctypes.c_int64 * 12)()
     L.sqh_plan_blocks.argtypes = [ctypes.c_void_p] * 2 + [ctypes.c_int32] + [ctypes.c_void_p] * 2 + \
         [ctypes.c_int32] * 3 + [ctypes.c_int64] + [ctypes.c_void_p] * 7
     args = [c.h, arr(handles), len(handles), arr(n_q), None if parents is None else arr(parents), window,
@@ -24,7 +24,7 @@ def plan(c, handles, n_q, parents=None, window=0, sinks=0, ctas=152, part_limit=
     rc = L.sqh_plan_blocks(*args, *[None] * 6)
     if rc:
         return rc, None
-    names = "tiles items merges rows n_words n_pieces BP n_parts one unit_rows max_splits".split()
+    names = "tiles items merges rows n_words n_pieces BP n_parts one unit_rows max_splits n_ctas".split()
     p = dict(zip(names, list(info)))
     buf = {}
     queries = sum(n_q)
@@ -91,8 +91,9 @@ def check(c, P, G, Hkv, handles, n_q, parents=None, window=0, sinks=0, **kw):
         head, two = it[0] & (TWO - 1), bool(it[0] & TWO)
         assert 0 <= head < Hkv and two == (it[5] > BP) and 1 <= it[5] <= 2 * BP
         assert 0 <= it[1] and it[2] >= 1 and it[1] + it[2] <= len(p["tiles"])
-        assert last is None or it[2] <= last + 1   # longest first
-        last = it[2] if last is None else min(last, it[2])
+        if not p["one"]:
+            assert last is None or it[2] <= last + 1   # longest first
+            last = it[2] if last is None else min(last, it[2])
         unit = (it[4], it[5], head)
         for t in range(it[1], it[1] + it[2]):
             assert t not in cover.setdefault(unit, set())
@@ -130,6 +131,18 @@ def check(c, P, G, Hkv, handles, n_q, parents=None, window=0, sinks=0, **kw):
                     pg = int(p["tile_pages"][t, i])
                     assert pg == (tables[q][k // P] if k < ends[q] else -1)
     assert got == want
+    # the items of one-tile blocks are dealt out: every CTA's chain, each item once
+    if p["one"]:
+        ctas, seen = kw.get("ctas", 152), []
+        assert p["n_ctas"] <= ctas
+        for first in range(p["n_ctas"]):
+            i = first
+            while i >= 0:
+                seen.append(i)
+                i = int(p["items"][i, 11])
+        assert sorted(seen) == list(range(len(p["items"])))
+    else:
+        assert p["n_ctas"] == len(p["items"]) and (p["items"][:, 11] == -1).all()
     # every head the same tiles; partial results in bounds, each once, and merged
     for (q, m, head), tiles in cover.items():
         assert tiles == cover[(q, m, 0)] and len(cover) % Hkv == 0
@@ -208,3 +221,35 @@ def test_drafted_rows_across_a_partial_page_are_refused():
     # the last page holds 8 rows, the page before it lacks two
     assert plan(c, [h], [8], tree(random.Random(1), 8))[0] == 0
     assert plan(c, [h], [9], tree(random.Random(1), 9))[0] == -8
+
+
+@pytest.mark.parametrize("D,lengths,window", [
+    (128, [30000], 4096), (128, [30000] * 3, 0), (64, [200 * i + 7 for i in range(1, 49)], 4096),
+    (128, [60000 // i for i in range(1, 40)], 4096), (64, [5000] * 20, 128)])
+def test_even_shares(D, lengths, window):
+    """No CTA has much more than its share of the key tiles (a piece costs a few
+    tiles' worth more), and short units stay whole."""
+    c = hostlib.HostCache(1, 32, 8, D, 64, sum(n // 64 + 1 for n in lengths), max_seqs=64)
+    handles = [c.seq_new()[1] for _ in lengths]
+    for h, n in zip(handles, lengths):
+        assert c.append(h, n) == 0
+    rc, p = plan(c, handles, [1] * len(handles), window=window, sinks=4)
+    assert rc == 0 and p["one"]
+    fixed, load = (2 if D == 128 else 4), []
+    for i in range(p["n_ctas"]):
+        load.append(0)
+        while i >= 0:
+            load[-1] += int(p["items"][i, 2]) + fixed
+            i = int(p["items"][i, 11])
+    assert max(load) <= sum(load) / min(152, p["n_ctas"]) + 4 + 2 * fixed
+    if window == 128:
+        assert p["n_parts"] == 0
+
+
+def test_a_unit_of_more_shares_than_a_merge_takes():
+    c = hostlib.HostCache(1, 8, 1, 128, 256, 4000)
+    h = c.seq_new()[1]
+    assert c.append(h, 1000000) == 0
+    rc, p = plan(c, [h], [1])
+    assert rc == 0 and 50 < p["max_splits"] <= 64
+    assert p["items"][:, 2].max() <= 1.1 * len(p["tiles"]) / 60
