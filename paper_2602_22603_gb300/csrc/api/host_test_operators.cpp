@@ -39,4 +39,24 @@ int sqh_plan_blocks(void* c, const int32_t* handles, int32_t n_seqs, const int32
     return kOk;
 }
 
+// Plans windowed decode; layout and buffer as sqh_plan_decode's.
+int sqh_plan_window_decode(void* c, const int32_t* handles, int32_t n_seqs, int32_t n_ctas,
+                           int32_t window, int32_t n_sink, int64_t* layout_out, uint8_t* buf,
+                           int64_t buf_bytes) {
+    HostCache* h = static_cast<HostCache*>(c);
+    DecodePlanHost p;
+    const int rc = plan_window_decode(*h, handles, n_seqs, n_ctas, window, n_sink, &p);
+    if (rc != kOk) return rc;
+    const DecodePlanLayout L = plan_layout(p, n_seqs, h->geom().Hkv);
+    const int64_t v[] = {L.segs, L.items, L.cta_begin, L.page_ids, L.comb_off, L.arrive, L.total,
+                         L.n_segs, L.n_items, L.n_ctas, L.n_page_ids, L.n_comb_keys, L.n_comb_ent,
+                         p.unique_tokens, p.logical_tokens, (int64_t)sizeof(DecodeSeg), L.page_fill};
+    std::memcpy(layout_out, v, sizeof v);
+    if (buf) {
+        if (buf_bytes < L.total) return kInvalidArg;
+        plan_serialize(p, L, buf);
+    }
+    return kOk;
+}
+
 }  // extern "C"

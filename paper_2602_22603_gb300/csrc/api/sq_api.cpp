@@ -50,6 +50,7 @@ struct WriteTickets {
 struct PlanEntry {
     bool valid = false;
     int32_t n_ctas = 0;
+    int32_t window = 0, n_sink = 0;  // window 0: all rows
     std::vector<int32_t> handles;
     std::vector<uint64_t> versions;
     DecodePlanLayout lay{};
@@ -57,7 +58,8 @@ struct PlanEntry {
     int32_t first_busy_cta = 0;  // lowest CTA with work (target of the test hook)
     WriteTickets writes;
     // per call-local sequence: the segment holding its last page when that
-    // segment has it alone (else -1), the slot-space start of that run, and
+    // segment has it alone (else -1; a window's is never listed: an append moves
+    // it), the slot-space start of that run, and
     // the last page's entry in page_fill (plans with page fills)
     std::vector<int32_t> tail_seg, tail_base, tail_fill;
     uint8_t* d_plan = nullptr;
@@ -973,11 +975,11 @@ static bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
     return na > 0 && nb > 0 && x < y + nb && y < x + na;
 }
 
-int sq_decode_attention(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t layer,
-                        const void* q, void* out, int32_t out_dtype, float sm_scale,
-                        void* stream) {
-    TraceRange trace_("sq_decode_attention");
-    if (!c) return SQ_ERR_BAD_HANDLE;
+// Decode attention of one token each over all rows (window 0), or over the last
+// `window` and the first n_sink.
+static int decode_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t layer, const void* q,
+                       void* out, int32_t out_dtype, float sm_scale, int32_t window, int32_t n_sink,
+                       void* stream) {
     const Geometry& g = c->g;
     if (!seqs || n_seqs < 1 || n_seqs > g.max_seqs || !q || !out) return SQ_ERR_INVALID_ARG;
     if (layer < 0 || layer >= g.L) return SQ_ERR_INVALID_ARG;
@@ -999,6 +1001,7 @@ int sq_decode_attention(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t
     PlanEntry* hit = nullptr;
     for (auto& p : c->plans) {
         if (!p.valid || p.n_ctas != c->decode_ctas || (int32_t)p.handles.size() != n_seqs) continue;
+        if (p.window != window || p.n_sink != n_sink) continue;
         bool same = true;
         for (int32_t i = 0; i < n_seqs && same; ++i)
             same = p.handles[i] == seqs[i] && p.versions[i] == c->host->seq(seqs[i])->version;
@@ -1015,7 +1018,8 @@ int sq_decode_attention(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t
     bool plan_ready = false;
     if (!hit) {
         DecodePlanHost plan;
-        int rc = plan_decode(*c->host, seqs, n_seqs, c->decode_ctas, &plan);
+        int rc = window > 0 ? plan_window_decode(*c->host, seqs, n_seqs, c->decode_ctas, window, n_sink, &plan)
+                            : plan_decode(*c->host, seqs, n_seqs, c->decode_ctas, &plan);
         if (rc != SQ_OK) return rc;
         DecodePlanLayout lay = plan_layout(plan, n_seqs, g.Hkv);
         // least recently used entry
@@ -1059,6 +1063,8 @@ int sq_decode_attention(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t
         c->stats.decode_plans_built += 1;
         victim->valid = true;
         victim->n_ctas = c->decode_ctas;
+        victim->window = window;
+        victim->n_sink = n_sink;
         victim->handles.assign(seqs, seqs + n_seqs);
         victim->versions.resize(n_seqs);
         for (int32_t i = 0; i < n_seqs; ++i) victim->versions[i] = c->host->seq(seqs[i])->version;
@@ -1134,6 +1140,14 @@ int sq_decode_attention(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t
     c->stats.decode_logical_bytes += hit->logical_tokens * g.token_layer_bytes();
     c->stats.decode_unique_bytes += hit->unique_tokens * g.token_layer_bytes();
     return SQ_OK;
+}
+
+int sq_decode_attention(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t layer,
+                        const void* q, void* out, int32_t out_dtype, float sm_scale,
+                        void* stream) {
+    TraceRange trace_("sq_decode_attention");
+    if (!c) return SQ_ERR_BAD_HANDLE;
+    return decode_impl(c, seqs, n_seqs, layer, q, out, out_dtype, sm_scale, 0, 0, stream);
 }
 
 }  // extern "C"

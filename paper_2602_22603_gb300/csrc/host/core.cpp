@@ -525,6 +525,95 @@ void evict_chunks(const std::vector<int32_t>& window_tile, int32_t n_tiles, int3
 // ---------------------------------------------------------------------------
 // decode planning
 
+// The second half of a decode plan: the stages of out->segs (seg_fam: the family
+// of each; seg_first: its first stage, empty: 0) dealt out to the CTAs.
+static int deal_decode_stages(const Geometry& g, int32_t n_seqs, int32_t n_ctas,
+                              const std::vector<int32_t>& seg_fam, const std::vector<int32_t>& seg_first,
+                              DecodePlanHost* out) {
+    // (segment, head) units and an even split of their cost over the
+    // persistent CTAs.  On the cost line a unit occupies its start-up cost
+    // followed by its stages; an item is the overlap of a
+    // CTA's share with a unit's stages.  Units go family by family, head by
+    // head, each family's segments in tree order: a fork's own short tail
+    // follows the shared prefix of the same head, so it lands in the CTA that
+    // finishes that prefix instead of in a pile of tails at the end of the
+    // line (whose one CTA would then merge every fork's rows alone).
+    const int32_t n_segs = (int32_t)out->segs.size();
+    auto first_stage = [&](int32_t seg) { return seg_first.empty() ? 0 : seg_first[seg]; };
+    std::vector<int32_t> by_fam(n_segs);
+    for (int32_t s = 0; s < n_segs; ++s) by_fam[s] = s;
+    std::stable_sort(by_fam.begin(), by_fam.end(),
+                     [&](int32_t x, int32_t y) { return seg_fam[x] < seg_fam[y]; });
+    std::vector<int32_t> unit_seg, unit_head;
+    for (int32_t b = 0; b < n_segs;) {
+        int32_t e = b;
+        while (e < n_segs && seg_fam[by_fam[e]] == seg_fam[by_fam[b]]) ++e;
+        for (int32_t h = 0; h < g.Hkv; ++h)
+            for (int32_t x = b; x < e; ++x) {
+                unit_seg.push_back(by_fam[x]);
+                unit_head.push_back(h);
+            }
+        b = e;
+    }
+    std::vector<int64_t> unit_start;  // where the unit's stages begin on the cost line
+    std::vector<int64_t> unit_end;
+    int64_t total = 0, stages = 0;
+    for (size_t v = 0; v < unit_seg.size(); ++v) {
+        const int32_t n = ceil_div(out->segs[unit_seg[v]].n_tok, kStageTokens) - first_stage(unit_seg[v]);
+        total += n <= kShortUnitStages ? kDecodeShortUnitCost : kDecodeUnitCost;
+        unit_start.push_back(total);
+        total += n;
+        stages += n;
+        unit_end.push_back(total);
+    }
+    const int64_t n_units = (int64_t)unit_start.size();
+    const int32_t ctas = (int32_t)std::min<int64_t>(n_ctas, stages);
+    out->n_ctas = ctas;
+    out->cta_begin.resize(ctas + 1);
+    int64_t u = 0;
+    for (int32_t cta = 0; cta < ctas; ++cta) {
+        const int64_t b = total * cta / ctas, e = total * (cta + 1) / ctas;
+        out->cta_begin[cta] = (int32_t)out->items.size();
+        while (u < n_units && unit_end[u] <= b) ++u;
+        for (int64_t v = u; v < n_units && (v == 0 ? 0 : unit_end[v - 1]) < e; ++v) {
+            const int64_t lo = std::max(b, unit_start[v]), hi = std::min(e, unit_end[v]);
+            if (hi <= lo) continue;
+            DecodeItem it;
+            std::memset(&it, 0, sizeof it);
+            it.seg = unit_seg[v];
+            it.head = unit_head[v];
+            it.s0 = (int32_t)(lo - unit_start[v]) + first_stage(it.seg);
+            it.s1 = (int32_t)(hi - unit_start[v]) + first_stage(it.seg);
+            out->items.push_back(it);
+        }
+    }
+    out->cta_begin[ctas] = (int32_t)out->items.size();
+
+    // partial entries per (sequence, KV head), contiguous, in item order
+    const int32_t keys = n_seqs * g.Hkv;
+    out->comb_off.assign(keys + 1, 0);
+    for (const DecodeItem& it : out->items) {
+        const DecodeSeg& s = out->segs[it.seg];
+        for (int32_t j = 0; j < s.n_grp; ++j) ++out->comb_off[s.grp_seq[j] * g.Hkv + it.head + 1];
+    }
+    for (int32_t k = 0; k < keys; ++k) {
+        // the kernel counts a run's entries in 16 bits
+        if (out->comb_off[k + 1] > kMaxRunEntries) return kCapacity;
+        out->comb_off[k + 1] += out->comb_off[k];
+    }
+    std::vector<int32_t> fill(out->comb_off.begin(), out->comb_off.end() - 1);
+    for (DecodeItem& it : out->items) {
+        const DecodeSeg& s = out->segs[it.seg];
+        it.sole = 0;
+        for (int32_t j = 0; j < s.n_grp; ++j) {
+            const int32_t key = s.grp_seq[j] * g.Hkv + it.head;
+            it.ent[j] = fill[key]++;
+            if (out->comb_off[key + 1] - out->comb_off[key] == 1) it.sole |= 1 << j;
+        }
+    }
+    return kOk;
+}
+
 int plan_decode(const HostCache& c, const int32_t* handles, int32_t n_seqs,
                 int32_t n_ctas, DecodePlanHost* out) {
     *out = DecodePlanHost();
@@ -642,87 +731,68 @@ int plan_decode(const HostCache& c, const int32_t* handles, int32_t n_seqs,
         for (auto it = next.rbegin(); it != next.rend(); ++it) stack.push_back(std::move(*it));
     }
 
-    // (segment, head) units and an even split of their cost over the
-    // persistent CTAs.  On the cost line a unit occupies its start-up cost
-    // followed by its stages; an item is the overlap of a
-    // CTA's share with a unit's stages.  Units go family by family, head by
-    // head, each family's segments in tree order: a fork's own short tail
-    // follows the shared prefix of the same head, so it lands in the CTA that
-    // finishes that prefix instead of in a pile of tails at the end of the
-    // line (whose one CTA would then merge every fork's rows alone).
-    const int32_t n_segs = (int32_t)out->segs.size();
-    std::vector<int32_t> by_fam(n_segs);
-    for (int32_t s = 0; s < n_segs; ++s) by_fam[s] = s;
-    std::stable_sort(by_fam.begin(), by_fam.end(),
-                     [&](int32_t x, int32_t y) { return seg_fam[x] < seg_fam[y]; });
-    std::vector<int32_t> unit_seg, unit_head;
-    for (int32_t b = 0; b < n_segs;) {
-        int32_t e = b;
-        while (e < n_segs && seg_fam[by_fam[e]] == seg_fam[by_fam[b]]) ++e;
-        for (int32_t h = 0; h < g.Hkv; ++h)
-            for (int32_t x = b; x < e; ++x) {
-                unit_seg.push_back(by_fam[x]);
-                unit_head.push_back(h);
-            }
-        b = e;
-    }
-    std::vector<int64_t> unit_start;  // where the unit's stages begin on the cost line
-    std::vector<int64_t> unit_end;
-    int64_t total = 0, stages = 0;
-    for (size_t v = 0; v < unit_seg.size(); ++v) {
-        const int32_t n = ceil_div(out->segs[unit_seg[v]].n_tok, kStageTokens);
-        total += n <= kShortUnitStages ? kDecodeShortUnitCost : kDecodeUnitCost;
-        unit_start.push_back(total);
-        total += n;
-        stages += n;
-        unit_end.push_back(total);
-    }
-    const int64_t n_units = (int64_t)unit_start.size();
-    const int32_t ctas = (int32_t)std::min<int64_t>(n_ctas, stages);
-    out->n_ctas = ctas;
-    out->cta_begin.resize(ctas + 1);
-    int64_t u = 0;
-    for (int32_t cta = 0; cta < ctas; ++cta) {
-        const int64_t b = total * cta / ctas, e = total * (cta + 1) / ctas;
-        out->cta_begin[cta] = (int32_t)out->items.size();
-        while (u < n_units && unit_end[u] <= b) ++u;
-        for (int64_t v = u; v < n_units && (v == 0 ? 0 : unit_end[v - 1]) < e; ++v) {
-            const int64_t lo = std::max(b, unit_start[v]), hi = std::min(e, unit_end[v]);
-            if (hi <= lo) continue;
-            DecodeItem it;
-            std::memset(&it, 0, sizeof it);
-            it.seg = unit_seg[v];
-            it.head = unit_head[v];
-            it.s0 = (int32_t)(lo - unit_start[v]);
-            it.s1 = (int32_t)(hi - unit_start[v]);
-            out->items.push_back(it);
-        }
-    }
-    out->cta_begin[ctas] = (int32_t)out->items.size();
+    return deal_decode_stages(g, n_seqs, n_ctas, seg_fam, {}, out);
+}
 
-    // partial entries per (sequence, KV head), contiguous, in item order
-    const int32_t keys = n_seqs * g.Hkv;
-    out->comb_off.assign(keys + 1, 0);
-    for (const DecodeItem& it : out->items) {
-        const DecodeSeg& s = out->segs[it.seg];
-        for (int32_t j = 0; j < s.n_grp; ++j) ++out->comb_off[s.grp_seq[j] * g.Hkv + it.head + 1];
-    }
-    for (int32_t k = 0; k < keys; ++k) {
-        // the kernel counts a run's entries in 16 bits
-        if (out->comb_off[k + 1] > kMaxRunEntries) return kCapacity;
-        out->comb_off[k + 1] += out->comb_off[k];
-    }
-    std::vector<int32_t> fill(out->comb_off.begin(), out->comb_off.end() - 1);
-    for (DecodeItem& it : out->items) {
-        const DecodeSeg& s = out->segs[it.seg];
-        it.sole = 0;
-        for (int32_t j = 0; j < s.n_grp; ++j) {
-            const int32_t key = s.grp_seq[j] * g.Hkv + it.head;
-            it.ent[j] = fill[key]++;
-            if (out->comb_off[key + 1] - out->comb_off[key] == 1) it.sole |= 1 << j;
+int plan_window_decode(const HostCache& c, const int32_t* handles, int32_t n_seqs, int32_t n_ctas,
+                       int32_t window, int32_t n_sink, DecodePlanHost* out) {
+    *out = DecodePlanHost();
+    const Geometry& g = c.geom();
+    if (n_seqs < 1 || !handles || n_ctas < 1 || window < 1 || n_sink < 0) return kInvalidArg;
+    const int32_t P = g.P;
+    std::vector<int32_t> seg_fam, seg_first;
+    for (int32_t i = 0; i < n_seqs; ++i) {
+        const Seq* s = c.seq(handles[i]);
+        if (!s) return kBadHandle;
+        if (s->n < 1) return kInvalidArg;
+        for (int32_t j = 0; j < i; ++j)
+            if (handles[j] == handles[i]) return kInvalidArg;
+        // rows [0, sinks) and [low, n); sinks that reach the window join it
+        int32_t low = std::max(0, s->n - window), sinks = n_sink;
+        if (sinks >= low) low = sinks = 0;
+        out->logical_tokens += sinks + s->n - low;
+        DecodeSeg seg;
+        auto open = [&]() {
+            std::memset(&seg, 0, sizeof seg);
+            seg.page_off = (int32_t)out->page_ids.size();
+            seg.n_grp = 1;
+            seg.grp_seq[0] = i;
+        };
+        auto close = [&](int32_t first_stage) {
+            seg.grp_lim[0] = seg.n_tok;
+            out->segs.push_back(seg);
+            seg_fam.push_back(i);
+            seg_first.push_back(first_stage);
+        };
+        // the pages that hold a sink (its first `a` rows) or a row of the window
+        // (from row b on), in order
+        auto add = [&](int32_t q, int32_t a, int32_t b) {
+            out->page_ids.push_back(s->pages[q]);
+            out->page_fill.push_back(s->fill[q] | b << kFillFirstBit | a << kFillSinkBit);
+            seg.n_tok = seg.n_pages++ * P + (b < s->fill[q] ? s->fill[q] : a);
+        };
+        open();
+        // a stage spans pages of at most kStageTokens tokens; where it lies inside
+        // one, the window gets a run of its own that starts at its first stage
+        const bool apart = sinks > 0 && P > kStageTokens;
+        int32_t skipped = 0, row = 0;
+        for (int32_t q = 0; q < (int32_t)s->pages.size(); row += s->fill[q++]) {
+            const int32_t a = std::min(std::max(sinks - row, 0), s->fill[q]);
+            const int32_t b = std::min(std::max(low - row, 0), s->fill[q]);
+            if (a > 0) add(q, a, apart ? s->fill[q] : b);
+            if (apart && a > 0 && row + s->fill[q] >= sinks) {
+                close(0);
+                open();
+            }
+            if (b < s->fill[q] && (apart || a == 0)) {
+                if (seg.n_pages == 0) skipped = b / kStageTokens;
+                add(q, 0, b);
+            }
         }
+        close(skipped);
     }
-    return kOk;
+    out->unique_tokens = out->logical_tokens;
+    return deal_decode_stages(g, n_seqs, n_ctas, seg_fam, seg_first, out);
 }
 
 static int64_t align16(int64_t x) { return (x + 15) & ~int64_t(15); }

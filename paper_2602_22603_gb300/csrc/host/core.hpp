@@ -214,9 +214,9 @@ struct DecodePlanHost {
     std::vector<DecodeItem> items;
     std::vector<int32_t> cta_begin;   // n_ctas + 1
     std::vector<int32_t> page_ids;
-    // rows held by each page of page_ids; filled only when some sequence of
-    // the call has a partial page before its last (else every page is full
-    // up to the members' limits)
+    // rows held by each page of page_ids (for windows see kFillFirstBit); filled only for windows and when some sequence of the call has a
+    // partial page before its last (else every page is full up to the members'
+    // limits)
     std::vector<int32_t> page_fill;
     // partial entries of (sequence i, KV head h): [comb_off[k], comb_off[k + 1]),
     // k = i * Hkv + h, in item order
@@ -240,6 +240,12 @@ constexpr int32_t kMaxRunEntries = 65535;
 // stages, kDecodeShortUnitCost for a unit of at most kShortUnitStages.
 int plan_decode(const HostCache& c, const int32_t* handles, int32_t n_seqs,
                 int32_t n_ctas, DecodePlanHost* out);
+
+// The same for one token of each sequence that sees its last `window` rows (>= 1)
+// and the first n_sink: each sequence's segments are its own (the pages of its
+// sinks and of its window).
+int plan_window_decode(const HostCache& c, const int32_t* handles, int32_t n_seqs, int32_t n_ctas,
+                       int32_t window, int32_t n_sink, DecodePlanHost* out);
 
 // Serialises a plan into one buffer (8-byte aligned arrays).
 DecodePlanLayout plan_layout(const DecodePlanHost& p, int32_t n_seqs,

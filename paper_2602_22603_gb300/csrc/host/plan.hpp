@@ -63,6 +63,10 @@ struct DecodeSeg {
                                       // others' limit is the whole run)
 };
 
+// A page's entry among a plan's fills: the rows it holds; for a window also the
+// first of them in the window (0: all) and how many at its start are sinks.
+constexpr int32_t kFillFirstBit = 10, kFillSinkBit = 20, kFillMask = 1023;
+
 // A contiguous range of stages of one (segment, KV head) — one partial result
 // per group member.  Member j's G rows go to partial entry ent[j]; the entries
 // of one (sequence, KV head) are contiguous, so that its merge reads them

@@ -49,6 +49,10 @@
 // first items before the dependency wait, and stages in pages that no running
 // work writes are loaded before it.
 //
+// Windows (single tokens of sq_window_attention): a sequence's pages are then the
+// sinks' and the window's, the rows before the window's first masked the way a
+// page's unused slots are.
+//
 // Page fills: after a ragged eviction a page may hold fewer rows than it has
 // slots (its rows first, then zeros or rows once appended).  Stages are in
 // slot space (page index x P + slot); the plan then carries every page's
@@ -422,13 +426,18 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
                 const int t0 = s * kStageTokens + w4 * 16;  // segment slot position
                 const int pq = t0 >> (__ffs(P) - 1);
                 const int f0 = pq < seg->n_pages ? __ldg(&a.page_fill[seg->page_off + pq]) : 0;
+                auto rows = [](int f, int from, int most) {
+                    // the first rows up to x, of `most` from row `from` on
+                    auto up_to = [&](int x) { return (1u << min(max(x - from, 0), most)) - 1u; };
+                    return (up_to(f & kFillMask) & ~up_to(f >> kFillFirstBit & kFillMask)) |
+                           up_to(f >> kFillSinkBit);
+                };
                 if (P >= 16) {
-                    const int v = min(max(f0 - (t0 & (P - 1)), 0), 16);
-                    vm = (uint32_t)((1u << v) - 1u);   // v = 16 gives 0xffff
+                    vm = rows(f0, t0 & (P - 1), 16);
                 } else {
                     const int f1 =
                         pq + 1 < seg->n_pages ? __ldg(&a.page_fill[seg->page_off + pq + 1]) : 0;
-                    vm = ((1u << min(f0, 8)) - 1u) | (((1u << min(f1, 8)) - 1u) << 8);
+                    vm = rows(f0, 0, 8) | rows(f1, 0, 8) << 8;
                 }
             }
             if (!dead) {

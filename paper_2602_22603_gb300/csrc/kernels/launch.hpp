@@ -20,8 +20,9 @@ struct DecodeArgs {
     const DecodeItem* items;
     const int32_t* cta_begin;
     const int32_t* page_ids;
-    // rows held by each page of page_ids, or null when every page of the
-    // call is full up to the members' limits (no sequence with partial pages)
+    // rows held by each page of page_ids (for windows see kFillFirstBit), or null
+    // when every page of the call is full up to the members' limits (no sequence
+    // with partial pages)
     const int32_t* page_fill;
     const int32_t* comb_off;    // [n_seqs * Hkv + 1] partial entries of each (sequence, KV head)
     unsigned int* arrive;       // [n_seqs * Hkv] arrival counts, zero between calls

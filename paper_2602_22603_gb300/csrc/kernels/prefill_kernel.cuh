@@ -1129,8 +1129,16 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
     // weight of a row is then more often exactly 1, and not rounded (with 2^16
     // the log-sum-exp of 3 queries over 9,892 tokens was off by 2.4e-5 instead
     // of 1.3e-5 of its size).
-    const float accept = __all_sync(0xffffffffu, valid) ? 65536.f : 256.f;
-    float m_run = -INFINITY, l = 0.f;
+    //
+    // A block of queries has few key tiles, often the sinks' few keys first, whose
+    // maxima the window's raise: there a row starts at a maximum of 0 and a tile's
+    // weights are accepted while its sum stays below 2^40 (and above 2^-40 where
+    // they are the row's first), since a weight rounded to bf16 keeps its 8 bits at
+    // any size and sums are fp32.  16,384 queries at a window of 1,024 with 4 sinks,
+    // logits to 2^20: 430 -> 262 us a layer, half of it the maxima of first tiles.
+    constexpr float kLeast = 0x1p-40f;
+    const float accept = of_blocks<M> ? 0x1p40f : __all_sync(0xffffffffu, valid) ? 65536.f : 256.f;
+    float m_run = of_blocks<M> ? 0.f : -INFINITY, l = 0.f;
     // {first keys, flags} of the next key tile; its visibility bits are read
     // only where a tile is masked (they would hold eight registers of the loop)
     const PrefillTile* tp = a.tiles + t0 + kfirst;
@@ -1163,6 +1171,7 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
         // Nothing is stored: S stays intact until the weights are accepted.
         const uint64_t sc2 = f2pack(sc, sc);
         uint32_t wt[2][32];
+        uint32_t seen = unmasked ? 1u : 0u;  // (blocks) the row sees some key of the tile
         auto weights = [&](float m, float& tile_sum) {
             const float nmu = m == -INFINITY ? 0.f : -m;
             const uint64_t nmu2 = f2pack(nmu, nmu);
@@ -1179,6 +1188,7 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
                         const int ww = 2 * hh + w;
                         const uint32_t mw =
                             __ldg(&tp->vis[ww]) & mask.word((ww < 2 ? wk.x : wb_) + 32 * (ww & 1));
+                        if constexpr (of_blocks<M>) seen |= mw;
 #pragma unroll
                         for (int c = 0; c < 32; ++c)
                             if (!((mw >> c) & 1u)) x[32 * w + c] = 0xff800000u;  // -inf
@@ -1204,7 +1214,11 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
         // one by more than 2^8.
         float mt = -INFINITY, tsum = 0.f;
         bool done = false;
-        if (__all_sync(0xffffffffu, m_run != -INFINITY || !valid)) {
+        if constexpr (of_blocks<M>) {
+            weights(m_run, tsum);
+            done = !__any_sync(0xffffffffu,
+                               valid && (tsum > accept || (l == 0.f && seen && tsum < kLeast)));
+        } else if (__all_sync(0xffffffffu, m_run != -INFINITY || !valid)) {
             weights(m_run, tsum);
             done = !__any_sync(0xffffffffu, valid && tsum > accept);
         }
@@ -1243,10 +1257,11 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
         if (done) {
             l += tsum;
         } else {
-            const bool need = valid && mt > m_run + 8.f;
+            // (a block's row without weights yet may also come down)
+            const bool need = valid && (mt > m_run + 8.f || (of_blocks<M> && l == 0.f && seen && mt < m_run - 8.f));
             float alpha = 1.f;
             if (need) {
-                alpha = exp2f(m_run - mt);
+                alpha = of_blocks<M> && l == 0.f ? 1.f : exp2f(m_run - mt);
                 m_run = mt;
                 l *= alpha;
             }
@@ -1294,6 +1309,7 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
         if (!warp_wait(sm.bar<D, M>(C::kBarO + t), (ph.par & kParO) != 0, abort_flag)) return false;
         ph.par ^= kParO;
     }
+    if (of_blocks<M> && l == 0.f) m_run = -INFINITY;  // no key seen
     // dual-key mode: tile b hands its (max, normaliser) to tile a, which
     // merges the two partial results of each row (weights 2^(m_t - max)) and
     // reads O_b, complete by tile b's wait above

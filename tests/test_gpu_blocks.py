@@ -126,6 +126,89 @@ def test_single_tokens(Hq, Hkv, D, P, window, sinks):
 
 
 @pytest.mark.parametrize("Hq,Hkv,D,P", GEOMETRIES)
+@pytest.mark.parametrize("window,sinks", [(1, 0), (5, 1), (64, 4), (65, 64), (200, 130), (0, 0), (4000, 7)])
+def test_single_tokens_without_log_sums(Hq, Hkv, D, P, window, sinks):
+    """Without log-sum-exps single tokens take the decode kernel: the same rows,
+    within both kernels' budgets; sequences without a query in between."""
+    b = Batch(Hq, Hkv, D, P, [1, 63, 64, 65, 129, 700, 3000], seed=window + P)
+    q, out, _ = b.check(None, window=window, sinks=sinks)
+    got = torch.full_like(out, float("nan"))
+    kw = dict(out_dtype=sq.SQ_OUT_F32, sm_scale=D ** -0.5)
+    b.c.window_attention(b.h, None, 0, q, got, window, sinks, **kw)
+    some = torch.full_like(out[:3], float("nan"))
+    b.c.window_attention(b.h, [1, 0, 0, 1, 0, 1, 0], 0, q[[0, 3, 5]], some, window, sinks, **kw)
+    assert b.c.sync_status() == sq.SQ_OK
+    assert torch.isfinite(got).all()
+    for i, h in enumerate(b.h):
+        k, v = b.rows(h)
+        see = torch.arange(k.shape[0], device="cuda")
+        see = (see >= k.shape[0] - (window or 1 << 30)) | (see < sinks)
+        G = Hq // Hkv
+        z = torch.einsum("ghd,tgd->ght", q[i].double().view(Hkv, G, -1), k[see]) * D ** -0.5
+        w = torch.softmax(z, -1)
+        o = torch.einsum("ght,tgd->ghd", w, v[see]).reshape(Hq, D)
+        dev = torch.stack([torch.einsum("ht,htd->hd", w[g], (v[see][:, g][None] - o.view(Hkv, G, D)[g][:, None]).abs())
+                           for g in range(Hkv)]).reshape(Hq, D)
+        absv = torch.einsum("ght,tgd->ghd", w, v[see].abs()).reshape(Hq, D)
+        budget = decode_budget(dev.cpu().numpy(), absv.cpu().numpy(), int(see.sum()))
+        assert_budget(got[i], o.cpu().numpy(), budget)
+        if i in (0, 3, 5):
+            assert_budget(some[(0, 3, 5).index(i)], o.cpu().numpy(), budget)
+    b.c.close()
+
+
+def test_windows_follow_appended_rows():
+    """Decode steps: the window moves with every row, also where a plain decode
+    plan of the same sequences is kept, and on another stream."""
+    b = Batch(8, 2, 128, 64, [300, 64, 1000], seed=77)
+    for step in range(5):
+        for h in b.h:
+            b.append(h, 1)
+        q = b.queries(3)
+        for window, sinks in ((100, 4), (100, 0), (0, 0), (64, 4)):
+            got, ref = (torch.empty(3, 8, 128, device="cuda") for _ in range(2))
+            kw = dict(out_dtype=sq.SQ_OUT_F32, sm_scale=0.1)
+            b.c.window_attention(b.h, None, 0, q, got, window, sinks, **kw)
+            b.c.window_attention(b.h, None, 0, q, ref, window, sinks, lse=torch.empty(3, 8, device="cuda"), **kw)
+            torch.cuda.synchronize()
+            assert (got - ref).abs().max() <= 1e-2
+        b.c.decode_attention(b.h, 0, q, ref, sq.SQ_OUT_F32, 0.1)
+        b.c.window_attention(b.h, None, 0, q, got, 0, 9, **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(got, ref)
+    assert b.c.sync_status() == sq.SQ_OK
+    b.c.close()
+
+
+@pytest.mark.parametrize("value", [-300.0, -90.0, 60.0, 400.0])
+def test_logits_far_from_zero(value):
+    """Rows whose logits all lie far below or above zero, and rows that a tile
+    without visible keys comes before."""
+    b = Batch(8, 2, 64, 64, [900], seed=3)
+    page, slot = row_slots(b.c, b.h[0])
+    k = b.pool[0, page, 0, :, slot]
+    k[..., 0] = 8.0
+    b.pool[0, page, 0, :, slot] = k
+    q = b.queries(200)
+    q[:, :, 0] = value
+    parents = None
+    for window, sinks in ((100, 0), (100, 3), (0, 0)):
+        out, lse = b.call([200], q, parents, window, sinks, scale=0.125)
+        assert b.c.sync_status() == sq.SQ_OK
+        kk, vv = b.rows(b.h[0])
+        at = torch.arange(900, device="cuda")
+        see = (at[None] <= at[700:, None]) & ((at[None] > at[700:, None] - (window or 9999)) | (at[None] < sinks))
+        z = torch.einsum("nghd,tgd->nght", q.double().view(200, 2, 4, 64), kk) * 0.125
+        z = z.masked_fill(~see[:, None, None], -math.inf)
+        w = torch.softmax(z, -1)
+        o = torch.einsum("nght,tgd->nghd", w, vv).reshape(200, 8, 64)
+        assert (out.double() - o).abs().max() <= 1e-2
+        ref = torch.logsumexp(z, -1).reshape(200, 8)
+        assert ((lse.double() - ref).abs() <= LSE_ABS + ref.abs() * 2.0 ** -20).all()
+    b.c.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,P", GEOMETRIES)
 @pytest.mark.parametrize("window,sinks", [(3, 2), (64, 0), (100, 70), (0, 0)])
 def test_prompts_and_tokens_together(Hq, Hkv, D, P, window, sinks):
     b = Batch(Hq, Hkv, D, P, [300, 1, 517, 90, 128], seed=window + D + 1)
