@@ -221,46 +221,56 @@ def _spans(spans):
 
 
 def _ints(x):
-    """(address, what keeps it alive) of host int32 values: a sequence of them,
-    an int32 buffer (array.array, numpy) or a ctypes array; None stays None."""
+    """(address, what keeps it alive) of host int32 values: a sequence of them, an
+    array.array("i") or a ctypes int32 array; None stays None."""
     if x is None:
         return None, None
-    if isinstance(x, ctypes.Array):
-        return ctypes.addressof(x), x
-    if not (isinstance(x, array.array) and x.itemsize == 4):
-        x = array.array("i", x)
+    if x.__class__ is not list and x.__class__ is not tuple:
+        if isinstance(x, ctypes.Array):
+            return ctypes.addressof(x), x
+        if isinstance(x, array.array) and x.typecode == "i":
+            return x.buffer_info()[0], x
+    x = array.array("i", x)
     return x.buffer_info()[0], x
 
 
-def _rows(x, heads, dim, name):
-    """(address, elements between tokens) of a [tokens, heads, dim] tensor whose
-    rows are contiguous; an address alone stands for a contiguous one."""
-    if isinstance(x, int):
-        return x, heads * dim
-    if x.dim() != 3 or x.shape[1:] != (heads, dim):
-        raise ValueError(f"{name}: [tokens, {heads}, {dim}] expected, not {list(x.shape)}")
-    if x.stride(2) != 1 or x.stride(1) != dim:
-        raise ValueError(f"{name}: the rows of a token must be contiguous")
-    _dtype(x, "bfloat16", name)
+# torch's types, once a call has tensors to check (their names cost a
+# microsecond a tensor to compare)
+_BF16 = _FLOAT = _INT = None
+
+
+def _types():
+    global _BF16, _FLOAT, _INT
+    import torch
+    _BF16, _FLOAT, _INT = torch.bfloat16, torch.float32, torch.int32
+
+
+def _wrong(name, want, x):
+    raise ValueError(f"{name}: {want} expected, not {x.dtype} {list(x.shape)} of strides {x.stride()}")
+
+
+def _rows(x, heads, dim, name, n=None):
+    """(address, elements between tokens, tokens) of a bfloat16 [tokens, heads,
+    dim] tensor whose rows are contiguous; an address alone stands for a
+    contiguous one of n tokens."""
+    if x.__class__ is int:
+        return x, heads * dim, n
+    shape, stride = x.shape, x.stride()
+    if (len(shape) != 3 or shape[1] != heads or shape[2] != dim or stride[2] != 1 or stride[1] != dim
+            or x.dtype is not _BF16 or (n is not None and shape[0] != n)):
+        _wrong(name, f"bfloat16 [{'tokens' if n is None else n}, {heads}, {dim}] of contiguous rows", x)
     # (one token has no distance to the next)
-    return int(x.data_ptr()), max(x.stride(0), heads * dim) if x.shape[0] > 1 else heads * dim
-
-
-def _dtype(x, want, name):
-    got = str(x.dtype).rpartition(".")[2]
-    if got != want:
-        raise ValueError(f"{name}: {want} expected, not {got}")
+    return x.data_ptr(), stride[0] if shape[0] > 1 else heads * dim, shape[0]
 
 
 def _flat(x, want, count, name):
-    """Address of a contiguous tensor of `count` elements (None and addresses as
-    they are)."""
-    if x is None or isinstance(x, int):
+    """Address of a contiguous tensor of `count` elements of a type (None and
+    addresses as they are)."""
+    if x is None or x.__class__ is int:
         return x
-    _dtype(x, want, name)
-    if not x.is_contiguous() or x.numel() != count:
-        raise ValueError(f"{name}: {count} contiguous elements expected, not {list(x.shape)}")
-    return int(x.data_ptr())
+    if x.dtype is not want or x.numel() != count or not x.is_contiguous():
+        _wrong(name, f"{count} contiguous elements of {want}", x)
+    return x.data_ptr()
 
 
 def norm_rope(rope=None, rot_dim=0, eps=1e-6, q_weight=None, k_weight=None,
@@ -268,21 +278,18 @@ def norm_rope(rope=None, rot_dim=0, eps=1e-6, q_weight=None, k_weight=None,
     """The parameters of the norms and the rotation: `rope` a float32 CUDA tensor
     [max_pos, rot_dim / 2, 2] of cosines and sines (rope_table makes one),
     weights bfloat16 or float32 tensors [head_dim] of one type, or None (ones)."""
+    _types()
     weights = [w for w in (q_weight, k_weight) if w is not None]
-    f32 = [str(w.dtype).endswith("float32") for w in weights]
-    for w, single in zip(weights, f32):
-        if not single:
-            _dtype(w, "bfloat16", "weight")
-        if not w.is_contiguous():
-            raise ValueError("weight: not contiguous")
-    if len(set(f32)) > 1:
-        raise ValueError("weights: both bfloat16 or both float32")
+    for w in weights:
+        if w.dtype not in (_BF16, _FLOAT) or w.dtype is not weights[0].dtype or not w.is_contiguous():
+            _wrong("weights", "contiguous, both bfloat16 or both float32", w)
+    f32 = bool(weights) and weights[0].dtype is _FLOAT
     max_pos = 0
     if rope is not None and rot_dim:
         max_pos = rope.shape[0]
-        _flat(rope, "float32", max_pos * rot_dim, "rope")
+        _flat(rope, _FLOAT, max_pos * rot_dim, "rope")
     p = sq_norm_rope(_ptr(q_weight), _ptr(k_weight), _ptr(rope) if max_pos else None,
-                     SQ_OUT_F32 if f32 and f32[0] else SQ_OUT_BF16, rot_dim, int(interleaved),
+                     SQ_OUT_F32 if f32 else SQ_OUT_BF16, rot_dim, int(interleaved),
                      max_pos, eps)
     p._keep = (rope, q_weight, k_weight)
     return p
@@ -569,65 +576,69 @@ class Cache:
                          sm_scale=1.0, spans=(), stream=None:
                          sq_prefill_attention(self.handle, seq, layer, n_q, q, out, out_dtype, lse,
                                               sm_scale, spans, stream))
+    extend = lambda self, seqs, n_new=None, stream=None: sq_extend(self.handle, seqs, n_new, stream)
+
     def _counted(self, seqs, counts, n, what):
-        """The call's rows per sequence add up to the tensors' tokens."""
-        total = len(seqs) if counts is None else sum(counts)
-        if counts is not None and len(counts) != len(seqs):
-            raise ValueError(f"{what}: {len(counts)} counts for {len(seqs)} sequences")
+        """The call's rows, which the tensors' tokens (n) have to be."""
+        if counts is None:
+            total = len(seqs)
+        else:
+            total = sum(counts)
+            if len(counts) != len(seqs):
+                raise ValueError(f"{what}: {len(counts)} counts for {len(seqs)} sequences")
         if n is not None and n != total:
             raise ValueError(f"{what}: {n} tokens given, {total} counted")
         return total
-
-    extend = lambda self, seqs, n_new=None, stream=None: sq_extend(self.handle, seqs, n_new, stream)
 
     def qk_norm_rope_store(self, seqs, n_new, layer, q, k, v, positions, params, q_out, stream=None):
         """q [tokens, Hq, D], k and v [tokens, Hkv, D] (parts of a fused projection
         do) of the sequences' newest rows: queries normed and rotated into q_out,
         keys into the cache with the values."""
-        n = self._counted(seqs, n_new, getattr(q, "shape", (None,))[0], "qk_norm_rope_store")
-        q, qs = _rows(q, self.Hq, self.D, "q")
-        k, ks = self._kv(k, n, "k")
-        v, vs = self._kv(v, n, "v")
+        if _BF16 is None:
+            _types()
+        hq, hkv, d = self.Hq, self.Hkv, self.D
+        q, qs, n = _rows(q, hq, d, "q")
+        n = self._counted(seqs, n_new, n, "qk_norm_rope_store")
+        k, ks, _ = _rows(k, hkv, d, "k", n)
+        v, vs, _ = _rows(v, hkv, d, "v", n)
         sq_qk_norm_rope_store(self.handle, seqs, n_new, layer, q, qs, k, ks, v, vs,
-                              _flat(positions, "int32", n, "positions"), params,
-                              _flat(q_out, "bfloat16", n * self.Hq * self.D, "q_out"), stream)
-
-    def _kv(self, x, n, name):
-        if not isinstance(x, int) and x.shape[0] != n:
-            raise ValueError(f"{name}: {n} tokens expected, not {x.shape[0]}")
-        return _rows(x, self.Hkv, self.D, name)
+                              _flat(positions, _INT, n, "positions"), params,
+                              _flat(q_out, _BF16, n * hq * d, "q_out"), stream)
 
     def qk_norm_rope(self, q, k, positions, params, q_out, k_out, stream=None):
         """Norms and rotation of q [tokens, Hq, D] and k [tokens, Hkv, D] into tensors."""
-        n = q.shape[0]
-        q, qs = _rows(q, self.Hq, self.D, "q")
-        k, ks = self._kv(k, n, "k")
-        sq_qk_norm_rope(self.handle, n, q, qs, k, ks, _flat(positions, "int32", n, "positions"), params,
-                        _flat(q_out, "bfloat16", n * self.Hq * self.D, "q_out"),
-                        _flat(k_out, "bfloat16", n * self.Hkv * self.D, "k_out"), stream)
+        if _BF16 is None:
+            _types()
+        hq, hkv, d = self.Hq, self.Hkv, self.D
+        q, qs, n = _rows(q, hq, d, "q")
+        k, ks, _ = _rows(k, hkv, d, "k", n)
+        sq_qk_norm_rope(self.handle, n, q, qs, k, ks, _flat(positions, _INT, n, "positions"), params,
+                        _flat(q_out, _BF16, n * hq * d, "q_out"),
+                        _flat(k_out, _BF16, n * hkv * d, "k_out"), stream)
 
     def qk_norm_rope_backward(self, q, k, positions, params, dq_out, dk_out, dq, dk, dq_weight=None,
                               dk_weight=None, stream=None):
         """Gradients of qk_norm_rope: dq and dk (rows apart as they are) and, where
         wanted, the weights' (float32)."""
-        n = q.shape[0]
-        q, qs = _rows(q, self.Hq, self.D, "q")
-        k, ks = self._kv(k, n, "k")
-        if not isinstance(dq, int) and dq.shape[0] != n:
-            raise ValueError(f"dq: {n} tokens expected, not {dq.shape[0]}")
-        dq, dqs = _rows(dq, self.Hq, self.D, "dq")
-        dk, dks = self._kv(dk, n, "dk")
-        sq_qk_norm_rope_backward(self.handle, n, q, qs, k, ks, _flat(positions, "int32", n, "positions"),
-                                 params, _flat(dq_out, "bfloat16", n * self.Hq * self.D, "dq_out"),
-                                 _flat(dk_out, "bfloat16", n * self.Hkv * self.D, "dk_out"), dq, dqs,
-                                 dk, dks, _flat(dq_weight, "float32", self.D, "dq_weight"),
-                                 _flat(dk_weight, "float32", self.D, "dk_weight"), stream)
+        if _BF16 is None:
+            _types()
+        hq, hkv, d = self.Hq, self.Hkv, self.D
+        q, qs, n = _rows(q, hq, d, "q")
+        k, ks, _ = _rows(k, hkv, d, "k", n)
+        dq, dqs, _ = _rows(dq, hq, d, "dq", n)
+        dk, dks, _ = _rows(dk, hkv, d, "dk", n)
+        sq_qk_norm_rope_backward(self.handle, n, q, qs, k, ks, _flat(positions, _INT, n, "positions"),
+                                 params, _flat(dq_out, _BF16, n * hq * d, "dq_out"),
+                                 _flat(dk_out, _BF16, n * hkv * d, "dk_out"), dq, dqs, dk, dks,
+                                 _flat(dq_weight, _FLOAT, d, "dq_weight"),
+                                 _flat(dk_weight, _FLOAT, d, "dk_weight"), stream)
 
     def window_attention(self, seqs, n_q, layer, q, out, window, n_sink=0, out_dtype=SQ_OUT_BF16,
                          lse=None, sm_scale=1.0, stream=None):
         """Attention of the newest n_q[i] tokens (None: one) of each sequence, each
         seeing its last `window` tokens and the first n_sink."""
-        self._counted(seqs, n_q, getattr(q, "shape", (None,))[0], "window_attention")
+        n = None if q.__class__ is int else q.shape[0]
+        self._counted(seqs, n_q, n, "window_attention")
         sq_window_attention(self.handle, seqs, n_q, layer, q, out, window, n_sink, out_dtype, lse,
                             sm_scale, stream)
 
@@ -635,7 +646,7 @@ class Cache:
                        out_dtype=SQ_OUT_BF16, lse=None, sm_scale=1.0, stream=None):
         """Attention of trees of drafted tokens, each sequence's newest n_draft[i]
         rows; parents: every drafted token's parent in its tree, -1 the context."""
-        n = self._counted(seqs, n_draft, getattr(q, "shape", (None,))[0], "tree_attention")
+        n = self._counted(seqs, n_draft, None if q.__class__ is int else q.shape[0], "tree_attention")
         if len(parents) != n:
             raise ValueError(f"tree_attention: {len(parents)} parents of {n} drafted tokens")
         sq_tree_attention(self.handle, seqs, n_draft, parents, layer, q, out, window, n_sink, out_dtype,

@@ -22,11 +22,16 @@ bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 // n_seqs distinct live handles.
 int check_handles(sq_cache* c, const sq_seq* seqs, int32_t n_seqs) {
     if (n_seqs < 0 || (n_seqs > 0 && !seqs)) return SQ_ERR_INVALID_ARG;
+    // (a live handle's slot, its low 20 bits, is below max_seqs)
+    if (c->slot_mark.empty()) c->slot_mark.assign(c->g.max_seqs, 0);
+    const uint64_t mark = ++c->mark;
     for (int32_t i = 0; i < n_seqs; ++i)
         if (!c->host->seq(seqs[i])) return SQ_ERR_BAD_HANDLE;
-    std::vector<int32_t> sorted(seqs, seqs + n_seqs);
-    std::sort(sorted.begin(), sorted.end());
-    if (std::adjacent_find(sorted.begin(), sorted.end()) != sorted.end()) return SQ_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < n_seqs; ++i) {
+        uint64_t& m = c->slot_mark[seqs[i] & 0xfffff];
+        if (m == mark) return SQ_ERR_INVALID_ARG;
+        m = mark;
+    }
     return SQ_OK;
 }
 
@@ -151,6 +156,8 @@ int used_buffer(TurnBuffer& b, cudaStream_t st) {
 // plans made before do not list these writes: the cache does (early_writes), the
 // pages of the newest store one by one.
 void note_store(sq_cache* c, std::vector<int32_t>&& pages, void* stream) {
+    // (stores may go on without an attention call, which would look after them)
+    if (c->write_pending.size() >= 32) poll_writes(c);
     note_writes(c, pages.data(), pages.size(), stream);
     if (pages != c->store_pages) {
         c->store_rest = c->store_ticket;

@@ -196,6 +196,9 @@ struct sq_cache {
     PinnedSlot pinned[kPinnedSlots];
     int next_pinned = 0;
     std::vector<uint8_t> staging;
+    // the call that last named a sequence's slot (a call names each once)
+    std::vector<uint64_t> slot_mark;
+    uint64_t mark = 0;
     // sq_decode_attention_noalloc: the device address of the library's fixed
     // scratch on this cache's device (resolved at creation; null if that
     // failed, with the status kept), and pinned staging for its plan uploads,
