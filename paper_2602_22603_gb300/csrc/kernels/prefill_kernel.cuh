@@ -485,17 +485,19 @@ __device__ void prefill_produce(const CUtensorMap* pool_map, const CUtensorMap* 
             take_next(clc_parity);
         }
         // pages of fewer than 64 tokens: a lane issues one box of one of the two
-        // loads; its page is read a step ahead
+        // loads; its page is read kAhead steps before
         auto piece_page = [&](int u) -> int32_t {
             int j, kv;
             load_of(u + (lane >> 4), T, it.dual, j, kv);
-            return (lane & 15) < n_pieces && j < T
+            return u < n_units && (lane & 15) < n_pieces
                        ? __ldg(&a.tile_pages[(size_t)(it.t0 + j) * n_pieces + (lane & 15)])
                        : -1;
         };
-        int32_t piece = -1;
+        constexpr int kAhead = 4;
+        int32_t pieces[kAhead];
         if constexpr (of_blocks<M>) {
-            if (n_pieces > 2 && T > 0) piece = piece_page(u_early);
+#pragma unroll
+            for (int x = 0; x < kAhead; ++x) pieces[x] = n_pieces > 2 ? piece_page(u_early + 2 * x) : -1;
         }
         int fill_b = 1;    // the next batch to read
         int merge_b = -1;  // the batch read into `pend`, not yet in place
@@ -514,9 +516,12 @@ __device__ void prefill_produce(const CUtensorMap* pool_map, const CUtensorMap* 
                 if ((lane >> 4) == (fill_b & 1)) pend = load_rec(it.t0, T, fill_b * kBatch);
                 merge_b = fill_b++;
             }
-            const int32_t my_piece = piece;
+            int32_t my_piece = -1;
             if constexpr (of_blocks<M>) {
-                if (n_pieces > 2 && u0 + 2 < n_units) piece = piece_page(u0 + 2);
+                my_piece = pieces[0];
+#pragma unroll
+                for (int x = 0; x + 1 < kAhead; ++x) pieces[x] = pieces[x + 1];
+                if (n_pieces > 2) pieces[kAhead - 1] = piece_page(u0 + 2 * kAhead);
             }
             const uint32_t U0 = ub + u0;
             const uint32_t slot1 = slot0 + 1 == C::kSlots ? 0 : slot0 + 1;
@@ -949,6 +954,24 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const v
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort));
 }
 
+// Pairs of lanes trade halves of their rows so that each writes 32 bytes of one
+// row next to its neighbour's 32: in `own` this lane's 16 words of its row, in
+// `out[0]` and `out[1]` afterwards the even and the odd lane's row, the lane's own
+// half of the 64 bytes.
+__device__ __forceinline__ void trade_halves(const uint32_t (&own)[16], uint32_t (&out)[2][8], bool odd) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? own[i] : own[8 + i], 1);
+        out[0][i] = odd ? got : own[i];
+        out[1][i] = odd ? own[8 + i] : got;
+    }
+}
+__device__ __forceinline__ void st_32(void* p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]),
+                 "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+
 // Normalises and writes one row of O_t (with tile b's part in dual-key mode) to
 // the outputs, or to the item's partial result.
 template <int D, int M>
@@ -972,7 +995,22 @@ __device__ __forceinline__ void prefill_write(const PrefillArgs& a, const Item& 
                   ((size_t)qi * a.Hq + h) * D * (a.out_f32 ? 4 : 2);
         if (valid && a.lse) a.lse[(size_t)qi * a.Hq + h] = lse2 * 0.69314718055994531f;
     }
-#pragma unroll
+    // A block of queries has few key tiles to hide its output behind.  A row for
+    // each lane, 16 bytes at a time, takes the store unit a cycle for every row and
+    // instruction; where the output allows 32-byte stores, pairs of lanes write 64
+    // bytes of one row together (16,384 queries at a window of 1,024: %EPI%).
+    uint8_t* to = part_row ? reinterpret_cast<uint8_t*>(part_row) : out_row;
+    const bool paired = of_blocks<M> && (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
+    uint8_t* to_even = nullptr;   // the pair's rows, null: no query
+    uint8_t* to_odd = nullptr;
+    if (paired) {
+        const uint64_t mine = valid ? reinterpret_cast<uint64_t>(to) : 0u;
+        const uint64_t other = __shfl_xor_sync(0xffffffffu, mine, 1);
+        to_even = reinterpret_cast<uint8_t*>(row & 1 ? other : mine);
+        to_odd = reinterpret_cast<uint8_t*>(row & 1 ? mine : other);
+    }
+    // (a block's: rolled up, for the instruction cache)
+#pragma unroll (of_blocks<M> ? 1 : D / 32)
     for (int c = 0; c < D / 32; ++c) {
         uint32_t o[32];
         if (any_keys) {
@@ -993,6 +1031,29 @@ __device__ __forceinline__ void prefill_write(const PrefillArgs& a, const Item& 
         } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(o[i]) * inv;
+        }
+        if (paired) {
+            const bool odd = row & 1;
+            uint32_t w[16], x[2][8];
+            if (part_row || a.out_f32) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(f[16 * half + i]);
+                    trade_halves(w, x, odd);
+                    const int at = c * 128 + half * 64 + (odd ? 32 : 0);
+                    if (to_even) st_32(to_even + at, x[0]);
+                    if (to_odd) st_32(to_odd + at, x[1]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
+                trade_halves(w, x, odd);
+                const int at = c * 64 + (odd ? 32 : 0);
+                if (to_even) st_32(to_even + at, x[0]);
+                if (to_odd) st_32(to_odd + at, x[1]);
+            }
+            continue;
         }
         if (!valid) continue;
         if (part_row || a.out_f32) {
@@ -1163,6 +1224,10 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
         // taken 64 columns at a time to keep registers low: one pass for the
         // row maximum, one for the weights.
         const bool unmasked = (wk.y & kPrefillTileFull) && mask.whole(wk.x) && mask.whole(wb_);
+        // (a block's window masks many tiles of which every key exists: no load)
+        auto exists = [&](int ww) {
+            return of_blocks<M> && (wk.y & kPrefillTileFull) ? 0xffffffffu : __ldg(&tp->vis[ww]);
+        };
         // Weights 2^(s * scale - m) with the running maximum m, two arguments
         // at a time with a packed FMA, rounded to bf16 into wt (32 words per
         // 64 keys).  The normaliser sums the same rounded weights that the PV
@@ -1187,7 +1252,7 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
                     for (int w = 0; w < 2; ++w) {
                         const int ww = 2 * hh + w;
                         const uint32_t mw =
-                            __ldg(&tp->vis[ww]) & mask.word((ww < 2 ? wk.x : wb_) + 32 * (ww & 1));
+                            exists(ww) & mask.word((ww < 2 ? wk.x : wb_) + 32 * (ww & 1));
                         if constexpr (of_blocks<M>) seen |= mw;
 #pragma unroll
                         for (int c = 0; c < 32; ++c)
@@ -1238,7 +1303,7 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
                     for (int w = 0; w < 2; ++w) {
                         const int ww = 2 * hh + w;
                         const uint32_t mw =
-                            __ldg(&tp->vis[ww]) & mask.word((ww < 2 ? wk.x : wb_) + 32 * (ww & 1));
+                            exists(ww) & mask.word((ww < 2 ? wk.x : wb_) + 32 * (ww & 1));
 #pragma unroll
                         for (int c = 0; c < 32; ++c)
                             if (!((mw >> c) & 1u)) x[32 * w + c] = 0xff800000u;  // -inf
