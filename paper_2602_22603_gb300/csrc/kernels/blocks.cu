@@ -16,6 +16,8 @@ template <int D>
 cudaError_t prepare() {
     cudaError_t e = prepare_one<D, BlockArgs>();
     if (e == cudaSuccess) e = prepare_one<D, BlockShortArgs>();
+    if (e == cudaSuccess) e = prepare_one<D, SmallBlockArgs>();
+    if (e == cudaSuccess) e = prepare_one<D, SmallBlockShortArgs>();
     // (the merging kernels share every SM with the kernel above)
     if (e == cudaSuccess)
         e = cudaFuncSetAttribute(dev::sq_prefill_combine_kernel<D, 2, 24, BlockCombineArgs>,
@@ -55,13 +57,27 @@ cudaError_t launch_one(const CUtensorMap& pool_map, const CUtensorMap& qmap, con
 
 cudaError_t blocks_prepare(int D) { return D == 128 ? prepare<128>() : prepare<64>(); }
 
+template <int D>
+static cudaError_t launch_d(const CUtensorMap& pool_map, const CUtensorMap& qmap, const BlockShortArgs& a,
+                            bool one, cudaStream_t st) {
+    if (a.n_pieces > 2) {
+        SmallBlockShortArgs s;
+        static_cast<BlockShortArgs&>(s) = a;
+        if (one) return launch_one<D>(pool_map, qmap, s, st);
+        SmallBlockArgs t;
+        static_cast<BlockArgs&>(t) = a;
+        return launch_one<D>(pool_map, qmap, t, st);
+    }
+    if (one) return launch_one<D>(pool_map, qmap, a, st);
+    const BlockArgs& base = a;
+    return launch_one<D>(pool_map, qmap, base, st);
+}
+
+// one: every item's queries fit in one query tile
 cudaError_t launch_blocks(const CUtensorMap& pool_map, const CUtensorMap& qmap, const BlockShortArgs& a,
                           int D, bool one, cudaStream_t st) {
     if (a.n_items == 0) return cudaSuccess;
-    const BlockArgs& base = a;
-    if (D == 128)
-        return one ? launch_one<128>(pool_map, qmap, a, st) : launch_one<128>(pool_map, qmap, base, st);
-    return one ? launch_one<64>(pool_map, qmap, a, st) : launch_one<64>(pool_map, qmap, base, st);
+    return D == 128 ? launch_d<128>(pool_map, qmap, a, one, st) : launch_d<64>(pool_map, qmap, a, one, st);
 }
 
 cudaError_t launch_blocks_combine(const BlockCombineArgs& a, int D, cudaStream_t st) {

@@ -81,6 +81,9 @@ struct BlockShortArgs : BlockArgs {
     int32_t n_unsafe;
     int32_t unsafe[kMaxUnsafe];
 };
+// The same on pages of fewer than 64 tokens (instances of their own).
+struct SmallBlockArgs : BlockArgs {};
+struct SmallBlockShortArgs : BlockShortArgs {};
 struct BlockCombineArgs {
     const BlockMerge* merges;
     int32_t n_merges;

@@ -92,21 +92,25 @@ namespace {
 // Instances.  kOneTile: every query of an item fits in tile a.  kBlocks: items
 // carry what they need of their own sequence and have key tiles of their own
 // (query blocks of a batch, see BlockItem); otherwise all items belong to one
-// sequence, whose newest n_q tokens they share out.
-constexpr int kOneTile = 1, kBlocks = 2;
+// sequence, whose newest n_q tokens they share out.  kSmallPages: blocks on pages of
+// fewer than 64 tokens, whose many boxes two producer warps load.
+constexpr int kOneTile = 1, kBlocks = 2, kSmallPages = 4;
 template <int M>
 constexpr bool one_tile = (M & kOneTile) != 0;
 template <int M>
 constexpr bool of_blocks = (M & kBlocks) != 0;
+template <int M>
+constexpr int producers = (M & kSmallPages) != 0 ? 2 : 1;
 
 // Items in flight between the producer and the other roles, and the warps that
 // read each (MMA warp and eight softmax warps).
 constexpr int kItemSlots = 4;
 constexpr int kItemReaders = 9;
+constexpr int kProducer2 = 10;  // query blocks: the warp of their odd loads
 
 template <int D, int M>
 struct PreCfg {
-    static constexpr int kThreads = 320;
+    static constexpr int kThreads = 320 + 32 * (producers<M> - 1);
     static constexpr int kColBlocks = D / 64;                  // 64-column (128-byte) blocks
     static constexpr int kBlockBytes = kPrefillRows * 128;      // one block of a 128-row tile
     static constexpr int kQBytes = kColBlocks * kBlockBytes;    // one query tile
@@ -280,17 +284,21 @@ __device__ __forceinline__ int4 tile_record(const PrefillArgs& a, int t0, int T,
 // Block items: what a lane needs of the piece that it loads in a batch of loads.  A
 // load is n_pieces boxes of min(P, 64) rows, so 32 / n_pieces loads are a batch, a
 // lane to a box; the batch's records are read together, a batch ahead of their use.
+template <int M>
+__device__ __forceinline__ int pieces_of(const PrefillArgs& a) { return producers<M> > 1 ? a.n_pieces : 2; }
+template <int M>
 struct BlockBatch {
     int32_t key, page;  // the box's first key; its page, -1: no such box
-    __device__ __forceinline__ void read(const PrefillArgs& a, const Item& it, int u0, int lane) {
-        const int per = a.n_pieces, i = lane & (per - 1), u = u0 + lane / per;
+    // the producer warp w's loads from its x0-th on
+    __device__ __forceinline__ void read(const PrefillArgs& a, const Item& it, int x0, int w, int lane) {
+        const int per = pieces_of<M>(a), i = lane & (per - 1), u = (x0 + lane / per) * producers<M> + w;
         key = 0;
         page = -1;
         if (u >= 2 * it.T) return;
         int j, kv;
         load_of(u, it.T, it.dual, j, kv);
         const PrefillTile* t = a.tiles + it.t0 + j;
-        const int half = per >> 1, br = a.P < 64 ? a.P : 64;
+        const int half = per >> 1, br = 64 / half;
         key = i < half ? __ldg(&t->key0) + i * br : __ldg(&t->key0b) + (i - half) * br;
         page = __ldg(&a.tile_pages[(size_t)(it.t0 + j) * per + i]);
     }
@@ -311,6 +319,14 @@ struct ItemRecord {
             raw = __ldg(reinterpret_cast<const int4*>(a.items) + i);
         }
     }
+    __device__ __forceinline__ void copy(const uint8_t* slot) {
+        const int4* p = reinterpret_cast<const int4*>(slot);
+        raw = p[0];
+        if constexpr (of_blocks<M>) {
+            more[0] = p[1];
+            more[1] = p[2];
+        }
+    }
     __device__ __forceinline__ void write(uint8_t* slot) const {
         int4* p = reinterpret_cast<int4*>(slot);
         p[0] = raw;
@@ -319,7 +335,7 @@ struct ItemRecord {
             p[2] = more[1];
         }
     }
-    // the CTA's next item (blocks of one query tile, dealt out beforehand)
+    // (block items) the CTA's next item (blocks of one query tile, dealt out beforehand)
     __device__ __forceinline__ int next() const { return more[of_blocks<M> ? 1 : 0].w; }
     // slots of the item's sequence, and the row of its first query
     __device__ __forceinline__ int n(const PrefillArgs& a) const { return of_blocks<M> ? more[0].z : a.n; }
@@ -331,10 +347,10 @@ template <int M>
 struct FirstItem {
     ItemRecord<M> item;
     int4 rec;         // (one sequence's prefill)
-    BlockBatch batch;  // (block items)
-    __device__ void read(const PrefillArgs& a, int lane) {
+    BlockBatch<M> batch;  // (block items)
+    __device__ void read(const PrefillArgs& a, int w, int lane) {
         item.read(a, blockIdx.x);
-        if constexpr (of_blocks<M>) batch.read(a, make_item<M>(a, item.raw), 0, lane);
+        if constexpr (of_blocks<M>) batch.read(a, make_item<M>(a, item.raw), 0, w, lane);
         else rec = tile_record(a, item.raw.y, item.raw.z, 0, lane);
     }
 };
@@ -381,8 +397,8 @@ __device__ __forceinline__ int early_loads(const CUtensorMap* pool_map, const Pr
     return safe ? 2 : 0;
 }
 
-// The same for a block item: its first two loads, K_0 and K_1, are the first four
-// lanes' boxes.
+// The same for a block item: its first two loads (on pages of 64 tokens or more one
+// warp's) are the first four lanes' boxes.
 template <int D, int M>
 __device__ __forceinline__ int early_loads(const CUtensorMap* pool_map, const BlockShortArgs& a,
                                            const Smem& sm, const FirstItem<M>& start, const Item& it,
@@ -390,21 +406,27 @@ __device__ __forceinline__ int early_loads(const CUtensorMap* pool_map, const Bl
     using C = PreCfg<D, M>;
     const int32_t unsafe = lane < a.n_unsafe ? a.unsafe[lane] : -1;
     const int32_t page = start.batch.page, key = start.batch.key;
-    // (pages of 64 tokens or more: two boxes a load; whole ones inside the sequence)
-    bool safe = it.dual && (lane > 3 || ((uint32_t)page < (uint32_t)a.num_pages && key <= start.item.n(a) - 64));
+    // (whole boxes inside the sequence)
+    bool safe = lane > 3 || ((uint32_t)page < (uint32_t)a.num_pages && key <= start.item.n(a) - 64);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) safe = safe && !(unsafe >= 0 && unsafe == __shfl_sync(0xffffffffu, page, x));
+    for (int x = 0; x < 4; ++x) {
+        const int32_t p = __shfl_sync(0xffffffffu, page, x);  // (every lane's)
+        safe = safe && !(unsafe >= 0 && unsafe == p);
+    }
     safe = __all_sync(0xffffffffu, safe);
     __syncwarp();  // (lane 0 initialised the barriers)
     if (safe && lane < 4) {
         const int u = lane >> 1;
+        int j, kv;
+        load_of(u, it.T, it.dual, j, kv);
         const uint32_t fb = sm.bar<D, M>(C::kBarFull + u);
         if (!(lane & 1)) mbar_arrive_expect_tx(fb, C::kSlotBytes);
         __syncwarp(0xfu);
 #pragma unroll
         for (int cb = 0; cb < C::kColBlocks; ++cb)
             tma_load_4d(sm.base + C::kOffRing + u * C::kSlotBytes + cb * C::kBlockBytes + (lane & 1) * 64 * 128,
-                        pool_map, fb, cb * 64, it.g * a.P + (key & (a.P - 1)), page, a.layer);
+                        pool_map, fb, cb * 64, (kv ? a.Hkv + it.g : it.g) * a.P + (key & (a.P - 1)), page,
+                        a.layer);
     }
     __syncwarp();
     return safe ? 2 : 0;
@@ -656,39 +678,43 @@ __device__ void prefill_produce(const CUtensorMap* pool_map, const CUtensorMap* 
     }
 }
 
-// The producer warp of block items.  As above, but a lane holds what one box of the
-// next loads needs (BlockBatch), so that a load costs the warp a wait, an expected
-// byte count and the boxes' copies, each by its own lane: the issue of two loads
-// takes 0.4 us instead of 1.2, which bounded items of 32 KB tiles and of pages
-// under 64 tokens (their boxes: eight a load at 16 tokens).  The next item is known
-// a few loads before the end of this one and its first records are read then.
+// The producer warps of block items.  A lane holds what one box of the next loads
+// needs (BlockBatch), so that a load costs a warp a wait, an expected byte count and
+// the boxes' copies.  Pages of 64 tokens or more are one warp's loads.  Smaller pages
+// have 4, 8 or 16 boxes a load; there the even loads are one warp's, the odd ones
+// the other's, and every load's slot has a commit of its own (8 trees of 16 over
+// 32,768 tokens on pages of 16 and 8 tokens, 4 and 8 KV heads of 64 dimensions: 83 ->
+// 60 and 221 -> 136 us; with two warps on pages of 64 tokens the issuing lane, which
+// bounds two-tile items, ran 3% slower).  The first warp (w = 0) also loads the
+// queries and takes the next item a few loads before the end of this one; either
+// reads its next records then.
 template <int D, int M, typename Args>
 __device__ void block_produce(const CUtensorMap* pool_map, const CUtensorMap* qmap, const Args& a,
-                              const Smem& sm, const FirstItem<M>& start, int u_early,
-                              volatile int* abort_flag, int lane) {
+                              const Smem& sm, const FirstItem<M>& start, int early,
+                              volatile int* abort_flag, int w, int lane) {
     using C = PreCfg<D, M>;
     // blocks of one tile are dealt out to the CTAs beforehand: HBM bounds them, and
     // an even share of the bytes beats handing out whole items
     constexpr bool kDealt = one_tile<M>;
-    const int per = a.n_pieces, br = a.P < 64 ? a.P : 64;
-    const int n_batch = 32 / per;                 // loads of a batch
+    constexpr int kWarps = producers<M>;
+    const int per = pieces_of<M>(a), br = 128 / per;
+    const int n_batch = 32 / per;  // loads of a batch
     const int mine = lane / per, piece = lane & (per - 1);
+    const uint32_t group = (uint32_t)((1ull << per) - 1);
     ItemRecord<M> item = start.item, next = start.item;
-    BlockBatch first = start.batch;
-    uint32_t n_items = 1;     // items published (the first at start-up)
+    BlockBatch<M> first = start.batch;
+    uint32_t k = 0;           // the item's number
     bool asked = false;       // an answer of the launch hardware is due
-    uint32_t ub = 0;          // loads issued before this item (even)
     uint32_t n_queries = 0;   // items whose queries were loaded
+    uint32_t issued = 0;      // this warp's loads
+    uint32_t slot = w, phase = 0;  // of its next load
+    // (one warp: slots are freed as in prefill_produce)
+    uint32_t own = early > 0 ? 3 : 0, par = 0;
     uint32_t n_fix = 0;       // uses of the fix-up barrier
-    uint32_t issued = u_early;
-    uint32_t own = u_early > 0 ? 3 : 0, par = 0;  // as in prefill_produce
-    uint32_t slot = u_early;  // slot of the next load
-    uint32_t tail_u = 0;      // the load that used the fix-up barrier last
-    bool tail_open = false;   // ... and was not handed over on its slot's barrier
+    bool tail_open = false;   // the last load's V is still to be handed over
     bool ok = true;
     auto load_queries = [&](const Item& it) {
-        if (n_queries > 0)
-            ok = mbar_wait(sm.bar<D, M>(C::kBarQFree), (n_queries - 1) & 1, abort_flag);
+        if (k > 0) ok = mbar_wait(sm.bar<D, M>(C::kBarQFree), (k - 1) & 1, abort_flag);
         ok = __all_sync(0xffffffffu, ok);
         if (ok && lane == 0) {
             const int nq = it.two ? 2 : 1;  // tile b is loaded only when it holds queries
@@ -700,19 +726,8 @@ __device__ void block_produce(const CUtensorMap* pool_map, const CUtensorMap* qm
         }
         if (ok) ++n_queries;
     };
-    // hands an item (or the end mark) to the other roles
-    auto publish = [&](const ItemRecord<M>& r) {
-        const int at = n_items % kItemSlots;
-        if (n_items >= kItemSlots)
-            ok = __all_sync(0xffffffffu, mbar_wait(sm.bar<D, M>(C::kBarItemFree + at),
-                                                   (n_items / kItemSlots - 1) & 1, abort_flag));
-        if (ok && lane == 0) {
-            r.write(sm.ptr + C::kOffItems + at * C::kItemBytes);
-            mbar_arrive(sm.bar<D, M>(C::kBarItem + at));
-        }
-        if (ok) ++n_items;
-    };
-    // The next item, in three steps: asked for, taken, its first records read.
+    // The first warp asks for the item after this one, and hands it (or the end
+    // mark) to the other roles; the second waits for it.
     auto request = [&]() {
         if constexpr (!kDealt) {
             if (lane == 0) {
@@ -723,12 +738,20 @@ __device__ void block_produce(const CUtensorMap* pool_map, const CUtensorMap* qm
         }
     };
     auto take_next = [&]() {
+        const uint32_t at = (k + 1) % kItemSlots;
+        if (w == 1) {
+            ok = __all_sync(0xffffffffu, item_wait<D, M>(sm, k + 1, abort_flag));
+            if (!ok) return;
+            next.copy(sm.ptr + C::kOffItems + at * C::kItemBytes);
+            __syncwarp();
+            if (lane == 0) item_free<D, M>(sm, k + 1);
+            return;
+        }
         int index;
         if constexpr (kDealt) {
             index = item.next();
         } else {
-            ok = __all_sync(0xffffffffu,
-                            mbar_wait(sm.bar<D, M>(C::kBarClc), (n_items - 1) & 1, abort_flag));
+            ok = __all_sync(0xffffffffu, mbar_wait(sm.bar<D, M>(C::kBarClc), k & 1, abort_flag));
             if (!ok) return;
             asked = false;
             const int cta = clc_answer(sm.base + C::kOffClc);
@@ -739,28 +762,36 @@ __device__ void block_produce(const CUtensorMap* pool_map, const CUtensorMap* qm
         }
         next.raw = make_int4(0, 0, -1, 0);
         if (index >= 0) next.read(a, index);
+        if (k + 1 >= kItemSlots)
+            ok = __all_sync(0xffffffffu, mbar_wait(sm.bar<D, M>(C::kBarItemFree + at),
+                                                   ((k + 1) / kItemSlots - 1) & 1, abort_flag));
+        if (ok && lane == 0) {
+            next.write(sm.ptr + C::kOffItems + at * C::kItemBytes);
+            mbar_arrive(sm.bar<D, M>(C::kBarItem + at));
+        }
     };
-    while (ok && item.raw.z >= 0) {
+    if (kWarps > 1 && w == 1 && lane == 0) item_free<D, M>(sm, 0);  // (its first item it has read itself)
+    for (; ok && item.raw.z >= 0; ++k) {
         const Item it = make_item<M>(a, item.raw);
-        const int n = item.n(a);
-        const int n_units = 2 * it.T;
-        const bool late_queries = ub > 0;
-        const int ask_at = max(n_units - 14, u_early), take_at = max(n_units - 8, u_early),
-                  read_at = max(n_units - 3, u_early);
-        if (!late_queries) load_queries(it);
-        BlockBatch cur = first, ahead;
-        for (int u0 = 0; ok && u0 < n_units; u0 += n_batch) {
-            ahead.read(a, it, u0 + n_batch, lane);
+        const int n = item.n(a), T = 2 * it.T / kWarps;  // this warp's loads of the item
+        // (the second warp waits for the item only after loads that the first one's
+        // way there may depend on)
+        const int ask_at = max(T - 14 / kWarps, 0), take_at = max(w ? T - 2 : T - 8 / kWarps, 0),
+                  read_at = max(T - 4 / kWarps, 0), query_at = kWarps == 2 ? 0 : 1;
+        if (w == 0 && k == 0) load_queries(it);
+        BlockBatch<M> cur = first, ahead;
+        for (int x0 = 0; ok && x0 < T; x0 += n_batch) {
+            ahead.read(a, it, x0 + n_batch, w, lane);
             // this lane's box
             int j, kv;
-            load_of(min(u0 + mine, n_units - 1), it.T, it.dual, j, kv);
+            load_of(min(x0 + mine, T - 1) * kWarps + w, it.T, it.dual, j, kv);
             const bool box = cur.page >= 0;
-            const uint32_t boxes = __ballot_sync(0xffffffffu, box) >> (mine * per) & (uint32_t)((1ull << per) - 1);
+            const uint32_t boxes = __ballot_sync(0xffffffffu, box) >> (mine * per) & group;
             const uint32_t bytes = (uint32_t)__popc(boxes) * br * 128 * C::kColBlocks;
             const int rows = box ? min(br, n - cur.key) : 0;  // rows of the sequence in the box
-            // V of the sequence's last key tile: its rows past the end are zeroed
-            const bool vfix = kv == 1 && rows < br;
-            const uint32_t fixes = __ballot_sync(0xffffffffu, vfix && u0 + mine < n_units);
+            // V of the sequence's last key tile (an odd load): its rows past the end
+            // are zeroed
+            const uint32_t fixes = __ballot_sync(0xffffffffu, kv == 1 && rows < br && x0 + mine < T);
             const int row = (kv ? a.Hkv + it.g : it.g) * a.P + (cur.key & (a.P - 1));  // P is a power of two
             int32_t page = cur.page;
             if (box && page >= a.num_pages) {
@@ -769,78 +800,93 @@ __device__ void block_produce(const CUtensorMap* pool_map, const CUtensorMap* qm
                 set_error(a.err, kErrBounds);
                 page = 0;
             }
-            const int last = min(n_batch, n_units - u0);
-            for (int b = u0 == 0 ? u_early : 0; b < last; ++b) {
-                const int u = u0 + b;
-                const uint32_t U = ub + u;
-                // every lane polls the slot's barrier: a warp-uniform wait
-                if (U >= C::kSlots && ((own >> (C::kSlots - 1)) & 1u)) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(sm.bar<D, M>(C::kBarEmpty + slot),
-                                                           (par >> slot) & 1u, abort_flag));
-                    par ^= 1u << slot;
-                    if (!ok) break;
-                }
-                // (V tiles, an item's first K and in dual-key mode all have a commit
-                // of their own)
-                own = own << 1 | (it.dual || (u & 1) || u == 0 ? 1u : 0u);
-                const uint32_t fix = fixes >> (b * per) & (uint32_t)((1ull << per) - 1);
-                const uint32_t bar = fix ? sm.bar<D, M>(C::kBarVfix) : sm.bar<D, M>(C::kBarFull + slot);
-                if (mine == b && piece == 0) mbar_arrive_expect_tx(bar, bytes);
-                __syncwarp();
-                if (mine == b && box) {
-                    const uint32_t dst = sm.base + C::kOffRing + slot * C::kSlotBytes + piece * br * 128;
+            const int last = min(n_batch, T - x0);
+            for (int b = 0; b < last; ++b) {
+                const int x = x0 + b;
+                if ((int)issued < early) {
+                    // (the first loads went out before the dependency wait)
+                } else {
+                    const uint32_t empty = sm.bar<D, M>(C::kBarEmpty + slot);
+                    // every lane polls the slot's barrier: a warp-uniform wait
+                    if (kWarps * issued + w >= C::kSlots && (kWarps > 1 || ((own >> (C::kSlots - 1)) & 1u))) {
+                        const uint32_t parity = kWarps > 1 ? phase ^ 1 : (par >> slot) & 1u;
+                        ok = __all_sync(0xffffffffu, mbar_wait(empty, parity, abort_flag));
+                        par ^= 1u << slot;
+                        if (!ok) break;
+                    }
+                    own = own << 1 | (it.dual || (x & 1) || x == 0 ? 1u : 0u);
+                    const uint32_t fix = fixes >> (b * per) & group;
+                    const uint32_t bar = fix ? sm.bar<D, M>(C::kBarVfix) : sm.bar<D, M>(C::kBarFull + slot);
+                    if (mine == b) {
+                        if (piece == 0) mbar_arrive_expect_tx(bar, bytes);
+                        __syncwarp(group << (b * per));
+                        if (box) {
+                            const uint32_t dst =
+                                sm.base + C::kOffRing + slot * C::kSlotBytes + piece * br * 128;
 #pragma unroll
-                    for (int cb = 0; cb < C::kColBlocks; ++cb)
-                        tma_load_4d(dst + cb * C::kBlockBytes, pool_map, bar, cb * 64, row, page, a.layer);
+                            for (int cb = 0; cb < C::kColBlocks; ++cb)
+                                tma_load_4d(dst + cb * C::kBlockBytes, pool_map, bar, cb * 64, row, page,
+                                            a.layer);
+                        }
+                    }
+                    if (fix) {
+                        // stale or never-written data: their weights are zero, but
+                        // 0 * NaN is not, so the rows are zeroed before the MMAs read
+                        // them
+                        tail_open = true;
+                        ++issued;
+                        const int r0 = __reduce_add_sync(0xffffffffu, mine == b ? rows : 0);
+                        ok = __all_sync(0xffffffffu,
+                                        mbar_wait(sm.bar<D, M>(C::kBarVfix), n_fix & 1, abort_flag));
+                        if (!ok) break;
+                        --issued;
+                        ++n_fix;
+                        const int chunks = (kPrefillKeys - r0) * 8;
+                        uint8_t* vsp = sm.ptr + C::kOffRing + slot * C::kSlotBytes;
+                        for (int cb = 0; cb < C::kColBlocks; ++cb)
+                            for (int c = lane; c < chunks; c += 32)
+                                *reinterpret_cast<uint4*>(vsp + cb * C::kBlockBytes + (r0 + (c >> 3)) * 128 +
+                                                          (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(sm.bar<D, M>(C::kBarFull + slot));
+                        tail_open = false;
+                    }
                 }
-                issued = U + 1;
-                if (fix) {
-                    // stale or never-written data: their weights are zero, but
-                    // 0 * NaN is not, so the rows are zeroed before the MMAs read them
-                    tail_u = U;
-                    tail_open = true;
-                    int r0 = mine == b ? rows : 0;
-                    r0 = __reduce_add_sync(0xffffffffu, r0);
-                    ok = __all_sync(0xffffffffu, mbar_wait(sm.bar<D, M>(C::kBarVfix), n_fix & 1, abort_flag));
-                    if (!ok) break;
-                    ++n_fix;
-                    const int chunks = (kPrefillKeys - r0) * 8;
-                    uint8_t* vsp = sm.ptr + C::kOffRing + slot * C::kSlotBytes;
-                    for (int cb = 0; cb < C::kColBlocks; ++cb)
-                        for (int c = lane; c < chunks; c += 32)
-                            *reinterpret_cast<uint4*>(vsp + cb * C::kBlockBytes + (r0 + (c >> 3)) * 128 +
-                                                      (c & 7) * 16) = make_uint4(0, 0, 0, 0);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(sm.bar<D, M>(C::kBarFull + slot));
-                    tail_open = false;
+                ++issued;
+                slot += kWarps;
+                if (slot >= C::kSlots) {
+                    slot -= C::kSlots;
+                    phase ^= 1;
                 }
-                slot = slot + 1 == C::kSlots ? 0 : slot + 1;
-                if (u == ask_at) request();
-                if (u == take_at) take_next();
-                if (u == read_at) first.read(a, make_item<M>(a, next.raw), 0, lane);
-                if (u == 1 && late_queries) load_queries(it);
+                if (w == 0) {
+                    if (x == ask_at) request();
+                    if (x == query_at && k > 0) load_queries(it);
+                }
+                if (x == take_at) take_next();
+                if (x == read_at && ok) first.read(a, make_item<M>(a, next.raw), 0, w, lane);
                 if (!ok) break;
             }
             cur = ahead;
         }
-        ub += n_units;
-        u_early = 0;
-        item = next;
-        if (ok) publish(item);  // an item, or the end mark
+        if (ok) item = next;
     }
     if (!ok && lane == 0) {
         if (!*abort_flag) set_error(a.err, kErrTimeout);
         *abort_flag = 1;
     }
-    // Drain: every copy this CTA issued lands before the CTA exits (immediate
-    // unless a consumer gave up early).
+    // Drain: every copy this warp issued lands before the CTA exits (immediate
+    // unless a consumer gave up early).  Of the last kSlots loads (either warp has
+    // issued as many) the slots were not filled again, by the other warp either,
+    // so their barriers still are in the phase waited for.
     if (lane == 0) {
-        if (asked) mbar_wait(sm.bar<D, M>(C::kBarClc), (n_items - 1) & 1);
+        if (asked) mbar_wait(sm.bar<D, M>(C::kBarClc), (k - 1) & 1);
         if (n_queries > 0) mbar_wait(sm.bar<D, M>(C::kBarQ), (n_queries - 1) & 1);
-        for (uint32_t u = issued > C::kSlots ? issued - C::kSlots : 0; u < issued; ++u) {
-            if (u == tail_u && tail_open) mbar_wait(sm.bar<D, M>(C::kBarVfix), n_fix & 1);
-            else mbar_wait(sm.bar<D, M>(C::kBarFull + u % C::kSlots), (u / C::kSlots) & 1);
+        const uint32_t total = kWarps * issued;
+        for (uint32_t x = total > C::kSlots ? (total - C::kSlots + kWarps - 1 - w) / kWarps : 0; x < issued; ++x) {
+            const uint32_t U = kWarps * x + w;
+            if (tail_open && x + 1 == issued) mbar_wait(sm.bar<D, M>(C::kBarVfix), n_fix & 1);
+            else mbar_wait(sm.bar<D, M>(C::kBarFull + U % C::kSlots), (U / C::kSlots) & 1);
         }
     }
 }
@@ -973,6 +1019,8 @@ __device__ __forceinline__ bool prefill_mma_step(const Smem& sm, const MmaDesc& 
         mma_commit(sm.bar<D, M>(kMore ? C::kBarS + t : C::kBarO + t));
     }
     mma_commit(sm.bar<D, M>(C::kBarEmpty + vslot));  // V_j, and K_{j+1} with it
+    // (two producer warps: on its own, for the warp that waits for it)
+    if (producers<M> > 1 && kMore) mma_commit(sm.bar<D, M>(C::kBarEmpty + kslot));
     return true;
 }
 
@@ -1154,7 +1202,8 @@ __device__ __forceinline__ void prefill_write(const PrefillArgs& a, const Item& 
     // A block of queries has few key tiles to hide its output behind.  A row for
     // each lane, 16 bytes at a time, takes the store unit a cycle for every row and
     // instruction; where the output allows 32-byte stores, pairs of lanes write 64
-    // bytes of one row together (16,384 queries at a window of 1,024: %EPI%).
+    // bytes of one row together (16,384 queries at a window of 1,024: 254 -> 238 us,
+    // with the loop rolled up).
     uint8_t* to = part_row ? reinterpret_cast<uint8_t*>(part_row) : out_row;
     const bool paired = of_blocks<M> && (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
     uint8_t* to_even = nullptr;   // the pair's rows, null: no query
@@ -1278,6 +1327,10 @@ template <>
 struct RowMask<kBlocks> : BlockRowMask {};
 template <>
 struct RowMask<kBlocks | kOneTile> : BlockRowMask {};
+template <>
+struct RowMask<kBlocks | kSmallPages> : BlockRowMask {};
+template <>
+struct RowMask<kBlocks | kOneTile | kSmallPages> : BlockRowMask {};
 
 // What a softmax warp carries from item to item, in two words so that the
 // loop over key tiles keeps its registers: the loads of the items before, and,
@@ -1581,9 +1634,13 @@ template <>
 struct ModeOf<BlockArgs> : std::integral_constant<int, kBlocks> {};
 template <>
 struct ModeOf<BlockShortArgs> : std::integral_constant<int, kBlocks | kOneTile> {};
+template <>
+struct ModeOf<SmallBlockArgs> : std::integral_constant<int, kBlocks | kSmallPages> {};
+template <>
+struct ModeOf<SmallBlockShortArgs> : std::integral_constant<int, kBlocks | kOneTile | kSmallPages> {};
 
 template <int D, typename Args>
-__global__ void __launch_bounds__(320, 1)
+__global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
     sq_prefill_kernel(const __grid_constant__ CUtensorMap pool_map,
                       const __grid_constant__ CUtensorMap qmap, const Args a) {
     constexpr int M = ModeOf<Args>::value;
@@ -1614,7 +1671,7 @@ __global__ void __launch_bounds__(320, 1)
         mbar_init(sm.bar<D, M>(C::kBarDone), 1);
         for (int s = 0; s < kItemSlots; ++s) {
             mbar_init(sm.bar<D, M>(C::kBarItem + s), 1);
-            mbar_init(sm.bar<D, M>(C::kBarItemFree + s), kItemReaders);
+            mbar_init(sm.bar<D, M>(C::kBarItemFree + s), kItemReaders + producers<M> - 1);
         }
         mbar_init(sm.bar<D, M>(C::kBarClc), 1);
         mbar_init(sm.bar<D, M>(C::kBarX), 128);
@@ -1628,14 +1685,15 @@ __global__ void __launch_bounds__(320, 1)
     }
     FirstItem<M> start;
     int u_early = 0;
-    if (warp == 0) {
-        if (lane == 0) {
+    const bool second = producers<M> > 1 && warp == kProducer2;  // the second producer warp
+    if (warp == 0 || second) {
+        if (warp == 0 && lane == 0) {
             prefetch_tmap(&pool_map);
             prefetch_tmap(&qmap);
         }
-        if (a.plan_ready) start.read(a, lane);
+        if (a.plan_ready) start.read(a, second, lane);
         if constexpr (one_tile<M>) {
-            if (a.kv_early) {
+            if (a.kv_early && warp == 0) {
                 const Item it = make_item<M>(a, start.item.raw);
                 u_early = early_loads<D, M>(&pool_map, a, sm, start, it, lane);
             }
@@ -1646,9 +1704,9 @@ __global__ void __launch_bounds__(320, 1)
     // not on the device before that kernel, are read only from here on (but for
     // the first K/V tiles of early_loads).
     grid_dependency_wait();
-    if (warp == 0) {
-        if (!a.plan_ready) start.read(a, lane);
-        if (lane == 0) {  // the thread that initialised the barriers
+    if (warp == 0 || second) {
+        if (!a.plan_ready) start.read(a, second, lane);
+        if (warp == 0 && lane == 0) {  // the thread that initialised the barriers
             start.item.write(sm.ptr + C::kOffItems);
             mbar_arrive(sm.bar<D, M>(C::kBarItem));
         }
@@ -1659,9 +1717,12 @@ __global__ void __launch_bounds__(320, 1)
     const uint32_t tmem = *tmem_slot;
     if (warp == 0) {
         if constexpr (of_blocks<M>)
-            block_produce<D, M>(&pool_map, &qmap, a, sm, start, u_early, abort_flag, lane);
+            block_produce<D, M>(&pool_map, &qmap, a, sm, start, u_early, abort_flag, 0, lane);
         else
             prefill_produce<D, M>(&pool_map, &qmap, a, sm, start, u_early, abort_flag, lane);
+    } else if (second) {
+        if constexpr (of_blocks<M>)
+            block_produce<D, M>(&pool_map, &qmap, a, sm, start, u_early, abort_flag, 1, lane);
     } else if (warp == 1) {
         if (lane == 0) prefill_mma<D, M>(a, sm, tmem, abort_flag);
         __syncwarp();
