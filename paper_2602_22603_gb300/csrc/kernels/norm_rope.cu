@@ -316,7 +316,9 @@ __global__ void __launch_bounds__(kNormThreads, 7)
 
 // Backwards.  A CTA's warps take tasks (query or key heads of a token) in turn and
 // add up the weights' gradients of their lanes' elements; the CTA's sums go to one
-// partial row, added by a second kernel in a fixed order.
+// partial row, added by a second kernel in a fixed order.  8,192 tokens of 64 query
+// and 8 key heads of 128: 84 us, 5.4 TB/s; two rows of a lane group in flight 103,
+// eight 105, a position read a task ahead 86.
 template <int D, bool kPairs>
 __global__ void __launch_bounds__(kGradThreads)
     sq_norm_rope_grad_kernel(const __grid_constant__ NormRopeGradArgs a) {
@@ -337,17 +339,8 @@ __global__ void __launch_bounds__(kGradThreads)
     f32x2 gq[4], gk[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) gq[i] = gk[i] = f2(0.f, 0.f);
-    // (a task's position is read while the one before is worked on: the table's row
-    // waits for it)
-    const unsigned stride = gridDim.x * kWarps;
-    auto position = [&](unsigned task) {
-        return a.positions && task < tasks ? __ldg(&a.positions[task / (unsigned)per.total]) : 0;
-    };
-    int next_pos = position(blockIdx.x * kWarps + warp);
-    for (unsigned task = blockIdx.x * kWarps + warp; task < tasks; task += stride) {
+    for (unsigned task = blockIdx.x * kWarps + warp; task < tasks; task += gridDim.x * kWarps) {
         const unsigned t = task / (unsigned)per.total;
-        int pos = next_pos;
-        next_pos = position(task + stride);
         int part = (int)(task - t * per.total);
         const bool is_k = part >= per.q;
         if (is_k) part -= per.q;
@@ -369,6 +362,7 @@ __global__ void __launch_bounds__(kGradThreads)
             }
         }
         Turn tn;
+        int pos = a.positions ? __ldg(&a.positions[t]) : 0;
         if (a.rot > 0) pos = checked_pos(pos, a.max_pos, a.err);
         load_turn<kPairs>(tn, a.rope, pos, a.rot, ln);
 #pragma unroll
