@@ -448,9 +448,11 @@ SQ_API int sq_qk_norm_rope_backward(sq_cache *cache, int32_t n_tokens, const voi
  *         overlap nowhere (INVALID_ARG)
  *   sm_scale: finite, >= 0; window, n_sink >= 0
  * Rows of partial pages (sq_evict_spans_ragged) are counted as the rows they are.
- * Only the 64-row runs of pages that some query sees a row of are read; the rows
- * in those that a query does not see must be finite, as rows stored once are
- * (their weights are zero), while slots past a sequence's end may hold anything.
+ * Only the 64-row runs of pages that some query sees a row of are read.  Rows that
+ * a query does not see, and slots past a sequence's end, may hold anything: an
+ * infinity or NaN there does not reach its output (it costs time: the queries of
+ * such a run are taken once more).
+ * Single tokens without lse run as sq_decode_attention does.
  * Weights and normaliser are rounded as in sq_prefill_attention, whose limits on
  * library memory for partial results hold too.  A plan of more than 2^24 key
  * tiles (all queries of the call together) is refused.
@@ -481,7 +483,8 @@ SQ_API int sq_tree_attention(sq_cache *cache, const sq_seq *seqs, int32_t n_seqs
 
 /* After verification: of the newest n_draft rows of `seq` those with the indices
  * path[0] < path[1] < ... (a path of the tree from its root, n_path of them, 0:
- * none) stay, in order, and the others leave, as by sq_evict_spans_ragged, but
+ * none) stay, in order, and the others leave: as by sq_evict_spans, or as by
+ * sq_evict_spans_ragged where the sequence has partial pages already.  But
  * sq_seq_next_pos goes back by as many: their positions are handed out again.
  * Errors: BAD_HANDLE, INVALID_ARG, NO_PAGES, NO_MEMORY, CUDA. */
 SQ_API int sq_accept_draft(sq_cache *cache, sq_seq seq, int32_t n_draft, const int32_t *path,

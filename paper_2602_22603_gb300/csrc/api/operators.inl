@@ -644,6 +644,8 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
     a.rows = plan.o_rows ? reinterpret_cast<const int2*>(plan.d + plan.o_rows) : nullptr;
     a.bits = reinterpret_cast<const uint32_t*>(plan.d + plan.o_bits);
     a.n_words = plan.n_words;
+    a.pool = c->pool;
+    a.q = q;
     a.n_ctas = plan.n_ctas;
     a.n_pieces = plan.n_pieces;
     a.n_tiles = a.n = a.n_q = 0;  // (the items')

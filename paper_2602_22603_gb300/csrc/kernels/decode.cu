@@ -416,8 +416,8 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
             const uint32_t empty = smem_addr(&bars[C::kStages + slot]);
             // Pages a ragged eviction left partial: bit r of vm says whether
             // row r of this warp's 16 holds a row of its page (read before
-            // the wait, off the critical path).  The unused slots hold zeros
-            // or rows once appended, so only their scores are masked.
+            // the wait, off the critical path).  The others' scores are masked,
+            // and their V rows zeroed before the product.
             uint32_t vm = 0xffffu;
             if (a.page_fill) {
                 // P is a power of two >= 8 and the 16 rows start at a multiple
@@ -523,18 +523,18 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
                 }
 
                 // Rows past the last valid token hold stale or never-written
-                // shared memory: zero this warp's such V rows so 0 * V stays 0.
-                const bool tail = tbase + 16 > n_tok;
+                // shared memory, and rows that their page's fill hides may hold
+                // anything: zero this warp's such V rows so 0 * V stays 0.
+                const bool tail = tbase + 16 > n_tok || vm != 0xffffu;
                 if (tail) {
-                    const int first = max(0, n_tok - tbase);
-                    const int per_row = C::kColBlocks * 8;  // 16-byte chunks per row
-                    const int total = (16 - first) * per_row;
+                    const uint32_t live = vm & ((1u << min(max(n_tok - tbase, 0), 16)) - 1u);
+                    constexpr int per_row = C::kColBlocks * 8;  // 16-byte chunks per row
                     uint8_t* vgen = ring + slot * C::kStageBytes + C::kTileBytes;
-                    for (int idx = lane; idx < total; idx += 32) {
-                        const int row = w4 * 16 + first + idx / per_row;
-                        const int rem = idx % per_row;
-                        *reinterpret_cast<uint4*>(vgen + (rem >> 3) * C::kBlockBytes + row * 128 +
-                                                  (rem & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    for (uint32_t dead_rows = ~live & 0xffffu; dead_rows; dead_rows &= dead_rows - 1) {
+                        const int row = w4 * 16 + __ffs(dead_rows) - 1;
+                        for (int rem = lane; rem < per_row; rem += 32)
+                            *reinterpret_cast<uint4*>(vgen + (rem >> 3) * C::kBlockBytes + row * 128 +
+                                                      (rem & 7) * 16) = make_uint4(0, 0, 0, 0);
                     }
                     __syncwarp();
                 }

@@ -72,6 +72,9 @@ struct BlockArgs : PrefillArgs {
     const uint32_t* bits;   // [queries][n_words] drafted trees' visibility from the
                             // item's base on
     int32_t n_words;
+    // as the tensor maps have them (rows that are taken once more read them plainly)
+    const void* pool;       // bf16 [layers][num_pages][2][Hkv][P][D]
+    const void* q;          // bf16 [queries][Hq][D]
     int32_t n_ctas;         // CTAs launched (one-tile blocks are dealt out to them;
                             // otherwise one for each item)
 };

@@ -1177,9 +1177,10 @@ __device__ __forceinline__ void st_32(void* p, const uint32_t (&v)[8]) {
 }
 
 // Normalises and writes one row of O_t (with tile b's part in dual-key mode) to
-// the outputs, or to the item's partial result.
+// the outputs, or to the item's partial result.  True (blocks): some value of the
+// row is an infinity or NaN.
 template <int D, int M>
-__device__ __forceinline__ void prefill_write(const PrefillArgs& a, const Item& it, int q_row, uint32_t tl,
+__device__ __forceinline__ bool prefill_write(const PrefillArgs& a, const Item& it, int q_row, uint32_t tl,
                                               uint32_t col_o, int t, int row, bool valid,
                                               float m_run, float l, float wa, float wb) {
     using C = PreCfg<D, M>;
@@ -1214,6 +1215,7 @@ __device__ __forceinline__ void prefill_write(const PrefillArgs& a, const Item& 
         to_even = reinterpret_cast<uint8_t*>(row & 1 ? other : mine);
         to_odd = reinterpret_cast<uint8_t*>(row & 1 ? mine : other);
     }
+    uint64_t odd_values = 0;  // two sums of 0 * value: NaN where one is not finite
     // (a block's: rolled up, for the instruction cache)
 #pragma unroll (of_blocks<M> ? 1 : D / 32)
     for (int c = 0; c < D / 32; ++c) {
@@ -1236,6 +1238,10 @@ __device__ __forceinline__ void prefill_write(const PrefillArgs& a, const Item& 
         } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(o[i]) * inv;
+        }
+        if constexpr (of_blocks<M>) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) odd_values = ffma2(f2pack(f[2 * i], f[2 * i + 1]), 0, odd_values);
         }
         if (paired) {
             const bool odd = row & 1;
@@ -1281,6 +1287,9 @@ __device__ __forceinline__ void prefill_write(const PrefillArgs& a, const Item& 
             }
         }
     }
+    float x, y;
+    f2unpack(odd_values, x, y);
+    return valid && !(x + y == 0.f);
 }
 
 // Which keys a row sees, beside the tiles' own visibility bits (positions are
@@ -1331,6 +1340,79 @@ template <>
 struct RowMask<kBlocks | kSmallPages> : BlockRowMask {};
 template <>
 struct RowMask<kBlocks | kOneTile | kSmallPages> : BlockRowMask {};
+
+// A key that a row does not see has the weight 0 in the row's tile product, and
+// 0 times an infinity or NaN in that key's V row is NaN.  So a block's row whose
+// output is not finite is taken once more, over the keys that it does see and with
+// the maximum and normaliser that it has: a warp on the rows in `rows` one by one,
+// a lane to a key for the weights and to D / 32 columns for the sum.  (It costs the
+// item D fused multiply-adds a row to look, and nothing more as long as stored rows
+// are finite.)
+template <int D, int M, typename Args>
+__device__ __noinline__ void rows_again(const Args& a, const BlockItem& it, int tile, uint32_t rows, int row0,
+                                        float m_run, float l, int lane) {
+    constexpr int kCols = D / 32;
+    const int g = it.head & (kBlockTwoTiles - 1), per = pieces_of<M>(a), br = 128 / per;
+    const size_t run = (size_t)a.P * D;  // a head's rows in a page
+    const __nv_bfloat16* keys =
+        static_cast<const __nv_bfloat16*>(a.pool) + ((size_t)a.layer * a.num_pages * 2 * a.Hkv + g) * run;
+    for (; rows; rows &= rows - 1) {
+        const int src = __ffs(rows) - 1, row = row0 + src;
+        const float m = __shfl_sync(0xffffffffu, m_run, src), sum = __shfl_sync(0xffffffffu, l, src);
+        const int qi = tile * a.BP + row / a.G, h = g * a.G + row % a.G;
+        BlockRowMask mask;
+        mask.init(a, it, qi);
+        const size_t q_head = (size_t)(it.q_row + qi) * a.Hq + h;
+        const uint4* q = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + q_head * D);
+        float acc[kCols];
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
+        for (int x = 0; x < 4 * it.n_tiles; ++x) {
+            const int j = it.t0 + (x >> 2), w = x & 3;
+            const PrefillTile* t = a.tiles + j;
+            const int key = __ldg(w < 2 ? &t->key0 : &t->key0b) + 32 * (w & 1) + lane;
+            const uint32_t see = __ldg(&t->vis[w]) & mask.word(key - lane);
+            int64_t at = 0;  // of the key's K row
+            float p = 0.f;
+            if ((see >> lane) & 1u) {
+                // (a page outside the pool was flagged, and page 0 read)
+                const int page = __ldg(&a.tile_pages[(size_t)j * per + (w * 32 + lane) / br]);
+                at = (int64_t)((uint32_t)page < (uint32_t)a.num_pages ? page : 0) * 2 * a.Hkv * run +
+                     (size_t)(key & (a.P - 1)) * D;
+                float s = 0.f;
+                for (int c = 0; c < D / 8; ++c) {
+                    const uint4 kk = reinterpret_cast<const uint4*>(keys + at)[c], qq = q[c];
+                    const uint32_t kw[4] = {kk.x, kk.y, kk.z, kk.w}, qw[4] = {qq.x, qq.y, qq.z, qq.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        s = fmaf(__uint_as_float(kw[i] << 16), __uint_as_float(qw[i] << 16), s);
+                        s = fmaf(__uint_as_float(kw[i] & 0xffff0000u), __uint_as_float(qw[i] & 0xffff0000u), s);
+                    }
+                }
+                p = __bfloat162float(__float2bfloat16(ex2_ftz(fmaf(s, a.scale_log2, m == -INFINITY ? 0.f : -m))));
+            }
+            for (uint32_t left = see; left; left &= left - 1) {
+                const int c = __ffs(left) - 1;
+                const float pc = __shfl_sync(0xffffffffu, p, c);
+                const __nv_bfloat16* v = keys + __shfl_sync(0xffffffffu, at, c) + a.Hkv * run;
+#pragma unroll
+                for (int i = 0; i < kCols; ++i) acc[i] = fmaf(pc, __bfloat162float(v[lane + 32 * i]), acc[i]);
+            }
+        }
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) {
+            const float f = acc[i] * inv;
+            const int col = lane + 32 * i;
+            if (it.part >= 0)
+                a.part_o[(((size_t)it.part * kPrefillQTiles + tile) * kPrefillRows + row) * D + col] = f;
+            else if (a.out_f32)
+                static_cast<float*>(a.out)[q_head * D + col] = f;
+            else
+                static_cast<__nv_bfloat16*>(a.out)[q_head * D + col] = __float2bfloat16(f);
+        }
+    }
+}
 
 // What a softmax warp carries from item to item, in two words so that the
 // loop over key tiles keeps its registers: the loads of the items before, and,
@@ -1616,10 +1698,15 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
     const Item end = make_item<M>(a, item_read<D, M>(sm, k));
     int q_row = end.pos_lo;
     if constexpr (of_blocks<M>) q_row = item_block<D, M>(sm, k).q_row;
-    prefill_write<D, M>(a, end, q_row, tl, col_o, t, row, valid, m_run, l, wa, wb);
+    const bool again = prefill_write<D, M>(a, end, q_row, tl, col_o, t, row, valid, m_run, l, wa, wb);
     if (dual) {
         tc_fence_before();
         mbar_arrive(sm.bar<D, M>(C::kBarXFree));
+    }
+    if constexpr (of_blocks<M>) {
+        const uint32_t rows = __ballot_sync(0xffffffffu, again);
+        __syncwarp();  // the pairs' stores come before those of rows_again
+        if (rows) rows_again<D, M>(a, item_block<D, M>(sm, k), t, rows, wq * 32, m_run, l, lane);
     }
     return true;
 }
