@@ -530,10 +530,10 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
                     const uint32_t live = vm & ((1u << min(max(n_tok - tbase, 0), 16)) - 1u);
                     constexpr int per_row = C::kColBlocks * 8;  // 16-byte chunks per row
                     uint8_t* vgen = ring + slot * C::kStageBytes + C::kTileBytes;
-                    for (uint32_t dead_rows = ~live & 0xffffu; dead_rows; dead_rows &= dead_rows - 1) {
-                        const int row = w4 * 16 + __ffs(dead_rows) - 1;
-                        for (int rem = lane; rem < per_row; rem += 32)
-                            *reinterpret_cast<uint4*>(vgen + (rem >> 3) * C::kBlockBytes + row * 128 +
+                    for (int idx = lane; idx < 16 * per_row; idx += 32) {
+                        const int r = idx / per_row, rem = idx % per_row;
+                        if (!((live >> r) & 1u))
+                            *reinterpret_cast<uint4*>(vgen + (rem >> 3) * C::kBlockBytes + (w4 * 16 + r) * 128 +
                                                       (rem & 7) * 16) = make_uint4(0, 0, 0, 0);
                     }
                     __syncwarp();
