@@ -15,9 +15,9 @@ cudaError_t prepare_one() {
 template <int D>
 cudaError_t prepare() {
     cudaError_t e = prepare_one<D, BlockArgs>();
-    if (e == cudaSuccess) e = prepare_one<D, BlockShortArgs>();
-    if (e == cudaSuccess) e = prepare_one<D, SmallBlockArgs>();
-    if (e == cudaSuccess) e = prepare_one<D, SmallBlockShortArgs>();
+    if (e == cudaSuccess && D == 128) e = prepare_one<128, BlockShortArgs>();
+    if (e == cudaSuccess) e = prepare_one<D, BlockArgs2>();
+    if (e == cudaSuccess) e = prepare_one<D, BlockShortArgs2>();
     // (the merging kernels share every SM with the kernel above)
     if (e == cudaSuccess)
         e = cudaFuncSetAttribute(dev::sq_prefill_combine_kernel<D, 2, 24, BlockCombineArgs>,
@@ -60,15 +60,19 @@ cudaError_t blocks_prepare(int D) { return D == 128 ? prepare<128>() : prepare<6
 template <int D>
 static cudaError_t launch_d(const CUtensorMap& pool_map, const CUtensorMap& qmap, const BlockShortArgs& a,
                             bool one, cudaStream_t st) {
-    if (a.n_pieces > 2) {
-        SmallBlockShortArgs s;
+    // (two producer warps: see block_produce)
+    if (one && (D == 64 || a.n_pieces > 2)) {
+        BlockShortArgs2 s;
         static_cast<BlockShortArgs&>(s) = a;
-        if (one) return launch_one<D>(pool_map, qmap, s, st);
-        SmallBlockArgs t;
-        static_cast<BlockArgs&>(t) = a;
-        return launch_one<D>(pool_map, qmap, t, st);
+        return launch_one<D>(pool_map, qmap, s, st);
     }
-    if (one) return launch_one<D>(pool_map, qmap, a, st);
+    if constexpr (D == 128)
+        if (one) return launch_one<D>(pool_map, qmap, a, st);
+    if (a.n_pieces > 2) {
+        BlockArgs2 s;
+        static_cast<BlockArgs&>(s) = a;
+        return launch_one<D>(pool_map, qmap, s, st);
+    }
     const BlockArgs& base = a;
     return launch_one<D>(pool_map, qmap, base, st);
 }

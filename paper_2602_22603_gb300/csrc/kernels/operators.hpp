@@ -84,9 +84,9 @@ struct BlockShortArgs : BlockArgs {
     int32_t n_unsafe;
     int32_t unsafe[kMaxUnsafe];
 };
-// The same on pages of fewer than 64 tokens (instances of their own).
-struct SmallBlockArgs : BlockArgs {};
-struct SmallBlockShortArgs : BlockShortArgs {};
+// The same with two producer warps (instances of their own).
+struct BlockArgs2 : BlockArgs {};
+struct BlockShortArgs2 : BlockShortArgs {};
 struct BlockCombineArgs {
     const BlockMerge* merges;
     int32_t n_merges;

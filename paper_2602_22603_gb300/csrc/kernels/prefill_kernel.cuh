@@ -71,10 +71,11 @@
 // sees; the roles, the ring and the products are those above.
 //
 // Warp roles (320 threads): warp 0 loads (lanes 0 and 1 issue the TMA copies,
-// two loads at a time), lane 0 of warp 1 issues the MMAs and warp 1 owns the
-// TMEM allocation, warps 2-5
+// two loads at a time; query blocks: a lane to a box), lane 0 of warp 1 issues
+// the MMAs and warp 1 owns the TMEM allocation, warps 2-5
 // are the softmax warpgroup of tile a and warps 6-9 that of tile b (warp w
-// reads TMEM lanes 32 (w mod 4) .. +31, one row per thread).  Every wait is
+// reads TMEM lanes 32 (w mod 4) .. +31, one row per thread), and warp 10, in
+// instances that have it, is the second producer.  Every wait is
 // bounded; a wait that runs out sets the error word and the CTA winds down
 // after its copies and MMAs in flight have completed.
 #pragma once
@@ -92,15 +93,24 @@ namespace {
 // Instances.  kOneTile: every query of an item fits in tile a.  kBlocks: items
 // carry what they need of their own sequence and have key tiles of their own
 // (query blocks of a batch, see BlockItem); otherwise all items belong to one
-// sequence, whose newest n_q tokens they share out.  kSmallPages: blocks on pages of
-// fewer than 64 tokens, whose many boxes two producer warps load.
-constexpr int kOneTile = 1, kBlocks = 2, kSmallPages = 4;
+// sequence, whose newest n_q tokens they share out.  kTwoProducers: blocks whose loads
+// are two producer warps': on pages of fewer than 64 tokens, which take many boxes,
+// and one-tile blocks of 64 dimensions, whose loads are short.
+constexpr int kOneTile = 1, kBlocks = 2, kTwoProducers = 4;
 template <int M>
 constexpr bool one_tile = (M & kOneTile) != 0;
 template <int M>
 constexpr bool of_blocks = (M & kBlocks) != 0;
 template <int M>
-constexpr int producers = (M & kSmallPages) != 0 ? 2 : 1;
+constexpr int producers = (M & kTwoProducers) != 0 ? 2 : 1;
+
+// S buffers: one for each softmax warpgroup, and a third for one-tile blocks of 64
+// dimensions, whose O leaves the columns (S_2 after O_b).  With two a warpgroup that has handed over
+// P waits for its PV and for the QK after it before it has work again; with three that
+// QK is done by then.  8 trees of 16 over 32,768 tokens, 64/8/64 heads, pages of 32:
+// 121 -> 107 us by an issuing lane that waits for P alone, 100 with the third buffer.
+template <int D, int M>
+constexpr int s_buffers = D == 64 && M == (kBlocks | kOneTile | kTwoProducers) ? 3 : 2;
 
 // Items in flight between the producer and the other roles, and the warps that
 // read each (MMA warp and eight softmax warps).
@@ -123,9 +133,11 @@ struct PreCfg {
     static constexpr int kBarFull = 1;                  // [kSlots] tile landed (V: and ready)
     static constexpr int kBarEmpty = kBarFull + kSlots; // [kSlots] slot consumed by the MMAs
     static constexpr int kBarS = kBarEmpty + kSlots;    // [2] S_t written (and PV_t before it done)
-    static constexpr int kBarP = kBarS + 2;             // [2] P_t written (128 arrivals)
-    static constexpr int kBarO = kBarP + 2;             // [2] last PV_t done
-    static constexpr int kBarVfix = kBarO + 2;          // V of the last key tile landed
+    static constexpr int kBufs = s_buffers<D, M>;
+    static constexpr int kBarP = kBarS + kBufs;         // [2] P_t written (128 arrivals)
+    static constexpr int kBarO = kBarP + kBufs;         // [2] last PV_t done
+    static constexpr int kBarPV = kBarO + 2;            // (three S buffers) the last PV but two done
+    static constexpr int kBarVfix = kBarPV + (kBufs > 2 ? 1 : 0);          // V of the last key tile landed
     static constexpr int kBarQFree = kBarVfix + 1;      // the item's last QK product done
     static constexpr int kBarDone = kBarQFree + 1;      // every MMA of the CTA done
     static constexpr int kBarItem = kBarDone + 1;       // [kItemSlots] item written
@@ -144,6 +156,10 @@ struct PreCfg {
     static constexpr uint32_t kTmemCols = 512;
     static constexpr uint32_t kColS = 0;    // S_t (fp32) at 128 t; P_t (bf16 pairs) over its first 64
     static constexpr uint32_t kColO = 256;  // O_t (fp32) at 256 + 128 t
+    static constexpr uint32_t kOStep = kBufs > 2 ? 64 : 128;  // (256 + 64 t; S_2 at 384)
+    __device__ static uint32_t col_s(uint32_t buf) {
+        return kBufs > 2 && buf == 2 ? 384u : kColS + buf * kPrefillKeys;
+    }
     static constexpr uint32_t kIdescQK = mma_idesc_bf16(128, kPrefillKeys, false);
     static constexpr uint32_t kIdescPV = mma_idesc_bf16(128, D, true);
     static_assert(kSmemBytes <= 232448, "shared memory");
@@ -248,20 +264,23 @@ __device__ __forceinline__ uint32_t low_bits_through(int x) {
 // is V_j.  In dual-key mode (tile a takes the even key tiles, tile b the odd
 // ones) the loads follow the order in which the MMA warp consumes them, so
 // that no tile waits in the ring for a later one: K_0, K_1, then V_j and
-// K_{j+2} in turn, and the last two V tiles.
+// K_{j+2} in turn, and the last two V tiles.  (kLead: the K tiles ahead of their V,
+// one for each S buffer.)
+template <int kLead = 2>
 __device__ __forceinline__ void load_of(int u, int T, bool dual, int& j, int& kv) {
     if (!dual) {
         j = u >> 1;
         kv = u & 1;
-    } else if (u < 2) {
+    } else if (u < kLead && (kLead == 2 || u < T)) {
         j = u;
         kv = 0;
-    } else if (u >= 2 * T - 2) {
+    } else if (u >= 2 * T - kLead) {
         j = u - T;
         kv = 1;
     } else {
-        j = ((u - 2) >> 1) + ((u & 1) ? 2 : 0);
-        kv = (u & 1) ? 0 : 1;
+        const bool k = (u ^ kLead) & 1;
+        j = ((u - kLead) >> 1) + (k ? kLead : 0);
+        kv = k ? 0 : 1;
     }
 }
 
@@ -286,7 +305,7 @@ __device__ __forceinline__ int4 tile_record(const PrefillArgs& a, int t0, int T,
 // lane to a box; the batch's records are read together, a batch ahead of their use.
 template <int M>
 __device__ __forceinline__ int pieces_of(const PrefillArgs& a) { return producers<M> > 1 ? a.n_pieces : 2; }
-template <int M>
+template <int D, int M>
 struct BlockBatch {
     int32_t key, page;  // the box's first key; its page, -1: no such box
     // the producer warp w's loads from its x0-th on
@@ -296,7 +315,7 @@ struct BlockBatch {
         page = -1;
         if (u >= 2 * it.T) return;
         int j, kv;
-        load_of(u, it.T, it.dual, j, kv);
+        load_of<s_buffers<D, M>>(u, it.T, it.dual, j, kv);
         const PrefillTile* t = a.tiles + it.t0 + j;
         const int half = per >> 1, br = 64 / half;
         key = i < half ? __ldg(&t->key0) + i * br : __ldg(&t->key0b) + (i - half) * br;
@@ -343,11 +362,11 @@ struct ItemRecord {
 };
 
 // A CTA's own item and the first records of its loads, in the producer's lanes.
-template <int M>
+template <int D, int M>
 struct FirstItem {
     ItemRecord<M> item;
     int4 rec;         // (one sequence's prefill)
-    BlockBatch<M> batch;  // (block items)
+    BlockBatch<D, M> batch;  // (block items)
     __device__ void read(const PrefillArgs& a, int w, int lane) {
         item.read(a, blockIdx.x);
         if constexpr (of_blocks<M>) batch.read(a, make_item<M>(a, item.raw), 0, w, lane);
@@ -364,7 +383,7 @@ struct FirstItem {
 // layers back to back 85.4, 85.4 and 86.3).
 template <int D, int M>
 __device__ __forceinline__ int early_loads(const CUtensorMap* pool_map, const PrefillShortArgs& a,
-                                           const Smem& sm, const FirstItem<M>& start, const Item& it,
+                                           const Smem& sm, const FirstItem<D, M>& start, const Item& it,
                                            int lane) {
     using C = PreCfg<D, M>;
     static_assert(C::kSlots > 2, "ring");
@@ -397,31 +416,32 @@ __device__ __forceinline__ int early_loads(const CUtensorMap* pool_map, const Pr
     return safe ? 2 : 0;
 }
 
-// The same for a block item: its first two loads (on pages of 64 tokens or more one
-// warp's) are the first four lanes' boxes.
+// The same for a block item on pages of 64 tokens or more: its first two loads, the
+// first four lanes' boxes, or, of two producer warps' loads, the first one's.
 template <int D, int M>
 __device__ __forceinline__ int early_loads(const CUtensorMap* pool_map, const BlockShortArgs& a,
-                                           const Smem& sm, const FirstItem<M>& start, const Item& it,
+                                           const Smem& sm, const FirstItem<D, M>& start, const Item& it,
                                            int lane) {
     using C = PreCfg<D, M>;
     const int32_t unsafe = lane < a.n_unsafe ? a.unsafe[lane] : -1;
+    constexpr int kBoxes = producers<M> > 1 ? 2 : 4;
     const int32_t page = start.batch.page, key = start.batch.key;
     // (whole boxes inside the sequence)
-    bool safe = lane > 3 || ((uint32_t)page < (uint32_t)a.num_pages && key <= start.item.n(a) - 64);
+    bool safe = lane >= kBoxes || ((uint32_t)page < (uint32_t)a.num_pages && key <= start.item.n(a) - 64);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
+    for (int x = 0; x < kBoxes; ++x) {
         const int32_t p = __shfl_sync(0xffffffffu, page, x);  // (every lane's)
         safe = safe && !(unsafe >= 0 && unsafe == p);
     }
     safe = __all_sync(0xffffffffu, safe);
     __syncwarp();  // (lane 0 initialised the barriers)
-    if (safe && lane < 4) {
+    if (safe && lane < kBoxes) {
         const int u = lane >> 1;
         int j, kv;
-        load_of(u, it.T, it.dual, j, kv);
+        load_of<s_buffers<D, M>>(u, it.T, it.dual, j, kv);
         const uint32_t fb = sm.bar<D, M>(C::kBarFull + u);
         if (!(lane & 1)) mbar_arrive_expect_tx(fb, C::kSlotBytes);
-        __syncwarp(0xfu);
+        __syncwarp((1u << kBoxes) - 1);
 #pragma unroll
         for (int cb = 0; cb < C::kColBlocks; ++cb)
             tma_load_4d(sm.base + C::kOffRing + u * C::kSlotBytes + cb * C::kBlockBytes + (lane & 1) * 64 * 128,
@@ -429,7 +449,7 @@ __device__ __forceinline__ int early_loads(const CUtensorMap* pool_map, const Bl
                         a.layer);
     }
     __syncwarp();
-    return safe ? 2 : 0;
+    return safe ? kBoxes / 2 : 0;
 }
 
 // The producer warp, item by item: the query tiles, then the K and V tiles of
@@ -447,7 +467,7 @@ __device__ __forceinline__ int early_loads(const CUtensorMap* pool_map, const Bl
 // their page from global memory.
 template <int D, int M>
 __device__ void prefill_produce(const CUtensorMap* pool_map, const CUtensorMap* qmap,
-                                const PrefillArgs& a, const Smem& sm, const FirstItem<M>& start,
+                                const PrefillArgs& a, const Smem& sm, const FirstItem<D, M>& start,
                                 int u_early, volatile int* abort_flag, int lane) {
     using C = PreCfg<D, M>;
     const int br = a.P < 64 ? a.P : 64;  // rows of one TMA box
@@ -680,7 +700,9 @@ __device__ void prefill_produce(const CUtensorMap* pool_map, const CUtensorMap* 
 
 // The producer warps of block items.  A lane holds what one box of the next loads
 // needs (BlockBatch), so that a load costs a warp a wait, an expected byte count and
-// the boxes' copies.  Pages of 64 tokens or more are one warp's loads.  Smaller pages
+// the boxes' copies.  Pages of 64 tokens or more are one warp's loads (one-tile blocks
+// of 64 dimensions: two warps', 108 -> 99 us for 8 trees of 16 over 32,768 tokens at
+// 64/8/64 heads, where one warp is the bound).  Smaller pages
 // have 4, 8 or 16 boxes a load; there the even loads are one warp's, the odd ones
 // the other's, and every load's slot has a commit of its own (8 trees of 16 over
 // 32,768 tokens on pages of 16 and 8 tokens, 4 and 8 KV heads of 64 dimensions: 83 ->
@@ -690,7 +712,7 @@ __device__ void prefill_produce(const CUtensorMap* pool_map, const CUtensorMap* 
 // reads its next records then.
 template <int D, int M, typename Args>
 __device__ void block_produce(const CUtensorMap* pool_map, const CUtensorMap* qmap, const Args& a,
-                              const Smem& sm, const FirstItem<M>& start, int early,
+                              const Smem& sm, const FirstItem<D, M>& start, int early,
                               volatile int* abort_flag, int w, int lane) {
     using C = PreCfg<D, M>;
     // blocks of one tile are dealt out to the CTAs beforehand: HBM bounds them, and
@@ -702,7 +724,7 @@ __device__ void block_produce(const CUtensorMap* pool_map, const CUtensorMap* qm
     const int mine = lane / per, piece = lane & (per - 1);
     const uint32_t group = (uint32_t)((1ull << per) - 1);
     ItemRecord<M> item = start.item, next = start.item;
-    BlockBatch<M> first = start.batch;
+    BlockBatch<D, M> first = start.batch;
     uint32_t k = 0;           // the item's number
     bool asked = false;       // an answer of the launch hardware is due
     uint32_t n_queries = 0;   // items whose queries were loaded
@@ -779,12 +801,12 @@ __device__ void block_produce(const CUtensorMap* pool_map, const CUtensorMap* qm
         const int ask_at = max(T - 14 / kWarps, 0), take_at = max(w ? T - 2 : T - 8 / kWarps, 0),
                   read_at = max(T - 4 / kWarps, 0), query_at = kWarps == 2 ? 0 : 1;
         if (w == 0 && k == 0) load_queries(it);
-        BlockBatch<M> cur = first, ahead;
+        BlockBatch<D, M> cur = first, ahead;
         for (int x0 = 0; ok && x0 < T; x0 += n_batch) {
             ahead.read(a, it, x0 + n_batch, w, lane);
             // this lane's box
             int j, kv;
-            load_of(min(x0 + mine, T - 1) * kWarps + w, it.T, it.dual, j, kv);
+            load_of<s_buffers<D, M>>(min(x0 + mine, T - 1) * kWarps + w, it.T, it.dual, j, kv);
             const bool box = cur.page >= 0;
             const uint32_t boxes = __ballot_sync(0xffffffffu, box) >> (mine * per) & group;
             const uint32_t bytes = (uint32_t)__popc(boxes) * br * 128 * C::kColBlocks;
@@ -917,22 +939,22 @@ __device__ __forceinline__ MmaDesc mma_desc(const Smem& sm, uint32_t tmem) {
     return d;
 }
 
-// S_t = Q_q K^T for the K tile in `slot`, into TMEM columns 128 t (q = t
-// except in dual-key mode, where both tiles use query tile 0).
+// S_t = Q_q K^T for the K tile in `slot`, into S buffer t (q = t except in
+// dual-key mode, where both tiles use query tile 0).
 template <int D, int M>
 __device__ __forceinline__ void issue_qk(const MmaDesc& d, int t, int q, uint32_t slot) {
     using C = PreCfg<D, M>;
-    mma_bf16_ss_steps<D / 16>(d.tmem + C::kColS + (uint32_t)t * kPrefillKeys, d.q[q],
+    mma_bf16_ss_steps<D / 16>(d.tmem + C::col_s(t), d.q[q],
                               d.k + slot * (C::kSlotBytes >> 4), d.k_hi, C::kIdescQK);
 }
 
-// O_t += P_t V for the V tile in `slot`; P_t from TMEM over the first half of S_t.
+// O_t += P_t V for the V tile in `slot`; P_t from TMEM over the first half of S
+// buffer `buf` (t where there are two).
 template <int D, int M>
-__device__ __forceinline__ void issue_pv(const MmaDesc& d, int t, uint32_t slot, bool first) {
+__device__ __forceinline__ void issue_pv(const MmaDesc& d, int t, int buf, uint32_t slot, bool first) {
     using C = PreCfg<D, M>;
     static_assert(kPrefillKeys == 128, "8 steps of 16 keys");
-    mma_bf16_ts_steps8(d.tmem + C::kColO + (uint32_t)t * 128,
-                       d.tmem + C::kColS + (uint32_t)t * kPrefillKeys,
+    mma_bf16_ts_steps8(d.tmem + C::kColO + (uint32_t)t * C::kOStep, d.tmem + C::col_s(buf),
                        d.v + slot * (C::kSlotBytes >> 4), d.v_hi, C::kIdescPV, first ? 0u : 1u);
 }
 
@@ -987,7 +1009,7 @@ __device__ bool prefill_mma_dual(const Smem& sm, const MmaDesc& d, int T, MmaPha
         if (!mbar_wait(sm.bar<D, M>(C::kBarP + t), (ph.p >> t) & 1, abort_flag)) return false;
         ph.p ^= 1u << t;
         tc_fence_after();
-        issue_pv<D, M>(d, t, slot, j < 2);
+        issue_pv<D, M>(d, t, t, slot, j < 2);
         used();
         if (j + 2 >= T) {  // the last key tile of tile t
             mma_commit(sm.bar<D, M>(C::kBarO + t));
@@ -998,6 +1020,56 @@ __device__ bool prefill_mma_dual(const Smem& sm, const MmaDesc& d, int T, MmaPha
         mma_commit(sm.bar<D, M>(C::kBarS + t));
         used();
         if (j + 3 == T) mma_commit(sm.bar<D, M>(C::kBarQFree));  // the item's last QK
+    }
+    ph.slot = slot;
+    return true;
+}
+
+// The same with three S buffers: key tile number u of the CTA's life (the item's
+// first is u0) in buffer u mod 3, its phase u / 3; PV_j and the QK of key tile
+// j + 3, into the buffer that held P_j, are issued together.
+template <int D, int M>
+__device__ bool prefill_mma_three(const Smem& sm, const MmaDesc& d, int T, MmaPhase& ph,
+                                  volatile int* abort_flag) {
+    using C = PreCfg<D, M>;
+    uint32_t slot = ph.slot, full = (ph.ub / C::kSlots) & 1;
+    auto used = [&]() {
+        mma_commit(sm.bar<D, M>(C::kBarEmpty + slot));
+        if (++slot == C::kSlots) {
+            slot = 0;
+            full ^= 1;
+        }
+    };
+    const uint32_t u0 = ph.ub / 2;
+    for (int j = 0; j < min(3, T); ++j) {  // S = Q_a K_j
+        const uint32_t buf = (u0 + j) % 3;
+        if (!mbar_wait(sm.bar<D, M>(C::kBarFull + slot), full, abort_flag)) return false;
+        issue_qk<D, M>(d, (int)buf, 0, slot);
+        mma_commit(sm.bar<D, M>(C::kBarS + buf));
+        used();
+    }
+    if (T <= 3) mma_commit(sm.bar<D, M>(C::kBarQFree));  // the item's last QK
+    uint32_t buf = u0 % 3, parity = (u0 / 3) & 1;
+    for (int j = 0; j < T; ++j) {
+        const int t = j & 1;
+        if (!mbar_wait(sm.bar<D, M>(C::kBarP + buf), parity, abort_flag)) return false;
+        tc_fence_after();
+        issue_pv<D, M>(d, t, (int)buf, slot, j < 2);
+        if (j + 3 < T) {
+            used();
+            issue_qk<D, M>(d, (int)buf, 0, slot);
+            mma_commit(sm.bar<D, M>(C::kBarS + buf));
+            used();
+            if (j + 4 == T) mma_commit(sm.bar<D, M>(C::kBarQFree));
+        } else {
+            if (j + 3 == T) mma_commit(sm.bar<D, M>(C::kBarPV));
+            if (j + 2 >= T) mma_commit(sm.bar<D, M>(C::kBarO + t));  // the last key tile of tile t
+            used();
+        }
+        if (++buf == 3) {
+            buf = 0;
+            parity ^= 1;
+        }
     }
     ph.slot = slot;
     return true;
@@ -1014,7 +1086,7 @@ __device__ __forceinline__ bool prefill_mma_step(const Smem& sm, const MmaDesc& 
     for (int t = 0; t < 2; ++t) {
         if (!mbar_wait(sm.bar<D, M>(C::kBarP + t), t ? pb : pa, abort_flag)) return false;
         tc_fence_after();
-        issue_pv<D, M>(d, t, vslot, kFirst);
+        issue_pv<D, M>(d, t, t, vslot, kFirst);
         if (kMore) issue_qk<D, M>(d, t, t, kslot);
         mma_commit(sm.bar<D, M>(kMore ? C::kBarS + t : C::kBarO + t));
     }
@@ -1045,7 +1117,7 @@ __device__ bool prefill_mma_item(const Smem& sm, const MmaDesc& d, int T, bool t
         mma_commit(sm.bar<D, M>(C::kBarQFree));
         if (!mbar_wait(sm.bar<D, M>(C::kBarP + 0), ph.p & 1, abort_flag)) return false;
         tc_fence_after();
-        issue_pv<D, M>(d, 0, vslot, true);
+        issue_pv<D, M>(d, 0, 0, vslot, true);
         mma_commit(sm.bar<D, M>(C::kBarO + 0));
         mma_commit(sm.bar<D, M>(C::kBarEmpty + vslot));
         ph.p ^= 1u;
@@ -1099,8 +1171,11 @@ __device__ void prefill_mma(const PrefillArgs& a, const Smem& sm, uint32_t tmem,
         tc_fence_after();
         ++ph.q;
         any = true;
-        ok = it.dual ? prefill_mma_dual<D, M>(sm, d, it.T, ph, abort_flag)
-                     : prefill_mma_item<D, M>(sm, d, it.T, it.two, ph, abort_flag);
+        if constexpr (C::kBufs > 2)  // (an item of one key tile as well)
+            ok = prefill_mma_three<D, M>(sm, d, it.T, ph, abort_flag);
+        else
+            ok = it.dual ? prefill_mma_dual<D, M>(sm, d, it.T, ph, abort_flag)
+                         : prefill_mma_item<D, M>(sm, d, it.T, it.two, ph, abort_flag);
         if (!ok) break;
         ph.ub += 2 * it.T;
     }
@@ -1230,7 +1305,7 @@ __device__ __forceinline__ bool prefill_write(const PrefillArgs& a, const Item& 
         float f[32];
         if (dual) {
             uint32_t ob[32];
-            tmem_ld32(tl + C::kColO + 128 + c * 32, ob);
+            tmem_ld32(tl + C::kColO + C::kOStep + c * 32, ob);
             tmem_wait_ld();
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -1337,9 +1412,9 @@ struct RowMask<kBlocks> : BlockRowMask {};
 template <>
 struct RowMask<kBlocks | kOneTile> : BlockRowMask {};
 template <>
-struct RowMask<kBlocks | kSmallPages> : BlockRowMask {};
+struct RowMask<kBlocks | kTwoProducers> : BlockRowMask {};
 template <>
-struct RowMask<kBlocks | kOneTile | kSmallPages> : BlockRowMask {};
+struct RowMask<kBlocks | kOneTile | kTwoProducers> : BlockRowMask {};
 
 // A key that a row does not see has the weight 0 in the row's tile product, and
 // 0 times an infinity or NaN in that key's V row is NaN.  So a block's row whose
@@ -1422,6 +1497,7 @@ struct SoftmaxPhase {
     uint32_t ub, par;
 };
 constexpr uint32_t kParS = 1, kParO = 2, kParX = 4;  // S_t, O_t, dual-key exchange
+constexpr uint32_t kParPV = 8;  // (three S buffers) items of three key tiles or more
 
 // Softmax warpgroup of query tile t (one row per thread) and its epilogue,
 // for one item.  False: a wait ran out.
@@ -1444,17 +1520,27 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
     const int T = dual ? (T_cta + 1 - t) / 2 : T_cta;
     const int kstep = dual ? 2 : 1, kfirst = dual ? t : 0;
     float* xchg = reinterpret_cast<float*>(sm.ptr + C::kOffXchg);
+    // (three S buffers) the buffer of this tile's j-th key tile and the parity of its
+    // hand-overs go by the key tile's number in the CTA's life, ub / 2 before
+    const uint32_t number0 = ph.ub / 2 + kfirst;
+    auto number = [=](int j) { return number0 + kstep * j; };
     // A warp none of whose rows is a query only keeps the barrier count: it
     // waits for each S and signals its P without computing (its rows of P
     // and O are never read back).
     if (!__any_sync(0xffffffffu, valid)) {
         for (int j = 0; j < T; ++j) {
-            if (!warp_wait(sm.bar<D, M>(C::kBarS + t), ph.par & kParS, abort_flag)) return false;
-            ph.par ^= kParS;
+            uint32_t buf = t, parity = ph.par & kParS;
+            if constexpr (C::kBufs > 2) {
+                buf = number(j) % 3;
+                parity = (number(j) / 3) & 1;
+            }
+            if (!warp_wait(sm.bar<D, M>(C::kBarS + buf), parity, abort_flag)) return false;
+            if (C::kBufs == 2) ph.par ^= kParS;
             tc_fence_before();
-            mbar_arrive(sm.bar<D, M>(C::kBarP + t));
+            mbar_arrive(sm.bar<D, M>(C::kBarP + buf));
         }
         if (T > 0) ph.par ^= kParO;
+        if (C::kBufs > 2 && T_cta > 2) ph.par ^= kParPV;
         if (dual) {
             mbar_arrive(sm.bar<D, M>(t == 1 ? C::kBarX : C::kBarXFree));
             // (tile b's next P waits for tile a's reads also here)
@@ -1471,8 +1557,9 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
     if constexpr (of_blocks<M>) mask.init(a, item_block<D, M>(sm, k), valid ? qi : n_q - 1);
     else mask.init(a, valid ? qi : n_q - 1);
     const uint32_t tl = tmem + ((uint32_t)(wq * 32) << 16);
-    const uint32_t col_s = C::kColS + (uint32_t)t * kPrefillKeys;
-    const uint32_t col_o = C::kColO + (uint32_t)t * 128;
+    uint32_t buf = t;
+    uint32_t col_s = C::kColS + (uint32_t)t * kPrefillKeys;
+    const uint32_t col_o = C::kColO + (uint32_t)t * C::kOStep;
     const float sc = a.scale_log2;  // > 0 (the host raises a zero scale to a tiny one)
     // most that a row's weights of one tile may sum to without a look at their
     // maximum (a power of two above the running one).  A warp with rows that are
@@ -1508,8 +1595,14 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
             nk = __ldg(reinterpret_cast<const int2*>(tp + kstep));
             nb = __ldg(&tp[kstep].key0b);
         }
-        if (!warp_wait(sm.bar<D, M>(C::kBarS + t), ph.par & kParS, abort_flag)) return false;
-        ph.par ^= kParS;
+        uint32_t parity = ph.par & kParS;
+        if constexpr (C::kBufs > 2) {
+            buf = number(j) % 3;
+            col_s = C::col_s(buf);
+            parity = (number(j) / 3) & 1;
+        }
+        if (!warp_wait(sm.bar<D, M>(C::kBarS + buf), parity, abort_flag)) return false;
+        if (C::kBufs == 2) ph.par ^= kParS;
         tc_fence_after();
         // Raw logits q.k (the scale is applied inside the exponent; it is > 0),
         // taken 64 columns at a time to keep registers low: one pass for the
@@ -1623,7 +1716,16 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
             }
             if (j > 0 && __any_sync(0xffffffffu, need)) {
                 // O_t holds the products up to key tile j - 1 (complete: S_t(j)
-                // was issued after them): rescale it in place
+                // was issued after them; with three buffers before the last, which
+                // is waited for: the next needs this row's P): rescale it in place
+                if constexpr (C::kBufs > 2) {
+                    const int u = number(j) + 1;  // its QK was issued after that PV
+                    const bool more = kfirst + kstep * j + 1 < T_cta;
+                    if (!warp_wait(sm.bar<D, M>(more ? C::kBarS + u % 3 : C::kBarPV),
+                                   more ? u / 3 & 1 : (ph.par & kParPV) != 0, abort_flag))
+                        return false;
+                    tc_fence_after();
+                }
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t o[32];
@@ -1643,7 +1745,17 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
         // landed (long ago, as a rule): V_j, and the K tile of the next S.
         bool landed = true;
         uint32_t fv = 0, fk = 0, pv = 0, pk = 0;
-        if (wq == 0 && t == 0 && !dual) {
+        if (C::kBufs > 2 && wq == 0) {
+            // (V_jj and K_{jj+3}, in the order of load_of)
+            const int jj = kfirst + kstep * j;
+            const bool more = jj + 3 < T_cta;
+            const uint32_t uv = ph.ub + (more ? 2 * jj + 3 : T_cta + jj), uk = more ? uv + 1 : uv;
+            fv = sm.bar<D, M>(C::kBarFull + uv % C::kSlots);
+            pv = (uv / C::kSlots) & 1;
+            fk = sm.bar<D, M>(C::kBarFull + uk % C::kSlots);
+            pk = (uk / C::kSlots) & 1;
+            landed = mbar_try_wait(fv, pv) & mbar_try_wait(fk, pk);
+        } else if (wq == 0 && t == 0 && !dual) {
             const uint32_t uv = ph.ub + 2 * j + 1, uk = uv + 1;
             fv = sm.bar<D, M>(C::kBarFull + uv % C::kSlots);
             pv = (uv / C::kSlots) & 1;
@@ -1658,13 +1770,14 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
             if (!warp_wait(fv, pv, abort_flag) || !warp_wait(fk, pk, abort_flag)) return false;
         }
         tc_fence_before();
-        mbar_arrive(sm.bar<D, M>(C::kBarP + t));
+        mbar_arrive(sm.bar<D, M>(C::kBarP + buf));
         tp += kstep;
     }
     if (T > 0) {
         if (!warp_wait(sm.bar<D, M>(C::kBarO + t), (ph.par & kParO) != 0, abort_flag)) return false;
         ph.par ^= kParO;
     }
+    if (C::kBufs > 2 && T_cta > 2) ph.par ^= kParPV;
     if (of_blocks<M> && l == 0.f) m_run = -INFINITY;  // no key seen
     // dual-key mode: tile b hands its (max, normaliser) to tile a, which
     // merges the two partial results of each row (weights 2^(m_t - max)) and
@@ -1722,9 +1835,9 @@ struct ModeOf<BlockArgs> : std::integral_constant<int, kBlocks> {};
 template <>
 struct ModeOf<BlockShortArgs> : std::integral_constant<int, kBlocks | kOneTile> {};
 template <>
-struct ModeOf<SmallBlockArgs> : std::integral_constant<int, kBlocks | kSmallPages> {};
+struct ModeOf<BlockArgs2> : std::integral_constant<int, kBlocks | kTwoProducers> {};
 template <>
-struct ModeOf<SmallBlockShortArgs> : std::integral_constant<int, kBlocks | kOneTile | kSmallPages> {};
+struct ModeOf<BlockShortArgs2> : std::integral_constant<int, kBlocks | kOneTile | kTwoProducers> {};
 
 template <int D, typename Args>
 __global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
@@ -1748,11 +1861,14 @@ __global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
             mbar_init(sm.bar<D, M>(C::kBarFull + s), 1);
             mbar_init(sm.bar<D, M>(C::kBarEmpty + s), 1);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < C::kBufs; ++b) {
             mbar_init(sm.bar<D, M>(C::kBarS + b), 1);
             mbar_init(sm.bar<D, M>(C::kBarP + b), 128);
+        }
+        for (int b = 0; b < 2; ++b) {
             mbar_init(sm.bar<D, M>(C::kBarO + b), 1);
         }
+        if (C::kBufs > 2) mbar_init(sm.bar<D, M>(C::kBarPV), 1);
         mbar_init(sm.bar<D, M>(C::kBarVfix), 1);
         mbar_init(sm.bar<D, M>(C::kBarQFree), 1);
         mbar_init(sm.bar<D, M>(C::kBarDone), 1);
@@ -1770,7 +1886,7 @@ __global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
         tmem_alloc(smem_addr(tmem_slot), C::kTmemCols);
         tmem_relinquish();
     }
-    FirstItem<M> start;
+    FirstItem<D, M> start;
     int u_early = 0;
     const bool second = producers<M> > 1 && warp == kProducer2;  // the second producer warp
     if (warp == 0 || second) {
