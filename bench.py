@@ -94,7 +94,8 @@ KERNEL_SOURCES = {
                                 "host/plan.hpp"],
     "sq_evict_compact_kernel": ["kernels/kv.cu", "kernels/ptx.cuh", "kernels/launch.hpp",
                                 "host/plan.hpp"],
-    "sq_prefill_kernel": ["kernels/prefill.cu", "kernels/ptx.cuh", "kernels/tc.cuh",
+    "sq_prefill_kernel": ["kernels/prefill.cu", "kernels/prefill_kernel.cuh", "kernels/operators.hpp",
+                          "kernels/ptx.cuh", "kernels/tc.cuh",
                           "kernels/launch.hpp", "host/plan.hpp"],
 }
 

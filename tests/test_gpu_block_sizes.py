@@ -81,3 +81,47 @@ def test_offsets_past_32_bits():
         assert torch.equal(got[:, 1], v[at:at + x])
         at += x
     b.c.close()
+
+
+@pytest.mark.parametrize("P", [16, 64, 256])
+def test_stores_between_layers_are_seen_at_64_dimensions(P):
+    """Calls that reuse their plans, and load keys ahead of the launch before them,
+    read the rows stored just before: back to back as with waits in between, bit
+    for bit; contexts cut into pieces, several streams."""
+    L, D, lengths, m = 4, 64, [5000, 700, 130], 6
+    c = sq.Cache(L, 16, 4, D, P, sum(lengths) // P + 20)
+    g = torch.Generator("cuda").manual_seed(P)
+    hs = [c.seq_new() for _ in lengths]
+    for h, n in zip(hs, lengths):
+        c.append_kv(h, n, *(torch.randn(L, n, 4, D, generator=g, device="cuda").bfloat16() for _ in range(2)))
+    torch.cuda.synchronize()
+    counts, par = [m] * 3, sq.norm_rope()
+    c.extend(hs, counts)
+    qkv = torch.randn(L, 3 * m, 24, D, generator=g, device="cuda").bfloat16()
+    parents = [-1, 0, 0, 1, 1, 4] * 3
+    side = torch.cuda.Stream()
+    outs = []
+    for slow in (True, False):
+        out = torch.empty(L, 2, 3 * m, 16, D, device="cuda")
+        torch.cuda.synchronize()
+        for rep in range(5):
+            for layer in range(L):
+                x = qkv[(layer + rep) % L]
+                q = torch.empty(3 * m, 16, D, dtype=torch.bfloat16, device="cuda")
+                stream = side if rep == 3 else torch.cuda.current_stream()
+                stream.wait_stream(torch.cuda.current_stream())
+                with torch.cuda.stream(stream):
+                    c.qk_norm_rope_store(hs, counts, layer, x[:, :16], x[:, 16:20], x[:, 20:], None, par, q)
+                    if slow:
+                        torch.cuda.synchronize()
+                    kw = dict(out_dtype=sq.SQ_OUT_F32, sm_scale=D ** -0.5)
+                    c.tree_attention(hs, counts, parents, layer, q, out[layer, 0], **kw)
+                    c.window_attention(hs, counts, layer, q, out[layer, 1], 3000, 2, **kw)
+                    if slow:
+                        torch.cuda.synchronize()
+                torch.cuda.current_stream().wait_stream(stream)
+        assert c.sync_status() == sq.SQ_OK
+        outs.append(out)
+    assert torch.isfinite(outs[0]).all()
+    assert torch.equal(*outs)
+    c.close()
