@@ -1417,12 +1417,45 @@ template <>
 struct RowMask<kBlocks | kOneTile | kTwoProducers> : BlockRowMask {};
 
 // A key that a row does not see has the weight 0 in the row's tile product, and
-// 0 times an infinity or NaN in that key's V row is NaN.  So a block's row whose
-// output is not finite is taken once more, over the keys that it does see and with
-// the maximum and normaliser that it has: a warp on the rows in `rows` one by one,
-// a lane to a key for the weights and to D / 32 columns for the sum.  (It costs the
-// item D fused multiply-adds a row to look, and nothing more as long as stored rows
-// are finite.)
+// 0 times an infinity or NaN in that key's V row is NaN.  So where a block's row has
+// an output that is not finite though its normaliser is, and some key that its tiles
+// hide has such a V row, it is taken once more, over the keys that it does see and
+// with the maximum and normaliser that it has: a warp on the rows in `rows` one by
+// one, a lane to a key for the weights and to D / 32 columns for the sum.  (An item
+// pays D fused multiply-adds a row to look, and nothing more as long as stored rows
+// are finite.  A row taken again costs ~40 us for 1,000 keys: the longest items would
+// run out the other roles' waits, which the hidden rows' search alone does not.)
+template <int D, int M, typename Args>
+__device__ bool hides_odd_values(const Args& a, const BlockItem& it, const BlockRowMask& mask,
+                                 const __nv_bfloat16* values, int lane) {
+    const int per = pieces_of<M>(a), br = 128 / per;
+    for (int j = it.t0; j < it.t0 + it.n_tiles; ++j) {
+        const PrefillTile* t = a.tiles + j;
+        const int2 r = __ldg(reinterpret_cast<const int2*>(t));
+        const int key_b = __ldg(&t->key0b);
+        if ((r.y & kPrefillTileFull) && mask.whole(r.x) && mask.whole(key_b)) continue;
+        for (int w = 0; w < 4; ++w) {
+            const int key = (w < 2 ? r.x : key_b) + 32 * (w & 1) + lane;
+            const uint32_t see = __ldg(&t->vis[w]) & mask.word(key - lane);
+            // (rows past the end were zeroed, a box that does not exist as well)
+            const int page = __ldg(&a.tile_pages[(size_t)j * per + (w * 32 + lane) / br]);
+            bool odd = false;
+            if (!((see >> lane) & 1u) && page >= 0 && page < a.num_pages && key < it.n) {
+                const uint4* v = reinterpret_cast<const uint4*>(
+                    values + (int64_t)page * 2 * a.Hkv * a.P * D + (size_t)(key & (a.P - 1)) * D);
+                for (int c = 0; c < D / 8; ++c) {
+                    const uint4 x = v[c];
+                    const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        odd |= (xw[i] & 0x7f80u) == 0x7f80u || (xw[i] & 0x7f800000u) == 0x7f800000u;
+                }
+            }
+            if (__any_sync(0xffffffffu, odd)) return true;
+        }
+    }
+    return false;
+}
 template <int D, int M, typename Args>
 __device__ __noinline__ void rows_again(const Args& a, const BlockItem& it, int tile, uint32_t rows, int row0,
                                         float m_run, float l, int lane) {
@@ -1437,6 +1470,7 @@ __device__ __noinline__ void rows_again(const Args& a, const BlockItem& it, int 
         const int qi = tile * a.BP + row / a.G, h = g * a.G + row % a.G;
         BlockRowMask mask;
         mask.init(a, it, qi);
+        if (!hides_odd_values<D, M>(a, it, mask, keys + a.Hkv * run, lane)) continue;
         const size_t q_head = (size_t)(it.q_row + qi) * a.Hq + h;
         const uint4* q = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + q_head * D);
         float acc[kCols];
@@ -1817,7 +1851,7 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
         mbar_arrive(sm.bar<D, M>(C::kBarXFree));
     }
     if constexpr (of_blocks<M>) {
-        const uint32_t rows = __ballot_sync(0xffffffffu, again);
+        const uint32_t rows = __ballot_sync(0xffffffffu, again && l < INFINITY);
         __syncwarp();  // the pairs' stores come before those of rows_again
         if (rows) rows_again<D, M>(a, item_block<D, M>(sm, k), t, rows, wq * 32, m_run, l, lane);
     }

@@ -140,3 +140,36 @@ def test_rows_evicted_from_partial_pages(P, D):
     for o in (got, out):
         assert_rows(o[0], q[0], k, v, 8, 2, D)
     b.c.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,P", [(8, 2, 128, 64), (16, 2, 64, 16)])
+@pytest.mark.parametrize("m", [20, 200])
+def test_what_a_query_sees_is_not_hidden(Hq, Hkv, D, P, m):
+    """Values that are not finite reach the queries that see them, and those alone,
+    also where hidden ones lie beside them."""
+    n, window, sinks = 3000, 100, 3
+    b = Batch(Hq, Hkv, D, P, [n], seed=m)
+    q = b.queries(m)
+    q[m - 1, 1] = math.nan
+    seen = n - m // 2                       # a row that the queries from it on see
+    page, slot = (t[seen] for t in row_slots(b.c, b.h[0]))
+    b.pool[0, page, 1, :, slot, 5] = math.inf     # one column of V
+    poison(b, b.h[0], [n - m - 90])         # hidden from all but the first queries
+    out, _ = b.call([m], q, None, window, sinks)
+    assert b.c.sync_status() == sq.SQ_OK
+    k, v = b.rows(b.h[0])
+    for i in range(m):
+        p = n - m + i
+        see = [j for j in range(p + 1) if j > p - window or j < sinks]
+        if n - m - 90 in see:
+            assert not torch.isfinite(out[i]).any()
+            continue
+        ok = torch.isfinite(out[i])
+        want = torch.ones_like(ok)
+        want[:, 5] = seen not in see
+        if i == m - 1:
+            want[1] = False
+        assert torch.equal(ok, want)
+        if i != m - 1 and seen not in see:
+            assert_rows(out[i], q[i], k[see], v[see], Hq, Hkv, D)
+    b.c.close()
