@@ -1262,7 +1262,8 @@ __device__ __forceinline__ bool prefill_write(const PrefillArgs& a, const Item& 
     const bool dual = it.dual, any_keys = it.T > 0;
     const int qi = q_row + (dual ? 0 : t) * a.BP + row / a.G;
     const float inv = l > 0.f ? 1.f / l : 0.f;
-    const float lse2 = l > 0.f ? m_run + __log2f(l) : -INFINITY;
+    // (a block's row whose weights are NaN says so, to its merge too)
+    const float lse2 = l > 0.f ? m_run + __log2f(l) : (of_blocks<M> && l != 0.f ? NAN : -INFINITY);
     const int h = it.g * a.G + row % a.G;
     float* part_row = nullptr;
     uint8_t* out_row = nullptr;
@@ -1423,8 +1424,8 @@ struct RowMask<kBlocks | kOneTile | kTwoProducers> : BlockRowMask {};
 // with the maximum and normaliser that it has: a warp on the rows in `rows` one by
 // one, a lane to a key for the weights and to D / 32 columns for the sum.  (An item
 // pays D fused multiply-adds a row to look, and nothing more as long as stored rows
-// are finite.  A row taken again costs ~40 us for 1,000 keys: the longest items would
-// run out the other roles' waits, which the hidden rows' search alone does not.)
+// are finite.  A row taken again costs ~40 us for 1,000 keys, so a warp's 32 rows over
+// a million keys still end within the other roles' bounded waits of 2 s.)
 template <int D, int M, typename Args>
 __device__ bool hides_odd_values(const Args& a, const BlockItem& it, const BlockRowMask& mask,
                                  const __nv_bfloat16* values, int lane) {
@@ -2078,6 +2079,9 @@ __global__ void __launch_bounds__(kCombineThreads, U > kCombineFew ? 6 : 8)
     float W = w0 + w1;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) W += __shfl_xor_sync(0xffffffffu, W, off);
+    float none = 0.f;  // of a row without weights; (blocks) NaN where a piece's are NaN
+    if constexpr (kOfBlocks)
+        if (__any_sync(0xffffffffu, ml0 != ml0 || ml1 != ml1)) W = none = NAN;
     float acc[V] = {};
     for (int s0 = 0; W > 0.f && s0 < n_split; s0 += U) {
         if (s0 > 0) load(s0);
@@ -2091,7 +2095,7 @@ __global__ void __launch_bounds__(kCombineThreads, U > kCombineFew ? 6 : 8)
             }
         }
     }
-    const float inv = W > 0.f ? 1.f / W : 0.f;
+    const float inv = W > 0.f ? 1.f / W : none;
     const size_t o = ((size_t)qi * a.Hq + h) * D + col;
     if (a.out_f32) {
         float* out = reinterpret_cast<float*>(a.out) + o;
@@ -2112,7 +2116,7 @@ __global__ void __launch_bounds__(kCombineThreads, U > kCombineFew ? 6 : 8)
         }
     }
     if (lane == 0 && col == 0 && a.lse)
-        a.lse[(size_t)qi * a.Hq + h] = W > 0.f ? (M + __log2f(W)) * 0.69314718055994531f : -INFINITY;
+        a.lse[(size_t)qi * a.Hq + h] = W > 0.f ? (M + __log2f(W)) * 0.69314718055994531f : none - INFINITY;
 }
 
 }  // namespace

@@ -173,3 +173,28 @@ def test_what_a_query_sees_is_not_hidden(Hq, Hkv, D, P, m):
         if i != m - 1 and seen not in see:
             assert_rows(out[i], q[i], k[see], v[see], Hq, Hkv, D)
     b.c.close()
+
+
+@pytest.mark.parametrize("n", [50, 700, 9000])
+@pytest.mark.parametrize("what", ["q", "k", "v"])
+@pytest.mark.parametrize("m", [1, 4, 100])
+def test_nan_is_not_lost(n, what, m):
+    """NaN in a query, or in a key or value that it sees, is NaN in its output, also
+    where the keys are cut into pieces; a NaN weight in its log-sum-exp too."""
+    b = Batch(8, 2, 128, 64, [n + m], seed=n)
+    q = b.queries(m)
+    if what == "q":
+        q[:, 1] = math.nan
+    else:
+        page, slot = (t[n // 2] for t in row_slots(b.c, b.h[0]))
+        b.pool[0, page, 0 if what == "k" else 1, :, slot] = math.nan
+    out, lse = b.call([m], q)
+    assert b.c.sync_status() == sq.SQ_OK
+    nan = torch.zeros(m, 8, dtype=torch.bool, device="cuda")
+    nan[:, 1 if what == "q" else slice(None)] = True
+    assert torch.equal(torch.isnan(out), nan[:, :, None].expand_as(out))
+    assert torch.equal(torch.isnan(lse), nan & (what != "v"))
+    got = torch.zeros_like(out)
+    b.c.tree_attention(b.h, [m], list(range(-1, m - 1)), 0, q, got, out_dtype=sq.SQ_OUT_F32, sm_scale=0.1)
+    assert torch.equal(torch.isnan(got), nan[:, :, None].expand_as(out))
+    b.c.close()
