@@ -255,12 +255,13 @@ def _rows(x, heads, dim, name, n=None):
     contiguous one of n tokens."""
     if x.__class__ is int:
         return x, heads * dim, n
-    shape, stride = x.shape, x.stride()
-    if (len(shape) != 3 or shape[1] != heads or shape[2] != dim or stride[2] != 1 or stride[1] != dim
-            or x.dtype is not _BF16 or (n is not None and shape[0] != n)):
-        _wrong(name, f"bfloat16 [{'tokens' if n is None else n}, {heads}, {dim}] of contiguous rows", x)
-    # (one token has no distance to the next)
-    return x.data_ptr(), stride[0] if shape[0] > 1 else heads * dim, shape[0]
+    if x.dim() == 3:
+        (tokens, h, d), (apart, s1, s2) = x.shape, x.stride()
+        if (h == heads and d == dim and s2 == 1 and s1 == dim and x.dtype is _BF16
+                and (n is None or tokens == n)):
+            # (one token has no distance to the next)
+            return x.data_ptr(), apart if tokens > 1 else heads * dim, tokens
+    _wrong(name, f"bfloat16 [{'tokens' if n is None else n}, {heads}, {dim}] of contiguous rows", x)
 
 
 def _flat(x, want, count, name):
@@ -268,9 +269,9 @@ def _flat(x, want, count, name):
     addresses as they are)."""
     if x is None or x.__class__ is int:
         return x
-    if x.dtype is not want or x.numel() != count or not x.is_contiguous():
-        _wrong(name, f"{count} contiguous elements of {want}", x)
-    return x.data_ptr()
+    if x.dtype is want and x.numel() == count and x.is_contiguous():
+        return x.data_ptr()
+    _wrong(name, f"{count} contiguous elements of {want}", x)
 
 
 def norm_rope(rope=None, rot_dim=0, eps=1e-6, q_weight=None, k_weight=None,
@@ -633,12 +634,22 @@ class Cache:
                                  _flat(dq_weight, _FLOAT, d, "dq_weight"),
                                  _flat(dk_weight, _FLOAT, d, "dk_weight"), stream)
 
+    def _attention(self, seqs, counts, q, out, out_dtype, lse, what):
+        """Addresses of the tensors of a call on query blocks, and its queries."""
+        if _BF16 is None:
+            _types()
+        n = self._counted(seqs, counts, None, what)
+        rows = n * self.Hq
+        size = rows * self.D
+        return (_flat(q, _BF16, size, "q"),
+                _flat(out, _FLOAT if out_dtype == SQ_OUT_F32 else _BF16, size, "out"),
+                lse if lse is None else _flat(lse, _FLOAT, rows, "lse"), n)
+
     def window_attention(self, seqs, n_q, layer, q, out, window, n_sink=0, out_dtype=SQ_OUT_BF16,
                          lse=None, sm_scale=1.0, stream=None):
         """Attention of the newest n_q[i] tokens (None: one) of each sequence, each
         seeing its last `window` tokens and the first n_sink."""
-        n = None if q.__class__ is int else q.shape[0]
-        self._counted(seqs, n_q, n, "window_attention")
+        q, out, lse, _ = self._attention(seqs, n_q, q, out, out_dtype, lse, "window_attention")
         sq_window_attention(self.handle, seqs, n_q, layer, q, out, window, n_sink, out_dtype, lse,
                             sm_scale, stream)
 
@@ -646,7 +657,7 @@ class Cache:
                        out_dtype=SQ_OUT_BF16, lse=None, sm_scale=1.0, stream=None):
         """Attention of trees of drafted tokens, each sequence's newest n_draft[i]
         rows; parents: every drafted token's parent in its tree, -1 the context."""
-        n = self._counted(seqs, n_draft, None if q.__class__ is int else q.shape[0], "tree_attention")
+        q, out, lse, n = self._attention(seqs, n_draft, q, out, out_dtype, lse, "tree_attention")
         if len(parents) != n:
             raise ValueError(f"tree_attention: {len(parents)} parents of {n} drafted tokens")
         sq_tree_attention(self.handle, seqs, n_draft, parents, layer, q, out, window, n_sink, out_dtype,
