@@ -318,7 +318,8 @@ __global__ void __launch_bounds__(kNormThreads, 7)
 // add up the weights' gradients of their lanes' elements; the CTA's sums go to one
 // partial row, added by a second kernel in a fixed order.  8,192 tokens of 64 query
 // and 8 key heads of 128: 84 us, 5.4 TB/s; two rows of a lane group in flight 103,
-// eight 105, a position read a task ahead 86.
+// eight 105, a position read a task ahead 86, the next task's rows copied into shared
+// memory ahead 85.
 template <int D, bool kPairs>
 __global__ void __launch_bounds__(kGradThreads)
     sq_norm_rope_grad_kernel(const __grid_constant__ NormRopeGradArgs a) {

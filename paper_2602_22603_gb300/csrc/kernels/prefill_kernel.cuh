@@ -1421,11 +1421,12 @@ struct RowMask<kBlocks | kOneTile | kTwoProducers> : BlockRowMask {};
 // 0 times an infinity or NaN in that key's V row is NaN.  So where a block's row has
 // an output that is not finite though its normaliser is, and some key that its tiles
 // hide has such a V row, it is taken once more, over the keys that it does see and
-// with the maximum and normaliser that it has: a warp on the rows in `rows` one by
-// one, a lane to a key for the weights and to D / 32 columns for the sum.  (An item
+// with the maximum and normaliser that it has: a warp on four rows of a query at a
+// time, a lane to a key for the weights and to D / 32 columns for the sums.  (An item
 // pays D fused multiply-adds a row to look, and nothing more as long as stored rows
-// are finite.  A row taken again costs ~40 us for 1,000 keys, so a warp's 32 rows over
-// a million keys still end within the other roles' bounded waits of 2 s.)
+// are finite.  A row taken again costs 40 us for 1,000 keys, 130 where a KV head has
+// one query head: a warp's 32 rows over 400,000 keys still end within the other
+// roles' bounded waits of 2 s.)
 template <int D, int M, typename Args>
 __device__ bool hides_odd_values(const Args& a, const BlockItem& it, const BlockRowMask& mask,
                                  const __nv_bfloat16* values, int lane) {
@@ -1460,66 +1461,107 @@ __device__ bool hides_odd_values(const Args& a, const BlockItem& it, const Block
 template <int D, int M, typename Args>
 __device__ __noinline__ void rows_again(const Args& a, const BlockItem& it, int tile, uint32_t rows, int row0,
                                         float m_run, float l, int lane) {
-    constexpr int kCols = D / 32;
+    constexpr int kCols = D / 32, kRows = 4, kAhead = 8;
     const int g = it.head & (kBlockTwoTiles - 1), per = pieces_of<M>(a), br = 128 / per;
     const size_t run = (size_t)a.P * D;  // a head's rows in a page
     const __nv_bfloat16* keys =
         static_cast<const __nv_bfloat16*>(a.pool) + ((size_t)a.layer * a.num_pages * 2 * a.Hkv + g) * run;
-    for (; rows; rows &= rows - 1) {
-        const int src = __ffs(rows) - 1, row = row0 + src;
-        const float m = __shfl_sync(0xffffffffu, m_run, src), sum = __shfl_sync(0xffffffffu, l, src);
-        const int qi = tile * a.BP + row / a.G, h = g * a.G + row % a.G;
+    const __nv_bfloat16* values = keys + a.Hkv * run;
+    while (rows) {
+        // up to kRows rows of one query: they see the same keys
+        const int qi = tile * a.BP + (row0 + __ffs(rows) - 1) / a.G;
+        int n_rows = 0, row[kRows];
+        float m[kRows], sum[kRows], acc[kRows][kCols];
+        const uint4* q[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int next = row0 + __ffs(rows) - 1;
+            const bool more = rows && tile * a.BP + next / a.G == qi;
+            row[r] = more ? next : row[0];
+            if (more) {
+                rows &= rows - 1;
+                ++n_rows;
+            }
+            m[r] = __shfl_sync(0xffffffffu, m_run, row[r] - row0);
+            if (m[r] == -INFINITY) m[r] = 0.f;
+            sum[r] = __shfl_sync(0xffffffffu, l, row[r] - row0);
+            q[r] = reinterpret_cast<const uint4*>(
+                static_cast<const __nv_bfloat16*>(a.q) +
+                ((size_t)(it.q_row + qi) * a.Hq + g * a.G + row[r] % a.G) * D);
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) acc[r][i] = 0.f;
+        }
         BlockRowMask mask;
         mask.init(a, it, qi);
-        if (!hides_odd_values<D, M>(a, it, mask, keys + a.Hkv * run, lane)) continue;
-        const size_t q_head = (size_t)(it.q_row + qi) * a.Hq + h;
-        const uint4* q = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + q_head * D);
-        float acc[kCols];
-#pragma unroll
-        for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
+        if (!hides_odd_values<D, M>(a, it, mask, values, lane)) continue;
         for (int x = 0; x < 4 * it.n_tiles; ++x) {
             const int j = it.t0 + (x >> 2), w = x & 3;
             const PrefillTile* t = a.tiles + j;
             const int key = __ldg(w < 2 ? &t->key0 : &t->key0b) + 32 * (w & 1) + lane;
             const uint32_t see = __ldg(&t->vis[w]) & mask.word(key - lane);
-            int64_t at = 0;  // of the key's K row
-            float p = 0.f;
+            if (!see) continue;
+            int64_t at = 0;  // of the key's row
+            float p[kRows] = {};
             if ((see >> lane) & 1u) {
                 // (a page outside the pool was flagged, and page 0 read)
                 const int page = __ldg(&a.tile_pages[(size_t)j * per + (w * 32 + lane) / br]);
                 at = (int64_t)((uint32_t)page < (uint32_t)a.num_pages ? page : 0) * 2 * a.Hkv * run +
                      (size_t)(key & (a.P - 1)) * D;
-                float s = 0.f;
+#pragma unroll 4
                 for (int c = 0; c < D / 8; ++c) {
-                    const uint4 kk = reinterpret_cast<const uint4*>(keys + at)[c], qq = q[c];
-                    const uint32_t kw[4] = {kk.x, kk.y, kk.z, kk.w}, qw[4] = {qq.x, qq.y, qq.z, qq.w};
+                    const uint4 kk = reinterpret_cast<const uint4*>(keys + at)[c];
+                    const uint32_t kw[4] = {kk.x, kk.y, kk.z, kk.w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        s = fmaf(__uint_as_float(kw[i] << 16), __uint_as_float(qw[i] << 16), s);
-                        s = fmaf(__uint_as_float(kw[i] & 0xffff0000u), __uint_as_float(qw[i] & 0xffff0000u), s);
+                    for (int r = 0; r < kRows; ++r) {
+                        const uint4 qq = q[r][c];
+                        const uint32_t qw[4] = {qq.x, qq.y, qq.z, qq.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            p[r] = fmaf(__uint_as_float(kw[i] << 16), __uint_as_float(qw[i] << 16), p[r]);
+                            p[r] = fmaf(__uint_as_float(kw[i] & 0xffff0000u),
+                                        __uint_as_float(qw[i] & 0xffff0000u), p[r]);
+                        }
                     }
                 }
-                p = __bfloat162float(__float2bfloat16(ex2_ftz(fmaf(s, a.scale_log2, m == -INFINITY ? 0.f : -m))));
-            }
-            for (uint32_t left = see; left; left &= left - 1) {
-                const int c = __ffs(left) - 1;
-                const float pc = __shfl_sync(0xffffffffu, p, c);
-                const __nv_bfloat16* v = keys + __shfl_sync(0xffffffffu, at, c) + a.Hkv * run;
 #pragma unroll
-                for (int i = 0; i < kCols; ++i) acc[i] = fmaf(pc, __bfloat162float(v[lane + 32 * i]), acc[i]);
+                for (int r = 0; r < kRows; ++r)
+                    p[r] = __bfloat162float(__float2bfloat16(ex2_ftz(fmaf(p[r], a.scale_log2, -m[r]))));
+            }
+            for (int c0 = 0; c0 < 32; c0 += kAhead) {
+                float v[kAhead][kCols];
+#pragma unroll
+                for (int c = 0; c < kAhead; ++c) {
+                    const __nv_bfloat16* from = values + __shfl_sync(0xffffffffu, at, c0 + c);
+                    const bool seen = (see >> (c0 + c)) & 1u;
+#pragma unroll
+                    for (int i = 0; i < kCols; ++i) v[c][i] = seen ? __bfloat162float(from[lane + 32 * i]) : 0.f;
+                }
+#pragma unroll
+                for (int c = 0; c < kAhead; ++c)
+#pragma unroll
+                    for (int r = 0; r < kRows; ++r) {
+                        const float pc = __shfl_sync(0xffffffffu, p[r], c0 + c);
+#pragma unroll
+                        for (int i = 0; i < kCols; ++i) acc[r][i] = fmaf(pc, v[c][i], acc[r][i]);
+                    }
             }
         }
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
-        for (int i = 0; i < kCols; ++i) {
-            const float f = acc[i] * inv;
-            const int col = lane + 32 * i;
-            if (it.part >= 0)
-                a.part_o[(((size_t)it.part * kPrefillQTiles + tile) * kPrefillRows + row) * D + col] = f;
-            else if (a.out_f32)
-                static_cast<float*>(a.out)[q_head * D + col] = f;
-            else
-                static_cast<__nv_bfloat16*>(a.out)[q_head * D + col] = __float2bfloat16(f);
+        for (int r = 0; r < kRows; ++r) {
+            if (r >= n_rows) break;
+            const float inv = sum[r] > 0.f ? 1.f / sum[r] : 0.f;
+            const size_t q_head = (size_t)(it.q_row + qi) * a.Hq + g * a.G + row[r] % a.G;
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) {
+                const float f = acc[r][i] * inv;
+                const int col = lane + 32 * i;
+                if (it.part >= 0)
+                    a.part_o[(((size_t)it.part * kPrefillQTiles + tile) * kPrefillRows + row[r]) * D + col] = f;
+                else if (a.out_f32)
+                    static_cast<float*>(a.out)[q_head * D + col] = f;
+                else
+                    static_cast<__nv_bfloat16*>(a.out)[q_head * D + col] = __float2bfloat16(f);
+            }
         }
     }
 }
