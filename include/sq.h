@@ -451,8 +451,8 @@ SQ_API int sq_qk_norm_rope_backward(sq_cache *cache, int32_t n_tokens, const voi
  * Only the 64-row runs of pages that some query sees a row of are read.  Rows that
  * a query does not see, and slots past a sequence's end, may hold anything: an
  * infinity or NaN there does not reach its output (it costs time: such a query is
- * taken once more, 40 to 130 us a head for 1,000 keys).  NaN in a query, or in a key or value
- * that it sees, is NaN in its output.
+ * taken once more, 40 to 130 us a head for 1,000 keys).  NaN in a query, or in a
+ * key or value that it sees, is NaN in its output.
  * Single tokens without lse run as sq_decode_attention does.
  * Weights and normaliser are rounded as in sq_prefill_attention, whose limits on
  * library memory for partial results hold too.  A plan of more than 2^24 key
