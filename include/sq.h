@@ -229,7 +229,9 @@ SQ_API int sq_evict_spans_ragged(sq_cache *cache, sq_seq seq, const sq_span *spa
  * the n_q queries must lie in consecutive page slots, that is no partial page
  * may hold one of them but the last (true for rows appended after the last
  * ragged eviction); otherwise UNSUPPORTED.  The sequence and the cache are
- * not modified.  The
+ * not modified.  Rows that a span hides and unused slots of partial pages may
+ * never have been stored (sq_extend): they reach no output.  Rows that were
+ * appended or stored are taken to be finite, hidden or not.  The
  * kernel runs on the tensor cores (bf16 products, fp32 accumulation; the
  * softmax weights are rounded to bf16 before the value product, and the
  * normaliser sums the same rounded weights).  Where key ranges are shared out

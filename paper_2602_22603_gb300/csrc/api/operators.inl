@@ -242,6 +242,7 @@ int extend_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
     note_writes(c, copied.data(), copied.size(), stream);
     for (int32_t i = 0; i < n_seqs; ++i) {
         if (plans[i].n_new == 0) continue;
+        c->host->seq_mut(seqs[i])->extended = true;
         const uint64_t nv = c->host->seq(seqs[i])->version;
         if (passed[i])
             for (const LenUpdate& u : ups[i]) plan_len_apply(c, u, nv, plans[i].n_new, plans[i].pages[0], st);

@@ -86,6 +86,7 @@ struct PrefillPlanEntry {
     size_t o_items = 0, o_merges = 0, o_pages = 0;  // byte offsets of the parts of d
     int32_t n_tiles = 0, n_pieces = 0, BP = 0, n_items = 0, n_merges = 0, n_parts = 0;
     int32_t max_splits = 0;
+    bool hides = false;    // it hides rows that may never have been written
     int64_t visible_pairs = 0;
     WriteTickets writes;   // of the sequence's pages, as a decode plan has them
     uint8_t* d = nullptr;  // [tiles][items][merges][tile_pages]
@@ -1393,6 +1394,8 @@ int sq_prefill_attention(sq_cache* c, sq_seq seq, int32_t layer, int32_t n_q, co
         victim->max_splits = 0;
         for (const PrefillMerge& m : plan.merges)
             victim->max_splits = std::max(victim->max_splits, m.n);
+        // (spans, or unused slots of partial pages)
+        victim->hides = s->extended && !sa.empty();
         victim->visible_pairs = plan.visible_pairs;
         list_writes(c, s->pages.data(), s->pages.size(), &victim->writes);
         victim->valid = true;
@@ -1447,6 +1450,7 @@ int sq_prefill_attention(sq_cache* c, sq_seq seq, int32_t layer, int32_t n_q, co
                          early_writes(c, plan.writes, a.unsafe, &a.n_unsafe)
                      ? 1
                      : 0;
+    a.hides = plan.hides;
     // the kernel keeps the scale inside the exponent (s * scale - m); a zero
     // scale runs as 1e-30, whose weights 2^(s * 1e-30 - m) are exactly 1
     a.scale_log2 = std::max(sm_scale * 1.4426950408889634f, 1e-30f);

@@ -121,6 +121,7 @@ int HostCache::seq_new(int32_t* handle) {
     s.next_pos = 0;
     s.version = g_version_counter++;
     s.last_stream = nullptr;
+    s.extended = false;
     *handle = (int32_t)((s.gen << 20) | (uint32_t)slot);
     return kOk;
 }
@@ -133,6 +134,7 @@ int HostCache::fork(int32_t parent, int32_t* child) {
     int32_t n = ps->n;
     const int64_t next_pos = ps->next_pos;
     void* st = ps->last_stream;
+    const bool extended = ps->extended;
     int rc = seq_new(child);
     if (rc != kOk) return rc;
     Seq* cs = seq_mut(*child);
@@ -141,6 +143,7 @@ int HostCache::fork(int32_t parent, int32_t* child) {
     cs->n = n;
     cs->next_pos = next_pos;
     cs->last_stream = st;
+    cs->extended = extended;
     for (int32_t p : cs->pages) alloc_.add_ref(p);
     return kOk;
 }

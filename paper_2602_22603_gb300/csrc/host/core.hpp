@@ -95,6 +95,10 @@ struct Seq {
     // phase of their original positions
     int64_t next_pos = 0;
     void* last_stream = nullptr;
+    // rows were added before their keys and values existed (sq_extend; a fork takes
+    // this from its parent): slots that the sequence uses, or used, may never have
+    // been written
+    bool extended = false;
 };
 
 // Slot-space end of a sequence: (pages - 1) * P + last fill (0 when empty).

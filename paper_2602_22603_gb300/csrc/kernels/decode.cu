@@ -54,7 +54,7 @@
 // page's unused slots are.
 //
 // Page fills: after a ragged eviction a page may hold fewer rows than it has
-// slots (its rows first, then zeros or rows once appended).  Stages are in
+// slots (its rows first; what the others hold is masked).  Stages are in
 // slot space (page index x P + slot); the plan then carries every page's
 // fill, and the rows past a page's fill get no weight.
 //

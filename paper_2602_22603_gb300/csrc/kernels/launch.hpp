@@ -85,7 +85,12 @@ struct PrefillShortArgs : PrefillArgs {
     int32_t kv_early;
     int32_t n_unsafe;
     int32_t unsafe[kMaxUnsafe];
+    // (for the launch) 1: rows that the plan hides may never have been written
+    int32_t hides;
 };
+// The same for plans that hide such rows (instances of their own).
+struct PrefillHideArgs : PrefillArgs {};
+struct PrefillHideShortArgs : PrefillShortArgs {};
 
 struct PrefillCombineArgs {
     const PrefillMerge* merges;

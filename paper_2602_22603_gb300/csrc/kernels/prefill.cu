@@ -13,6 +13,13 @@ static cudaError_t prepare() {
     e = cudaFuncSetAttribute(dev::sq_prefill_kernel<D, PrefillShortArgs>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              dev::PreCfg<D, dev::kOneTile>::kSmemBytes);
     if (e != cudaSuccess) return e;
+    e = cudaFuncSetAttribute(dev::sq_prefill_kernel<D, PrefillHideArgs>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             dev::PreCfg<D, dev::kHides>::kSmemBytes);
+    if (e != cudaSuccess) return e;
+    e = cudaFuncSetAttribute(dev::sq_prefill_kernel<D, PrefillHideShortArgs>,
+                             cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             dev::PreCfg<D, dev::kHides | dev::kOneTile>::kSmemBytes);
+    if (e != cudaSuccess) return e;
     // the same split of L1 and shared memory as the prefill kernel's: they take
     // turns on every SM
     e = cudaFuncSetAttribute(dev::sq_prefill_combine_kernel<D, 2, 24, PrefillCombineArgs>,
@@ -54,6 +61,18 @@ cudaError_t launch_prefill(const CUtensorMap& pool_map, const CUtensorMap& qmap,
     };
     const PrefillArgs& base = a;
     const bool one = a.n_q <= a.BP;  // every query in tile a of the only CTA tile
+    if (a.hides) {
+        PrefillHideShortArgs s;
+        static_cast<PrefillShortArgs&>(s) = a;
+        PrefillHideArgs b;
+        static_cast<PrefillArgs&>(b) = a;
+        constexpr int kH = dev::kHides, kHO = dev::kHides | dev::kOneTile;
+        if (D == 128)
+            return one ? launch(dev::PreCfg<128, kHO>{}, dev::sq_prefill_kernel<128, PrefillHideShortArgs>, s)
+                       : launch(dev::PreCfg<128, kH>{}, dev::sq_prefill_kernel<128, PrefillHideArgs>, b);
+        return one ? launch(dev::PreCfg<64, kHO>{}, dev::sq_prefill_kernel<64, PrefillHideShortArgs>, s)
+                   : launch(dev::PreCfg<64, kH>{}, dev::sq_prefill_kernel<64, PrefillHideArgs>, b);
+    }
     if (D == 128)
         return one ? launch(dev::PreCfg<128, dev::kOneTile>{}, dev::sq_prefill_kernel<128, PrefillShortArgs>, a)
                    : launch(dev::PreCfg<128, 0>{}, dev::sq_prefill_kernel<128, PrefillArgs>, base);

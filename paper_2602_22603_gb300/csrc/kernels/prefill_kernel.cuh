@@ -95,12 +95,15 @@ namespace {
 // (query blocks of a batch, see BlockItem); otherwise all items belong to one
 // sequence, whose newest n_q tokens they share out.  kTwoProducers: blocks whose loads
 // are two producer warps': on pages of fewer than 64 tokens, which take many boxes,
-// and one-tile blocks of 64 dimensions, whose loads are short.
-constexpr int kOneTile = 1, kBlocks = 2, kTwoProducers = 4;
+// and one-tile blocks of 64 dimensions, whose loads are short.  kHides: prefill of a
+// sequence whose hidden rows may hold anything (zero_hidden_values).
+constexpr int kOneTile = 1, kBlocks = 2, kTwoProducers = 4, kHides = 8;
 template <int M>
 constexpr bool one_tile = (M & kOneTile) != 0;
 template <int M>
 constexpr bool of_blocks = (M & kBlocks) != 0;
+template <int M>
+constexpr bool hides = (M & kHides) != 0;
 template <int M>
 constexpr int producers = (M & kTwoProducers) != 0 ? 2 : 1;
 
@@ -1576,6 +1579,39 @@ struct SoftmaxPhase {
 constexpr uint32_t kParS = 1, kParO = 2, kParX = 4;  // S_t, O_t, dual-key exchange
 constexpr uint32_t kParPV = 8;  // (three S buffers) items of three key tiles or more
 
+// A V row whose key no query sees (a span's, or in an unused slot of a partial page)
+// has the weight 0, and 0 times an infinity or NaN is NaN.  Rows that sq_append_kv
+// wrote are taken to be finite; those that sq_extend added may never have been
+// written.  So in the instances for sequences that have such rows (kHides) the softmax
+// warps zero the hidden rows of a tile's V before they hand over the P that the
+// tile's first PV waits for: tile a's, or in dual-key mode the tile's own, warp wq of
+// the four the rows of word wq of the visibility.  V of the item's key tile j (its
+// loads begin with number ub) is waited for; its load needs no P of this tile or of
+// the one before.  (Rows past the end the producer has zeroed.)  In every instance this would cost 32,768 queries, 40% masked, 3.25 ->
+// 3.30 ms by the code generated around it, and by a warp of its own that takes V over
+// from the loads 3.43 ms.
+template <int D, int M>
+__device__ __forceinline__ bool zero_hidden_values(const Smem& sm, const PrefillTile* tile, int n, uint32_t ub,
+                                                   int j, int T, bool dual, int wq, volatile int* abort_flag,
+                                                   int lane) {
+    using C = PreCfg<D, M>;
+    static_assert(C::kSlots >= 5, "V's slot was last that of a tile at least two before");
+    const uint32_t u = ub + (!dual ? 2 * j + 1 : j + 2 < T ? 2 * j + 2 : T + j);  // (see load_of)
+    const int key = __ldg(wq < 2 ? &tile->key0 : &tile->key0b) + 32 * (wq & 1);
+    const uint32_t hidden = ~__ldg(&tile->vis[wq]) & low_bits_through(n - 1 - key);
+    if (!hidden) return true;
+    if (!warp_wait(sm.bar<D, M>(C::kBarFull + u % C::kSlots), (u / C::kSlots) & 1, abort_flag)) return false;
+    uint8_t* v = sm.ptr + C::kOffRing + u % C::kSlots * C::kSlotBytes + wq * 32 * 128;
+    for (int i = lane; i < 32 * C::kColBlocks * 8; i += 32) {
+        const int r = i >> 3 & 31;
+        if ((hidden >> r) & 1u)
+            *reinterpret_cast<uint4*>(v + (i >> 8) * C::kBlockBytes + r * 128 + (i & 7) * 16) =
+                make_uint4(0, 0, 0, 0);
+    }
+    fence_proxy_async_smem();
+    return true;
+}
+
 // Softmax warpgroup of query tile t (one row per thread) and its epilogue,
 // for one item.  False: a wait ran out.
 template <int D, int M, typename Args>
@@ -1606,6 +1642,13 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
     // and O are never read back).
     if (!__any_sync(0xffffffffu, valid)) {
         for (int j = 0; j < T; ++j) {
+            if constexpr (hides<M>) {
+                const PrefillTile* tile = a.tiles + t0 + kfirst + kstep * j;
+                if ((t == 0 || dual) && !(__ldg(&tile->flags) & kPrefillTileFull) &&
+                    !zero_hidden_values<D, M>(sm, tile, a.n, ph.ub, kfirst + kstep * j, T_cta, dual, wq,
+                                              abort_flag, lane))
+                    return false;
+            }
             uint32_t buf = t, parity = ph.par & kParS;
             if constexpr (C::kBufs > 2) {
                 buf = number(j) % 3;
@@ -1671,6 +1714,12 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
         if (j + 1 < T) {
             nk = __ldg(reinterpret_cast<const int2*>(tp + kstep));
             nb = __ldg(&tp[kstep].key0b);
+        }
+        if constexpr (hides<M>) {
+            if ((t == 0 || dual) && !(wk.y & kPrefillTileFull) &&
+                !zero_hidden_values<D, M>(sm, tp, a.n, ph.ub, kfirst + kstep * j, T_cta, dual, wq, abort_flag,
+                                          lane))
+                return false;
         }
         uint32_t parity = ph.par & kParS;
         if constexpr (C::kBufs > 2) {
@@ -1907,6 +1956,10 @@ template <>
 struct ModeOf<PrefillArgs> : std::integral_constant<int, 0> {};
 template <>
 struct ModeOf<PrefillShortArgs> : std::integral_constant<int, kOneTile> {};
+template <>
+struct ModeOf<PrefillHideArgs> : std::integral_constant<int, kHides> {};
+template <>
+struct ModeOf<PrefillHideShortArgs> : std::integral_constant<int, kHides | kOneTile> {};
 template <>
 struct ModeOf<BlockArgs> : std::integral_constant<int, kBlocks> {};
 template <>
