@@ -231,7 +231,8 @@ SQ_API int sq_evict_spans_ragged(sq_cache *cache, sq_seq seq, const sq_span *spa
  * ragged eviction); otherwise UNSUPPORTED.  The sequence and the cache are
  * not modified.  Rows that a span hides and unused slots of partial pages may
  * never have been stored (sq_extend): they reach no output.  Rows that were
- * appended or stored are taken to be finite, hidden or not.  The
+ * appended or stored are taken to be finite, hidden or not; NaN in a query, or
+ * in a key or value that it sees, is NaN in its output.  The
  * kernel runs on the tensor cores (bf16 products, fp32 accumulation; the
  * softmax weights are rounded to bf16 before the value product, and the
  * normaliser sums the same rounded weights).  Where key ranges are shared out

@@ -1265,8 +1265,8 @@ __device__ __forceinline__ bool prefill_write(const PrefillArgs& a, const Item& 
     const bool dual = it.dual, any_keys = it.T > 0;
     const int qi = q_row + (dual ? 0 : t) * a.BP + row / a.G;
     const float inv = l > 0.f ? 1.f / l : 0.f;
-    // (a block's row whose weights are NaN says so, to its merge too)
-    const float lse2 = l > 0.f ? m_run + __log2f(l) : (of_blocks<M> && l != 0.f ? NAN : -INFINITY);
+    // (a row whose weights are NaN says so, to its merge too)
+    const float lse2 = l > 0.f ? m_run + __log2f(l) : (l != 0.f ? NAN : -INFINITY);
     const int h = it.g * a.G + row % a.G;
     float* part_row = nullptr;
     uint8_t* out_row = nullptr;
@@ -2174,9 +2174,8 @@ __global__ void __launch_bounds__(kCombineThreads, U > kCombineFew ? 6 : 8)
     float W = w0 + w1;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) W += __shfl_xor_sync(0xffffffffu, W, off);
-    float none = 0.f;  // of a row without weights; (blocks) NaN where a piece's are NaN
-    if constexpr (kOfBlocks)
-        if (__any_sync(0xffffffffu, ml0 != ml0 || ml1 != ml1)) W = none = NAN;
+    float none = 0.f;  // of a row without weights; NaN where a piece's are NaN
+    if (__any_sync(0xffffffffu, ml0 != ml0 || ml1 != ml1)) W = none = NAN;
     float acc[V] = {};
     for (int s0 = 0; W > 0.f && s0 < n_split; s0 += U) {
         if (s0 > 0) load(s0);
