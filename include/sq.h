@@ -455,7 +455,9 @@ SQ_API int sq_qk_norm_rope_backward(sq_cache *cache, int32_t n_tokens, const voi
  * a query does not see, and slots past a sequence's end, may hold anything: an
  * infinity or NaN there does not reach its output (it costs time: such a query is
  * taken once more, 40 to 130 us a head for 1,000 keys).  NaN in a query, or in a
- * key or value that it sees, is NaN in its output.
+ * key or value that it sees, is NaN in its output.  Values may have any finite
+ * size: a query whose weighted sums pass 32 bits on the way (values of 1e26 and
+ * more, weights being relative to 1) is taken once more too.
  * Single tokens without lse run as sq_decode_attention does.
  * Weights and normaliser are rounded as in sq_prefill_attention, whose limits on
  * library memory for partial results hold too.  A plan of more than 2^24 key

@@ -1421,27 +1421,35 @@ template <>
 struct RowMask<kBlocks | kOneTile | kTwoProducers> : BlockRowMask {};
 
 // A key that a row does not see has the weight 0 in the row's tile product, and
-// 0 times an infinity or NaN in that key's V row is NaN.  So where a block's row has
-// an output that is not finite though its normaliser is, and some key that its tiles
-// hide has such a V row, it is taken once more, over the keys that it does see and
-// with the maximum and normaliser that it has: a warp on four rows of a query at a
-// time, a lane to a key for the weights and to D / 32 columns for the sums.  (An item
+// 0 times an infinity or NaN in that key's V row is NaN.  Besides, a row's weights may
+// sum to 2^40 and more (its maximum starts at 0), and times large values they pass
+// what fp32 holds where their average is finite.  So where a block's row has an output
+// that is not finite though its normaliser is, and some key that its tiles hide has
+// such a V row, or no key of the item has one (then the sums overflowed), it is taken
+// once more, over the keys that it does see and with the maximum and normaliser that
+// it has, the weights divided by the normaliser first, so that every sum is an average
+// of values: a warp on four rows of a query at a time, a lane to a key for the weights
+// and to D / 32 columns for the sums.  (Sums that overflow beside a key that the row
+// sees whose value is not finite stay as they are.)  (An item
 // pays D fused multiply-adds a row to look, and nothing more as long as stored rows
 // are finite.  A row taken again costs 40 us for 1,000 keys, 130 where a KV head has
 // one query head: a warp's 32 rows over 400,000 keys still end within the other
 // roles' bounded waits of 2 s.)
+//
+// Whether some V row of the item is not finite; with a mask only of those that it
+// hides.
 template <int D, int M, typename Args>
-__device__ bool hides_odd_values(const Args& a, const BlockItem& it, const BlockRowMask& mask,
-                                 const __nv_bfloat16* values, int lane) {
+__device__ bool has_odd_values(const Args& a, const BlockItem& it, const BlockRowMask* mask,
+                               const __nv_bfloat16* values, int lane) {
     const int per = pieces_of<M>(a), br = 128 / per;
     for (int j = it.t0; j < it.t0 + it.n_tiles; ++j) {
         const PrefillTile* t = a.tiles + j;
         const int2 r = __ldg(reinterpret_cast<const int2*>(t));
         const int key_b = __ldg(&t->key0b);
-        if ((r.y & kPrefillTileFull) && mask.whole(r.x) && mask.whole(key_b)) continue;
+        if (mask && (r.y & kPrefillTileFull) && mask->whole(r.x) && mask->whole(key_b)) continue;
         for (int w = 0; w < 4; ++w) {
             const int key = (w < 2 ? r.x : key_b) + 32 * (w & 1) + lane;
-            const uint32_t see = __ldg(&t->vis[w]) & mask.word(key - lane);
+            const uint32_t see = mask ? __ldg(&t->vis[w]) & mask->word(key - lane) : 0u;
             // (rows past the end were zeroed, a box that does not exist as well)
             const int page = __ldg(&a.tile_pages[(size_t)j * per + (w * 32 + lane) / br]);
             bool odd = false;
@@ -1470,11 +1478,12 @@ __device__ __noinline__ void rows_again(const Args& a, const BlockItem& it, int 
     const __nv_bfloat16* keys =
         static_cast<const __nv_bfloat16*>(a.pool) + ((size_t)a.layer * a.num_pages * 2 * a.Hkv + g) * run;
     const __nv_bfloat16* values = keys + a.Hkv * run;
+    const bool odd = has_odd_values<D, M>(a, it, nullptr, values, lane);
     while (rows) {
         // up to kRows rows of one query: they see the same keys
         const int qi = tile * a.BP + (row0 + __ffs(rows) - 1) / a.G;
         int n_rows = 0, row[kRows];
-        float m[kRows], sum[kRows], acc[kRows][kCols];
+        float m[kRows], inv[kRows], sum[kRows], acc[kRows][kCols];
         const uint4* q[kRows];
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
@@ -1487,7 +1496,10 @@ __device__ __noinline__ void rows_again(const Args& a, const BlockItem& it, int 
             }
             m[r] = __shfl_sync(0xffffffffu, m_run, row[r] - row0);
             if (m[r] == -INFINITY) m[r] = 0.f;
-            sum[r] = __shfl_sync(0xffffffffu, l, row[r] - row0);
+            // (half of an average's weights: their own sum, taken below, may pass 1)
+            const float l_row = __shfl_sync(0xffffffffu, l, row[r] - row0);
+            inv[r] = l_row > 0.f ? 0.5f / l_row : 0.f;
+            sum[r] = 0.f;
             q[r] = reinterpret_cast<const uint4*>(
                 static_cast<const __nv_bfloat16*>(a.q) +
                 ((size_t)(it.q_row + qi) * a.Hq + g * a.G + row[r] % a.G) * D);
@@ -1496,7 +1508,7 @@ __device__ __noinline__ void rows_again(const Args& a, const BlockItem& it, int 
         }
         BlockRowMask mask;
         mask.init(a, it, qi);
-        if (!hides_odd_values<D, M>(a, it, mask, values, lane)) continue;
+        if (odd && !has_odd_values<D, M>(a, it, &mask, values, lane)) continue;
         for (int x = 0; x < 4 * it.n_tiles; ++x) {
             const int j = it.t0 + (x >> 2), w = x & 3;
             const PrefillTile* t = a.tiles + j;
@@ -1527,8 +1539,10 @@ __device__ __noinline__ void rows_again(const Args& a, const BlockItem& it, int 
                     }
                 }
 #pragma unroll
-                for (int r = 0; r < kRows; ++r)
-                    p[r] = __bfloat162float(__float2bfloat16(ex2_ftz(fmaf(p[r], a.scale_log2, -m[r]))));
+                for (int r = 0; r < kRows; ++r) {
+                    p[r] = __bfloat162float(__float2bfloat16(ex2_ftz(fmaf(p[r], a.scale_log2, -m[r])))) * inv[r];
+                    sum[r] += p[r];
+                }
             }
             for (int c0 = 0; c0 < 32; c0 += kAhead) {
                 float v[kAhead][kCols];
@@ -1552,11 +1566,14 @@ __device__ __noinline__ void rows_again(const Args& a, const BlockItem& it, int 
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
             if (r >= n_rows) break;
-            const float inv = sum[r] > 0.f ? 1.f / sum[r] : 0.f;
+            float total = sum[r];
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
+            const float scale = total > 0.f ? 1.f / total : 0.f;
             const size_t q_head = (size_t)(it.q_row + qi) * a.Hq + g * a.G + row[r] % a.G;
 #pragma unroll
             for (int i = 0; i < kCols; ++i) {
-                const float f = acc[r][i] * inv;
+                const float f = acc[r][i] * scale;
                 const int col = lane + 32 * i;
                 if (it.part >= 0)
                     a.part_o[(((size_t)it.part * kPrefillQTiles + tile) * kPrefillRows + row[r]) * D + col] = f;
@@ -2176,6 +2193,14 @@ __global__ void __launch_bounds__(kCombineThreads, U > kCombineFew ? 6 : 8)
     for (int off = 16; off > 0; off >>= 1) W += __shfl_xor_sync(0xffffffffu, W, off);
     float none = 0.f;  // of a row without weights; NaN where a piece's are NaN
     if (__any_sync(0xffffffffu, ml0 != ml0 || ml1 != ml1)) W = none = NAN;
+    float inv = W > 0.f ? 1.f / W : none;
+    const float lse = W > 0.f ? (M + __log2f(W)) * 0.69314718055994531f : none - INFINITY;
+    // (blocks: an average at every step, so that the largest values do not overflow)
+    if (kOfBlocks && W > 0.f) {
+        w0 *= inv;
+        w1 *= inv;
+        inv = 1.f;
+    }
     float acc[V] = {};
     for (int s0 = 0; W > 0.f && s0 < n_split; s0 += U) {
         if (s0 > 0) load(s0);
@@ -2189,7 +2214,6 @@ __global__ void __launch_bounds__(kCombineThreads, U > kCombineFew ? 6 : 8)
             }
         }
     }
-    const float inv = W > 0.f ? 1.f / W : none;
     const size_t o = ((size_t)qi * a.Hq + h) * D + col;
     if (a.out_f32) {
         float* out = reinterpret_cast<float*>(a.out) + o;
@@ -2209,8 +2233,7 @@ __global__ void __launch_bounds__(kCombineThreads, U > kCombineFew ? 6 : 8)
             *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
         }
     }
-    if (lane == 0 && col == 0 && a.lse)
-        a.lse[(size_t)qi * a.Hq + h] = W > 0.f ? (M + __log2f(W)) * 0.69314718055994531f : none - INFINITY;
+    if (lane == 0 && col == 0 && a.lse) a.lse[(size_t)qi * a.Hq + h] = lse;
 }
 
 }  // namespace
