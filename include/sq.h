@@ -287,7 +287,11 @@ SQ_API int sq_page_refcount(sq_cache *cache, int32_t page, int32_t *out);
 /* Number of free pages. */
 SQ_API int sq_free_pages(sq_cache *cache, int32_t *out);
 
-/* Device pointer of the KV pool (layout above). */
+/* Device pointer of the KV pool (layout above).  A caller that writes rows itself
+ * (those of sq_extend) asks for it first, also where the pool is its own
+ * (kv_pool): attention reads ahead of its stream's earlier work only what this
+ * library is known to have written, and from then on nothing of sequences that
+ * sq_extend lengthened. */
 SQ_API int sq_pool_ptr(sq_cache *cache, void **out);
 
 typedef struct {

@@ -661,7 +661,7 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
     a.plan_ready = plan_ready;
     a.n_unsafe = 0;
     a.kv_early = plan.one && plan_ready && g.P >= kPrefillKeys / 2 &&
-                         early_writes(c, plan.writes, a.unsafe, &a.n_unsafe)
+                         early_writes(c, plan.writes, seqs, n_seqs, a.unsafe, &a.n_unsafe)
                      ? 1
                      : 0;
     // (a zero scale as in sq_prefill_attention)

@@ -220,6 +220,9 @@ struct sq_cache {
     // is known complete.
     uint64_t write_seq = 0, write_done = 0;
     bool early_ok = true;
+    // the caller has the pool's address (sq_pool_ptr) and may write rows that it
+    // added (sq_extend) unseen
+    bool pool_given = false;
     // the newest store of rows already counted (sq_qk_norm_rope_store), which
     // changes no version: its pages and ticket, and the newest ticket of the
     // stores before it to other pages
@@ -407,10 +410,15 @@ void list_writes(sq_cache* c, const int32_t* pages, size_t n, WriteTickets* w) {
 
 // Whether every write to a plan's pages outside its newest few is complete: a
 // kernel may then load its first K/V before its dependency wait, except from
-// the pages whose writes may still be running (listed in `unsafe`).
-bool early_writes(sq_cache* c, const WriteTickets& w, int32_t* unsafe, int32_t* n_unsafe) {
+// the pages whose writes may still be running (listed in `unsafe`).  Rows that
+// the caller may write itself are never known to be complete.
+bool early_writes(sq_cache* c, const WriteTickets& w, const sq_seq* seqs, int32_t n_seqs, int32_t* unsafe,
+                  int32_t* n_unsafe) {
     *n_unsafe = 0;
     if (!c->early_ok) return false;
+    if (c->pool_given)
+        for (int32_t i = 0; i < n_seqs; ++i)
+            if (c->host->seq(seqs[i])->extended) return false;
     poll_writes(c);
     if (w.rest > c->write_done || c->store_rest > c->write_done) return false;
     if (c->store_ticket > c->write_done) {
@@ -1126,7 +1134,7 @@ static int decode_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t 
     a.num_pages = g.num_pages;
     a.scale_log2 = sm_scale * 1.4426950408889634f;
     a.debug_drop_cta = (c->debug_flags & SQ_DEBUG_DROP_DECODE_STAGE) ? hit->first_busy_cta : -1;
-    a.kv_early = plan_ready && early_writes(c, hit->writes, a.unsafe, &a.n_unsafe) ? 1 : 0;
+    a.kv_early = plan_ready && early_writes(c, hit->writes, seqs, n_seqs, a.unsafe, &a.n_unsafe) ? 1 : 0;
     if (a.kv_early) {
         c->stats.decode_early_calls += 1;
         c->stats.decode_early_held += a.n_unsafe;
@@ -1447,7 +1455,7 @@ int sq_prefill_attention(sq_cache* c, sq_seq seq, int32_t layer, int32_t n_q, co
     a.plan_ready = plan_ready;
     a.n_unsafe = 0;
     a.kv_early = plan_ready && g.P >= kPrefillKeys / 2 &&
-                         early_writes(c, plan.writes, a.unsafe, &a.n_unsafe)
+                         early_writes(c, plan.writes, &seq, 1, a.unsafe, &a.n_unsafe)
                      ? 1
                      : 0;
     a.hides = plan.hides;
@@ -1574,6 +1582,7 @@ int sq_pool_ptr(sq_cache* c, void** out) {
     if (!c) return SQ_ERR_BAD_HANDLE;
     if (!out) return SQ_ERR_INVALID_ARG;
     *out = c->pool;
+    c->pool_given = true;
     return SQ_OK;
 }
 
