@@ -137,7 +137,9 @@ inline void cut_units(const std::vector<Unit>& units, int32_t heads, int32_t cta
 // tiles: the units' heads in a line, cut into stretches of equal cost (key tiles
 // and a fixed part for each piece).  A cut is moved to a unit's end when it would
 // leave a sliver on either side.  Short units are left whole while that leaves no
-// CTA with a second one: a merge would cost more than it saves.
+// CTA with a second one: a merge would cost more than it saves.  Without room for
+// partial results no unit is cut: the longest first, each goes to the CTA that has
+// least.
 // pieces[c]: those of CTA c, in order.
 inline void deal_units(const std::vector<Unit>& units, int32_t heads, int32_t ctas, int64_t max_parts,
                        int32_t D, std::vector<std::vector<Piece>>* out) {
@@ -152,6 +154,23 @@ inline void deal_units(const std::vector<Unit>& units, int32_t heads, int32_t ct
     }
     const int64_t n = (int64_t)units.size() * heads;
     const bool whole = max_parts < 2 || (n <= ctas && T_max <= short_unit);
+    if (whole && n > ctas) {
+        std::vector<int32_t> order(units.size());
+        for (size_t u = 0; u < order.size(); ++u) order[u] = (int32_t)u;
+        std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return units[x].T > units[y].T; });
+        typedef std::pair<double, int32_t> Load;  // and its CTA; the least in front
+        std::vector<Load> load;
+        for (int32_t c = 0; c < ctas; ++c) load.push_back({0.0, c});
+        out->resize(ctas);
+        for (int32_t u : order)
+            for (int32_t h = 0; h < heads; ++h) {
+                std::pop_heap(load.begin(), load.end(), std::greater<Load>());
+                (*out)[load.back().second].push_back({u, h, 0, units[u].T});
+                load.back().first += units[u].T + fixed;
+                std::push_heap(load.begin(), load.end(), std::greater<Load>());
+            }
+        return;
+    }
     // (a cut at the end of each share adds a piece)
     // and a unit has at most kPrefillMaxSplit pieces
     const double share = std::max({2.0 * sliver, (total + fixed * n) / ctas + fixed,
@@ -169,7 +188,7 @@ inline void deal_units(const std::vector<Unit>& units, int32_t heads, int32_t ct
                 int32_t take = left;
                 const bool may = (int32_t)out->size() < ctas;
                 if (whole) {
-                    if (may && !out->back().empty() && n <= ctas) {
+                    if (may && !out->back().empty()) {
                         out->emplace_back();
                         room += share;
                     }
