@@ -246,7 +246,8 @@ def _types():
 
 
 def _wrong(name, want, x):
-    raise ValueError(f"{name}: {want} expected, not {x.dtype} {list(x.shape)} of strides {x.stride()}")
+    raise ValueError(f"{name}: {want} on a cuda device expected, not {x.dtype} {list(x.shape)} of strides "
+                     f"{x.stride()} on {x.device}")
 
 
 def _rows(x, heads, dim, name, n=None):
@@ -257,7 +258,7 @@ def _rows(x, heads, dim, name, n=None):
         return x, heads * dim, n
     if x.dim() == 3:
         (tokens, h, d), (apart, s1, s2) = x.shape, x.stride()
-        if (h == heads and d == dim and s2 == 1 and s1 == dim and x.dtype is _BF16
+        if (h == heads and d == dim and s2 == 1 and s1 == dim and x.dtype is _BF16 and x.is_cuda
                 and (n is None or tokens == n)):
             # (one token has no distance to the next)
             return x.data_ptr(), apart if tokens > 1 else heads * dim, tokens
@@ -265,11 +266,11 @@ def _rows(x, heads, dim, name, n=None):
 
 
 def _flat(x, want, count, name):
-    """Address of a contiguous tensor of `count` elements of a type (None and
-    addresses as they are)."""
+    """Address of a contiguous tensor of `count` elements of a type on a device (None
+    and addresses as they are)."""
     if x is None or x.__class__ is int:
         return x
-    if x.dtype is want and x.numel() == count and x.is_contiguous():
+    if x.dtype is want and x.numel() == count and x.is_contiguous() and x.is_cuda:
         return x.data_ptr()
     _wrong(name, f"{count} contiguous elements of {want}", x)
 
@@ -278,12 +279,13 @@ def norm_rope(rope=None, rot_dim=0, eps=1e-6, q_weight=None, k_weight=None,
               interleaved=False) -> sq_norm_rope:
     """The parameters of the norms and the rotation: `rope` a float32 CUDA tensor
     [max_pos, rot_dim / 2, 2] of cosines and sines (rope_table makes one),
-    weights bfloat16 or float32 tensors [head_dim] of one type, or None (ones)."""
+    weights bfloat16 or float32 CUDA tensors [head_dim] of one type, or None (ones)."""
     _types()
     weights = [w for w in (q_weight, k_weight) if w is not None]
     for w in weights:
-        if w.dtype not in (_BF16, _FLOAT) or w.dtype is not weights[0].dtype or not w.is_contiguous():
-            _wrong("weights", "contiguous, both bfloat16 or both float32", w)
+        if (w.dtype not in (_BF16, _FLOAT) or w.dtype is not weights[0].dtype or not w.is_contiguous()
+                or not w.is_cuda or w.numel() != weights[0].numel()):
+            _wrong("weights", "contiguous, of one size, both bfloat16 or both float32", w)
     f32 = bool(weights) and weights[0].dtype is _FLOAT
     max_pos = 0
     if rope is not None and rot_dim:
@@ -293,7 +295,16 @@ def norm_rope(rope=None, rot_dim=0, eps=1e-6, q_weight=None, k_weight=None,
                      SQ_OUT_F32 if f32 else SQ_OUT_BF16, rot_dim, int(interleaved),
                      max_pos, eps)
     p._keep = (rope, q_weight, k_weight)
+    p._dim = weights[0].numel() if weights else None
     return p
+
+
+def _weights_fit(params, dim):
+    """Refuses parameters whose weights are not one head's (those of a structure filled
+    by hand are not known)."""
+    n = getattr(params, "_dim", None)
+    if n is not None and n != dim:
+        raise ValueError(f"weights: {dim} elements expected, not {n}")
 
 
 def rope_table(max_pos, rot_dim, theta=10000.0, device="cuda"):
@@ -598,6 +609,7 @@ class Cache:
         if _BF16 is None:
             _types()
         hq, hkv, d = self.Hq, self.Hkv, self.D
+        _weights_fit(params, d)
         q, qs, n = _rows(q, hq, d, "q")
         n = self._counted(seqs, n_new, n, "qk_norm_rope_store")
         k, ks, _ = _rows(k, hkv, d, "k", n)
@@ -611,6 +623,7 @@ class Cache:
         if _BF16 is None:
             _types()
         hq, hkv, d = self.Hq, self.Hkv, self.D
+        _weights_fit(params, d)
         q, qs, n = _rows(q, hq, d, "q")
         k, ks, _ = _rows(k, hkv, d, "k", n)
         sq_qk_norm_rope(self.handle, n, q, qs, k, ks, _flat(positions, _INT, n, "positions"), params,
@@ -624,6 +637,7 @@ class Cache:
         if _BF16 is None:
             _types()
         hq, hkv, d = self.Hq, self.Hkv, self.D
+        _weights_fit(params, d)
         q, qs, n = _rows(q, hq, d, "q")
         k, ks, _ = _rows(k, hkv, d, "k", n)
         dq, dqs, _ = _rows(dq, hq, d, "dq", n)
