@@ -157,7 +157,7 @@ int used_buffer(TurnBuffer& b, cudaStream_t st) {
 // pages of the newest store one by one.
 void note_store(sq_cache* c, std::vector<int32_t>&& pages, void* stream) {
     // (stores may go on without an attention call, which would look after them)
-    if (c->write_pending.size() >= 32) poll_writes(c);
+    if (c->early_ok && c->write_pending.size() >= 32 && !capturing(as_stream(stream))) poll_writes(c);
     note_writes(c, pages.data(), pages.size(), stream);
     if (pages != c->store_pages) {
         c->store_rest = c->store_ticket;

@@ -341,11 +341,27 @@ int record_freed(sq_cache* c, const std::vector<int32_t>& freed, void* stream) {
     return SQ_OK;
 }
 
+// Whether what is enqueued on a stream goes into a graph (to be run any number of
+// times, after any work); also where that cannot be told.
+bool capturing(cudaStream_t st) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &status) != cudaSuccess) {
+        cudaGetLastError();
+        return true;
+    }
+    return status != cudaStreamCaptureStatusNone;
+}
+
 // Stamps the pages a pool-writing launch just enqueued on `stream` writes.
-// If the event cannot be recorded, decode stops loading anything before its
-// dependency wait for the rest of the cache's life.
+// If the event cannot be recorded, or says nothing (a captured launch writes
+// whenever its graph runs), nothing is loaded before a dependency wait for the
+// rest of the cache's life.
 void note_writes(sq_cache* c, const int32_t* pages, size_t n, void* stream) {
     if (n == 0 || !c->early_ok) return;
+    if (capturing(as_stream(stream))) {
+        c->early_ok = false;
+        return;
+    }
     const uint64_t t = ++c->write_seq;
     for (size_t i = 0; i < n; ++i)
         if (pages[i] >= 0 && pages[i] < c->g.num_pages) c->page_ticket[pages[i]] = t;
@@ -1104,7 +1120,7 @@ static int decode_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t 
         e = cudaStreamWaitEvent(st, hit->ev, 0);
         if (e != cudaSuccess) return cuda_status(e);
     } else {
-        plan_ready = true;
+        plan_ready = window == 0 || !capturing(st);  // (as in sq_prefill_attention)
     }
     hit->last_use = ++c->use_clock;
     const DecodePlanLayout& L = hit->lay;
