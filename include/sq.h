@@ -360,7 +360,18 @@ SQ_API int sq_decode_attention_noalloc(sq_cache *cache, const sq_seq *seqs, int3
                                        int32_t layer, const void *q, void *out,
                                        int32_t out_dtype, float sm_scale, void *stream);
 
-/* ---- norms and rotation of queries and keys; rows stored layer by layer ---- */
+/* ---- norms and rotation of queries and keys; rows stored layer by layer ----
+ *
+ * The stores, norms and attention calls from here on may be captured into a graph.
+ * Its runs repeat them with the rows that the sequences had then, and take turns
+ * with the cache's other calls by the caller's order.  A captured call uploads
+ * nothing: sq_window_attention, sq_tree_attention and a store of more than 240 rows
+ * need the same call to have been made on the same stream and not to have been
+ * followed by too many others (four plans of query blocks, eight of single tokens
+ * and the places of two such stores are kept), sq_qk_norm_rope_backward with the
+ * weights' gradients one of as many tokens; else UNSUPPORTED.  What a captured call
+ * was given is kept for the cache's life.  A cache whose stores were captured reads
+ * nothing ahead of its stream's earlier work any more. */
 
 /* The norm of every query and key head and the position rotation after it.  For
  * a row x of head_dim elements with the weights w of its kind,

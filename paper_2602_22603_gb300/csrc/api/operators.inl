@@ -110,19 +110,25 @@ const __nv_bfloat16* bf16(const void* p) { return reinterpret_cast<const __nv_bf
 __nv_bfloat16* bf16(void* p) { return reinterpret_cast<__nv_bfloat16*>(p); }
 
 // A buffer of the cache that calls on any stream take turns with: `bytes` of it,
-// usable by work on `st` from here on.
-int take_buffer(TurnBuffer& b, size_t bytes, cudaStream_t st) {
+// usable by work on `st` from here on.  While `st` is captured: what there is, for
+// the graph to keep.
+int take_buffer(sq_cache* c, TurnBuffer& b, size_t bytes, cudaStream_t st, bool captured) {
     cudaError_t e;
+    if (captured) {
+        if (bytes > b.cap) return SQ_ERR_UNSUPPORTED;
+        b.captured = true;
+        return SQ_OK;
+    }
     if (!b.ev) {
         e = cudaEventCreateWithFlags(&b.ev, cudaEventDisableTiming);
         if (e != cudaSuccess) return cuda_status(e);
     }
     if (bytes > b.cap) {
         if (b.ev_recorded) cudaEventSynchronize(b.ev);
-        if (b.d) cudaFree(b.d);
+        retire(c, b.d, b.captured);
         b.d = nullptr;
         b.cap = 0;
-        b.ev_recorded = false;
+        b.ev_recorded = b.captured = false;
         const size_t cap = std::max<size_t>(bytes * 5 / 4, 4096);
         e = cudaMalloc(&b.d, cap);
         if (e != cudaSuccess) {
@@ -139,7 +145,8 @@ int take_buffer(TurnBuffer& b, size_t bytes, cudaStream_t st) {
 }
 
 // After the work that uses it has been enqueued (or may have been).
-int used_buffer(TurnBuffer& b, cudaStream_t st) {
+int used_buffer(TurnBuffer& b, cudaStream_t st, bool captured) {
+    if (captured) return SQ_OK;
     const cudaError_t e = cudaEventRecord(b.ev, st);
     if (e != cudaSuccess) {
         cudaStreamSynchronize(st);
@@ -300,7 +307,7 @@ int store_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n
         return SQ_ERR_INVALID_ARG;
     // where each row goes; more places than go with the launch stay on the device
     // for the next layer's store
-    const bool upload_places = n > kNormInline;
+    const bool upload_places = n > kNormInline, captured = upload_places && capturing(as_stream(stream));
     StorePlanEntry* hit = nullptr;
     for (auto& p : c->store_plans) {
         if (!upload_places || !p.valid || (int32_t)p.handles.size() != n_seqs) continue;
@@ -340,14 +347,15 @@ int store_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n
         if (e != cudaSuccess) return cuda_status(e);
     } else {
         const bool fresh = !hit;
+        // (a graph takes places that are there, uploaded on its stream)
+        if (captured && (fresh || hit->buf.ev_stream != st)) return SQ_ERR_UNSUPPORTED;
+        if (captured) keep_captured(c->store_plans, *hit);
         if (fresh) {
-            hit = &c->store_plans[0];
-            for (auto& p : c->store_plans)
-                if (!p.valid || p.last_use < hit->last_use) hit = &p;
+            hit = entry_to_replace(c->store_plans);
             hit->valid = false;
         }
         const size_t bytes = (size_t)n * sizeof(RowPlace);
-        rc = take_buffer(hit->buf, bytes, st);
+        rc = take_buffer(c, hit->buf, bytes, st, captured);
         if (rc != SQ_OK) return rc;
         if (fresh) rc = staged_copy(c, hit->buf.d, places.data(), bytes, stream);
         e = cudaSuccess;
@@ -355,7 +363,7 @@ int store_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n
             a.places = reinterpret_cast<const RowPlace*>(hit->buf.d);
             e = launch_norm_rope(a, g.D, true, st);
         }
-        const int used = used_buffer(hit->buf, st);
+        const int used = used_buffer(hit->buf, st, captured);
         if (rc != SQ_OK || e != cudaSuccess || used != SQ_OK) {
             hit->valid = false;
             return rc != SQ_OK ? rc : (e != cudaSuccess ? cuda_status(e) : used);
@@ -455,11 +463,12 @@ int norm_backward_impl(sq_cache* c, int32_t n_tokens, const void* q, int64_t q_s
     a.ctas = norm_rope_grad_ctas(n_tokens, g.Hq, g.Hkv, g.D, c->num_sms);
     fill_params(c, params, &a);
     if (!weights) return cuda_status(launch_norm_rope_grad(a, g.D, st));
-    rc = take_buffer(c->norm_part, (size_t)a.ctas * 2 * g.D * sizeof(float), st);
+    const bool captured = capturing(st);
+    rc = take_buffer(c, c->norm_part, (size_t)a.ctas * 2 * g.D * sizeof(float), st, captured);
     if (rc != SQ_OK) return rc;
     a.part = reinterpret_cast<float*>(c->norm_part.d);
     const cudaError_t e = launch_norm_rope_grad(a, g.D, st);
-    rc = used_buffer(c->norm_part, st);
+    rc = used_buffer(c->norm_part, st, captured);
     return e != cudaSuccess ? cuda_status(e) : rc;
 }
 
@@ -526,6 +535,9 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
         }
     }
     int32_t plan_ready = 0;
+    // (a graph takes a kept plan of its own stream, or none)
+    const bool captured = capturing(st);
+    if (captured && (!hit || (hit->ev_recorded && hit->ev_stream != st))) return SQ_ERR_UNSUPPORTED;
     if (!hit) {
         std::vector<BlockSeq> in(n_seqs);
         for (int32_t i = 0, at = 0; i < n_seqs; ++i) {
@@ -555,9 +567,7 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
             p.at = bytes;
             bytes += p.bytes;
         }
-        BlockPlanEntry* victim = &c->block_plans[0];
-        for (auto& p : c->block_plans)
-            if (!p.valid || p.last_use < victim->last_use) victim = &p;
+        BlockPlanEntry* victim = entry_to_replace(c->block_plans);
         victim->valid = false;
         if (!victim->ev) {
             e = cudaEventCreateWithFlags(&victim->ev, cudaEventDisableTiming);
@@ -620,14 +630,14 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
     } else {
         // (a captured launch may run after any work, also work that writes what
         // this one would read ahead of its dependency wait)
-        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-        e = cudaStreamIsCapturing(st, &capture);
-        if (e != cudaSuccess) return cuda_status(e);
-        plan_ready = capture == cudaStreamCaptureStatusNone;
+        plan_ready = !captured;
     }
+    if (captured) keep_captured(c->block_plans, *hit);
     hit->last_use = ++c->use_clock;
     const BlockPlanEntry& plan = *hit;
-    if (plan.n_parts > 0) {
+    if (plan.n_parts > 0 && captured) {
+        c->pre_part_captured = true;
+    } else if (plan.n_parts > 0) {
         const PrefillPlanEntry* last = c->pre_last;
         if (last && last->ev_recorded && last->ev_stream != st) {
             e = cudaStreamWaitEvent(st, last->ev, 0);
@@ -692,10 +702,12 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
         e = launch_blocks_combine(ca, g.D, st);
         if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
     }
-    e = cudaEventRecord(hit->ev, st);
-    if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
-    hit->ev_recorded = true;
-    hit->ev_stream = st;
+    if (!captured) {
+        e = cudaEventRecord(hit->ev, st);
+        if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
+        hit->ev_recorded = true;
+        hit->ev_stream = st;
+    }
     for (int32_t i = 0; i < n_seqs; ++i) c->host->seq_mut(seqs[i])->last_stream = stream;
     return SQ_OK;
 }

@@ -49,6 +49,7 @@ struct WriteTickets {
 
 struct PlanEntry {
     bool valid = false;
+    bool captured = false;  // see keep_captured
     int32_t n_ctas = 0;
     int32_t window = 0, n_sink = 0;  // window 0: all rows
     std::vector<int32_t> handles;
@@ -78,6 +79,7 @@ struct PlanEntry {
 constexpr int kPrefillPlanEntries = 4;
 struct PrefillPlanEntry {
     bool valid = false;
+    bool captured = false;  // see keep_captured
     int32_t seq = 0;
     uint64_t version = 0;
     int32_t n_q = 0;
@@ -118,12 +120,14 @@ struct TurnBuffer {
     cudaEvent_t ev = nullptr;   // recorded after the last work that used it
     bool ev_recorded = false;
     cudaStream_t ev_stream = nullptr;
+    bool captured = false;  // a captured launch was given it: kept until the end
 };
 
 // The places of a store's rows, kept for the same rows at the next layer.
 constexpr int kStorePlanEntries = 2;
 struct StorePlanEntry {
     bool valid = false;
+    bool captured = false;  // see keep_captured
     std::vector<int32_t> handles, counts;
     std::vector<uint64_t> versions;
     TurnBuffer buf;
@@ -186,11 +190,14 @@ struct sq_cache {
     // launch, and ordered after the ones before whatever becomes of the entry)
     // covers that use
     PrefillPlanEntry* pre_last = nullptr;
-    PlanEntry plans[kPlanCacheEntries];
-    PrefillPlanEntry pre_plans[kPrefillPlanEntries];
-    BlockPlanEntry block_plans[kBlockPlanEntries];
-    StorePlanEntry store_plans[kStorePlanEntries];
+    bool pre_part_captured = false;  // a captured launch was given pre_part
+    // (deques: an entry stays where it is when others are added)
+    std::deque<PlanEntry> plans = std::deque<PlanEntry>(kPlanCacheEntries);
+    std::deque<PrefillPlanEntry> pre_plans = std::deque<PrefillPlanEntry>(kPrefillPlanEntries);
+    std::deque<BlockPlanEntry> block_plans = std::deque<BlockPlanEntry>(kBlockPlanEntries);
+    std::deque<StorePlanEntry> store_plans = std::deque<StorePlanEntry>(kStorePlanEntries);
     TurnBuffer norm_part;  // partial gradients of the norms' weights
+    std::vector<void*> retired;  // outgrown buffers that captured launches were given
     uint64_t use_clock = 0;
     UploadSlot slots[kUploadSlots];
     int next_slot = 0;
@@ -350,6 +357,33 @@ bool capturing(cudaStream_t st) {
         return true;
     }
     return status != cudaStreamCaptureStatusNone;
+}
+
+// A captured launch reads its entry's plan whenever its graph runs: the entry stays
+// as it is for the cache's life, and another takes its turn among those that later
+// calls replace.  (Runs of graphs and other calls of the cache take turns by the
+// caller's order of them: no event of the cache covers a captured launch.)
+template <typename Entry>
+void keep_captured(std::deque<Entry>& all, Entry& e) {
+    if (e.captured) return;
+    all.emplace_back();
+    e.captured = true;
+}
+
+// The entry that a new plan replaces: the least recently used.
+template <typename Entry>
+Entry* entry_to_replace(std::deque<Entry>& all) {
+    Entry* victim = nullptr;
+    for (Entry& p : all)
+        if (!p.captured && (!victim || !p.valid || p.last_use < victim->last_use)) victim = &p;
+    return victim;
+}
+
+// Gives up a device buffer.
+void retire(sq_cache* c, void* d, bool captured) {
+    if (!d) return;
+    if (captured) c->retired.push_back(d);
+    else cudaFree(d);
 }
 
 // Stamps the pages a pool-writing launch just enqueued on `stream` writes.
@@ -521,7 +555,8 @@ int drop_plan(Entry& p, cudaStream_t st, int code) {
 int reserve_parts(sq_cache* c, size_t need) {
     if (need <= c->pre_part_cap) return SQ_OK;
     if (c->pre_last && c->pre_last->ev_recorded) cudaEventSynchronize(c->pre_last->ev);
-    if (c->pre_part) cudaFree(c->pre_part);
+    retire(c, c->pre_part, c->pre_part_captured);
+    c->pre_part_captured = false;
     c->pre_part = nullptr;
     c->pre_part_cap = 0;
     // (room for larger plans, up to the planner's limit)
@@ -710,6 +745,7 @@ int sq_cache_destroy(sq_cache* c) {
         if (p.buf.d) cudaFree(p.buf.d);
         if (p.buf.ev) cudaEventDestroy(p.buf.ev);
     }
+    for (void* d : c->retired) cudaFree(d);
     if (c->norm_part.d) cudaFree(c->norm_part.d);
     if (c->norm_part.ev) cudaEventDestroy(c->norm_part.ev);
     for (auto& s : c->slots) {
@@ -1044,6 +1080,9 @@ static int decode_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t 
     // anything this call enqueues: the kernel may read it before its
     // grid-dependency wait
     bool plan_ready = false;
+    // (windows) a graph takes a kept plan of its own stream, or none
+    const bool captured = window > 0 && capturing(st);
+    if (captured && (!hit || (hit->ev_recorded && hit->ev_stream != st))) return SQ_ERR_UNSUPPORTED;
     if (!hit) {
         DecodePlanHost plan;
         int rc = window > 0 ? plan_window_decode(*c->host, seqs, n_seqs, c->decode_ctas, window, n_sink, &plan)
@@ -1051,9 +1090,7 @@ static int decode_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t 
         if (rc != SQ_OK) return rc;
         DecodePlanLayout lay = plan_layout(plan, n_seqs, g.Hkv);
         // least recently used entry
-        PlanEntry* victim = &c->plans[0];
-        for (auto& p : c->plans)
-            if (!p.valid || p.last_use < victim->last_use) victim = &p;
+        PlanEntry* victim = entry_to_replace(c->plans);
         const size_t part_bytes = (size_t)decode_partial_bytes(lay.n_comb_ent, g.G(), g.D);
         if ((size_t)lay.total > victim->plan_cap || part_bytes > victim->part_cap) {
             if (victim->ev_recorded) cudaEventSynchronize(victim->ev);
@@ -1120,8 +1157,9 @@ static int decode_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t 
         e = cudaStreamWaitEvent(st, hit->ev, 0);
         if (e != cudaSuccess) return cuda_status(e);
     } else {
-        plan_ready = window == 0 || !capturing(st);  // (as in sq_prefill_attention)
+        plan_ready = !captured;  // (as in sq_prefill_attention)
     }
+    if (captured) keep_captured(c->plans, *hit);
     hit->last_use = ++c->use_clock;
     const DecodePlanLayout& L = hit->lay;
     float* part_o = hit->d_part;
@@ -1159,10 +1197,12 @@ static int decode_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t 
     a.err = c->d_err;
     e = launch_decode(c->tmap, a, L.n_ctas, g.D, st);
     if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
-    e = cudaEventRecord(hit->ev, st);
-    if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
-    hit->ev_recorded = true;
-    hit->ev_stream = st;
+    if (!captured) {
+        e = cudaEventRecord(hit->ev, st);
+        if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
+        hit->ev_recorded = true;
+        hit->ev_stream = st;
+    }
     for (int32_t i = 0; i < n_seqs; ++i) c->host->seq_mut(seqs[i])->last_stream = stream;
     c->stats.decode_calls += 1;
     c->stats.decode_logical_bytes += hit->logical_tokens * g.token_layer_bytes();
@@ -1324,6 +1364,7 @@ int sq_prefill_attention(sq_cache* c, sq_seq seq, int32_t layer, int32_t n_q, co
     // a reused plan that needs no cross-stream wait was on the device before
     // anything this call enqueues
     int32_t plan_ready = 0;
+    bool captured = false;
     for (auto& p : c->pre_plans)
         if (p.valid && p.seq == seq && p.version == s->version && p.n_q == n_q &&
             p.target == c->num_sms && p.spans == key) {
@@ -1367,9 +1408,7 @@ int sq_prefill_attention(sq_cache* c, sq_seq seq, int32_t layer, int32_t n_q, co
         const size_t o_pages = o_merges + plan.merges.size() * sizeof(PrefillMerge);
         const size_t bytes = o_pages + plan.tile_pages.size() * sizeof(int32_t);
         // least recently used entry
-        PrefillPlanEntry* victim = &c->pre_plans[0];
-        for (auto& p : c->pre_plans)
-            if (!p.valid || p.last_use < victim->last_use) victim = &p;
+        PrefillPlanEntry* victim = entry_to_replace(c->pre_plans);
         victim->valid = false;
         if (!victim->ev) {
             e = cudaEventCreateWithFlags(&victim->ev, cudaEventDisableTiming);
@@ -1431,14 +1470,15 @@ int sq_prefill_attention(sq_cache* c, sq_seq seq, int32_t layer, int32_t n_q, co
     } else {
         // (a captured launch may run after any work, also work that writes what
         // this one would read ahead of its dependency wait)
-        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-        e = cudaStreamIsCapturing(st, &capture);
-        if (e != cudaSuccess) return cuda_status(e);
-        plan_ready = capture == cudaStreamCaptureStatusNone;
+        captured = capturing(st);
+        if (captured) keep_captured(c->pre_plans, *hit);
+        plan_ready = !captured;
     }
     hit->last_use = ++c->use_clock;
     const PrefillPlanEntry& plan = *hit;
-    if (plan.n_parts > 0) {
+    if (plan.n_parts > 0 && captured) {
+        c->pre_part_captured = true;
+    } else if (plan.n_parts > 0) {
         // (reserved when the plan was made)
         const PrefillPlanEntry* last = c->pre_last;
         if (last && last->ev_recorded && last->ev_stream != st) {
@@ -1508,10 +1548,12 @@ int sq_prefill_attention(sq_cache* c, sq_seq seq, int32_t layer, int32_t n_q, co
         e = launch_prefill_combine(ca, g.D, st);
         if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
     }
-    e = cudaEventRecord(hit->ev, st);
-    if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
-    hit->ev_recorded = true;
-    hit->ev_stream = st;
+    if (!captured) {
+        e = cudaEventRecord(hit->ev, st);
+        if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
+        hit->ev_recorded = true;
+        hit->ev_stream = st;
+    }
     c->host->seq_mut(seq)->last_stream = stream;
     c->stats.prefill_calls += 1;
     c->stats.prefill_pairs += plan.visible_pairs;

@@ -10,6 +10,11 @@
 #define cudaMalloc plain_malloc
 #define cudaFree plain_free
 #define cudaMemcpyAsync plain_memcpy_async
+#define launch_blocks plain_launch_blocks
+#define launch_norm_rope plain_launch_norm_rope
+#define launch_norm_rope_grad plain_launch_norm_rope_grad
+#define launch_decode plain_launch_decode
+#define launch_prefill plain_launch_prefill
 extern "C" {
 cudaError_t plain_is_capturing(cudaStream_t, cudaStreamCaptureStatus*);
 cudaError_t plain_event_query(cudaEvent_t);
@@ -29,6 +34,11 @@ cudaError_t plain_memcpy_async(void*, const void*, size_t, cudaMemcpyKind, cudaS
 #undef cudaMalloc
 #undef cudaFree
 #undef cudaMemcpyAsync
+#undef launch_blocks
+#undef launch_norm_rope
+#undef launch_norm_rope_grad
+#undef launch_decode
+#undef launch_prefill
 
 #include <set>
 
@@ -40,16 +50,55 @@ std::set<void*> g_freed;
 cudaError_t wrong() { return ++g_wrong, cudaErrorStreamCaptureUnsupported; }
 }  // namespace
 
-EXPORT void fake_capture(void* stream) { g_capturing = stream; }  // null: the capture ends
+EXPORT void fake_capture(void* stream) {  // null: the capture ends
+    g_capturing = stream;
+    g_freed.clear();
+}
 EXPORT int64_t fake_wrong() { return g_wrong; }
 EXPORT int64_t fake_captured_uploads() { return g_uploads; }
-EXPORT int fake_was_freed(void* p) { return (int)g_freed.count(p); }
+EXPORT int fake_was_freed(void* p) { return (int)g_freed.count(p); }  // since the capture
 EXPORT void fake_capture_reset() {
     g_capturing = nullptr;
     g_wrong = g_uploads = 0;
     g_captured.clear();
     g_freed.clear();
 }
+
+// The buffers that the last launch of a kind was given.
+static const void *g_plan, *g_parts, *g_places, *g_grad_part;
+EXPORT void fake_given(const void** out) {
+    out[0] = g_plan;
+    out[1] = g_parts;
+    out[2] = g_places;
+    out[3] = g_grad_part;
+}
+namespace sq {
+cudaError_t launch_blocks(const CUtensorMap& m, const CUtensorMap& q, const BlockShortArgs& a, int D, bool one,
+                          cudaStream_t st) {
+    g_plan = a.tiles;
+    g_parts = a.part_o;
+    return plain_launch_blocks(m, q, a, D, one, st);
+}
+cudaError_t launch_norm_rope(const NormRopeArgs& a, int D, bool store, cudaStream_t st) {
+    g_places = a.places;
+    return plain_launch_norm_rope(a, D, store, st);
+}
+cudaError_t launch_norm_rope_grad(const NormRopeGradArgs& a, int D, cudaStream_t st) {
+    g_grad_part = a.part;
+    return plain_launch_norm_rope_grad(a, D, st);
+}
+cudaError_t launch_decode(const CUtensorMap& m, const DecodeArgs& a, int n, int D, cudaStream_t st) {
+    g_plan = a.segs;
+    g_parts = a.part_o;
+    return plain_launch_decode(m, a, n, D, st);
+}
+cudaError_t launch_prefill(const CUtensorMap& m, const CUtensorMap& q, const PrefillShortArgs& a, int D,
+                           cudaStream_t st) {
+    g_plan = a.tiles;
+    g_parts = a.part_o;
+    return plain_launch_prefill(m, q, a, D, st);
+}
+}  // namespace sq
 
 extern "C" {
 
@@ -77,9 +126,7 @@ cudaError_t cudaStreamWaitEvent(cudaStream_t st, cudaEvent_t e, unsigned f) {
 }
 cudaError_t cudaMalloc(void** p, size_t n) {
     if (g_capturing) return wrong();
-    const cudaError_t e = plain_malloc(p, n);
-    if (e == cudaSuccess) g_freed.erase(*p);
-    return e;
+    return plain_malloc(p, n);
 }
 cudaError_t cudaFree(void* p) {
     if (g_capturing) return wrong();
