@@ -50,9 +50,12 @@ std::set<void*> g_freed;
 cudaError_t wrong() { return ++g_wrong, cudaErrorStreamCaptureUnsupported; }
 }  // namespace
 
+// The buffers that the last launch of a kind was given (since a capture began).
+static const void *g_plan, *g_parts, *g_places, *g_grad_part;
 EXPORT void fake_capture(void* stream) {  // null: the capture ends
     g_capturing = stream;
     g_freed.clear();
+    if (stream) g_plan = g_parts = g_places = g_grad_part = nullptr;
 }
 EXPORT int64_t fake_wrong() { return g_wrong; }
 EXPORT int64_t fake_captured_uploads() { return g_uploads; }
@@ -64,8 +67,6 @@ EXPORT void fake_capture_reset() {
     g_freed.clear();
 }
 
-// The buffers that the last launch of a kind was given.
-static const void *g_plan, *g_parts, *g_places, *g_grad_part;
 EXPORT void fake_given(const void** out) {
     out[0] = g_plan;
     out[1] = g_parts;
