@@ -415,7 +415,8 @@ SQ_API int sq_extend(sq_cache *cache, const sq_seq *seqs, int32_t n_seqs, const 
  *            row is written as if at position 0)
  *   q_out:   device bf16 [rows][num_q_heads][head_dim], 16-byte aligned, as the
  *            attention calls take it; overlaps none of q, k, v (INVALID_ARG)
- * Sums are fp32; outputs are rounded once, to nearest even.  Rows in a page that
+ * Sums are fp32 (squares too: elements up to 1e18 in size, down to 1e-18 where eps is
+ * 0); outputs are rounded once, to nearest even.  Rows in a page that
  * another sequence holds too are INVALID_ARG (its rows would change with them).
  * Errors: BAD_HANDLE, INVALID_ARG, UNSUPPORTED, NO_MEMORY, CUDA. */
 SQ_API int sq_qk_norm_rope_store(sq_cache *cache, const sq_seq *seqs, int32_t n_seqs,

@@ -102,6 +102,9 @@ struct Lane {
         f = !kPairs && on ? 4 * l : 8 * l;
         g = !kPairs && on ? rot / 2 + 4 * l : 8 * l + 4;
     }
+    // the part of a pair's other: none where the elements do not turn (a sine of 0
+    // times an infinity is NaN)
+    __device__ __forceinline__ f32x2 turned(f32x2 v) const { return on ? v : 0; }
 };
 
 // Eight values of a lane as pairs: f's, then g's.
@@ -205,10 +208,11 @@ struct Tasks {
     }
 };
 
-// What is left to gain is the memory's: with 28 warps an SM (72 registers a thread)
-// 12,982 tokens of 32 query and 8 key heads of 128, stored, take 56.7 us, 5.7 TB/s
-// (24 warps 60, 32 warps, with spills, 57.5; a warp that takes a token's tasks in
-// turn, the next one's rows loaded ahead, in 16 warps 64).
+// What is left to gain is the memory's: with 28 warps an SM (72 registers a thread, 12
+// to 52 bytes of them spilled) 12,982 tokens of 32 query and 8 key heads of 128,
+// stored, take 57.3 us, 5.6 TB/s (24 warps 60, 32 warps, with more spills, 57.5 where
+// these took 56.7; a warp that takes a token's tasks in turn, the next one's rows
+// loaded ahead, in 16 warps 64).
 template <int D, bool kStore, bool kPairs, typename Args>
 __global__ void __launch_bounds__(kNormThreads, 7)
     sq_norm_rope_kernel(const __grid_constant__ Args a) {
@@ -305,7 +309,7 @@ __global__ void __launch_bounds__(kNormThreads, 7)
         uint32_t o[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            o[i] = pack2(mul2(fma2(x.v[i], A[i], mul2(x.other<kPairs>(i), B[i])), rr));
+            o[i] = pack2(mul2(fma2(x.v[i], A[i], ln.turned(mul2(x.other<kPairs>(i), B[i]))), rr));
         if (h + u * C::kGroups < heads && dst) {
             __nv_bfloat16* to = dst + u * C::kGroups * step;
             *reinterpret_cast<uint2*>(to + ln.f) = make_uint2(o[0], o[1]);
@@ -317,9 +321,9 @@ __global__ void __launch_bounds__(kNormThreads, 7)
 // Backwards.  A CTA's warps take tasks (query or key heads of a token) in turn and
 // add up the weights' gradients of their lanes' elements; the CTA's sums go to one
 // partial row, added by a second kernel in a fixed order.  8,192 tokens of 64 query
-// and 8 key heads of 128: 84 us, 5.4 TB/s; two rows of a lane group in flight 103,
-// eight 105, a position read a task ahead 86, the next task's rows copied into shared
-// memory ahead 85.
+// and 8 key heads of 128: 85 us, 5.3 TB/s (before the elements that do not turn were
+// kept apart 84; then two rows of a lane group in flight 103, eight 105, a position
+// read a task ahead 86, the next task's rows copied into shared memory ahead 85).
 template <int D, bool kPairs>
 __global__ void __launch_bounds__(kGradThreads)
     sq_norm_rope_grad_kernel(const __grid_constant__ NormRopeGradArgs a) {
@@ -383,7 +387,7 @@ __global__ void __launch_bounds__(kGradThreads)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 // dy: dz turned back
-                const f32x2 dy = fma2(z.v[i], tn.c[i], mul2(mul2(z.other<kPairs>(i), tn.s[i]), back));
+                const f32x2 dy = fma2(z.v[i], tn.c[i], ln.turned(mul2(mul2(z.other<kPairs>(i), tn.s[i]), back)));
                 x.v[i] = mul2(x.v[i], rr);
                 if (is_k) gk[i] = fma2(dy, x.v[i], gk[i]);
                 else gq[i] = fma2(dy, x.v[i], gq[i]);
