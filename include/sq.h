@@ -474,7 +474,8 @@ SQ_API int sq_qk_norm_rope_backward(sq_cache *cache, int32_t n_tokens, const voi
  * key or value that it sees, is NaN in its output.  Values may have any finite
  * size: a query whose weighted sums pass 32 bits on the way (values of 1e26 and
  * more, weights being relative to 1) is taken once more too.
- * Single tokens without lse run as sq_decode_attention does.
+ * Single tokens without lse run as sq_decode_attention does (values up to 3e38
+ * over the number of keys seen).
  * Weights and normaliser are rounded as in sq_prefill_attention, whose limits on
  * library memory for partial results hold too.  A plan of more than 2^24 key
  * tiles (all queries of the call together) is refused.

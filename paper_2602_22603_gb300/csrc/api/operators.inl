@@ -36,7 +36,7 @@ int check_handles(sq_cache* c, const sq_seq* seqs, int32_t n_seqs) {
 }
 
 // The newest rows of each sequence that a call is about (counts NULL: one each):
-// between 0 and the sequence's rows, `least` at least.  *total = their number.
+// between 0 and the sequence's rows.  *total = their number.
 int check_counts(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* counts, int64_t* total) {
     *total = 0;
     for (int32_t i = 0; i < n_seqs; ++i) {

@@ -24,7 +24,7 @@ struct BlockPlanHost {
                                        // window; empty: low0 + i, pos0 + i of the items
     std::vector<uint32_t> bits;        // [queries][n_words], drafted trees only
     int32_t n_words = 0, n_pieces = 0, BP = 0, n_parts = 0, max_splits = 0;
-    int32_t n_queries = 0, n_ctas = 0;
+    int32_t n_ctas = 0;
     int32_t unit_rows = 0;             // rows of a tile pair that can hold queries
     bool one = true;                   // every item's queries fit in one query tile
 };
@@ -239,7 +239,6 @@ inline int plan_blocks(const Geometry& g, const std::vector<BlockSeq>& seqs, int
         if (q.n_q > 0) table |= q.parents || has_partial_pages(*q.s, P);
     }
     if (queries > 0x7fffffff / std::max(1, g.Hq)) return kCapacity;
-    out->n_queries = (int32_t)queries;
     if (table) out->rows.resize(2 * (size_t)queries);
     // words of a drafted row's bitmap: the tree may begin anywhere in its first
     for (const BlockSeq& q : seqs)

@@ -218,9 +218,9 @@ struct DecodePlanHost {
     std::vector<DecodeItem> items;
     std::vector<int32_t> cta_begin;   // n_ctas + 1
     std::vector<int32_t> page_ids;
-    // rows held by each page of page_ids (for windows see kFillFirstBit); filled only for windows and when some sequence of the call has a
-    // partial page before its last (else every page is full up to the members'
-    // limits)
+    // rows held by each page of page_ids (for windows see kFillFirstBit); filled
+    // only for windows and when some sequence of the call has a partial page before
+    // its last (else every page is full up to the members' limits)
     std::vector<int32_t> page_fill;
     // partial entries of (sequence i, KV head h): [comb_off[k], comb_off[k + 1]),
     // k = i * Hkv + h, in item order

@@ -186,8 +186,6 @@ struct BlockMerge {
     int32_t g, part0, n, q_row;
     int32_t n_q, pad[3];
 };
-// Drafted rows of one sequence at most, and the words of a row's bitmap then.
-constexpr int32_t kMaxDraft = 256;
 // Key tiles a plan may have.
 constexpr int64_t kMaxBlockTiles = int64_t(1) << 24;
 

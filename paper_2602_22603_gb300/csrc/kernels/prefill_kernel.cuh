@@ -1604,9 +1604,9 @@ constexpr uint32_t kParPV = 8;  // (three S buffers) items of three key tiles or
 // tile's first PV waits for: tile a's, or in dual-key mode the tile's own, warp wq of
 // the four the rows of word wq of the visibility.  V of the item's key tile j (its
 // loads begin with number ub) is waited for; its load needs no P of this tile or of
-// the one before.  (Rows past the end the producer has zeroed.)  In every instance this would cost 32,768 queries, 40% masked, 3.25 ->
-// 3.30 ms by the code generated around it, and by a warp of its own that takes V over
-// from the loads 3.43 ms.
+// the one before.  (Rows past the end the producer has zeroed.)  In every instance
+// this would cost 32,768 queries, 40% masked, 3.25 -> 3.30 ms by the code generated
+// around it, and by a warp of its own that takes V over from the loads 3.43 ms.
 template <int D, int M>
 __device__ __forceinline__ bool zero_hidden_values(const Smem& sm, const PrefillTile* tile, int n, uint32_t ub,
                                                    int j, int T, bool dual, int wq, volatile int* abort_flag,
@@ -1710,8 +1710,9 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
     // maxima the window's raise: there a row starts at a maximum of 0 and a tile's
     // weights are accepted while its sum stays below 2^40 (and above 2^-40 where
     // they are the row's first), since a weight rounded to bf16 keeps its 8 bits at
-    // any size and sums are fp32.  16,384 queries at a window of 1,024 with 4 sinks,
-    // logits to 2^20: 430 -> 262 us a layer, half of it the maxima of first tiles.
+    // any size and sums are fp32 (those that overflow: rows_again).  16,384 queries at
+    // a window of 1,024 with 4 sinks: 367 -> 254 us, half of it the maxima of first
+    // tiles.
     constexpr float kLeast = 0x1p-40f;
     const float accept = of_blocks<M> ? 0x1p40f : __all_sync(0xffffffffu, valid) ? 65536.f : 256.f;
     float m_run = of_blocks<M> ? 0.f : -INFINITY, l = 0.f;
