@@ -35,8 +35,11 @@ def check(b, h, m, spans=(), sample=16):
     q = b.queries(m)
     out = torch.full(q.shape, float("inf"), device="cuda")
     lse = torch.full(q.shape[:2], float("inf"), device="cuda")
-    b.c.prefill_attention(h, 0, m, q, out, sq.SQ_OUT_F32, lse, b.D ** -0.5, list(spans))
-    assert b.c.sync_status() == sq.SQ_OK
+    for again in range(3):     # (a kept plan is read, and keys are loaded, ahead of the launch's wait)
+        first = out.clone()
+        b.c.prefill_attention(h, 0, m, q, out, sq.SQ_OUT_F32, lse, b.D ** -0.5, list(spans))
+        assert b.c.sync_status() == sq.SQ_OK
+        assert not again or torch.equal(out, first)
     k, v = b.rows(h)
     n, G = k.shape[0], b.Hq // b.Hkv
     shown = torch.ones(n, dtype=torch.bool, device="cuda")
