@@ -513,6 +513,64 @@ SQ_API int sq_tree_attention(sq_cache *cache, const sq_seq *seqs, int32_t n_seqs
 SQ_API int sq_accept_draft(sq_cache *cache, sq_seq seq, int32_t n_draft, const int32_t *path,
                            int32_t n_path, void *stream);
 
+/* ---- rows held in 8 bits ----
+ *
+ * A cache of twice the tokens: every row of keys and of values is held as e4m3 codes
+ * (sign, 4 exponent bits, 3 of the fraction; largest value 448), with one fp32 scale
+ * for each block: SQ_SCALE_ROWS consecutive slots of one page, plane and KV head.  An
+ * element's value is its code times its block's scale.  The scale is a power of two,
+ * the least one from 2^-100 on with which the largest finite element of the block's
+ * rows, before it is rounded, is at most 448; codes are rounded once, to nearest even.  A value then has 4
+ * significant bits down to 2^-13 of its block's largest, and steps of 2^-16 of it
+ * (or finer) below.  A block's rows may be taken from one scale to another (when a
+ * larger row joins them, or rows of several blocks are packed into one): that changes
+ * only values in those last steps.  An element that is an infinity or NaN is held as
+ * NaN, and counts for no scale; finite ones above 240 * 2^120 are held as that.
+ *
+ * Pool: codes [num_layers][num_pages][2][num_kv_heads][page_size][head_dim], a byte
+ * each, then scales [num_layers][num_pages][2][num_kv_heads][page_size / SQ_SCALE_ROWS]:
+ * sq_pool_bytes_8bit() bytes.
+ *
+ * The calls above take such a cache as any other, but for sq_prefill_attention
+ * (UNSUPPORTED: sq_window_attention with window 0 is plain causal attention of a
+ * prompt).  sq_append_kv, sq_append_kv_batch and sq_qk_norm_rope_store round what
+ * they are given (the latter after the norm and the rotation); the rows that a block
+ * holds before a stored one count in its scale, so rows are stored in the order in
+ * which they were added, or together.  Blocks with a row that was added (sq_extend) and
+ * never stored have no values to rely on.  Pages are shared and copied on write with
+ * their scales.  sq_evict_spans and sq_evict_spans_ragged pack codes, a block's scale
+ * made anew.  A caller that writes rows itself writes scales of the form above.
+ * A store of more than 200 blocks (or sq_append_kv of as many, and sq_read_kv of as
+ * many runs of rows in one page) is uploaded and may be captured as a store of more
+ * than 240 rows may (appends and sq_read_kv of that many may not: UNSUPPORTED).
+ *
+ * Attention takes the values as they are: logits are fp32 sums of exact products of the
+ * bf16 queries (elements below 2^-32 of their row's largest lose digits) and the
+ * values; single tokens round their softmax weights to 11 bits, and values of blocks
+ * smaller than the largest one seen by 2^10 and more count with an error of up to
+ * 2^-38 of that.  For query blocks (sq_window_attention of more than one token, and
+ * sq_tree_attention) the cache widens the pages that the call reads to bf16, exactly,
+ * into library memory (twice their bytes, kept with the cache), and the rest is as for
+ * bf16 rows; captured calls need an earlier one of as many pages. */
+#define SQ_SCALE_ROWS 8
+
+/* Bytes of the pool of an 8-bit cache (0 if the configuration is invalid). */
+SQ_API size_t sq_pool_bytes_8bit(const sq_config *cfg);
+
+/* sq_cache_create for a cache whose rows are held in 8 bits (cfg->kv_pool, if given,
+ * is of sq_pool_bytes_8bit() bytes).  Errors: INVALID_ARG, UNSUPPORTED, NO_MEMORY, CUDA. */
+SQ_API int sq_cache_create_8bit(const sq_config *cfg, sq_cache **out);
+
+/* The newest counts[i] rows (NULL: one) of each sequence at one layer, as bf16 (exact
+ * for 8-bit rows), one sequence after the other: what a consumer outside the cache
+ * takes.  For caches of either kind.
+ *   seqs: host, distinct live handles; counts: host, 0 .. the sequence's rows
+ *   k, v: device bf16 [rows][num_kv_heads][head_dim], 16-byte aligned, outside the
+ *         pool and not overlapping (INVALID_ARG)
+ * Errors: BAD_HANDLE, INVALID_ARG, UNSUPPORTED, NO_MEMORY, CUDA. */
+SQ_API int sq_read_kv(sq_cache *cache, const sq_seq *seqs, int32_t n_seqs, const int32_t *counts,
+                      int32_t layer, void *k, void *v, void *stream);
+
 /* Measurement helper: streams `bytes` (a multiple of 16, 16-byte aligned)
  * of device memory at `buf` once with plain loads and no writes, so that the
  * caller can time the read-only HBM bandwidth of this GPU next to the

@@ -35,6 +35,7 @@ SQ_OUT_BF16 = 0
 SQ_OUT_F32 = 1
 SQ_DEBUG_DROP_DECODE_STAGE = 1
 SQ_MAX_DRAFT = 256
+SQ_SCALE_ROWS = 8
 
 
 class sq_config(ctypes.Structure):
@@ -133,6 +134,9 @@ _SIGS = {
     "sq_tree_attention": (ctypes.c_int, [_P, _P, _I32, _P, _P, _I32, _P, _P, _I32, _P, _F32, _I32,
                                          _I32, _P]),
     "sq_accept_draft": (ctypes.c_int, [_P, _I32, _I32, _P, _I32, _P]),
+    "sq_pool_bytes_8bit": (ctypes.c_size_t, [ctypes.POINTER(sq_config)]),
+    "sq_cache_create_8bit": (ctypes.c_int, [ctypes.POINTER(sq_config), ctypes.POINTER(_P)]),
+    "sq_read_kv": (ctypes.c_int, [_P, _P, _I32, _P, _I32, _P, _P, _P]),
 }
 
 
@@ -333,6 +337,17 @@ def sq_cache_create(cfg: sq_config) -> int:
     return out.value
 
 
+def sq_pool_bytes_8bit(cfg: sq_config) -> int:
+    return int(lib().sq_pool_bytes_8bit(ctypes.byref(cfg)))
+
+
+def sq_cache_create_8bit(cfg: sq_config) -> int:
+    """sq_cache_create for rows held in 8 bits."""
+    out = _P()
+    _check(lib().sq_cache_create_8bit(ctypes.byref(cfg), ctypes.byref(out)), "sq_cache_create_8bit")
+    return out.value
+
+
 def sq_cache_destroy(cache: int) -> None:
     _check(lib().sq_cache_destroy(cache), "sq_cache_destroy")
 
@@ -464,6 +479,13 @@ def sq_accept_draft(cache: int, seq: int, n_draft: int, path, stream=None) -> No
            "sq_accept_draft")
 
 
+def sq_read_kv(cache: int, seqs, counts, layer: int, k, v, stream=None) -> None:
+    arr, _keep = _ints(seqs)
+    cnt, _keep2 = _ints(counts)
+    _check(lib().sq_read_kv(cache, arr, len(seqs), cnt, layer, _ptr(k), _ptr(v), _stream(stream)),
+           "sq_read_kv")
+
+
 def sq_release(cache: int, seq: int, stream=None) -> None:
     _check(lib().sq_release(cache, seq, _stream(stream)), "sq_release")
 
@@ -537,14 +559,20 @@ def sq_sync_status(cache: int, stream=None) -> int:
 
 # ---- a small object wrapper --------------------------------------------------
 class Cache:
-    """Owns one sq_cache.  Methods are the C calls with the cache bound."""
+    """Owns one sq_cache.  Methods are the C calls with the cache bound.  bits: 16
+    (bf16 rows), or 8 (e4m3 rows, a scale for every SQ_SCALE_ROWS slots of a page and
+    head)."""
 
     def __init__(self, num_layers, num_q_heads, num_kv_heads, head_dim, page_size, num_pages,
-                 max_seqs=64, max_pages_per_seq=None, kv_pool=None, decode_ctas=0):
+                 max_seqs=64, max_pages_per_seq=None, kv_pool=None, decode_ctas=0, bits=16):
+        self.handle = None
+        if bits not in (8, 16):
+            raise ValueError(f"bits: 8 or 16 expected, not {bits}")
         self.cfg = make_config(num_layers, num_q_heads, num_kv_heads, head_dim, page_size,
                                num_pages, max_seqs, max_pages_per_seq, kv_pool, decode_ctas)
         self._keep = kv_pool
-        self.handle = sq_cache_create(self.cfg)
+        self.bits = bits
+        self.handle = (sq_cache_create_8bit if bits == 8 else sq_cache_create)(self.cfg)
         self.L, self.Hq, self.Hkv = num_layers, num_q_heads, num_kv_heads
         self.D, self.P, self.num_pages = head_dim, page_size, num_pages
 
@@ -559,20 +587,35 @@ class Cache:
         except Exception:
             pass
 
-    def pool_view(self):
-        """The pool as a torch bf16 tensor [L, num_pages, 2, Hkv, P, D]
-        (a zero-copy view of library memory)."""
+    def _view(self, address, shape, typestr, dtype):
+        """A zero-copy view of library memory as a torch tensor."""
         import torch
 
         class _Arr:
             pass
 
         a = _Arr()
-        shape = (self.L, self.num_pages, 2, self.Hkv, self.P, self.D)
-        a.__cuda_array_interface__ = {
-            "shape": shape, "typestr": "<i2", "data": (sq_pool_ptr(self.handle), False),
-            "version": 3, "strides": None}
-        return torch.as_tensor(a, device="cuda").view(torch.bfloat16)
+        a.__cuda_array_interface__ = {"shape": shape, "typestr": typestr, "data": (address, False),
+                                      "version": 3, "strides": None}
+        return torch.as_tensor(a, device="cuda").view(dtype)
+
+    def pool_view(self):
+        """The pool as a torch tensor [L, num_pages, 2, Hkv, P, D] (a zero-copy view of
+        library memory): bf16, or the codes as float8_e4m3fn."""
+        import torch
+        wide = self.bits == 16
+        return self._view(sq_pool_ptr(self.handle), (self.L, self.num_pages, 2, self.Hkv, self.P, self.D),
+                          "<i2" if wide else "|u1", torch.bfloat16 if wide else torch.float8_e4m3fn)
+
+    def scale_view(self):
+        """The scales of an 8-bit cache, float32 [L, num_pages, 2, Hkv, P / SQ_SCALE_ROWS]
+        (a zero-copy view)."""
+        import torch
+        if self.bits != 8:
+            raise ValueError("scale_view: rows are not held in 8 bits")
+        shape = (self.L, self.num_pages, 2, self.Hkv, self.P // SQ_SCALE_ROWS)
+        codes = self.L * self.num_pages * 2 * self.Hkv * self.P * self.D
+        return self._view(sq_pool_ptr(self.handle) + codes, shape, "<f4", torch.float32)
 
     seq_new = lambda self: sq_seq_new(self.handle)
     append_kv = lambda self, seq, n, k, v, stream=None: sq_append_kv(self.handle, seq, n, k, v, stream)
@@ -676,6 +719,15 @@ class Cache:
             raise ValueError(f"tree_attention: {len(parents)} parents of {n} drafted tokens")
         sq_tree_attention(self.handle, seqs, n_draft, parents, layer, q, out, window, n_sink, out_dtype,
                           lse, sm_scale, stream)
+
+    def read_kv(self, seqs, counts, layer, k, v, stream=None):
+        """The newest counts[i] rows (None: one) of each sequence as bfloat16
+        [rows, Hkv, D]."""
+        if _BF16 is None:
+            _types()
+        size = self._counted(seqs, counts, None, "read_kv") * self.Hkv * self.D
+        sq_read_kv(self.handle, seqs, counts, layer, _flat(k, _BF16, size, "k"), _flat(v, _BF16, size, "v"),
+                   stream)
 
     accept_draft = (lambda self, seq, n_draft, path, stream=None:
                     sq_accept_draft(self.handle, seq, n_draft, path, stream))

@@ -26,6 +26,7 @@ LIBSQ_SOURCES = [
     "kernels/blocks.cu",
     "kernels/decode.cu",
     "kernels/kv.cu",
+    "kernels/kv8.cu",
     "kernels/noalloc_scratch.cu",
     "kernels/norm_rope.cu",
     "kernels/prefill.cu",

@@ -173,7 +173,10 @@ void note_store(sq_cache* c, std::vector<int32_t>&& pages, void* stream) {
     c->store_ticket = c->write_seq;
 }
 
-int extend_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new, void* stream) {
+// `then` is enqueued after the copies, with the rows counted; where it fails they are
+// taken back.
+template <typename Then>
+int extend_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new, void* stream, Then then) {
     int rc = check_handles(c, seqs, n_seqs);
     if (rc != SQ_OK) return rc;
     int64_t total = 0;
@@ -241,10 +244,24 @@ int extend_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
     for (size_t b = 0; b < copies.size() || a.lens.n > 0; b += kAppendBatchMax) {
         a.n_cow = b < copies.size() ? (int32_t)std::min<size_t>(kAppendBatchMax, copies.size() - b) : 0;
         std::copy_n(copies.begin() + std::min(b, copies.size()), a.n_cow, a.cow);
-        const cudaError_t e = launch_append_batch(a, st);
+        cudaError_t e;
+        if (c->kv8) {
+            Kv8CopyArgs ca;
+            ca.pool = kv8_pool(c);
+            ca.L = g.L;
+            ca.lens = a.lens;
+            ca.n_cow = a.n_cow;
+            std::copy_n(a.cow, a.n_cow, ca.cow);
+            ca.err = c->d_err;
+            e = launch_kv8_copy(ca, g.D, st);
+        } else {
+            e = launch_append_batch(a, st);
+        }
         if (e != cudaSuccess) return cuda_status(e);
         a.lens.n = 0;
     }
+    rc = then();
+    if (rc != SQ_OK) return rc;
     undo.planned = 0;
     note_writes(c, copied.data(), copied.size(), stream);
     for (int32_t i = 0; i < n_seqs; ++i) {
@@ -284,11 +301,38 @@ void list_places(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t*
     }
 }
 
+// The newest n_new[i] rows of each sequence as runs of consecutive slots, none over a
+// border of `most` slots (a power of two, at most a page), and their pages.
+void list_runs(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new, int32_t most,
+               std::vector<RowRun>* runs, std::vector<int32_t>* pages) {
+    const int32_t P = c->g.P;
+    int32_t first = 0;
+    for (int32_t i = 0; i < n_seqs; ++i) {
+        const Seq* s = c->host->seq(seqs[i]);
+        const int32_t m = n_new ? n_new[i] : 1;
+        int32_t left = m;
+        for (size_t p = s->pages.size(); left > 0; --p) {
+            int32_t end = s->fill[p - 1];
+            const int32_t low = std::max(0, end - left);
+            if (pages) pages->push_back(s->pages[p - 1]);
+            while (runs && end > low) {
+                const int32_t from = std::max(low, (end - 1) & ~(most - 1));
+                const int32_t at = left - (s->fill[p - 1] - from);  // of the sequence's, counted from its first
+                runs->push_back({s->pages[p - 1] * P + from, first + at, end - from,
+                                 (int32_t)std::min<int64_t>(s->next_pos - m + at, 0x7fffffff)});
+                end = from;
+            }
+            left -= std::min(left, s->fill[p - 1]);
+        }
+        first += m;
+    }
+}
+
 int store_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new, int32_t layer,
                const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                int64_t v_stride, const int32_t* positions, const sq_norm_rope* params, void* q_out,
                void* stream) {
-    if (!launch_norm_rope) return SQ_ERR_UNSUPPORTED;
+    if (!(c->kv8 ? (void*)launch_kv8_store : (void*)launch_norm_rope)) return SQ_ERR_UNSUPPORTED;
     const Geometry& g = c->g;
     int64_t n = 0;
     int rc = check_handles(c, seqs, n_seqs);
@@ -305,9 +349,14 @@ int store_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n
                      {v, rows_bytes(n, kw, v_stride)}},
                     {{q_out, rows_bytes(n, qw, qw)}, {c->pool, c->pool_bytes}}))
         return SQ_ERR_INVALID_ARG;
-    // where each row goes; more places than go with the launch stay on the device
-    // for the next layer's store
-    const bool upload_places = n > kNormInline, captured = upload_places && capturing(as_stream(stream));
+    // where each row goes (8-bit caches: each block's rows); more places than go with
+    // the launch stay on the device for the next layer's store
+    std::vector<RowPlace> places;
+    std::vector<RowRun> runs;
+    std::vector<int32_t> pages;
+    if (c->kv8) list_runs(c, seqs, n_seqs, n_new, kScaleRows, &runs, &pages);
+    const bool upload_places = c->kv8 ? runs.size() > (size_t)kRunsInline : n > kNormInline;
+    const bool captured = upload_places && capturing(as_stream(stream));
     StorePlanEntry* hit = nullptr;
     for (auto& p : c->store_plans) {
         if (!upload_places || !p.valid || (int32_t)p.handles.size() != n_seqs) continue;
@@ -317,33 +366,58 @@ int store_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n
                    p.counts[i] == (n_new ? n_new[i] : 1);
         if (same) hit = &p;
     }
-    std::vector<RowPlace> places;
-    std::vector<int32_t> pages;
-    list_places(c, seqs, n_seqs, n_new, n, hit ? nullptr : &places, &pages);
+    if (!c->kv8) list_places(c, seqs, n_seqs, n_new, n, hit ? nullptr : &places, &pages);
     for (int32_t p : pages)
         if (c->host->alloc().refcount(p) > 1) return SQ_ERR_INVALID_ARG;
     cudaStream_t st = as_stream(stream);
-    NormRopeInlineArgs a;
-    a.q = bf16(q);
-    a.k = bf16(k);
-    a.v = bf16(v);
-    a.q_stride = q_stride;
-    a.k_stride = k_stride;
-    a.v_stride = v_stride;
-    a.positions = positions;
-    a.places = nullptr;
-    a.q_out = bf16(q_out);
-    a.k_out = nullptr;
-    a.pool = c->pool;
-    a.num_pages = g.num_pages;
-    a.n = (int32_t)n;
-    a.P = g.P;
-    a.layer = layer;
-    fill_params(c, params, &a);
+    auto launch = [&](const uint8_t* uploaded) {
+        if (c->kv8) {
+            Kv8StoreInlineArgs a;
+            a.q = bf16(q);
+            a.k = bf16(k);
+            a.v = bf16(v);
+            a.q_stride = q_stride;
+            a.k_stride = k_stride;
+            a.v_stride = v_stride;
+            a.layer_stride = 0;
+            a.positions = positions;
+            a.runs = reinterpret_cast<const RowRun*>(uploaded);
+            a.q_out = bf16(q_out);
+            a.pool = kv8_pool(c);
+            a.n_runs = (int32_t)runs.size();
+            a.most = 0;
+            for (const RowRun& r : runs) a.most = std::max(a.most, r.n);
+            a.layer = layer;
+            a.n_layers = 1;
+            a.plain = 0;
+            fill_params(c, params, &a);
+            if (!uploaded) std::copy(runs.begin(), runs.end(), a.inline_run);
+            return launch_kv8_store(a, g.D, st);
+        }
+        NormRopeInlineArgs a;
+        a.q = bf16(q);
+        a.k = bf16(k);
+        a.v = bf16(v);
+        a.q_stride = q_stride;
+        a.k_stride = k_stride;
+        a.v_stride = v_stride;
+        a.positions = positions;
+        a.places = reinterpret_cast<const RowPlace*>(uploaded);
+        a.q_out = bf16(q_out);
+        a.k_out = nullptr;
+        a.pool = c->pool;
+        a.num_pages = g.num_pages;
+        a.n = (int32_t)n;
+        a.P = g.P;
+        a.layer = layer;
+        fill_params(c, params, &a);
+        if (uploaded) return launch_norm_rope(a, g.D, true, st);
+        std::copy(places.begin(), places.end(), a.inline_place);
+        return launch_norm_rope_inline(a, g.D, st);
+    };
     cudaError_t e;
     if (!upload_places) {
-        std::copy(places.begin(), places.end(), a.inline_place);
-        e = launch_norm_rope_inline(a, g.D, st);
+        e = launch(nullptr);
         if (e != cudaSuccess) return cuda_status(e);
     } else {
         const bool fresh = !hit;
@@ -354,15 +428,13 @@ int store_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n
             hit = entry_to_replace(c->store_plans);
             hit->valid = false;
         }
-        const size_t bytes = (size_t)n * sizeof(RowPlace);
+        const size_t bytes = c->kv8 ? runs.size() * sizeof(RowRun) : (size_t)n * sizeof(RowPlace);
         rc = take_buffer(c, hit->buf, bytes, st, captured);
         if (rc != SQ_OK) return rc;
-        if (fresh) rc = staged_copy(c, hit->buf.d, places.data(), bytes, stream);
+        if (fresh)
+            rc = staged_copy(c, hit->buf.d, c->kv8 ? (const void*)runs.data() : places.data(), bytes, stream);
         e = cudaSuccess;
-        if (rc == SQ_OK) {
-            a.places = reinterpret_cast<const RowPlace*>(hit->buf.d);
-            e = launch_norm_rope(a, g.D, true, st);
-        }
+        if (rc == SQ_OK) e = launch(hit->buf.d);
         const int used = used_buffer(hit->buf, st, captured);
         if (rc != SQ_OK || e != cudaSuccess || used != SQ_OK) {
             hit->valid = false;
@@ -472,6 +544,25 @@ int norm_backward_impl(sq_cache* c, int32_t n_tokens, const void* q, int64_t q_s
     return e != cudaSuccess ? cuda_status(e) : rc;
 }
 
+// The pages of a plan as bf16, in the order of its list, as a pool of one layer.
+int widen_pages(sq_cache* c, const BlockPlanEntry& plan, int32_t layer, cudaStream_t st, bool captured,
+                CUtensorMap* map) {
+    const Geometry& g = c->g;
+    const size_t page = (size_t)2 * g.Hkv * g.P * g.D * sizeof(__nv_bfloat16);
+    int rc = take_buffer(c, c->wide, std::max(1, plan.n_wide) * page, st, captured);
+    if (rc != SQ_OK) return rc;
+    rc = make_pool_map(c, c->wide.d, std::max(1, plan.n_wide), 1, map);
+    if (rc != SQ_OK) return rc;
+    Kv8WidenArgs a;
+    a.pool = kv8_pool(c);
+    a.pages = reinterpret_cast<const int32_t*>(plan.d + plan.o_wide);
+    a.n = plan.n_wide;
+    a.layer = layer;
+    a.out = bf16(static_cast<void*>(c->wide.d));
+    a.err = c->d_err;
+    return cuda_status(launch_kv8_widen(a, g.D, st));
+}
+
 // Attention of query blocks; parents null: sliding windows alone.
 int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_q, const int32_t* parents,
                 int32_t layer, const void* q, void* out, int32_t out_dtype, float* lse, float sm_scale,
@@ -552,6 +643,19 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
             if (rc == SQ_ERR_NO_MEMORY) rc = plan_blocks(g, in, window, n_sink, c->num_sms, 0, &plan);
         }
         if (rc != SQ_OK) return rc;
+        // (8-bit caches) the pages, which the tiles then name by their places
+        std::vector<int32_t> wide, read;
+        for (int32_t p : plan.tile_pages)
+            if (p >= 0 && (read.empty() || read.back() != p)) read.push_back(p);
+        if (c->kv8) {
+            std::unordered_map<int32_t, int32_t> place;
+            for (int32_t& p : plan.tile_pages) {
+                if (p < 0) continue;
+                const auto at = place.emplace(p, (int32_t)wide.size());
+                if (at.second) wide.push_back(p);
+                p = at.first->second;
+            }
+        }
         // upload: the records of 16 bytes first, so that each part is aligned
         struct Part {
             const void* p;
@@ -561,7 +665,8 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
                      {plan.merges.data(), plan.merges.size() * sizeof(BlockMerge), 0},
                      {plan.rows.data(), plan.rows.size() * sizeof(int32_t), 0},
                      {plan.bits.data(), plan.bits.size() * sizeof(uint32_t), 0},
-                     {plan.tile_pages.data(), plan.tile_pages.size() * sizeof(int32_t), 0}};
+                     {plan.tile_pages.data(), plan.tile_pages.size() * sizeof(int32_t), 0},
+                     {wide.data(), wide.size() * sizeof(int32_t), 0}};
         size_t bytes = 0;
         for (Part& p : parts) {
             p.at = bytes;
@@ -617,9 +722,8 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
         victim->unit_rows = plan.unit_rows;
         victim->one = plan.one;
         victim->n_ctas = plan.n_ctas;
-        std::vector<int32_t> read;
-        for (int32_t p : plan.tile_pages)
-            if (p >= 0 && (read.empty() || read.back() != p)) read.push_back(p);
+        victim->o_wide = parts[6].at;
+        victim->n_wide = (int32_t)wide.size();
         list_writes(c, read.data(), read.size(), &victim->writes);
         victim->valid = true;
         hit = victim;
@@ -645,8 +749,9 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
         }
         c->pre_last = hit;
     }
-    CUtensorMap qmap;
+    CUtensorMap qmap, wide_map;
     rc = make_query_map(c, q, (int32_t)n, plan.BP, &qmap);
+    if (rc == SQ_OK && c->kv8) rc = widen_pages(c, plan, layer, st, captured, &wide_map);
     if (rc != SQ_OK) return drop_plan(*hit, st, rc);
     BlockShortArgs a;
     a.tiles = reinterpret_cast<const PrefillTile*>(plan.d);
@@ -655,22 +760,22 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
     a.rows = plan.o_rows ? reinterpret_cast<const int2*>(plan.d + plan.o_rows) : nullptr;
     a.bits = reinterpret_cast<const uint32_t*>(plan.d + plan.o_bits);
     a.n_words = plan.n_words;
-    a.pool = c->pool;
+    a.pool = c->kv8 ? (const void*)c->wide.d : c->pool;
     a.q = q;
     a.n_ctas = plan.n_ctas;
     a.n_pieces = plan.n_pieces;
     a.n_tiles = a.n = a.n_q = 0;  // (the items')
-    a.layer = layer;
+    a.layer = c->kv8 ? 0 : layer;
     a.Hq = g.Hq;
     a.Hkv = g.Hkv;
     a.G = g.G();
     a.P = g.P;
-    a.num_pages = g.num_pages;
+    a.num_pages = c->kv8 ? plan.n_wide : g.num_pages;
     a.BP = plan.BP;
     a.n_items = plan.n_items;
     a.plan_ready = plan_ready;
     a.n_unsafe = 0;
-    a.kv_early = plan.one && plan_ready && g.P >= kPrefillKeys / 2 &&
+    a.kv_early = !c->kv8 && plan.one && plan_ready && g.P >= kPrefillKeys / 2 &&
                          early_writes(c, plan.writes, seqs, n_seqs, a.unsafe, &a.n_unsafe)
                      ? 1
                      : 0;
@@ -683,7 +788,9 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
     a.part_ml = c->pre_part ? c->pre_part + (size_t)plan.n_parts * kPrefillQTiles * kPrefillRows * g.D
                             : nullptr;
     a.err = c->d_err;
-    e = launch_blocks(c->tmap, qmap, a, g.D, plan.one, st);
+    e = launch_blocks(c->kv8 ? wide_map : c->tmap, qmap, a, g.D, plan.one, st);
+    if (c->kv8) rc = used_buffer(c->wide, st, captured);
+    if (rc != SQ_OK) return drop_plan(*hit, st, rc);
     if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
     if (plan.n_merges > 0) {
         BlockCombineArgs ca;
@@ -745,7 +852,7 @@ extern "C" {
 int sq_extend(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new, void* stream) {
     TraceRange trace_("sq_extend");
     if (!c) return SQ_ERR_BAD_HANDLE;
-    return guarded([&] { return extend_impl(c, seqs, n_seqs, n_new, stream); });
+    return guarded([&] { return extend_impl(c, seqs, n_seqs, n_new, stream, [] { return SQ_OK; }); });
 }
 
 int sq_qk_norm_rope_store(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new,

@@ -22,6 +22,7 @@
 #include "../host/core.hpp"
 #include "../kernels/launch.hpp"
 #include "../kernels/noalloc.hpp"
+#include "../kernels/kv8.hpp"
 #include "../kernels/operators.hpp"
 
 using namespace sq;
@@ -111,6 +112,9 @@ struct BlockPlanEntry : PrefillPlanEntry {
     size_t o_rows = 0, o_bits = 0;  // (o_rows 0: no table)
     int32_t n_words = 0, unit_rows = 0, n_ctas = 0;
     bool one = false;
+    // (8-bit caches) the plan's pages, which its tiles name by their place in the list
+    size_t o_wide = 0;
+    int32_t n_wide = 0;
 };
 
 // A device buffer that calls on any stream take turns with.
@@ -197,6 +201,8 @@ struct sq_cache {
     std::deque<BlockPlanEntry> block_plans = std::deque<BlockPlanEntry>(kBlockPlanEntries);
     std::deque<StorePlanEntry> store_plans = std::deque<StorePlanEntry>(kStorePlanEntries);
     TurnBuffer norm_part;  // partial gradients of the norms' weights
+    bool kv8 = false;      // rows are held in 8 bits (Kv8Pool)
+    TurnBuffer wide;       // (8-bit caches) a query-block call's pages as bf16
     std::vector<void*> retired;  // outgrown buffers that captured launches were given
     uint64_t use_clock = 0;
     UploadSlot slots[kUploadSlots];
@@ -265,8 +271,55 @@ int geometry_from(const sq_config* cfg, Geometry* g) {
     return check_geometry(*g);
 }
 
-size_t pool_bytes_of(const Geometry& g) {
-    return (size_t)g.L * g.num_pages * 2 * g.Hkv * g.P * g.D * sizeof(__nv_bfloat16);
+size_t pool_rows_of(const Geometry& g) { return (size_t)g.L * g.num_pages * 2 * g.Hkv * g.P; }
+size_t pool_bytes_of(const Geometry& g, bool kv8) {
+    if (kv8) return pool_rows_of(g) * g.D + pool_rows_of(g) / kScaleRows * sizeof(float);
+    return pool_rows_of(g) * g.D * sizeof(__nv_bfloat16);
+}
+
+Kv8Pool kv8_pool(const sq_cache* c) {
+    uint8_t* codes = reinterpret_cast<uint8_t*>(c->pool);
+    // (a page's rows of a head are 512 bytes at least: the scales are aligned)
+    return {codes, reinterpret_cast<float*>(codes + pool_rows_of(c->g) * c->g.D), c->g.num_pages, c->g.Hkv, c->g.P};
+}
+
+// Bytes of one token's K/V of one layer.
+int64_t token_bytes(const sq_cache* c) {
+    return c->kv8 ? (int64_t)2 * c->g.Hkv * c->g.D + c->g.Hkv * 2 * (int64_t)sizeof(float) / kScaleRows
+                  : c->g.token_layer_bytes();
+}
+
+// bf16 rows as a pool of `pages` pages: dims, innermost first: head dim, row within a
+// (layer, page) block ((kv * Hkv + head) * P + slot), page, layer
+int make_pool_map(sq_cache* c, void* pool, int32_t pages, int32_t layers, CUtensorMap* map) {
+    auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(c->encode_fn);
+    const Geometry& g = c->g;
+    cuuint64_t dims[4] = {(cuuint64_t)g.D, (cuuint64_t)2 * g.Hkv * g.P, (cuuint64_t)pages, (cuuint64_t)layers};
+    cuuint64_t strides[3] = {(cuuint64_t)g.D * 2, (cuuint64_t)2 * g.Hkv * g.P * g.D * 2,
+                             (cuuint64_t)pages * 2 * g.Hkv * g.P * g.D * 2};
+    cuuint32_t box[4] = {64, (cuuint32_t)std::min(g.P, kStageTokens), 1, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, pool, dims, strides, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SQ_OK : SQ_ERR_UNSUPPORTED;
+}
+
+// The codes of an 8-bit cache, the same dims: a box has whole rows, 128 bytes or 64
+// (whose 16-byte chunks are swizzled over 64).
+int make_code_map(sq_cache* c) {
+    auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(c->encode_fn);
+    const Geometry& g = c->g;
+    cuuint64_t dims[4] = {(cuuint64_t)g.D, (cuuint64_t)2 * g.Hkv * g.P, (cuuint64_t)g.num_pages, (cuuint64_t)g.L};
+    cuuint64_t strides[3] = {(cuuint64_t)g.D, (cuuint64_t)2 * g.Hkv * g.P * g.D,
+                             (cuuint64_t)g.num_pages * 2 * g.Hkv * g.P * g.D};
+    cuuint32_t box[4] = {(cuuint32_t)g.D, (cuuint32_t)std::min(g.P, kStageTokens), 1, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    CUresult r = encode(&c->tmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, c->pool, dims, strides, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        g.D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SQ_OK : SQ_ERR_UNSUPPORTED;
 }
 
 int make_tensor_map(sq_cache* c) {
@@ -277,20 +330,8 @@ int make_tensor_map(sq_cache* c) {
         q != cudaDriverEntryPointSuccess || !fn)
         return SQ_ERR_CUDA;
     c->encode_fn = fn;
-    auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
-    const Geometry& g = c->g;
-    // dims, innermost first: head dim, row within a (layer, page) block
-    // ((kv * Hkv + head) * P + slot), page, layer
-    cuuint64_t dims[4] = {(cuuint64_t)g.D, (cuuint64_t)2 * g.Hkv * g.P, (cuuint64_t)g.num_pages,
-                          (cuuint64_t)g.L};
-    cuuint64_t strides[3] = {(cuuint64_t)g.D * 2, (cuuint64_t)2 * g.Hkv * g.P * g.D * 2,
-                             (cuuint64_t)g.num_pages * 2 * g.Hkv * g.P * g.D * 2};
-    cuuint32_t box[4] = {64, (cuuint32_t)std::min(g.P, kStageTokens), 1, 1};
-    cuuint32_t estr[4] = {1, 1, 1, 1};
-    CUresult r = encode(&c->tmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, c->pool, dims, strides, box,
-                        estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? SQ_OK : SQ_ERR_UNSUPPORTED;
+    if (c->kv8) return make_code_map(c);
+    return make_pool_map(c, c->pool, c->g.num_pages, c->g.L, &c->tmap);
 }
 
 // Queries {D, Hq, n_q}: one box is the G heads of a KV head x BP positions.
@@ -534,6 +575,25 @@ int upload(sq_cache* c, UploadSlot& s, const void* src, size_t bytes, void* stre
     return staged_copy(c, s.d, src, bytes, stream);
 }
 
+// A launch that reads `bytes` from `src`, uploaded for it alone.
+template <typename Launch>
+int with_upload(sq_cache* c, const void* src, size_t bytes, void* stream, Launch launch) {
+    UploadSlot& s = c->slots[c->next_slot];
+    c->next_slot = (c->next_slot + 1) % kUploadSlots;
+    const int rc = upload(c, s, src, bytes, stream);
+    if (rc != SQ_OK) return rc;
+    const cudaError_t e = launch(static_cast<const uint8_t*>(s.d));
+    if (cudaEventRecord(s.ev, as_stream(stream)) == cudaSuccess) {
+        s.ev_recorded = true;
+        s.ev_stream = as_stream(stream);
+    } else {
+        cudaStreamSynchronize(as_stream(stream));
+        cudaGetLastError();
+        s.ev_recorded = false;
+    }
+    return cuda_status(e);
+}
+
 // A call fails after it has enqueued something that uses plan entry `p` on `st`
 // (its upload, a launch): the entry is not used again as it is, and its buffers
 // only after that work.
@@ -615,11 +675,16 @@ const char* sq_strerror(int code) {
 size_t sq_pool_bytes(const sq_config* cfg) {
     Geometry g;
     if (geometry_from(cfg, &g) != SQ_OK) return 0;
-    return pool_bytes_of(g);
+    return pool_bytes_of(g, false);
 }
 
-int sq_cache_create(const sq_config* cfg, sq_cache** out) {
-    TraceRange trace_("sq_cache_create");
+size_t sq_pool_bytes_8bit(const sq_config* cfg) {
+    Geometry g;
+    if (geometry_from(cfg, &g) != SQ_OK) return 0;
+    return pool_bytes_of(g, true);
+}
+
+static int create_impl(const sq_config* cfg, bool kv8, sq_cache** out) {
     if (!out) return SQ_ERR_INVALID_ARG;
     *out = nullptr;
     Geometry g;
@@ -630,6 +695,8 @@ int sq_cache_create(const sq_config* cfg, sq_cache** out) {
     std::unique_ptr<sq_cache> c(new (std::nothrow) sq_cache());
     if (!c) return SQ_ERR_NO_MEMORY;
     c->g = g;
+    c->kv8 = kv8;
+    if (kv8 && !kv8_prepare) return SQ_ERR_UNSUPPORTED;
     c->host.reset(new (std::nothrow) HostCache(g));
     if (!c->host) return SQ_ERR_NO_MEMORY;
     c->freed_on.assign(g.num_pages, nullptr);
@@ -651,8 +718,12 @@ int sq_cache_create(const sq_config* cfg, sq_cache** out) {
         e = blocks_prepare(g.D);
         if (e != cudaSuccess) return cuda_status(e);
     }
+    if (kv8) {
+        e = kv8_prepare(g.D);
+        if (e != cudaSuccess) return cuda_status(e);
+    }
     choose_evict_shape(c.get());
-    c->pool_bytes = pool_bytes_of(g);
+    c->pool_bytes = pool_bytes_of(g, kv8);
     if (cfg->kv_pool) {
         c->pool = reinterpret_cast<__nv_bfloat16*>(cfg->kv_pool);
     } else {
@@ -729,6 +800,16 @@ int sq_cache_create(const sq_config* cfg, sq_cache** out) {
     return SQ_OK;
 }
 
+int sq_cache_create(const sq_config* cfg, sq_cache** out) {
+    TraceRange trace_("sq_cache_create");
+    return create_impl(cfg, false, out);
+}
+
+int sq_cache_create_8bit(const sq_config* cfg, sq_cache** out) {
+    TraceRange trace_("sq_cache_create_8bit");
+    return create_impl(cfg, true, out);
+}
+
 int sq_cache_destroy(sq_cache* c) {
     if (!c) return SQ_ERR_BAD_HANDLE;
     cudaDeviceSynchronize();
@@ -748,6 +829,8 @@ int sq_cache_destroy(sq_cache* c) {
     for (void* d : c->retired) cudaFree(d);
     if (c->norm_part.d) cudaFree(c->norm_part.d);
     if (c->norm_part.ev) cudaEventDestroy(c->norm_part.ev);
+    if (c->wide.d) cudaFree(c->wide.d);
+    if (c->wide.ev) cudaEventDestroy(c->wide.ev);
     for (auto& s : c->slots) {
         if (s.d) cudaFree(s.d);
         if (s.ev) cudaEventDestroy(s.ev);
@@ -877,6 +960,10 @@ static void plan_len_apply(sq_cache* c, const LenUpdate& u, uint64_t new_version
     }
 }
 
+// (in kv8.inl)
+static int append_8bit(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new, const void* k,
+                       const void* v, void* stream);
+
 int sq_append_kv(sq_cache* c, sq_seq seq, int32_t n_tokens, const void* k, const void* v,
                  void* stream) {
     TraceRange trace_("sq_append_kv");
@@ -886,6 +973,7 @@ int sq_append_kv(sq_cache* c, sq_seq seq, int32_t n_tokens, const void* k, const
     if (n_tokens == 0) return SQ_OK;
     if (!k || !v || (reinterpret_cast<uintptr_t>(k) & 15) || (reinterpret_cast<uintptr_t>(v) & 15))
         return SQ_ERR_INVALID_ARG;
+    if (c->kv8) return append_8bit(c, &seq, 1, &n_tokens, k, v, stream);
     AppendPlan plan;
     const uint64_t old_version = c->host->seq(seq)->version;
     int rc = c->host->append(seq, n_tokens, &plan);
@@ -954,6 +1042,7 @@ int sq_append_kv_batch(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const vo
         for (int32_t j = 0; j < i; ++j)
             if (seqs[j] == seqs[i]) return SQ_ERR_INVALID_ARG;
     }
+    if (c->kv8) return append_8bit(c, seqs, n_seqs, nullptr, k, v, stream);
     const Geometry& g = c->g;
     std::vector<AppendPlan> plans(n_seqs);
     auto undo = [&](int32_t upto, int code) {
@@ -1165,7 +1254,7 @@ static int decode_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t 
     float* part_o = hit->d_part;
     float* part_ml = part_o + (size_t)L.n_comb_ent * g.G() * g.D;
 
-    DecodeArgs a;
+    DecodeKv8Args a;
     a.segs = reinterpret_cast<const DecodeSeg*>(hit->d_plan + L.segs);
     a.items = reinterpret_cast<const DecodeItem*>(hit->d_plan + L.items);
     a.cta_begin = reinterpret_cast<const int32_t*>(hit->d_plan + L.cta_begin);
@@ -1195,7 +1284,8 @@ static int decode_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t 
     }
     c->debug_flags &= ~SQ_DEBUG_DROP_DECODE_STAGE;
     a.err = c->d_err;
-    e = launch_decode(c->tmap, a, L.n_ctas, g.D, st);
+    a.scales = c->kv8 ? kv8_pool(c).scales : nullptr;
+    e = c->kv8 ? launch_decode_kv8(c->tmap, a, L.n_ctas, g.D, st) : launch_decode(c->tmap, a, L.n_ctas, g.D, st);
     if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
     if (!captured) {
         e = cudaEventRecord(hit->ev, st);
@@ -1205,8 +1295,8 @@ static int decode_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t 
     }
     for (int32_t i = 0; i < n_seqs; ++i) c->host->seq_mut(seqs[i])->last_stream = stream;
     c->stats.decode_calls += 1;
-    c->stats.decode_logical_bytes += hit->logical_tokens * g.token_layer_bytes();
-    c->stats.decode_unique_bytes += hit->unique_tokens * g.token_layer_bytes();
+    c->stats.decode_logical_bytes += hit->logical_tokens * token_bytes(c);
+    c->stats.decode_unique_bytes += hit->unique_tokens * token_bytes(c);
     return SQ_OK;
 }
 
@@ -1221,6 +1311,38 @@ int sq_decode_attention(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t
 }  // extern "C"
 
 namespace {
+
+// The moves of an eviction in an 8-bit cache: a tile for all the rows that a page gets,
+// chunks of whole windows.
+int launch_evict_8bit(sq_cache* c, const EvictPlan& plan, void* stream) {
+    const Geometry& g = c->g;
+    std::vector<EvictTile> tiles;
+    std::vector<EvictPiece> pieces;
+    std::vector<int32_t> window_tile, chunk;
+    evict_tiles(plan, g.P, &tiles, &pieces, &window_tile);
+    const int64_t planes = (int64_t)g.L * 2 * g.Hkv;
+    // about four waves of CTAs, of which an SM holds three or four
+    const int32_t max_chunks = (int32_t)std::max<int64_t>(1, 16 * (int64_t)c->num_sms / planes);
+    evict_chunks(window_tile, (int32_t)tiles.size(), max_chunks, 4, &chunk);
+    const size_t tb = tiles.size() * sizeof(EvictTile), pb = pieces.size() * sizeof(EvictPiece);
+    std::vector<uint8_t> buf(tb + pb + chunk.size() * sizeof(int32_t));
+    std::memcpy(buf.data(), tiles.data(), tb);
+    if (pb) std::memcpy(buf.data() + tb, pieces.data(), pb);
+    std::memcpy(buf.data() + tb + pb, chunk.data(), chunk.size() * sizeof(int32_t));
+    return with_upload(c, buf.data(), buf.size(), stream, [&](const uint8_t* d) {
+        Kv8EvictArgs a = {};
+        a.pool = kv8_pool(c);
+        a.L = g.L;
+        a.tiles = reinterpret_cast<const EvictTile*>(d);
+        a.pieces = reinterpret_cast<const EvictPiece*>(d + tb);
+        a.chunk = reinterpret_cast<const int32_t*>(d + tb + pb);
+        a.n_chunks = (int32_t)chunk.size() - 1;
+        a.n_tiles = (int32_t)tiles.size();
+        a.n_pieces = (int32_t)pieces.size();
+        a.err = c->d_err;
+        return launch_kv8_evict(a, g.D, as_stream(stream));
+    });
+}
 
 int evict_impl(sq_cache* c, sq_seq seq, const sq_span* spans, int32_t n_spans, void* stream,
                bool ragged) {
@@ -1244,7 +1366,10 @@ int evict_impl(sq_cache* c, sq_seq seq, const sq_span* spans, int32_t n_spans, v
     };
     rc = fence_taken_pages(c, plan.cow_pages, stream);
     if (rc != SQ_OK) return undo(rc);
-    if (!plan.moves.empty()) {
+    if (!plan.moves.empty() && c->kv8) {
+        rc = launch_evict_8bit(c, plan, stream);
+        if (rc != SQ_OK) return undo(rc);
+    } else if (!plan.moves.empty()) {
         std::vector<EvictTile> tiles;
         std::vector<EvictPiece> pieces;
         std::vector<int32_t> window_tile, chunk;
@@ -1298,6 +1423,8 @@ int evict_impl(sq_cache* c, sq_seq seq, const sq_span* spans, int32_t n_spans, v
             s.ev_recorded = true;
             s.ev_stream = st;
         }
+    }
+    if (!plan.moves.empty()) {
         std::vector<int32_t> written;
         for (const EvictMove& m : plan.moves)
             if (written.empty() || written.back() != m.dst_page) written.push_back(m.dst_page);
@@ -1310,7 +1437,7 @@ int evict_impl(sq_cache* c, sq_seq seq, const sq_span* spans, int32_t n_spans, v
     c->stats.evicted_tokens += plan.evicted;
     c->stats.evict_moved_rows += plan.moved_rows;
     // rows copied are read and written, zeroed rows only written
-    c->stats.evict_bytes += (2 * plan.moved_rows + plan.zeroed_rows) * g.L * g.token_layer_bytes();
+    c->stats.evict_bytes += (2 * plan.moved_rows + plan.zeroed_rows) * g.L * token_bytes(c);
     c->stats.cow_pages += (int64_t)plan.cow_pages.size();
     return SQ_OK;
 }
@@ -1338,6 +1465,7 @@ int sq_prefill_attention(sq_cache* c, sq_seq seq, int32_t layer, int32_t n_q, co
     const Seq* s = c->host->seq(seq);
     if (!s) return SQ_ERR_BAD_HANDLE;
     const Geometry& g = c->g;
+    if (c->kv8) return SQ_ERR_UNSUPPORTED;
     if (layer < 0 || layer >= g.L || n_q < 1 || n_q > s->n || !q || !out)
         return SQ_ERR_INVALID_ARG;
     if (out_dtype != SQ_OUT_BF16 && out_dtype != SQ_OUT_F32) return SQ_ERR_INVALID_ARG;
@@ -1744,7 +1872,7 @@ int sq_decode_attention_noalloc(sq_cache* c, const sq_seq* seqs, int32_t n_seqs,
     float* part_o = reinterpret_cast<float*>(scratch + part_off);
     float* part_ml = part_o + (size_t)L.n_comb_ent * g.G() * g.D;
 
-    DecodeArgs a;
+    DecodeKv8Args a;
     a.segs = reinterpret_cast<const DecodeSeg*>(scratch + L.segs);
     a.items = reinterpret_cast<const DecodeItem*>(scratch + L.items);
     a.cta_begin = reinterpret_cast<const int32_t*>(scratch + L.cta_begin);
@@ -1774,15 +1902,17 @@ int sq_decode_attention_noalloc(sq_cache* c, const sq_seq* seqs, int32_t n_seqs,
     a.n_unsafe = 0;
     c->debug_flags &= ~SQ_DEBUG_DROP_DECODE_STAGE;
     a.err = c->d_err;
-    e = launch_decode(c->tmap, a, L.n_ctas, g.D, st);
+    a.scales = c->kv8 ? kv8_pool(c).scales : nullptr;
+    e = c->kv8 ? launch_decode_kv8(c->tmap, a, L.n_ctas, g.D, st) : launch_decode(c->tmap, a, L.n_ctas, g.D, st);
     if (e != cudaSuccess) return cuda_status(e);
     for (int32_t i = 0; i < n_seqs; ++i) c->host->seq_mut(seqs[i])->last_stream = stream;
     c->stats.decode_calls += 1;
-    c->stats.decode_logical_bytes += plan.logical_tokens * g.token_layer_bytes();
-    c->stats.decode_unique_bytes += plan.unique_tokens * g.token_layer_bytes();
+    c->stats.decode_logical_bytes += plan.logical_tokens * token_bytes(c);
+    c->stats.decode_unique_bytes += plan.unique_tokens * token_bytes(c);
     return SQ_OK;
 }
 
 }  // extern "C"
 
 #include "operators.inl"
+#include "kv8.inl"

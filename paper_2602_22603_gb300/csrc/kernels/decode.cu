@@ -64,6 +64,9 @@
 // warp-level mma is the right size: the point is to keep HBM busy.
 #include <math.h>
 
+#include <type_traits>
+
+#include "e4m3.cuh"
 #include "launch.hpp"
 #include "ptx.cuh"
 
@@ -72,13 +75,16 @@ namespace {
 
 using namespace dev;
 
-template <int D>
+// kE8: rows in 8 bits (see kv8.hpp).
+template <int D, bool kE8>
 struct DecCfg {
-    static constexpr int kColBlocks = D / 64;                    // 128-byte column blocks
-    static constexpr int kBlockBytes = kStageTokens * 128;       // one column block of a tile
+    static constexpr int kColBlocks = kE8 ? 1 : D / 64;          // column blocks of a row
+    static constexpr int kRowBytes = kE8 ? D : 128;              // ... and a row's bytes in one
+    static constexpr int kBlockBytes = kStageTokens * kRowBytes; // one column block of a tile
     static constexpr int kTileBytes = kColBlocks * kBlockBytes;  // K (or V) of one stage
     static constexpr int kStageBytes = 2 * kTileBytes;
-    static constexpr int kStages = (D == 128) ? 3 : 6;           // per group: 96 KiB in flight
+    // per group: 96 KiB in flight (80 where rows are 128 bytes)
+    static constexpr int kStages = kE8 ? (D == 128 ? 5 : 12) : (D == 128 ? 3 : 6);
     static constexpr int kConsumers = kDecodeConsumerWarps * 32;
     static constexpr int kRingBytes = kDecodeGroups * kStages * kStageBytes;
     // warps: consumers, a producer per group, two that close items
@@ -90,7 +96,11 @@ struct DecCfg {
     static constexpr int kBarOut = kDecodeGroups * 2 * kStages;  // a pass's rows are written
     static constexpr int kBarOutFree = kBarOut + 1;              // ... and read
     static constexpr int kBarRuns = kBarOut + 2;                 // the last item's runs are listed
-    static constexpr int kOffRed = kOffBars + 256;
+    static constexpr int kBarBytes = kE8 ? 512 : 256;
+    // (8 bits) a stage's scales: its blocks' of keys, then of values
+    static constexpr int kStageScales = kE8 ? 2 * kStageTokens / kScaleRows : 0;
+    static constexpr int kOffScales = kOffBars + kBarBytes;
+    static constexpr int kOffRed = kOffScales + kDecodeGroups * kStages * kStageScales * 4;
     // item ends: per-warp row max / sum, eight rows of every warp's output, and
     // the runs an item completed
     static constexpr int kPassRows = 8;
@@ -101,7 +111,8 @@ struct DecCfg {
     static constexpr int kNT = D / 8;   // 8-wide output column tiles
     static constexpr int kKS = D / 16;  // 16-deep contraction steps
     static_assert(kSmemBytes <= 232448 && kOffOut % 16 == 0, "shared memory");
-    static_assert((kBarRuns + 1) * 8 + 4 <= 256, "mbarriers");
+    static_assert((kBarRuns + 1) * 8 + 4 <= kBarBytes, "mbarriers");
+    static_assert(kOffScales % 16 == 0 && kOffRed % 16 == 0, "alignment");
 };
 
 __device__ __forceinline__ uint32_t ld_u32(const __nv_bfloat16* p) {
@@ -119,13 +130,16 @@ __device__ __forceinline__ float bf16x2_sum(uint32_t v) {
 // the current one waits for its slot.  Whole-page stages (P >= 64) are issued by
 // lane 0; with smaller pages each lane issues one box (page, column block, K or
 // V).
-template <int D>
+template <bool kE8>
+using ArgsOf = std::conditional_t<kE8, DecodeKv8Args, DecodeArgs>;
+template <int D, bool kE8>
 struct Producer {
-    using C = DecCfg<D>;
+    using C = DecCfg<D, kE8>;
     const CUtensorMap* tmap;
-    const DecodeArgs& a;
+    const ArgsOf<kE8>& a;
     uint8_t* ring;      // the group's slots
     uint64_t* bars;     // the group's barriers: full [kStages], empty [kStages]
+    float* scales;      // (8 bits) the group's slots
     volatile int* abort_flag;
     int group, lane;
     // this lane's box within a stage of small pages
@@ -141,7 +155,7 @@ struct Producer {
     __device__ void init() {
         box_cb = lane % C::kColBlocks;
         box_kv = (lane / C::kColBlocks) % 2;
-        box_page = a.P < kStageTokens ? lane / (2 * C::kColBlocks) : 0;
+        box_page = kE8 || a.P < kStageTokens ? lane / (2 * C::kColBlocks) : 0;
         it = a.cta_begin[blockIdx.x];
         it1 = a.cta_begin[blockIdx.x + 1];
         slot = 0;
@@ -172,6 +186,13 @@ struct Producer {
             open_item();
             s += over;
         }
+        if constexpr (kE8) {
+            // a lane to the scale of a block (number box_page) of keys or of values;
+            // those whose block begins a box load it too
+            const int at = (s * kStageTokens + box_page * kScaleRows) / a.P;
+            pid = lane < C::kStageScales && at < n_pages ? a.page_ids[page_off + at] : -1;
+            return;
+        }
         const int pi = s * kStageTokens / a.P + box_page;
         const int per = a.P < kStageTokens ? kStageTokens / a.P : 1;
         pid = box_page < per && pi < n_pages ? a.page_ids[page_off + pi] : -1;
@@ -189,11 +210,40 @@ struct Producer {
         s += kDecodeGroups;
         settle();
     }
+    __device__ bool box_lane() const {
+        return kE8 ? lane < C::kStageScales && box_page * kScaleRows % min(a.P, kStageTokens) == 0
+                   : a.P < kStageTokens || lane < 2 * C::kColBlocks;
+    }
     // Issues the current stage into its (free) slot.
     __device__ void issue() {
         const uint32_t full = smem_addr(&bars[slot]);
         const uint32_t dst = smem_addr(ring) + slot * C::kStageBytes;
-        if (a.P >= kStageTokens) {
+        if constexpr (kE8) {
+            const bool valid = pid >= 0 && pid < a.num_pages;
+            if (pid < -1 || pid >= a.num_pages) set_error(a.err, kErrBounds);
+            const bool box = valid && box_lane();
+            const uint32_t n = __popc(__ballot_sync(0xffffffffu, box));
+            if (lane == 0) {
+                if (n) mbar_arrive_expect_tx(full, n * min(a.P, kStageTokens) * C::kRowBytes);
+                else mbar_arrive(full);
+            }
+            __syncwarp();
+            if (box)
+                tma_load_4d(dst + box_kv * C::kTileBytes + box_page * kScaleRows * C::kRowBytes, tmap, full, 0,
+                            row(box_kv), pid, a.layer);
+            if (lane < C::kStageScales) {
+                if (valid) {
+                    const int64_t plane = (((int64_t)a.layer * a.num_pages + pid) * 2 + box_kv) * a.Hkv + head;
+                    const int at = (s * kStageTokens + box_page * kScaleRows) & (a.P - 1);
+                    const float* src = a.scales + (plane * a.P + at) / kScaleRows;
+                    const uint32_t to = smem_addr(scales + slot * C::kStageScales +
+                                                  box_kv * (C::kStageScales / 2) + box_page);
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(src) : "memory");
+                }
+                // (arrives when this lane's copy has landed)
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full) : "memory");
+            }
+        } else if (a.P >= kStageTokens) {
             if (lane == 0) {
                 if ((uint32_t)pid < (uint32_t)a.num_pages) {
                     mbar_arrive_expect_tx(full, C::kStageBytes);
@@ -244,7 +294,7 @@ struct Producer {
         // (the walk goes on from here after the wait: look ahead on a copy)
         Producer ahead = *this;
         for (; n < kPrefetchStages && ahead.more(); ++n) {
-            if (ahead.pid >= 0 && ahead.pid < a.num_pages && (a.P < kStageTokens || lane < 2 * C::kColBlocks))
+            if (ahead.pid >= 0 && ahead.pid < a.num_pages && box_lane())
                 tma_prefetch_l2_4d(tmap, box_cb * 64, ahead.row(box_kv), ahead.pid, a.layer);
             ahead.advance();
         }
@@ -319,11 +369,11 @@ __device__ __forceinline__ void write_out(const DecodeArgs& a, size_t at, const 
 
 // Adds the consumer warps' rows rb .. rb + 7 of an item (weights 2^(m_w - M),
 // warps in order) and writes its partials or outputs: `n` threads, `v0` = which.
-template <int D>
+template <int D, bool kE8>
 __device__ __forceinline__ void close_rows(const DecodeArgs& a, const DecodeItem* item,
                                            const DecodeSeg* seg, int head, int sole, int rows, int rb,
                                            const uint8_t* smem, int v0, int n) {
-    using C = DecCfg<D>;
+    using C = DecCfg<D, kE8>;
     constexpr int kVec = D / 4;  // float4 per output row
     const int G = a.G;
     const float* red_m = reinterpret_cast<const float*>(smem + C::kOffRed);
@@ -360,10 +410,214 @@ __device__ __forceinline__ void close_rows(const DecodeArgs& a, const DecodeItem
     }
 }
 
+// ---- rows in 8 bits -------------------------------------------------------------
+// The products take fp16: an e4m3 code is exact in it, and one conversion makes two.
+// A power of two for each query row takes it from bf16 into fp16's range, the largest
+// element to 2^14 .. 2^15 (elements below 2^-32 of it lose digits); the logits are
+// taken back with the softmax's scale and their keys' block's, one factor for the
+// eight columns of a tile.  The weights are 2^(x - m + kLift), rounded to fp16 (11
+// digits down to 2^-28 of the largest), and sums of a tile's eight tokens share their
+// values' scale s, so that the weight times s / v_ref goes into the product, v_ref
+// being the largest scale of the warp's tokens so far, which takes the sums back at
+// the item's end.
+//
+// ldmatrix moves 16-bit pairs, here two neighbouring dimensions.  Keys: a lane gets
+// dimensions 4 tig .. 4 tig + 3 of sixteen, so the queries' fragments are loaded in that
+// order.  Values, transposed: the pairs of two tokens; the bytes are taken apart, and a
+// product of 16 dimensions is one of the even and one of the odd ones.
+constexpr float kLift = 14.f;
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32"
+        " {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float f16x2_sum(uint32_t v) {
+    const float2 f = f16x2_to_f32(v);
+    return f.x + f.y;
+}
+
+// Byte offset of a row's 16-byte chunk in a tile, as the tensor map swizzles it.
 template <int D>
+__device__ __forceinline__ uint32_t e8_chunk(int row, int chunk) {
+    return row * D + ((chunk ^ (D == 128 ? row & 7 : row >> 1 & 3)) << 4);
+}
+
+// Two query rows (heads h0 and h1 of the call; a row that is none is zero) as A
+// fragments, and the factors that their logits take.
+template <int D>
+__device__ __forceinline__ void load_queries_f16(const DecodeArgs& a, size_t h0, size_t h1, bool v0, bool v1,
+                                                 int tig, uint32_t (&qa)[D / 16][4], float& c0, float& c1) {
+    uint32_t most[2] = {0u, 0u};
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const uint2* row = reinterpret_cast<const uint2*>(a.q + (r ? h1 : h0) * D) + tig;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+            const uint2 x = (r ? v1 : v0) ? row[kk * 4] : make_uint2(0u, 0u);
+            qa[kk][r] = x.x;
+            qa[kk][2 + r] = x.y;
+            // (sizes of bf16 order as their bits)
+            most[r] = max(most[r], max(max(x.x << 16, x.x) & 0x7fffffffu, max(x.y << 16, x.y) & 0x7fffffffu));
+        }
+    }
+    float* c[2] = {&c0, &c1};
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        uint32_t m = most[r];
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        const int k = max((int)(m >> 23) - 127, -100) - 14;
+        *c[r] = a.scale_log2 * power_of_two(k);
+        const float f = power_of_two(-k);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const uint32_t x = qa[kk][e + r];
+                qa[kk][e + r] = pack_f16x2(__uint_as_float(x << 16) * f, __uint_as_float(x & 0xffff0000u) * f);
+            }
+    }
+}
+
+// One stage's 16 tokens of a warp.  True: some rows of V were zeroed in shared memory.
+template <int D>
+__device__ __forceinline__ bool e8_stage(const uint32_t (&qa)[D / 16][4], float (&o)[D / 8][4], uint32_t kb,
+                                         uint32_t vb, uint8_t* vgen, const float* sc_s, uint32_t vm, int tbase,
+                                         int n_tok, int lim0, int lim1, int w4, int lane, float c0, float c1,
+                                         float& m0, float& m1, float& l0, float& l1, float& v_ref) {
+    const int tig = lane & 3, mi = lane >> 3, rr = lane & 7;
+    // rows past the sequence's last and rows that their page's fill hides; a block
+    // without any other has no scale worth reading
+    const uint32_t live = vm & ((1u << min(max(n_tok - tbase, 0), 16)) - 1u);
+    float sk[2], sv[2];
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+        const bool some = (live >> (8 * nt)) & 0xffu;
+        sk[nt] = some ? sc_s[w4 * 2 + nt] : 0.f;
+        sv[nt] = some ? sc_s[kStageTokens / kScaleRows + w4 * 2 + nt] : 0.f;
+    }
+    // S = Q K^T over 16 tokens (two n8 tiles, even and odd steps apart)
+    float s4[2][2][4] = {};
+    {
+        const int t = w4 * 16 + (mi >> 1) * 8 + rr;
+#pragma unroll
+        for (int k2 = 0; k2 < D / 32; ++k2) {
+            uint32_t b[4];
+            ldsm_x4(kb + e8_chunk<D>(t, 2 * k2 + (mi & 1)), b[0], b[1], b[2], b[3]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                mma_f16(s4[x >> 1][x & 1], qa[2 * k2 + (x & 1)], e4m3_to_f16x2(b[x]), e4m3_to_f16x2(b[x] >> 16));
+        }
+    }
+    float x[2][4];
+    float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+        const float f0 = c0 * sk[nt], f1 = c1 * sk[nt];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int tk = tbase + nt * 8 + tig * 2 + e;
+            const bool rv = (vm >> (nt * 8 + tig * 2 + e)) & 1u;
+            x[nt][e] = tk < lim0 && rv ? (s4[nt][0][e] + s4[nt][1][e]) * f0 : -INFINITY;
+            x[nt][2 + e] = tk < lim1 && rv ? (s4[nt][0][2 + e] + s4[nt][1][2 + e]) * f1 : -INFINITY;
+            mx0 = fmaxf(mx0, x[nt][e]);
+            mx1 = fmaxf(mx1, x[nt][2 + e]);
+        }
+    }
+    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 1));
+    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 1));
+    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 2));
+    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 2));
+    const float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);
+    const float ms0 = mn0 == -INFINITY ? 0.f : mn0, ms1 = mn1 == -INFINITY ? 0.f : mn1;
+    float al0 = exp2f(m0 - ms0), al1 = exp2f(m1 - ms1);
+    m0 = mn0;
+    m1 = mn1;
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            x[nt][e] = exp2f(x[nt][e] - (ms0 - kLift));
+            x[nt][2 + e] = exp2f(x[nt][2 + e] - (ms1 - kLift));
+        }
+    // the normaliser sums the rounded weights
+    uint32_t pa[4];
+    pa[0] = pack_f16x2(x[0][0], x[0][1]);
+    pa[1] = pack_f16x2(x[0][2], x[0][3]);
+    pa[2] = pack_f16x2(x[1][0], x[1][1]);
+    pa[3] = pack_f16x2(x[1][2], x[1][3]);
+    l0 = l0 * al0 + (f16x2_sum(pa[0]) + f16x2_sum(pa[2]));
+    l1 = l1 * al1 + (f16x2_sum(pa[1]) + f16x2_sum(pa[3]));
+    const float sv_most = fmaxf(sv[0], sv[1]);
+    if (sv_most > v_ref) {  // (warp-uniform)
+        const float f = v_ref / sv_most;
+        al0 *= f;
+        al1 *= f;
+        v_ref = sv_most;
+    }
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+        const float f = sv[nt] / v_ref;
+        const uint32_t f2 = pack_f16x2(f, f);
+        pa[2 * nt] = mul_f16x2(pa[2 * nt], f2);
+        pa[2 * nt + 1] = mul_f16x2(pa[2 * nt + 1], f2);
+    }
+    if (__any_sync(0xffffffffu, al0 != 1.f || al1 != 1.f)) {
+#pragma unroll
+        for (int nd = 0; nd < D / 8; ++nd) {
+            o[nd][0] *= al0;
+            o[nd][1] *= al0;
+            o[nd][2] *= al1;
+            o[nd][3] *= al1;
+        }
+    }
+    // V rows that hold none of the sequence's may hold anything: zero them, so that
+    // 0 * V stays 0
+    const bool tail = live != 0xffffu;
+    if (tail) {
+        constexpr int per_row = D / 16;  // 16-byte chunks
+        for (int idx = lane; idx < 16 * per_row; idx += 32) {
+            const int r = idx / per_row;
+            if (!((live >> r) & 1u))
+                *reinterpret_cast<uint4*>(vgen + (w4 * 16 + r) * D + idx % per_row * 16) = make_uint4(0, 0, 0, 0);
+        }
+        __syncwarp();
+    }
+    // O += P V: of 16 dimensions the even ones, then the odd ones
+    {
+        const int t = w4 * 16 + (mi & 1) * 8 + rr;
+#pragma unroll
+        for (int j2 = 0; j2 < D / 32; ++j2) {
+            uint32_t b[4];
+            ldsm_x4_trans(vb + e8_chunk<D>(t, 2 * j2 + (mi >> 1)), b[0], b[1], b[2], b[3]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) b[x] = __byte_perm(b[x], 0u, 0x3120);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int j = 2 * j2 + h;
+                mma_f16(o[2 * j], pa, e4m3_to_f16x2(b[2 * h]), e4m3_to_f16x2(b[2 * h + 1]));
+                mma_f16(o[2 * j + 1], pa, e4m3_to_f16x2(b[2 * h] >> 16), e4m3_to_f16x2(b[2 * h + 1] >> 16));
+            }
+        }
+    }
+    return tail;
+}
+
+template <int D, bool kE8>
 __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, uint8_t* smem,
                         uint64_t* all_bars, volatile int* abort_flag, int warp, int lane) {
-    using C = DecCfg<D>;
+    using C = DecCfg<D, kE8>;
     const int gid = lane >> 2, tig = lane & 3;
     const int r0 = gid, r1 = gid + 8;
     const int mi = lane >> 3, rr = lane & 7;
@@ -376,6 +630,8 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
     float* red_o = reinterpret_cast<float*>(smem + C::kOffOut);     // [8][8][D], out_pos
     uint32_t n_pass = 0;  // item-end passes so far
     uint8_t* ring = smem + group * C::kStages * C::kStageBytes;  // the group's slots
+    const float* scales =
+        reinterpret_cast<const float*>(smem + C::kOffScales) + group * C::kStages * C::kStageScales;
     int slot = 0;
     uint32_t phase = 0;
     int skip = group;   // stages to the group's next one
@@ -390,7 +646,13 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
         const int n_tok = seg->n_tok;
 
         uint32_t qa[C::kKS][4];
-        {
+        // (8 bits) a row's scale of the logits; the largest scale of the values so far
+        float c0 = a.scale_log2, c1 = a.scale_log2, v_ref = power_of_two(kLeastScale);
+        if constexpr (kE8) {
+            load_queries_f16<D>(a, v0 ? (size_t)item.seq0 * a.Hq + item.head * G + r0 % G : 0,
+                                v1 ? (size_t)item.seq1 * a.Hq + item.head * G + r1 % G : 0, v0, v1, tig, qa, c0,
+                                c1);
+        } else {
             const __nv_bfloat16* q0 =
                 a.q + ((size_t)(v0 ? item.seq0 : 0) * a.Hq + item.head * G + r0 % G) * D;
             const __nv_bfloat16* q1 =
@@ -453,6 +715,12 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
                 const uint32_t vb = kb + C::kTileBytes;
                 const int tbase = s * kStageTokens + w4 * 16;  // segment-relative
 
+                bool tail;
+                if constexpr (kE8) {
+                    tail = e8_stage<D>(qa, o, kb, vb, ring + slot * C::kStageBytes + C::kTileBytes,
+                                       scales + slot * C::kStageScales, vm, tbase, n_tok, lim0, lim1, w4, lane,
+                                       c0, c1, m0, m1, l0, l1, v_ref);
+                } else {
                 // S = Q K^T over this warp's 16 tokens (two n8 tiles)
                 float sc[2][4];
 #pragma unroll
@@ -525,7 +793,7 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
                 // Rows past the last valid token hold stale or never-written
                 // shared memory, and rows that their page's fill hides may hold
                 // anything: zero this warp's such V rows so 0 * V stays 0.
-                const bool tail = tbase + 16 > n_tok || vm != 0xffffu;
+                tail = tbase + 16 > n_tok || vm != 0xffffu;
                 if (tail) {
                     const uint32_t live = vm & ((1u << min(max(n_tok - tbase, 0), 16)) - 1u);
                     constexpr int per_row = C::kColBlocks * 8;  // 16-byte chunks per row
@@ -553,6 +821,7 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
                         mma_bf16(o[2 * nd2], pa, b0, b1);
                         mma_bf16(o[2 * nd2 + 1], pa, b2, b3);
                     }
+                }
                 }
                 if (tail) fence_proxy_async_smem();  // generic writes before the next TMA fill
                 __syncwarp();
@@ -587,22 +856,33 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
             if (dead && !last) continue;
             const int r = rb + gid;  // this lane's row of the pass: r0, then r1
             if (tig == 0) {
-                red_m[warp * kRowsPerTile + r] = rb ? m1 : m0;
+                // (8 bits: the weights are 2^kLift times as large)
+                red_m[warp * kRowsPerTile + r] = (rb ? m1 : m0) - (kE8 ? kLift : 0.f);
                 red_l[warp * kRowsPerTile + r] = rb ? l1 : l0;
             }
             if (r < rows) {
                 float* wo = red_o + warp * C::kPassRows * D;
+                if constexpr (kE8) {
 #pragma unroll
-                for (int nd = 0; nd < C::kNT; ++nd)
-                    *reinterpret_cast<float2*>(wo + out_pos<D>(gid, nd * 8 + tig * 2)) =
-                        rb ? make_float2(o[nd][2], o[nd][3]) : make_float2(o[nd][0], o[nd][1]);
+                    for (int j = 0; j < C::kKS; ++j) {
+                        const float(&x)[4] = o[2 * j], (&y)[4] = o[2 * j + 1];
+                        *reinterpret_cast<float4*>(wo + out_pos<D>(gid, j * 16 + tig * 4)) =
+                            rb ? make_float4(x[2] * v_ref, y[2] * v_ref, x[3] * v_ref, y[3] * v_ref)
+                               : make_float4(x[0] * v_ref, y[0] * v_ref, x[1] * v_ref, y[1] * v_ref);
+                    }
+                } else {
+#pragma unroll
+                    for (int nd = 0; nd < C::kNT; ++nd)
+                        *reinterpret_cast<float2*>(wo + out_pos<D>(gid, nd * 8 + tig * 2)) =
+                            rb ? make_float2(o[nd][2], o[nd][3]) : make_float2(o[nd][0], o[nd][1]);
+                }
             }
             if (last) {
                 // nothing is left to stream: the consumers add the rows themselves
                 // (every warp gets here, also after a wait ran out)
                 const int sole = a.items[it].sole;
                 named_bar_sync(1, C::kConsumers);
-                close_rows<D>(a, a.items + it, seg, item.head, sole, rows, rb, smem, threadIdx.x,
+                close_rows<D, kE8>(a, a.items + it, seg, item.head, sole, rows, rb, smem, threadIdx.x,
                               C::kConsumers);
                 if (rb + C::kPassRows < rows) {
                     named_bar_sync(1, C::kConsumers);
@@ -743,10 +1023,10 @@ __device__ __forceinline__ void merge_finish(const DecodeArgs& a, const RunRef& 
 }
 
 // The closing warps (et: thread 0 .. 63 of them).
-template <int D>
+template <int D, bool kE8>
 __device__ void close_items(const DecodeArgs& a, int it0, int it1, uint8_t* smem, uint64_t* bars,
                             volatile int* abort_flag, int et) {
-    using C = DecCfg<D>;
+    using C = DecCfg<D, kE8>;
     constexpr int kVec = D / 4;  // float4 per output row
     const int G = a.G, lane = et & 31;
     int* n_runs = reinterpret_cast<int*>(smem + C::kOffRuns);
@@ -779,7 +1059,7 @@ __device__ void close_items(const DecodeArgs& a, int it0, int it1, uint8_t* smem
             }
             if (dead) continue;
             if (it + 1 == it1) break;  // the consumers have added and written its rows
-            close_rows<D>(a, item, seg, head, sole, rows, rb, smem, et, C::kClosers);
+            close_rows<D, kE8>(a, item, seg, head, sole, rows, rb, smem, et, C::kClosers);
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&bars[C::kBarOutFree]));
         }
@@ -828,10 +1108,10 @@ __device__ void close_items(const DecodeArgs& a, int it0, int it1, uint8_t* smem
 
 // The runs of the CTA's last item, by the consumers: a thread per share of an
 // output, the second shares through shared memory.
-template <int D>
+template <int D, bool kE8>
 __device__ void merge_last_runs(const DecodeArgs& a, uint8_t* smem, uint64_t* bars,
                                 volatile int* abort_flag, int lane) {
-    using C = DecCfg<D>;
+    using C = DecCfg<D, kE8>;
     constexpr int kT = C::kConsumers, kVec = D / 4;
     const int tid = threadIdx.x;
     const int outs = a.G * kVec;  // of one run, <= 512
@@ -880,11 +1160,11 @@ __device__ void merge_last_runs(const DecodeArgs& a, uint8_t* smem, uint64_t* ba
     }
 }
 
-template <int D>
-__global__ void __launch_bounds__(DecCfg<D>::kThreads, 1)
+template <int D, bool kE8>
+__global__ void __launch_bounds__(DecCfg<D, kE8>::kThreads, 1)
     sq_decode_splitk_kernel(const __grid_constant__ CUtensorMap tmap,
-                            const __grid_constant__ DecodeArgs a) {
-    using C = DecCfg<D>;
+                            const __grid_constant__ ArgsOf<kE8> a) {
+    using C = DecCfg<D, kE8>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -895,7 +1175,7 @@ __global__ void __launch_bounds__(DecCfg<D>::kThreads, 1)
         // per group: full [kStages], empty [kStages]
         for (int s = 0; s < kDecodeGroups * 2 * C::kStages; ++s)
             mbar_init(smem_addr(&bars[s]),
-                      s / C::kStages % 2 ? kDecodeConsumerWarps / kDecodeGroups : 1);
+                      s / C::kStages % 2 ? kDecodeConsumerWarps / kDecodeGroups : 1 + C::kStageScales);
         mbar_init(smem_addr(&bars[C::kBarOut]), kDecodeConsumerWarps);
         mbar_init(smem_addr(&bars[C::kBarOutFree]), C::kClosers / 32);
         mbar_init(smem_addr(&bars[C::kBarRuns]), 1);
@@ -906,8 +1186,10 @@ __global__ void __launch_bounds__(DecCfg<D>::kThreads, 1)
     const int group = warp - kDecodeConsumerWarps;
     if (group >= 0 && group < kDecodeGroups) {
         if (threadIdx.x == C::kConsumers) prefetch_tmap(&tmap);
-        Producer<D> pr{&tmap, a, smem + group * C::kStages * C::kStageBytes,
-                       bars + group * 2 * C::kStages, abort_flag, group, lane};
+        Producer<D, kE8> pr{&tmap, a, smem + group * C::kStages * C::kStageBytes,
+                            bars + group * 2 * C::kStages,
+                            reinterpret_cast<float*>(smem + C::kOffScales) + group * C::kStages * C::kStageScales,
+                            abort_flag, group, lane};
         // A reused plan is read before the wait.  Pages no in-flight work writes
         // (the host checked every library write to them is complete; the kernels
         // before this one write no other pool memory) are loaded before it too:
@@ -939,12 +1221,12 @@ __global__ void __launch_bounds__(DecCfg<D>::kThreads, 1)
     if (!a.plan_ready) read_plan();
     if (it0 == it1) return;
     if (closer) {
-        close_items<D>(a, it0, it1, smem, bars, abort_flag,
+        close_items<D, kE8>(a, it0, it1, smem, bars, abort_flag,
                        threadIdx.x - C::kConsumers - kDecodeGroups * 32);
         return;
     }
-    consume<D>(a, it0, it1, head, smem, bars, abort_flag, warp, lane);
-    merge_last_runs<D>(a, smem, bars, abort_flag, lane);
+    consume<D, kE8>(a, it0, it1, head, smem, bars, abort_flag, warp, lane);
+    merge_last_runs<D, kE8>(a, smem, bars, abort_flag, lane);
 }
 
 }  // namespace
@@ -953,31 +1235,36 @@ int64_t decode_partial_bytes(int32_t n_ent, int32_t G, int32_t D) {
     return (int64_t)n_ent * G * (D + 4) * (int64_t)sizeof(float);
 }
 
-template <int D>
+template <int D, bool kE8>
 static cudaError_t prepare_one() {
-    cudaError_t e = cudaFuncSetAttribute(sq_decode_splitk_kernel<D>,
+    cudaError_t e = cudaFuncSetAttribute(sq_decode_splitk_kernel<D, kE8>,
                                          cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         DecCfg<D>::kSmemBytes);
+                                         DecCfg<D, kE8>::kSmemBytes);
     if (e != cudaSuccess) return e;
     // the largest shared-memory carveout
-    return cudaFuncSetAttribute(sq_decode_splitk_kernel<D>,
+    return cudaFuncSetAttribute(sq_decode_splitk_kernel<D, kE8>,
                                 cudaFuncAttributePreferredSharedMemoryCarveout,
                                 cudaSharedmemCarveoutMaxShared);
 }
 
-cudaError_t decode_prepare(int D) { return D == 128 ? prepare_one<128>() : prepare_one<64>(); }
+cudaError_t decode_prepare(int D) {
+    const cudaError_t e = D == 128 ? prepare_one<128, false>() : prepare_one<64, false>();
+    if (e != cudaSuccess) return e;
+    return D == 128 ? prepare_one<128, true>() : prepare_one<64, true>();
+}
 
+// (that of rows in 8 bits is the same: a CTA's shared memory leaves no room for two)
 int decode_ctas_per_sm(int D) {
     int n = 0;
     cudaError_t e;
     if (D == 128)
-        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, sq_decode_splitk_kernel<128>,
-                                                          DecCfg<128>::kThreads,
-                                                          DecCfg<128>::kSmemBytes);
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, sq_decode_splitk_kernel<128, false>,
+                                                          DecCfg<128, false>::kThreads,
+                                                          DecCfg<128, false>::kSmemBytes);
     else
-        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, sq_decode_splitk_kernel<64>,
-                                                          DecCfg<64>::kThreads,
-                                                          DecCfg<64>::kSmemBytes);
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, sq_decode_splitk_kernel<64, false>,
+                                                          DecCfg<64, false>::kThreads,
+                                                          DecCfg<64, false>::kSmemBytes);
     if (e != cudaSuccess || n < 1) return 1;
     return n;
 }
@@ -992,22 +1279,26 @@ static cudaLaunchAttribute pdl_attr() {
     return at;
 }
 
-cudaError_t launch_decode(const CUtensorMap& tmap, const DecodeArgs& a, int n_ctas, int D,
-                          cudaStream_t st) {
+template <int D, bool kE8>
+static cudaError_t launch_one(const CUtensorMap& tmap, const ArgsOf<kE8>& a, int n_ctas, cudaStream_t st) {
     cudaLaunchAttribute at = pdl_attr();
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n_ctas);
+    cfg.blockDim = dim3(DecCfg<D, kE8>::kThreads);
+    cfg.dynamicSmemBytes = DecCfg<D, kE8>::kSmemBytes;
     cfg.stream = st;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    if (D == 128) {
-        cfg.blockDim = dim3(DecCfg<128>::kThreads);
-        cfg.dynamicSmemBytes = DecCfg<128>::kSmemBytes;
-        return cudaLaunchKernelEx(&cfg, sq_decode_splitk_kernel<128>, tmap, a);
-    }
-    cfg.blockDim = dim3(DecCfg<64>::kThreads);
-    cfg.dynamicSmemBytes = DecCfg<64>::kSmemBytes;
-    return cudaLaunchKernelEx(&cfg, sq_decode_splitk_kernel<64>, tmap, a);
+    return cudaLaunchKernelEx(&cfg, sq_decode_splitk_kernel<D, kE8>, tmap, a);
+}
+
+cudaError_t launch_decode(const CUtensorMap& tmap, const DecodeArgs& a, int n_ctas, int D,
+                          cudaStream_t st) {
+    return D == 128 ? launch_one<128, false>(tmap, a, n_ctas, st) : launch_one<64, false>(tmap, a, n_ctas, st);
+}
+cudaError_t launch_decode_kv8(const CUtensorMap& tmap, const DecodeKv8Args& a, int n_ctas, int D,
+                              cudaStream_t st) {
+    return D == 128 ? launch_one<128, true>(tmap, a, n_ctas, st) : launch_one<64, true>(tmap, a, n_ctas, st);
 }
 
 }  // namespace sq

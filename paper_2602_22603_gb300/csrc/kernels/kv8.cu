@@ -1,0 +1,517 @@
+// Rows of a cache held in 8 bits: stored (with the norms and the rotation on the
+// way), copied on write, read back, and compacted after an eviction.
+//
+// A block is kScaleRows slots of one page, plane and head, and has one scale s = 2^e;
+// an element x of it is held as the e4m3 code of x / s, so that
+//     e = max(kLeastScale, ceil(log2(max |x| / 448))),   x ~ code * s.
+// e4m3 has 4 significant bits at any size down to 2^-6, and a power of two moves
+// sizes alone: the values that a block stands for do not depend on its scale but
+// where they are below 2^-6 s, 2^-13 of the block's largest or less.  So rows may be
+// taken from scale to scale (a new row in a block that has rows, rows of several
+// blocks packed into one) without their errors adding up.
+#include <algorithm>
+#include <type_traits>
+
+#include "e4m3.cuh"
+#include "norm_rope.cuh"
+
+namespace sq {
+namespace {
+
+using namespace dev;
+
+constexpr int kStoreThreads = 128;
+constexpr int kHeadRows = 8;   // query rows of a lane group in flight
+
+__device__ __forceinline__ int log2_of(int power) { return __ffs(power) - 1; }
+
+// Offset of a plane's first row in the codes, in rows.
+__device__ __forceinline__ int64_t plane_row(const Kv8Pool& p, int layer, int64_t page, int kv, int head) {
+    return (((layer * p.num_pages + page) * 2 + kv) * p.Hkv + head) * p.P;
+}
+
+// Four elements of an input row.
+__device__ __forceinline__ float4 unpack4(uint2 v) {
+    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u),
+                       __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
+}
+
+// Tasks of a run: its keys' and its values' heads, then the query heads of `most`
+// rows.
+template <int D>
+struct StoreTasks {
+    int q, total;
+    __host__ __device__ StoreTasks(int Hq, int Hkv, int most) {
+        constexpr int n = NormCfg<D>::kGroups * kHeadRows;
+        q = (Hq + n - 1) / n;
+        total = 2 * Hkv + most * q;
+    }
+};
+
+// A warp to a block of keys or values (the rows it has before the run's first are
+// read, and written again where the scale changes), or to the query rows of up to
+// kHeadRows heads of each lane group of a token.
+template <int D, bool kPairs>
+__global__ void __launch_bounds__(kStoreThreads)
+    sq_kv8_store_kernel(const __grid_constant__ Kv8StoreInlineArgs a) {
+    using C = NormCfg<D>;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int lane = threadIdx.x & 31;
+    const StoreTasks<D> per(a.Hq, a.Hkv, a.most);
+    const unsigned task = blockIdx.x * (kStoreThreads / 32) + (threadIdx.x >> 5);
+    const unsigned r = task / (unsigned)per.total;
+    if (r >= (unsigned)a.n_runs) return;
+    int part = (int)(task - r * per.total);
+    const RowRun run = a.runs ? a.runs[r] : a.inline_run[r];
+    const int sub = lane / C::kLanes, l = lane % C::kLanes;
+    Lane ln;
+    if (part >= 2 * a.Hkv) {
+        part -= 2 * a.Hkv;
+        const int i = part / per.q;
+        if (i >= run.n) return;
+        const int64_t t = run.first + i;
+        const int h0 = (part - i * per.q) * C::kGroups * kHeadRows, h = h0 + sub;
+        const int n_pass = min(kHeadRows, (a.Hq - h0 + C::kGroups - 1) / C::kGroups);
+        ln.init<kPairs>(l, a.rot);
+        const __nv_bfloat16* src = a.q + t * a.q_stride + (int64_t)h * D;
+        __nv_bfloat16* dst = a.q_out + (t * a.Hq + h) * D;
+        uint2 rf[kHeadRows], rg[kHeadRows];
+#pragma unroll
+        for (int u = 0; u < kHeadRows; ++u) {
+            rf[u] = rg[u] = make_uint2(0, 0);
+            if (h + u * C::kGroups < a.Hq) {
+                rf[u] = ld_half_row(src + u * C::kGroups * D + ln.f);
+                rg[u] = ld_half_row(src + u * C::kGroups * D + ln.g);
+            }
+        }
+        Turn tn;
+        int pos = a.positions ? __ldg(&a.positions[t]) : run.pos + i;
+        if (a.rot > 0) pos = checked_pos(pos, a.max_pos, a.err);
+        load_turn<kPairs>(tn, a.rope, pos, a.rot, ln);
+        Eight w;
+        load_weights(a.q_weight, a.weight_f32, ln, w);
+        f32x2 A[4], B[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            A[k] = mul2(w.v[k], tn.c[k]);
+            B[k] = mul2(w.other<kPairs>(k), tn.s[k]);
+        }
+#pragma unroll
+        for (int u = 0; u < kHeadRows; ++u) {
+            if (u >= n_pass) break;  // (warp-uniform)
+            Eight x;
+            x.set(rf[u], rg[u]);
+            f32x2 ss = mul2(x.v[0], x.v[0]);
+#pragma unroll
+            for (int k = 1; k < 4; ++k) ss = fma2(x.v[k], x.v[k], ss);
+            const float rs = rsqrtf(row_sum<D>(ss) * (1.f / D) + a.eps);
+            const f32x2 rr = f2(rs, rs);
+            uint32_t o[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                o[k] = pack2(mul2(fma2(x.v[k], A[k], ln.turned(mul2(x.other<kPairs>(k), B[k]))), rr));
+            if (h + u * C::kGroups < a.Hq) {
+                __nv_bfloat16* to = dst + u * C::kGroups * D;
+                *reinterpret_cast<uint2*>(to + ln.f) = make_uint2(o[0], o[1]);
+                *reinterpret_cast<uint2*>(to + ln.g) = make_uint2(o[2], o[3]);
+            }
+        }
+        return;
+    }
+    const bool is_v = part >= a.Hkv;
+    const int head = is_v ? part - a.Hkv : part;
+    const bool norm = !is_v && !a.plain;
+    const int lp = log2_of(a.pool.P);
+    const int64_t page = run.row >> lp;
+    const int s0 = run.row & (kScaleRows - 1), s1 = s0 + run.n;
+    if (run.row < 0 || page >= a.pool.num_pages || s1 > kScaleRows) {
+        if (lane == 0) set_error(a.err, kErrBounds);
+        return;
+    }
+    const int64_t row0 = plane_row(a.pool, a.layer + blockIdx.y, page, is_v, head) +
+                         ((run.row & (a.pool.P - 1)) - s0);
+    uint8_t* codes = a.pool.codes + row0 * D;
+    float* scale = a.pool.scales + row0 / kScaleRows;
+    const int64_t stride = is_v ? a.v_stride : a.k_stride;
+    const __nv_bfloat16* src = (is_v ? a.v : a.k) + blockIdx.y * a.layer_stride + run.first * stride + head * D;
+    ln.init<kPairs>(l, norm ? a.rot : 0);
+    constexpr int kPass = kScaleRows / C::kGroups;
+    // raw: a new row's 16 bytes of this lane, or 8 codes of one that is there
+    uint2 rf[kPass], rg[kPass];
+#pragma unroll
+    for (int u = 0; u < kPass; ++u) {
+        const int i = u * C::kGroups + sub;
+        rf[u] = rg[u] = make_uint2(0, 0);
+        if (i >= s0 && i < s1) {
+            rf[u] = ld_half_row(src + (i - s0) * stride + ln.f);
+            rg[u] = ld_half_row(src + (i - s0) * stride + ln.g);
+        } else if (i < s0) {
+            rf[u].x = *reinterpret_cast<const uint32_t*>(codes + i * D + ln.f);
+            rg[u].x = *reinterpret_cast<const uint32_t*>(codes + i * D + ln.g);
+        }
+    }
+    const float old = s0 > 0 ? *scale : 0.f;
+    Eight w;
+    if (norm) load_weights(a.k_weight, a.weight_f32, ln, w);
+    float4 xf[kPass], xg[kPass];
+    float size = 0.f;
+#pragma unroll
+    for (int u = 0; u < kPass; ++u) {
+        const int i = u * C::kGroups + sub;
+        const bool fresh = i >= s0 && i < s1;
+        if (norm) {
+            // (every lane: the sums are the warp's)
+            Turn tn;
+            int pos = 0;
+            if (fresh) {
+                pos = a.positions ? __ldg(&a.positions[run.first + i - s0]) : run.pos + i - s0;
+                if (a.rot > 0) pos = checked_pos(pos, a.max_pos, a.err);
+            }
+            load_turn<kPairs>(tn, a.rope, pos, a.rot, ln);
+            Eight x;
+            x.set(rf[u], rg[u]);
+            f32x2 ss = mul2(x.v[0], x.v[0]);
+#pragma unroll
+            for (int k = 1; k < 4; ++k) ss = fma2(x.v[k], x.v[k], ss);
+            const float rs = rsqrtf(row_sum<D>(ss) * (1.f / D) + a.eps);
+            const f32x2 rr = f2(rs, rs);
+            float2 o[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                o[k] = un2(mul2(fma2(x.v[k], mul2(w.v[k], tn.c[k]),
+                                     ln.turned(mul2(x.other<kPairs>(k), mul2(w.other<kPairs>(k), tn.s[k])))),
+                                rr));
+            xf[u] = make_float4(o[0].x, o[0].y, o[1].x, o[1].y);
+            xg[u] = make_float4(o[2].x, o[2].y, o[3].x, o[3].y);
+        } else {
+            xf[u] = unpack4(rf[u]);
+            xg[u] = unpack4(rg[u]);
+        }
+        if (i < s0) {
+            xf[u] = e4m3_values(rf[u].x, old);
+            xg[u] = e4m3_values(rg[u].x, old);
+        }
+        if (i < s1) size = fmaxf(size, fmaxf(finite_size(xf[u]), finite_size(xg[u])));
+    }
+    const int e = scale_exponent(warp_size(size));
+    const float s = power_of_two(e);
+#pragma unroll
+    for (int u = 0; u < kPass; ++u) {
+        const int i = u * C::kGroups + sub;
+        if (i >= s1 || (i < s0 && s == old)) continue;
+        *reinterpret_cast<uint32_t*>(codes + i * D + ln.f) = to_e4m3(xf[u], e);
+        *reinterpret_cast<uint32_t*>(codes + i * D + ln.g) = to_e4m3(xg[u], e);
+    }
+    if (lane == 0) *scale = s;
+}
+
+// ---- copies of pages' first rows (copy-on-write) --------------------------------
+constexpr int kCopyThreads = 128;
+
+__global__ void __launch_bounds__(kCopyThreads)
+    sq_kv8_copy_kernel(const __grid_constant__ Kv8CopyArgs a, int D) {
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (blockIdx.x == 0 && threadIdx.x < a.lens.n) *a.lens.ptr[threadIdx.x] = a.lens.val[threadIdx.x];
+    const int planes = a.L * 2 * a.pool.Hkv;
+    const int copy = blockIdx.x / planes, plane = blockIdx.x % planes;
+    if (copy >= a.n_cow) return;
+    const CowCopy c = a.cow[copy];
+    if ((uint64_t)c.src_page >= (uint64_t)a.pool.num_pages || (uint64_t)c.dst_page >= (uint64_t)a.pool.num_pages ||
+        c.rows < 0 || c.rows > a.pool.P) {
+        if (threadIdx.x == 0) set_error(a.err, kErrBounds);
+        return;
+    }
+    const int head = plane % a.pool.Hkv, kv = plane / a.pool.Hkv % 2, layer = plane / (2 * a.pool.Hkv);
+    const int64_t from = plane_row(a.pool, layer, c.src_page, kv, head);
+    const int64_t to = plane_row(a.pool, layer, c.dst_page, kv, head);
+    const uint4* x = reinterpret_cast<const uint4*>(a.pool.codes + from * D);
+    uint4* y = reinterpret_cast<uint4*>(a.pool.codes + to * D);
+    for (int i = threadIdx.x; i < c.rows * (D / 16); i += kCopyThreads) y[i] = x[i];
+    if (threadIdx.x < (c.rows + kScaleRows - 1) / kScaleRows)
+        a.pool.scales[to / kScaleRows + threadIdx.x] = a.pool.scales[from / kScaleRows + threadIdx.x];
+}
+
+// ---- rows as bf16 ------------------------------------------------------------------
+constexpr int kReadThreads = 256;
+constexpr int kReadUnroll = 4;   // eights of elements a thread has in flight
+
+__device__ __forceinline__ uint4 widen8(uint2 codes, float scale) {
+    const float4 a = e4m3_values(codes.x, scale), b = e4m3_values(codes.y, scale);
+    return make_uint4(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w), pack_bf16x2(b.x, b.y),
+                      pack_bf16x2(b.z, b.w));
+}
+
+// A thread to kReadUnroll eights of a run's elements in the order of the output; the
+// values of 8 bits are exact in bf16.
+template <int D>
+__global__ void __launch_bounds__(kReadThreads)
+    sq_kv8_read_kernel(const __grid_constant__ Kv8ReadInlineArgs a, int parts) {
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int part = blockIdx.x % parts, r = blockIdx.x / parts, kv = blockIdx.y;
+    const RowRun run = a.runs ? a.runs[r] : a.inline_run[r];
+    const Kv8Pool& p = a.pool;
+    const int64_t page = run.row >> log2_of(p.P);
+    const int slot = run.row & (p.P - 1);
+    if (run.row < 0 || page >= p.num_pages || slot + run.n > p.P) {
+        if (threadIdx.x == 0) set_error(a.err, kErrBounds);
+        return;
+    }
+    constexpr int kEights = D / 8;
+    const int64_t plane = plane_row(p, a.layer, page, kv, 0) + slot;
+    uint4* out = reinterpret_cast<uint4*>((kv ? a.v : a.k) + (int64_t)run.first * p.Hkv * D);
+    const int n = run.n * p.Hkv * kEights;
+    uint4 x[kReadUnroll];
+    float s[kReadUnroll];
+#pragma unroll
+    for (int u = 0; u < kReadUnroll; ++u) {
+        const int i = (part * kReadUnroll + u) * kReadThreads + threadIdx.x;
+        if (i >= n) continue;
+        const int row = i / kEights, t = row / p.Hkv, head = row - t * p.Hkv;
+        const int64_t at = plane + (int64_t)head * p.P + t;
+        if (p.codes) {
+            const uint2 c = *reinterpret_cast<const uint2*>(p.codes + at * D + i % kEights * 8);
+            x[u] = make_uint4(c.x, c.y, 0, 0);
+            s[u] = p.scales[at / kScaleRows];
+        } else {
+            x[u] = *reinterpret_cast<const uint4*>(a.wide + at * D + i % kEights * 8);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kReadUnroll; ++u) {
+        const int i = (part * kReadUnroll + u) * kReadThreads + threadIdx.x;
+        if (i < n) out[i] = p.codes ? widen8(make_uint2(x[u].x, x[u].y), s[u]) : x[u];
+    }
+}
+
+// Whole pages of one layer, a CTA to kReadThreads * kReadUnroll eights of a page.
+template <int D>
+__global__ void __launch_bounds__(kReadThreads)
+    sq_kv8_widen_kernel(const __grid_constant__ Kv8WidenArgs a, int parts) {
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int part = blockIdx.x % parts, i0 = blockIdx.x / parts;
+    int64_t page = a.pages[i0];
+    if (page < 0 || page >= a.pool.num_pages) {
+        if (threadIdx.x == 0) set_error(a.err, kErrBounds);
+        page = 0;
+    }
+    constexpr int kEights = D / 8;
+    const int n = 2 * a.pool.Hkv * a.pool.P * kEights;
+    const int64_t row0 = plane_row(a.pool, a.layer, page, 0, 0);
+    uint4* out = reinterpret_cast<uint4*>(a.out) + (int64_t)i0 * n;
+    uint2 x[kReadUnroll];
+    float s[kReadUnroll];
+#pragma unroll
+    for (int u = 0; u < kReadUnroll; ++u) {
+        const int i = (part * kReadUnroll + u) * kReadThreads + threadIdx.x;
+        if (i >= n) continue;
+        x[u] = *(reinterpret_cast<const uint2*>(a.pool.codes + row0 * D) + i);
+        s[u] = a.pool.scales[(row0 + i / kEights) / kScaleRows];
+    }
+#pragma unroll
+    for (int u = 0; u < kReadUnroll; ++u) {
+        const int i = (part * kReadUnroll + u) * kReadThreads + threadIdx.x;
+        if (i < n) out[i] = widen8(x[u], s[u]);
+    }
+}
+
+// ---- eviction --------------------------------------------------------------------
+// A CTA takes one plane's tiles of a chunk in order: a tile's rows (all that a page
+// gets) are read into shared memory, then written block by block, with the scale of
+// the rows that are together now.  The tile after it is read before, which in-place
+// compaction allows: rows only move towards the front.
+constexpr int kEvictThreads = 256;
+
+template <int D>
+__global__ void __launch_bounds__(kEvictThreads)
+    sq_kv8_evict_kernel(const __grid_constant__ Kv8EvictArgs a) {
+    grid_dependency_wait();
+    grid_launch_dependents();
+    extern __shared__ uint4 tile_smem[];
+    const Kv8Pool& p = a.pool;
+    const int P = p.P;
+    const int planes = a.L * 2 * p.Hkv;
+    const int plane = blockIdx.x % planes, chunk = blockIdx.x / planes;
+    const int head = plane % p.Hkv, kv = plane / p.Hkv % 2, layer = plane / (2 * p.Hkv);
+    constexpr int kVecs = D / 16;
+    // two tiles: rows, then their scales
+    const int tile_bytes = P * (D + 4);
+    auto rows_of = [&](int b) { return reinterpret_cast<uint8_t*>(tile_smem) + b * tile_bytes; };
+    auto scales_of = [&](int b) { return reinterpret_cast<float*>(rows_of(b) + P * D); };
+    const int t0 = a.chunk[chunk], t1 = a.chunk[chunk + 1];
+    // the tile's rows, row i of it where its slot's is
+    auto read = [&](int t, int b) {
+        if (t < t1) {
+            const EvictTile tile = a.tiles[t];
+            const int end = t + 1 < a.n_tiles ? a.tiles[t + 1].piece_begin : a.n_pieces;
+            for (int k = tile.piece_begin; k < end; ++k) {
+                const EvictPiece pc = a.pieces[k];
+                const int to = tile.dst_slot + pc.dst_row;
+                if ((uint64_t)pc.src_page >= (uint64_t)p.num_pages || pc.src_slot + pc.n_rows > P ||
+                    to + pc.n_rows > P) {
+                    if (threadIdx.x == 0) set_error(a.err, kErrBounds);
+                    continue;
+                }
+                const int64_t from = plane_row(p, layer, pc.src_page, kv, head) + pc.src_slot;
+                const uint32_t dst = smem_addr(rows_of(b) + to * D);
+                const uint8_t* src = p.codes + from * D;
+                for (int i = threadIdx.x; i < pc.n_rows * kVecs; i += kEvictThreads)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + 16 * i),
+                                 "l"(src + 16 * i)
+                                 : "memory");
+                const uint32_t sdst = smem_addr(scales_of(b) + to);
+                for (int i = threadIdx.x; i < pc.n_rows; i += kEvictThreads)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(sdst + 4 * i),
+                                 "l"(p.scales + (from + i) / kScaleRows)
+                                 : "memory");
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    read(t0, 0);
+    for (int t = t0; t < t1; ++t) {
+        const int b = (t - t0) & 1;
+        read(t + 1, b ^ 1);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncthreads();
+        const EvictTile tile = a.tiles[t];
+        const int end = t + 1 < a.n_tiles ? a.tiles[t + 1].piece_begin : a.n_pieces;
+        const bool zero = tile.piece_begin == end;
+        if ((uint64_t)tile.dst_page >= (uint64_t)p.num_pages || tile.dst_slot + tile.n_rows > P) {
+            if (threadIdx.x == 0) set_error(a.err, kErrBounds);
+        } else {
+            const int64_t page_row = plane_row(p, layer, tile.dst_page, kv, head);
+            const int r0 = tile.dst_slot, r1 = tile.dst_slot + tile.n_rows;
+            const int lane = threadIdx.x & 31;
+            constexpr int kRowLanes = D / 16;              // 16 codes a lane
+            constexpr int kRows = 32 / kRowLanes;          // rows of a warp at once
+            constexpr int kPass = kScaleRows / kRows;
+            for (int blk = r0 / kScaleRows + (threadIdx.x >> 5); blk * kScaleRows < r1;
+                 blk += kEvictThreads / 32) {
+                uint8_t* codes = p.codes + (page_row + blk * kScaleRows) * D;
+                float* scale = p.scales + (page_row / kScaleRows + blk);
+                if (zero) {
+                    // a block that keeps rows keeps its scale
+                    for (int u = 0; u < kPass; ++u) {
+                        const int row = blk * kScaleRows + u * kRows + lane / kRowLanes;
+                        if (row >= r0 && row < r1)
+                            *reinterpret_cast<uint4*>(codes + (row - blk * kScaleRows) * D + lane % kRowLanes * 16) =
+                                make_uint4(0, 0, 0, 0);
+                    }
+                    if (lane == 0 && blk * kScaleRows >= r0) *scale = power_of_two(kLeastScale);
+                    continue;
+                }
+                // rows before the tile's first stay where they are
+                uint4 c[kPass];
+                float s[kPass], size = 0.f;
+                const float old = blk * kScaleRows < r0 ? *scale : 0.f;
+#pragma unroll
+                for (int u = 0; u < kPass; ++u) {
+                    const int i = u * kRows + lane / kRowLanes, row = blk * kScaleRows + i;
+                    c[u] = make_uint4(0, 0, 0, 0);
+                    s[u] = old;
+                    if (row >= r1) continue;
+                    if (row < r0) {
+                        c[u] = *reinterpret_cast<const uint4*>(codes + i * D + lane % kRowLanes * 16);
+                    } else {
+                        c[u] = *reinterpret_cast<const uint4*>(rows_of(b) + row * D + lane % kRowLanes * 16);
+                        s[u] = scales_of(b)[row];
+                    }
+                    const uint32_t cw[4] = {c[u].x, c[u].y, c[u].z, c[u].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) size = fmaxf(size, finite_size(e4m3_values(cw[k], s[u])));
+                }
+                const int e = scale_exponent(warp_size(size));
+                const float now = power_of_two(e);
+#pragma unroll
+                for (int u = 0; u < kPass; ++u) {
+                    const int i = u * kRows + lane / kRowLanes, row = blk * kScaleRows + i;
+                    if (row >= r1 || (row < r0 && now == old)) continue;
+                    if (s[u] != now) {
+                        c[u].x = to_e4m3(e4m3_values(c[u].x, s[u]), e);
+                        c[u].y = to_e4m3(e4m3_values(c[u].y, s[u]), e);
+                        c[u].z = to_e4m3(e4m3_values(c[u].z, s[u]), e);
+                        c[u].w = to_e4m3(e4m3_values(c[u].w, s[u]), e);
+                    }
+                    *reinterpret_cast<uint4*>(codes + i * D + lane % kRowLanes * 16) = c[u];
+                }
+                if (lane == 0) *scale = now;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <typename... P, typename... A>
+cudaError_t launch_after(void (*kernel)(P...), dim3 grid, unsigned block, int smem, cudaStream_t st,
+                         const A&... args) {
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int D>
+cudaError_t store(const Kv8StoreInlineArgs& a, cudaStream_t st) {
+    const int64_t warps = (int64_t)a.n_runs * StoreTasks<D>(a.Hq, a.Hkv, a.most).total;
+    constexpr int per = kStoreThreads / 32;
+    const dim3 grid((unsigned)((warps + per - 1) / per), (unsigned)a.n_layers);
+    return launch_after(a.interleaved ? sq_kv8_store_kernel<D, true> : sq_kv8_store_kernel<D, false>, grid,
+                        kStoreThreads, 0, st, a);
+}
+
+int evict_smem(int P, int D) { return 2 * P * (D + 4); }
+
+}  // namespace
+
+cudaError_t kv8_prepare(int D) {
+    return D == 128 ? cudaFuncSetAttribute(sq_kv8_evict_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                           evict_smem(256, 128))
+                    : cudaFuncSetAttribute(sq_kv8_evict_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                           evict_smem(256, 64));
+}
+
+cudaError_t launch_kv8_store(const Kv8StoreInlineArgs& a, int D, cudaStream_t st) {
+    if (a.n_runs == 0) return cudaSuccess;
+    return D == 128 ? store<128>(a, st) : store<64>(a, st);
+}
+
+cudaError_t launch_kv8_copy(const Kv8CopyArgs& a, int D, cudaStream_t st) {
+    const unsigned grid = std::max(1u, (unsigned)a.n_cow * a.L * 2 * a.pool.Hkv);
+    return launch_after(sq_kv8_copy_kernel, dim3(grid), kCopyThreads, 0, st, a, D);
+}
+
+cudaError_t launch_kv8_read(const Kv8ReadInlineArgs& a, int D, cudaStream_t st) {
+    if (a.n_runs == 0) return cudaSuccess;
+    const int eights = a.most * a.pool.Hkv * (D / 8), per = kReadThreads * kReadUnroll;
+    const int parts = (eights + per - 1) / per;
+    const dim3 grid((unsigned)a.n_runs * parts, 2);
+    return launch_after(D == 128 ? sq_kv8_read_kernel<128> : sq_kv8_read_kernel<64>, grid, kReadThreads, 0, st, a,
+                        parts);
+}
+
+cudaError_t launch_kv8_widen(const Kv8WidenArgs& a, int D, cudaStream_t st) {
+    if (a.n == 0) return cudaSuccess;
+    const int eights = 2 * a.pool.Hkv * a.pool.P * (D / 8), per = kReadThreads * kReadUnroll;
+    const int parts = (eights + per - 1) / per;
+    return launch_after(D == 128 ? sq_kv8_widen_kernel<128> : sq_kv8_widen_kernel<64>, dim3((unsigned)a.n * parts),
+                        kReadThreads, 0, st, a, parts);
+}
+
+cudaError_t launch_kv8_evict(const Kv8EvictArgs& a, int D, cudaStream_t st) {
+    const dim3 grid((unsigned)a.n_chunks * a.L * 2 * a.pool.Hkv);
+    return launch_after(D == 128 ? sq_kv8_evict_kernel<128> : sq_kv8_evict_kernel<64>, grid, kEvictThreads,
+                        evict_smem(a.pool.P, D), st, a);
+}
+
+}  // namespace sq
