@@ -24,6 +24,7 @@ NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-use_fast_math", "-Xcompiler", 
 
 LIBSQ_SOURCES = [
     "kernels/blocks.cu",
+    "kernels/blocks_kv8.cu",
     "kernels/decode.cu",
     "kernels/kv.cu",
     "kernels/kv8.cu",

@@ -544,14 +544,18 @@ int norm_backward_impl(sq_cache* c, int32_t n_tokens, const void* q, int64_t q_s
     return e != cudaSuccess ? cuda_status(e) : rc;
 }
 
-// The pages of a plan as bf16, in the order of its list, as a pool of one layer.
+// The pages of a plan as bf16, in the order of its list, as a pool of one layer.  Blocks
+// of two query tiles are the tensor cores' bound, and every page serves many of them:
+// it is widened once, before them (the kernel's own converters took as long as its
+// products twice over: 512 queries over 60,001 tokens, 32/8 heads of 128, 796 us against
+// 430 with the pages widened first).
 int widen_pages(sq_cache* c, const BlockPlanEntry& plan, int32_t layer, cudaStream_t st, bool captured,
                 CUtensorMap* map) {
     const Geometry& g = c->g;
     const size_t page = (size_t)2 * g.Hkv * g.P * g.D * sizeof(__nv_bfloat16);
-    int rc = take_buffer(c, c->wide, std::max(1, plan.n_wide) * page, st, captured);
+    int rc = take_buffer(c, c->wide, plan.n_wide * page, st, captured);
     if (rc != SQ_OK) return rc;
-    rc = make_pool_map(c, c->wide.d, std::max(1, plan.n_wide), 1, map);
+    rc = make_pool_map(c, c->wide.d, 2, 64, plan.n_wide, 1, map);
     if (rc != SQ_OK) return rc;
     Kv8WidenArgs a;
     a.pool = kv8_pool(c);
@@ -643,11 +647,12 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
             if (rc == SQ_ERR_NO_MEMORY) rc = plan_blocks(g, in, window, n_sink, c->num_sms, 0, &plan);
         }
         if (rc != SQ_OK) return rc;
-        // (8-bit caches) the pages, which the tiles then name by their places
-        std::vector<int32_t> wide, read;
+        std::vector<int32_t> read, wide;
         for (int32_t p : plan.tile_pages)
             if (p >= 0 && (read.empty() || read.back() != p)) read.push_back(p);
-        if (c->kv8) {
+        // (8-bit caches, blocks of two tiles) the pages are widened for the call; its
+        // tiles name them by their places in the list
+        if (c->kv8 && !plan.one) {
             std::unordered_map<int32_t, int32_t> place;
             for (int32_t& p : plan.tile_pages) {
                 if (p < 0) continue;
@@ -749,28 +754,29 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
         }
         c->pre_last = hit;
     }
+    const bool wide = plan.n_wide > 0;
     CUtensorMap qmap, wide_map;
     rc = make_query_map(c, q, (int32_t)n, plan.BP, &qmap);
-    if (rc == SQ_OK && c->kv8) rc = widen_pages(c, plan, layer, st, captured, &wide_map);
+    if (rc == SQ_OK && wide) rc = widen_pages(c, plan, layer, st, captured, &wide_map);
     if (rc != SQ_OK) return drop_plan(*hit, st, rc);
-    BlockShortArgs a;
+    BlockShortKv8Args a;
     a.tiles = reinterpret_cast<const PrefillTile*>(plan.d);
     a.items = reinterpret_cast<const PrefillItem*>(plan.d + plan.o_items);
     a.tile_pages = reinterpret_cast<const int32_t*>(plan.d + plan.o_pages);
     a.rows = plan.o_rows ? reinterpret_cast<const int2*>(plan.d + plan.o_rows) : nullptr;
     a.bits = reinterpret_cast<const uint32_t*>(plan.d + plan.o_bits);
     a.n_words = plan.n_words;
-    a.pool = c->kv8 ? (const void*)c->wide.d : c->pool;
+    a.pool = wide ? (const void*)c->wide.d : c->pool;
     a.q = q;
     a.n_ctas = plan.n_ctas;
     a.n_pieces = plan.n_pieces;
     a.n_tiles = a.n = a.n_q = 0;  // (the items')
-    a.layer = c->kv8 ? 0 : layer;
+    a.layer = wide ? 0 : layer;
     a.Hq = g.Hq;
     a.Hkv = g.Hkv;
     a.G = g.G();
     a.P = g.P;
-    a.num_pages = c->kv8 ? plan.n_wide : g.num_pages;
+    a.num_pages = wide ? plan.n_wide : g.num_pages;
     a.BP = plan.BP;
     a.n_items = plan.n_items;
     a.plan_ready = plan_ready;
@@ -788,8 +794,10 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
     a.part_ml = c->pre_part ? c->pre_part + (size_t)plan.n_parts * kPrefillQTiles * kPrefillRows * g.D
                             : nullptr;
     a.err = c->d_err;
-    e = launch_blocks(c->kv8 ? wide_map : c->tmap, qmap, a, g.D, plan.one, st);
-    if (c->kv8) rc = used_buffer(c->wide, st, captured);
+    a.scales = c->kv8 ? kv8_pool(c).scales : nullptr;
+    e = c->kv8 && !wide ? launch_blocks_kv8(c->tmap, qmap, a, g.D, st)
+                        : launch_blocks(wide ? wide_map : c->tmap, qmap, a, g.D, plan.one, st);
+    if (wide) rc = used_buffer(c->wide, st, captured);
     if (rc != SQ_OK) return drop_plan(*hit, st, rc);
     if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
     if (plan.n_merges > 0) {

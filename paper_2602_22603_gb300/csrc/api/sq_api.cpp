@@ -112,7 +112,8 @@ struct BlockPlanEntry : PrefillPlanEntry {
     size_t o_rows = 0, o_bits = 0;  // (o_rows 0: no table)
     int32_t n_words = 0, unit_rows = 0, n_ctas = 0;
     bool one = false;
-    // (8-bit caches) the plan's pages, which its tiles name by their place in the list
+    // (8-bit caches, blocks of two tiles) the plan's pages, which its tiles name by
+    // their place in the list; 0: they name pages of the pool
     size_t o_wide = 0;
     int32_t n_wide = 0;
 };
@@ -202,7 +203,7 @@ struct sq_cache {
     std::deque<StorePlanEntry> store_plans = std::deque<StorePlanEntry>(kStorePlanEntries);
     TurnBuffer norm_part;  // partial gradients of the norms' weights
     bool kv8 = false;      // rows are held in 8 bits (Kv8Pool)
-    TurnBuffer wide;       // (8-bit caches) a query-block call's pages as bf16
+    TurnBuffer wide;       // (8-bit caches) pages of a query-block call as bf16
     std::vector<void*> retired;  // outgrown buffers that captured launches were given
     uint64_t use_clock = 0;
     UploadSlot slots[kUploadSlots];
@@ -289,35 +290,22 @@ int64_t token_bytes(const sq_cache* c) {
                   : c->g.token_layer_bytes();
 }
 
-// bf16 rows as a pool of `pages` pages: dims, innermost first: head dim, row within a
-// (layer, page) block ((kv * Hkv + head) * P + slot), page, layer
-int make_pool_map(sq_cache* c, void* pool, int32_t pages, int32_t layers, CUtensorMap* map) {
+// Rows of `elem` bytes an element as a pool, dims innermost first: head dim, row within
+// a (layer, page) block ((kv * Hkv + head) * P + slot), page, layer.  A box has `cols`
+// elements of its rows: 64 of bf16, or all of codes (128 bytes, or 64, whose 16-byte
+// chunks are swizzled over 64).
+int make_pool_map(const sq_cache* c, void* pool, int elem, int cols, int32_t pages, int32_t layers,
+                  CUtensorMap* map) {
     auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(c->encode_fn);
     const Geometry& g = c->g;
+    const cuuint64_t row = (cuuint64_t)g.D * elem, block = 2 * g.Hkv * g.P * row;
     cuuint64_t dims[4] = {(cuuint64_t)g.D, (cuuint64_t)2 * g.Hkv * g.P, (cuuint64_t)pages, (cuuint64_t)layers};
-    cuuint64_t strides[3] = {(cuuint64_t)g.D * 2, (cuuint64_t)2 * g.Hkv * g.P * g.D * 2,
-                             (cuuint64_t)pages * 2 * g.Hkv * g.P * g.D * 2};
-    cuuint32_t box[4] = {64, (cuuint32_t)std::min(g.P, kStageTokens), 1, 1};
+    cuuint64_t strides[3] = {row, block, pages * block};
+    cuuint32_t box[4] = {(cuuint32_t)cols, (cuuint32_t)std::min(g.P, kStageTokens), 1, 1};
     cuuint32_t estr[4] = {1, 1, 1, 1};
-    CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, pool, dims, strides, box, estr,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? SQ_OK : SQ_ERR_UNSUPPORTED;
-}
-
-// The codes of an 8-bit cache, the same dims: a box has whole rows, 128 bytes or 64
-// (whose 16-byte chunks are swizzled over 64).
-int make_code_map(sq_cache* c) {
-    auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(c->encode_fn);
-    const Geometry& g = c->g;
-    cuuint64_t dims[4] = {(cuuint64_t)g.D, (cuuint64_t)2 * g.Hkv * g.P, (cuuint64_t)g.num_pages, (cuuint64_t)g.L};
-    cuuint64_t strides[3] = {(cuuint64_t)g.D, (cuuint64_t)2 * g.Hkv * g.P * g.D,
-                             (cuuint64_t)g.num_pages * 2 * g.Hkv * g.P * g.D};
-    cuuint32_t box[4] = {(cuuint32_t)g.D, (cuuint32_t)std::min(g.P, kStageTokens), 1, 1};
-    cuuint32_t estr[4] = {1, 1, 1, 1};
-    CUresult r = encode(&c->tmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, c->pool, dims, strides, box, estr,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        g.D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+    CUresult r = encode(map, elem == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, pool,
+                        dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        cols * elem == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? SQ_OK : SQ_ERR_UNSUPPORTED;
 }
@@ -330,8 +318,7 @@ int make_tensor_map(sq_cache* c) {
         q != cudaDriverEntryPointSuccess || !fn)
         return SQ_ERR_CUDA;
     c->encode_fn = fn;
-    if (c->kv8) return make_code_map(c);
-    return make_pool_map(c, c->pool, c->g.num_pages, c->g.L, &c->tmap);
+    return make_pool_map(c, c->pool, c->kv8 ? 1 : 2, c->kv8 ? c->g.D : 64, c->g.num_pages, c->g.L, &c->tmap);
 }
 
 // Queries {D, Hq, n_q}: one box is the G heads of a KV head x BP positions.
@@ -720,6 +707,7 @@ static int create_impl(const sq_config* cfg, bool kv8, sq_cache** out) {
     }
     if (kv8) {
         e = kv8_prepare(g.D);
+        if (e == cudaSuccess) e = blocks_kv8_prepare(g.D);
         if (e != cudaSuccess) return cuda_status(e);
     }
     choose_evict_shape(c.get());

@@ -100,6 +100,15 @@ struct DecodeKv8Args : DecodeArgs {
 SQ_OPTIONAL cudaError_t launch_decode_kv8(const CUtensorMap& tmap, const DecodeKv8Args& a, int n_ctas, int D,
                                           cudaStream_t st);
 
+// Query blocks of one tile over such rows, as BlockShortArgs and BlockShortArgs2.
+struct BlockShortKv8Args : BlockShortArgs {
+    const float* scales;
+};
+struct BlockShortKv8Args2 : BlockShortKv8Args {};
+SQ_OPTIONAL cudaError_t blocks_kv8_prepare(int D);
+SQ_OPTIONAL cudaError_t launch_blocks_kv8(const CUtensorMap& pool_map, const CUtensorMap& qmap,
+                                          const BlockShortKv8Args& a, int D, cudaStream_t st);
+
 SQ_OPTIONAL cudaError_t kv8_prepare(int D);
 SQ_OPTIONAL cudaError_t launch_kv8_store(const Kv8StoreInlineArgs& a, int D, cudaStream_t st);
 SQ_OPTIONAL cudaError_t launch_kv8_copy(const Kv8CopyArgs& a, int D, cudaStream_t st);

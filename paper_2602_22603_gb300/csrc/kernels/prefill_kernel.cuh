@@ -82,6 +82,7 @@
 
 #include <type_traits>
 
+#include "e4m3.cuh"
 #include "operators.hpp"
 #include "ptx.cuh"
 #include "tc.cuh"
@@ -97,7 +98,8 @@ namespace {
 // are two producer warps': on pages of fewer than 64 tokens, which take many boxes,
 // and one-tile blocks of 64 dimensions, whose loads are short.  kHides: prefill of a
 // sequence whose hidden rows may hold anything (zero_hidden_values).
-constexpr int kOneTile = 1, kBlocks = 2, kTwoProducers = 4, kHides = 8;
+// kE8: rows in 8 bits (convert_tiles).
+constexpr int kOneTile = 1, kBlocks = 2, kTwoProducers = 4, kHides = 8, kE8 = 16;
 template <int M>
 constexpr bool one_tile = (M & kOneTile) != 0;
 template <int M>
@@ -106,6 +108,8 @@ template <int M>
 constexpr bool hides = (M & kHides) != 0;
 template <int M>
 constexpr int producers = (M & kTwoProducers) != 0 ? 2 : 1;
+template <int M>
+constexpr bool e8 = (M & kE8) != 0;
 
 // S buffers: one for each softmax warpgroup, and a third for one-tile blocks of 64
 // dimensions, whose O leaves the columns (S_2 after O_b).  With two a warpgroup that has handed over
@@ -113,25 +117,31 @@ constexpr int producers = (M & kTwoProducers) != 0 ? 2 : 1;
 // QK is done by then.  8 trees of 16 over 32,768 tokens, 64/8/64 heads, pages of 32:
 // 121 -> 107 us by an issuing lane that waits for P alone, 100 with the third buffer.
 template <int D, int M>
-constexpr int s_buffers = D == 64 && M == (kBlocks | kOneTile | kTwoProducers) ? 3 : 2;
+constexpr int s_buffers = D == 64 && (M & ~kE8) == (kBlocks | kOneTile | kTwoProducers) ? 3 : 2;
 
 // Items in flight between the producer and the other roles, and the warps that
 // read each (MMA warp and eight softmax warps).
 constexpr int kItemSlots = 4;
 constexpr int kItemReaders = 9;
+constexpr int kConverters = 8;  // warps that widen tiles (kE8), a warp to 16 rows
 constexpr int kProducer2 = 10;  // query blocks: the warp of their odd loads
 
 template <int D, int M>
 struct PreCfg {
-    static constexpr int kThreads = 320 + 32 * (producers<M> - 1);
+    static constexpr int kThreads = e8<M> ? 640 : 320 + 32 * (producers<M> - 1);
     static constexpr int kColBlocks = D / 64;                  // 64-column (128-byte) blocks
     static constexpr int kBlockBytes = kPrefillRows * 128;      // one block of a 128-row tile
     static constexpr int kQBytes = kColBlocks * kBlockBytes;    // one query tile
     static constexpr int kSlotBytes = kColBlocks * kBlockBytes;  // 128 keys of K or of V
-    static constexpr int kSlots = D == 128 ? 5 : 12;
+    static constexpr int kSlots = e8<M> ? (D == 128 ? 6 : 8) : (D == 128 ? 5 : 12);
+    // (8 bits) where a tile's codes land: rows of 128 in the second half of its slot,
+    // where the converter of a row writes what it has read; of 64 in space of their own
+    static constexpr int kCodeStride = D == 128 ? kSlotBytes : kPrefillKeys * D;
+    static constexpr int kTileScales = e8<M> ? kPrefillKeys / kScaleRows : 0;
     static constexpr int kOffQ = 0;
     static constexpr int kOffRing = kOffQ + (one_tile<M> ? 1 : kPrefillQTiles) * kQBytes;
-    static constexpr int kOffBar = kOffRing + kSlots * kSlotBytes;
+    static constexpr int kOffCodes = kOffRing + (D == 128 ? kBlockBytes : kSlots * kSlotBytes);
+    static constexpr int kOffBar = kOffRing + kSlots * (kSlotBytes + (e8<M> && D == 64 ? kCodeStride : 0));
     static constexpr int kBarQ = 0;
     static constexpr int kBarFull = 1;                  // [kSlots] tile landed (V: and ready)
     static constexpr int kBarEmpty = kBarFull + kSlots; // [kSlots] slot consumed by the MMAs
@@ -148,14 +158,22 @@ struct PreCfg {
     static constexpr int kBarClc = kBarItemFree + kItemSlots;   // answer of the launch hardware
     static constexpr int kBarX = kBarClc + 1;           // dual-key mode: tile b's half handed over
     static constexpr int kBarXFree = kBarX + 1;         // ... and read by tile a
-    static constexpr int kNumBars = kBarXFree + 1;
+    static constexpr int kBarRaw = kBarXFree + 1;       // (8 bits) [kSlots] codes and scales landed
+    static constexpr int kNumBars = kBarRaw + (e8<M> ? kSlots : 0);
     static constexpr int kItemBytes = of_blocks<M> ? (int)sizeof(BlockItem) : (int)sizeof(PrefillItem);
     static constexpr int kOffItems = (kOffBar + kNumBars * 8 + 15) & ~15;  // [kItemSlots] items
     static constexpr int kOffClc = kOffItems + kItemSlots * kItemBytes;   // 16-byte answer
     static constexpr int kOffMisc = kOffClc + 16;
     // dual-key mode: tile b's (max, normaliser) of each row, for the merge
     static constexpr int kOffXchg = (kOffMisc + 32 + 15) & ~15;
-    static constexpr int kSmemBytes = kOffXchg + kPrefillRows * 8 + 1024;  // + alignment slack
+    // (8 bits) each slot's scales, and the rows of its tile that are the sequence's
+    static constexpr int kOffScales = kOffXchg + kPrefillRows * 8;
+    static constexpr int kOffRows = kOffScales + kSlots * kTileScales * 4;
+    static constexpr int kSmemBytes = kOffRows + (e8<M> ? kSlots * 4 : 0) + 1024;  // + alignment slack
+    // registers of a thread (8 bits; see the kernel): softmax warps, converters, others
+    static constexpr int kSoftmaxRegs = 152, kConvertRegs = 48, kOtherRegs = 72;
+    static constexpr int kAllRegs = 256 * kSoftmaxRegs + 32 * kConverters * kConvertRegs + 128 * kOtherRegs;
+    static_assert(!e8<M> || kThreads * 96 >= kAllRegs, "register split");
     static constexpr uint32_t kTmemCols = 512;
     static constexpr uint32_t kColS = 0;    // S_t (fp32) at 128 t; P_t (bf16 pairs) over its first 64
     static constexpr uint32_t kColO = 256;  // O_t (fp32) at 256 + 128 t
@@ -812,7 +830,7 @@ __device__ void block_produce(const CUtensorMap* pool_map, const CUtensorMap* qm
             load_of<s_buffers<D, M>>(min(x0 + mine, T - 1) * kWarps + w, it.T, it.dual, j, kv);
             const bool box = cur.page >= 0;
             const uint32_t boxes = __ballot_sync(0xffffffffu, box) >> (mine * per) & group;
-            const uint32_t bytes = (uint32_t)__popc(boxes) * br * 128 * C::kColBlocks;
+            const uint32_t bytes = (uint32_t)__popc(boxes) * br * (e8<M> ? D : 128 * C::kColBlocks);
             const int rows = box ? min(br, n - cur.key) : 0;  // rows of the sequence in the box
             // V of the sequence's last key tile (an odd load): its rows past the end
             // are zeroed
@@ -840,16 +858,45 @@ __device__ void block_produce(const CUtensorMap* pool_map, const CUtensorMap* qm
                         if (!ok) break;
                     }
                     own = own << 1 | (it.dual || (x & 1) || x == 0 ? 1u : 0u);
-                    const uint32_t fix = fixes >> (b * per) & group;
-                    const uint32_t bar = fix ? sm.bar<D, M>(C::kBarVfix) : sm.bar<D, M>(C::kBarFull + slot);
+                    const uint32_t fix = e8<M> ? 0u : fixes >> (b * per) & group;
+                    const uint32_t bar = e8<M> ? sm.bar<D, M>(C::kBarRaw + slot)
+                                         : fix ? sm.bar<D, M>(C::kBarVfix)
+                                               : sm.bar<D, M>(C::kBarFull + slot);
+                    if constexpr (e8<M>) {
+                        // (the converters zero the rows of V that the bf16 instances' fix does)
+                        const int r0 = __reduce_add_sync(0xffffffffu, mine == b ? rows : 0);
+                        if (mine == b && piece == 0)
+                            *reinterpret_cast<volatile int*>(sm.ptr + C::kOffRows + 4 * slot) =
+                                kv == 1 ? r0 : kPrefillKeys;
+                        // a lane to the scale of eight rows, whose box is lane `from`'s
+                        const int from = b * per + lane * kScaleRows / br;
+                        const int32_t spage = __shfl_sync(0xffffffffu, page, from & 31);
+                        const int skey = __shfl_sync(0xffffffffu, cur.key, from & 31);
+                        const int skv = __shfl_sync(0xffffffffu, kv, from & 31);
+                        if (lane < C::kTileScales) {
+                            if (spage >= 0) {
+                                const int at = (skey & (a.P - 1)) + lane * kScaleRows % br;
+                                const int64_t plane =
+                                    (((int64_t)a.layer * a.num_pages + spage) * 2 + skv) * a.Hkv + it.g;
+                                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(
+                                                 sm.base + C::kOffScales + (slot * C::kTileScales + lane) * 4),
+                                             "l"(a.scales + (plane * a.P + at) / kScaleRows)
+                                             : "memory");
+                            }
+                            // (arrives when this lane's copy has landed)
+                            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar)
+                                         : "memory");
+                        }
+                    }
                     if (mine == b) {
                         if (piece == 0) mbar_arrive_expect_tx(bar, bytes);
                         __syncwarp(group << (b * per));
                         if (box) {
                             const uint32_t dst =
-                                sm.base + C::kOffRing + slot * C::kSlotBytes + piece * br * 128;
+                                e8<M> ? sm.base + C::kOffCodes + slot * C::kCodeStride + piece * br * D
+                                      : sm.base + C::kOffRing + slot * C::kSlotBytes + piece * br * 128;
 #pragma unroll
-                            for (int cb = 0; cb < C::kColBlocks; ++cb)
+                            for (int cb = 0; cb < (e8<M> ? 1 : C::kColBlocks); ++cb)
                                 tma_load_4d(dst + cb * C::kBlockBytes, pool_map, bar, cb * 64, row, page,
                                             a.layer);
                         }
@@ -911,8 +958,76 @@ __device__ void block_produce(const CUtensorMap* pool_map, const CUtensorMap* qm
         for (uint32_t x = total > C::kSlots ? (total - C::kSlots + kWarps - 1 - w) / kWarps : 0; x < issued; ++x) {
             const uint32_t U = kWarps * x + w;
             if (tail_open && x + 1 == issued) mbar_wait(sm.bar<D, M>(C::kBarVfix), n_fix & 1);
-            else mbar_wait(sm.bar<D, M>(C::kBarFull + U % C::kSlots), (U / C::kSlots) & 1);
+            else mbar_wait(sm.bar<D, M>((e8<M> ? C::kBarRaw : C::kBarFull) + U % C::kSlots), (U / C::kSlots) & 1);
         }
+    }
+}
+
+// Registers of each of a warpgroup's threads from here on.
+template <int N, bool kMore>
+__device__ __forceinline__ void take_registers() {
+    if constexpr (kMore) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// Rows in 8 bits: the converters widen a tile's codes to bf16 where the products read
+// them: code times scale, exact, so that everything behind is as for bf16 rows.  A
+// thread takes half a row (a warp whole rows, which it has read before it writes).  V
+// rows past the sequence's end are zeroed, as the bf16 instances' producer does.
+template <int D, int M>
+__device__ void convert_tiles(const Smem& sm, int* err, volatile int* abort_flag, int w, int lane) {
+    using C = PreCfg<D, M>;
+    constexpr int kVecs = D / 32;  // 16 codes each
+    const int row = w * 16 + (lane & 15), half = lane >> 4;
+    const int turn = D == 128 ? row & 7 : row >> 1 & 3;  // (the tensor map's swizzle)
+    uint32_t slot = 0, phase = 0;
+    bool ok = true;
+    for (uint32_t k = 0; ok; ++k) {
+        ok = __all_sync(0xffffffffu, item_wait<D, M>(sm, k, abort_flag));
+        if (!ok) break;
+        const int T = item_read<D, M>(sm, k).z;
+        __syncwarp();
+        if (lane == 0) item_free<D, M>(sm, k);
+        if (T < 0) break;
+        for (int x = 0; x < 2 * T; ++x) {
+            ok = __all_sync(0xffffffffu, mbar_wait(sm.bar<D, M>(C::kBarRaw + slot), phase, abort_flag));
+            if (!ok) break;
+            const uint8_t* src = sm.ptr + C::kOffCodes + slot * C::kCodeStride + row * D;
+            uint4 c[kVecs];
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+                c[i] = *reinterpret_cast<const uint4*>(src + (((half * kVecs + i) ^ turn) << 4));
+            const float s =
+                reinterpret_cast<const float*>(sm.ptr + C::kOffScales)[slot * C::kTileScales + row / kScaleRows];
+            const bool on = row < *reinterpret_cast<const volatile int*>(sm.ptr + C::kOffRows + 4 * slot);
+            __syncwarp();
+            uint8_t* to = sm.ptr + C::kOffRing + slot * C::kSlotBytes + row * 128 +
+                          (D == 128 ? half * C::kBlockBytes : 0);
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+                const uint32_t cw[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float4 a = e4m3_values(cw[2 * h], s), b = e4m3_values(cw[2 * h + 1], s);
+                    const int chunk = (D == 128 ? 0 : 4 * half) + 2 * i + h;
+                    *reinterpret_cast<uint4*>(to + ((chunk ^ (row & 7)) << 4)) =
+                        on ? make_uint4(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w), pack_bf16x2(b.x, b.y),
+                                        pack_bf16x2(b.z, b.w))
+                           : make_uint4(0, 0, 0, 0);
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sm.bar<D, M>(C::kBarFull + slot));
+            if (++slot == C::kSlots) {
+                slot = 0;
+                phase ^= 1;
+            }
+        }
+    }
+    if (!ok && lane == 0) {
+        if (!*abort_flag) set_error(err, kErrTimeout);
+        *abort_flag = 1;
     }
 }
 
@@ -1419,6 +1534,10 @@ template <>
 struct RowMask<kBlocks | kTwoProducers> : BlockRowMask {};
 template <>
 struct RowMask<kBlocks | kOneTile | kTwoProducers> : BlockRowMask {};
+template <>
+struct RowMask<kE8 | kBlocks | kOneTile> : BlockRowMask {};
+template <>
+struct RowMask<kE8 | kBlocks | kOneTile | kTwoProducers> : BlockRowMask {};
 
 // A key that a row does not see has the weight 0 in the row's tile product, and
 // 0 times an infinity or NaN in that key's V row is NaN.  Besides, a row's weights may
@@ -1436,11 +1555,34 @@ struct RowMask<kBlocks | kOneTile | kTwoProducers> : BlockRowMask {};
 // one query head: a warp's 32 rows over 400,000 keys still end within the other
 // roles' bounded waits of 2 s.)
 //
+// Elements 8 c .. 8 c + 7 of a row of the pool (its number in the layer's), and one.
+template <int D, int M, typename Args>
+__device__ __forceinline__ uint4 pool_eight(const Args& a, int64_t row, int c) {
+    row += (int64_t)a.layer * a.num_pages * 2 * a.Hkv * a.P;
+    if constexpr (e8<M>) {
+        const uint2 x = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.pool) + row * D + 8 * c);
+        const float s = __ldg(a.scales + row / kScaleRows);
+        const float4 lo = e4m3_values(x.x, s), hi = e4m3_values(x.y, s);
+        return make_uint4(pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y),
+                          pack_bf16x2(hi.z, hi.w));
+    } else {
+        return reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.pool) + row * D)[c];
+    }
+}
+template <int D, int M, typename Args>
+__device__ __forceinline__ float pool_value(const Args& a, int64_t row, int e) {
+    row += (int64_t)a.layer * a.num_pages * 2 * a.Hkv * a.P;
+    if constexpr (e8<M>)
+        return e4m3_values(static_cast<const uint8_t*>(a.pool)[row * D + e], __ldg(a.scales + row / kScaleRows)).x;
+    else
+        return __bfloat162float(static_cast<const __nv_bfloat16*>(a.pool)[row * D + e]);
+}
+
 // Whether some V row of the item is not finite; with a mask only of those that it
 // hides.
 template <int D, int M, typename Args>
-__device__ bool has_odd_values(const Args& a, const BlockItem& it, const BlockRowMask* mask,
-                               const __nv_bfloat16* values, int lane) {
+__device__ bool has_odd_values(const Args& a, const BlockItem& it, const BlockRowMask* mask, int64_t values,
+                               int lane) {
     const int per = pieces_of<M>(a), br = 128 / per;
     for (int j = it.t0; j < it.t0 + it.n_tiles; ++j) {
         const PrefillTile* t = a.tiles + j;
@@ -1454,10 +1596,9 @@ __device__ bool has_odd_values(const Args& a, const BlockItem& it, const BlockRo
             const int page = __ldg(&a.tile_pages[(size_t)j * per + (w * 32 + lane) / br]);
             bool odd = false;
             if (!((see >> lane) & 1u) && page >= 0 && page < a.num_pages && key < it.n) {
-                const uint4* v = reinterpret_cast<const uint4*>(
-                    values + (int64_t)page * 2 * a.Hkv * a.P * D + (size_t)(key & (a.P - 1)) * D);
+                const int64_t v = values + (int64_t)page * 2 * a.Hkv * a.P + (key & (a.P - 1));
                 for (int c = 0; c < D / 8; ++c) {
-                    const uint4 x = v[c];
+                    const uint4 x = pool_eight<D, M>(a, v, c);
                     const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -1474,10 +1615,7 @@ __device__ __noinline__ void rows_again(const Args& a, const BlockItem& it, int 
                                         float m_run, float l, int lane) {
     constexpr int kCols = D / 32, kRows = 4, kAhead = 8;
     const int g = it.head & (kBlockTwoTiles - 1), per = pieces_of<M>(a), br = 128 / per;
-    const size_t run = (size_t)a.P * D;  // a head's rows in a page
-    const __nv_bfloat16* keys =
-        static_cast<const __nv_bfloat16*>(a.pool) + ((size_t)a.layer * a.num_pages * 2 * a.Hkv + g) * run;
-    const __nv_bfloat16* values = keys + a.Hkv * run;
+    const int64_t keys = (int64_t)g * a.P, values = keys + (int64_t)a.Hkv * a.P;  // rows of page 0
     const bool odd = has_odd_values<D, M>(a, it, nullptr, values, lane);
     while (rows) {
         // up to kRows rows of one query: they see the same keys
@@ -1520,11 +1658,11 @@ __device__ __noinline__ void rows_again(const Args& a, const BlockItem& it, int 
             if ((see >> lane) & 1u) {
                 // (a page outside the pool was flagged, and page 0 read)
                 const int page = __ldg(&a.tile_pages[(size_t)j * per + (w * 32 + lane) / br]);
-                at = (int64_t)((uint32_t)page < (uint32_t)a.num_pages ? page : 0) * 2 * a.Hkv * run +
-                     (size_t)(key & (a.P - 1)) * D;
+                at = (int64_t)((uint32_t)page < (uint32_t)a.num_pages ? page : 0) * 2 * a.Hkv * a.P +
+                     (key & (a.P - 1));
 #pragma unroll 4
                 for (int c = 0; c < D / 8; ++c) {
-                    const uint4 kk = reinterpret_cast<const uint4*>(keys + at)[c];
+                    const uint4 kk = pool_eight<D, M>(a, keys + at, c);
                     const uint32_t kw[4] = {kk.x, kk.y, kk.z, kk.w};
 #pragma unroll
                     for (int r = 0; r < kRows; ++r) {
@@ -1548,10 +1686,10 @@ __device__ __noinline__ void rows_again(const Args& a, const BlockItem& it, int 
                 float v[kAhead][kCols];
 #pragma unroll
                 for (int c = 0; c < kAhead; ++c) {
-                    const __nv_bfloat16* from = values + __shfl_sync(0xffffffffu, at, c0 + c);
+                    const int64_t from = values + __shfl_sync(0xffffffffu, at, c0 + c);
                     const bool seen = (see >> (c0 + c)) & 1u;
 #pragma unroll
-                    for (int i = 0; i < kCols; ++i) v[c][i] = seen ? __bfloat162float(from[lane + 32 * i]) : 0.f;
+                    for (int i = 0; i < kCols; ++i) v[c][i] = seen ? pool_value<D, M>(a, from, lane + 32 * i) : 0.f;
                 }
 #pragma unroll
                 for (int c = 0; c < kAhead; ++c)
@@ -1986,6 +2124,10 @@ template <>
 struct ModeOf<BlockArgs2> : std::integral_constant<int, kBlocks | kTwoProducers> {};
 template <>
 struct ModeOf<BlockShortArgs2> : std::integral_constant<int, kBlocks | kOneTile | kTwoProducers> {};
+template <>
+struct ModeOf<BlockShortKv8Args> : std::integral_constant<int, kE8 | kBlocks | kOneTile> {};
+template <>
+struct ModeOf<BlockShortKv8Args2> : std::integral_constant<int, kE8 | kBlocks | kOneTile | kTwoProducers> {};
 
 template <int D, typename Args>
 __global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
@@ -2001,12 +2143,18 @@ __global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm.ptr + C::kOffMisc);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sm.ptr + C::kOffMisc + 4);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // The warp's role by the numbers above.  Rows in 8 bits: the softmax warps come
+    // first (two whole warpgroups, which take registers that the others give up: 640
+    // threads start with 96 each), then producer, issuer, second producer and a warp
+    // without a role, then two warpgroups of converters.
+    const int role = !e8<M> ? warp : warp < 8 ? warp + 2 : warp < 10 ? warp - 8 : warp;
     // the split-merging kernel that follows may be scheduled from here on
     grid_launch_dependents();
-    if (threadIdx.x == 0) {
+    if (role == 0 && lane == 0) {
         mbar_init(sm.bar<D, M>(C::kBarQ), 1);
         for (int s = 0; s < C::kSlots; ++s) {
-            mbar_init(sm.bar<D, M>(C::kBarFull + s), 1);
+            mbar_init(sm.bar<D, M>(C::kBarFull + s), e8<M> ? kConverters : 1);
+            if (e8<M>) mbar_init(sm.bar<D, M>(C::kBarRaw + s), 1 + C::kTileScales);
             mbar_init(sm.bar<D, M>(C::kBarEmpty + s), 1);
         }
         for (int b = 0; b < C::kBufs; ++b) {
@@ -2022,7 +2170,7 @@ __global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
         mbar_init(sm.bar<D, M>(C::kBarDone), 1);
         for (int s = 0; s < kItemSlots; ++s) {
             mbar_init(sm.bar<D, M>(C::kBarItem + s), 1);
-            mbar_init(sm.bar<D, M>(C::kBarItemFree + s), kItemReaders + producers<M> - 1);
+            mbar_init(sm.bar<D, M>(C::kBarItemFree + s), kItemReaders + producers<M> - 1 + (e8<M> ? kConverters : 0));
         }
         mbar_init(sm.bar<D, M>(C::kBarClc), 1);
         mbar_init(sm.bar<D, M>(C::kBarX), 128);
@@ -2030,21 +2178,21 @@ __global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
         fence_mbar_init();
         *abort_flag = 0;
     }
-    if (warp == 1) {
+    if (role == 1) {
         tmem_alloc(smem_addr(tmem_slot), C::kTmemCols);
         tmem_relinquish();
     }
     FirstItem<D, M> start;
     int u_early = 0;
-    const bool second = producers<M> > 1 && warp == kProducer2;  // the second producer warp
-    if (warp == 0 || second) {
-        if (warp == 0 && lane == 0) {
+    const bool second = producers<M> > 1 && role == kProducer2;  // the second producer warp
+    if (role == 0 || second) {
+        if (role == 0 && lane == 0) {
             prefetch_tmap(&pool_map);
             prefetch_tmap(&qmap);
         }
         if (a.plan_ready) start.read(a, second, lane);
-        if constexpr (one_tile<M>) {
-            if (a.kv_early && warp == 0) {
+        if constexpr (one_tile<M> && !e8<M>) {
+            if (a.kv_early && role == 0) {
                 const Item it = make_item<M>(a, start.item.raw);
                 u_early = early_loads<D, M>(&pool_map, a, sm, start, it, lane);
             }
@@ -2055,9 +2203,9 @@ __global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
     // not on the device before that kernel, are read only from here on (but for
     // the first K/V tiles of early_loads).
     grid_dependency_wait();
-    if (warp == 0 || second) {
+    if (role == 0 || second) {
         if (!a.plan_ready) start.read(a, second, lane);
-        if (warp == 0 && lane == 0) {  // the thread that initialised the barriers
+        if (role == 0 && lane == 0) {  // the thread that initialised the barriers
             start.item.write(sm.ptr + C::kOffItems);
             mbar_arrive(sm.bar<D, M>(C::kBarItem));
         }
@@ -2066,7 +2214,22 @@ __global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    if (warp == 0) {
+    // (a warpgroup's registers change at the head of its roles' branch)
+    if (e8<M> && warp >= 12) {
+        if constexpr (e8<M>) {
+            take_registers<C::kConvertRegs, false>();
+            convert_tiles<D, M>(sm, a.err, abort_flag, warp - 12, lane);
+        }
+    } else if (e8<M> && warp >= 8) {
+        if constexpr (e8<M>) {
+            take_registers<C::kOtherRegs, false>();
+            if (role == 0 || second)
+                block_produce<D, M>(&pool_map, &qmap, a, sm, start, u_early, abort_flag, second, lane);
+            else if (role == 1 && lane == 0)
+                prefill_mma<D, M>(a, sm, tmem, abort_flag);
+            __syncwarp();
+        }
+    } else if (role == 0) {
         if constexpr (of_blocks<M>)
             block_produce<D, M>(&pool_map, &qmap, a, sm, start, u_early, abort_flag, 0, lane);
         else
@@ -2074,11 +2237,12 @@ __global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
     } else if (second) {
         if constexpr (of_blocks<M>)
             block_produce<D, M>(&pool_map, &qmap, a, sm, start, u_early, abort_flag, 1, lane);
-    } else if (warp == 1) {
+    } else if (role == 1) {
         if (lane == 0) prefill_mma<D, M>(a, sm, tmem, abort_flag);
         __syncwarp();
     } else {
-        const int t = (warp - 2) >> 2;
+        if constexpr (e8<M>) take_registers<C::kSoftmaxRegs, true>();
+        const int t = (role - 2) >> 2;
         SoftmaxPhase ph = {0, 0};
         bool ok;
         for (uint32_t k = 0;; ++k) {
@@ -2102,7 +2266,7 @@ __global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 1) {
+    if (role == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, C::kTmemCols);
     }

@@ -88,6 +88,13 @@ cudaError_t launch_kv8_widen(const Kv8WidenArgs& a, int, cudaStream_t st) {
         if (a.pages[i] < 0 || a.pages[i] >= a.pool.num_pages) ++g_bad;
     return cudaSuccess;
 }
+cudaError_t blocks_kv8_prepare(int) { return cudaSuccess; }
+cudaError_t launch_blocks_kv8(const CUtensorMap& m, const CUtensorMap& q, const BlockShortKv8Args& a, int D,
+                              cudaStream_t st) {
+    if (!a.scales) ++g_bad;
+    g_wide = 0;
+    return launch_blocks(m, q, a, D, true, st);
+}
 cudaError_t launch_kv8_evict(const Kv8EvictArgs& a, int D, cudaStream_t st) {
     if (fails8(kEvict8)) return cudaErrorLaunchFailure;
     const Clock& c = tick(st);
@@ -117,5 +124,5 @@ cudaError_t launch_decode_kv8(const CUtensorMap& m, const DecodeKv8Args& a, int 
 }  // namespace sq
 
 EXPORT void fake_fail8(int kind) { sq::g_fail8 = kind; }
-EXPORT int fake_wide() { return sq::g_wide; }
 EXPORT int64_t fake_bad() { return sq::g_bad; }
+EXPORT int fake_wide() { return sq::g_wide; }

@@ -448,8 +448,7 @@ def test_captured_step():
 
 
 def test_streams_take_turns():
-    """Two streams, ordered by events, with query blocks of different sizes: the widened
-    pages are one buffer."""
+    """Two streams with query blocks of different sizes and plans."""
     hq, hkv, d, page = 8, 2, 128, 64
     c = sq.Cache(1, hq, hkv, d, page, 200, bits=8)
     hs = fill_sequences(c, [2000, 5000], 20)

@@ -1,6 +1,6 @@
 """What an 8-bit cache's calls decide on the host (CPU), over a stand-in for the CUDA
-runtime and the kernels: where rows go, what failing calls leave, refusals, and the
-turns of the widened pages over streams."""
+runtime and the kernels: where rows go, what failing calls leave, refusals, and
+the turns of plans and workspaces over streams."""
 import ctypes
 import os
 import shutil
@@ -14,6 +14,7 @@ from paper_2602_22603_gb300 import build
 
 HQ, HKV, D, P, PAGES = 8, 2, 64, 16, 200
 STORE8, COPY8, READ8, WIDEN8, EVICT8 = range(5)
+BLOCKS = 7
 Q, OUT, LSE = 1 << 20, 1 << 30, 1 << 32   # never read or written by the stand-in
 _lib = None
 
@@ -170,31 +171,37 @@ def test_failed_appends_leave_nothing(L, cache):
     with pytest.raises(sq.SqError):
         cache.evict_spans(a, [(0, 1)], 1)
     assert ([cache.page_table(h) for h in (a, f)], cache.free_pages(), cache.next_pos(a)) == before
-    L.fake_fail8(WIDEN8)
-    with pytest.raises(sq.SqError):
-        sq.sq_window_attention(cache.handle, [a], [3], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
-    sq.sq_window_attention(cache.handle, [a], [3], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
+    append(cache, a, 80, 1)
+    for m, fail in ((3, lambda: L.fake_fail(BLOCKS)), (90, lambda: L.fake_fail(BLOCKS)),
+                    (90, lambda: L.fake_fail8(WIDEN8))):
+        fail()
+        with pytest.raises(sq.SqError):
+            sq.sq_window_attention(cache.handle, [a], [m], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
+        sq.sq_window_attention(cache.handle, [a], [m], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
 
 
-def test_query_blocks_widen_the_pages_that_they_see(L, cache):
+def test_blocks_of_two_tiles_widen_the_pages_that_they_see(L, cache):
     a, b = cache.seq_new(), cache.seq_new()
     append(cache, a, 1000, 1)
     append(cache, b, 40, 2)
-    sq.sq_window_attention(cache.handle, [a, b], [3, 3], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
+    rows = 128 // (HQ // HKV)   # queries of a tile
+    sq.sq_window_attention(cache.handle, [a, b], [rows, 3], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
+    assert L.fake_wide() == 0
+    sq.sq_window_attention(cache.handle, [a, b], [rows + 1, 3], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
     assert L.fake_wide() == sum(cache.seq_info(h)[1] for h in (a, b))
     # (whole 64-row boxes of the window's, and the sinks')
-    sq.sq_window_attention(cache.handle, [a], [3], 0, Q, OUT, 20, 2, sm_scale=0.1, stream=1)
-    rows = 64 + 1000 - (1000 - 3 - 19) // 64 * 64
-    assert L.fake_wide() <= -(-rows // cache.P) + 2
+    sq.sq_window_attention(cache.handle, [a], [rows + 1], 0, Q, OUT, 20, 2, sm_scale=0.1, stream=1)
+    seen = 64 + 1000 - (1000 - rows - 1 - 19) // 64 * 64
+    assert 0 < L.fake_wide() <= -(-seen // cache.P) + 2
 
 
-def test_widened_pages_take_turns_over_streams(L, cache):
+def test_query_blocks_take_turns_over_streams(L, cache):
     a, b = cache.seq_new(), cache.seq_new()
     append(cache, a, 300, 1)
     append(cache, b, 900, 2)
     for s in (1, 2, 3, 1, 2):
         for h in (a, b):
-            sq.sq_window_attention(cache.handle, [h], [40], 0, Q, OUT, 0, sm_scale=0.1, stream=s)
+            sq.sq_window_attention(cache.handle, [h], [90], 0, Q, OUT, 0, sm_scale=0.1, stream=s)
         sq.sq_tree_attention(cache.handle, [a, b], [2, 2], [-1, 0, -1, 0], 0, Q, OUT, sm_scale=0.1, stream=s)
     assert L.fake_races() == 0
 
@@ -202,15 +209,15 @@ def test_widened_pages_take_turns_over_streams(L, cache):
 def test_no_room_for_widened_pages(L):
     c = sq.Cache(1, HQ, HKV, D, 64, PAGES, bits=8)
     a = c.seq_new()
-    append_one = kv(5000, 1, 1)
-    c.append_kv(a, 5000, append_one.ctypes.data, append_one.ctypes.data, 1)
+    k = kv(5000, 1, 1)
+    c.append_kv(a, 5000, k.ctypes.data, k.ctypes.data, 1)
     L.fake_malloc_limit(1 << 20)
     with pytest.raises(sq.SqError) as e:
-        sq.sq_window_attention(c.handle, [a], [3], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
+        sq.sq_window_attention(c.handle, [a], [90], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
     assert e.value.code == sq.SQ_ERR_NO_MEMORY
-    L.fake_malloc_limit(-1)
-    sq.sq_window_attention(c.handle, [a], [3], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
     sq.sq_decode_attention(c.handle, [a], 0, Q, OUT, sm_scale=0.1, stream=1)
+    L.fake_malloc_limit(-1)
+    sq.sq_window_attention(c.handle, [a], [90], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
     c.close()
 
 
