@@ -108,8 +108,9 @@ struct DecCfg {
     static constexpr int kOffOut = kOffRuns + 256;
     static constexpr int kOutBytes = kDecodeConsumerWarps * kPassRows * D * 4;
     static constexpr int kSmemBytes = kOffOut + kOutBytes + 1024;  // + alignment slack
-    static constexpr int kNT = D / 8;   // 8-wide output column tiles
-    static constexpr int kKS = D / 16;  // 16-deep contraction steps
+    // (bf16 rows) 8-wide output column tiles, 16-deep contraction steps
+    static constexpr int kNT = D / 8;
+    static constexpr int kKS = D / 16;
     static_assert(kSmemBytes <= 232448 && kOffOut % 16 == 0, "shared memory");
     static_assert((kBarRuns + 1) * 8 + 4 <= kBarBytes, "mbarriers");
     static_assert(kOffScales % 16 == 0 && kOffRed % 16 == 0, "alignment");
@@ -410,214 +411,10 @@ __device__ __forceinline__ void close_rows(const DecodeArgs& a, const DecodeItem
     }
 }
 
-// ---- rows in 8 bits -------------------------------------------------------------
-// The products take fp16: an e4m3 code is exact in it, and one conversion makes two.
-// A power of two for each query row takes it from bf16 into fp16's range, the largest
-// element to 2^14 .. 2^15 (elements below 2^-32 of it lose digits); the logits are
-// taken back with the softmax's scale and their keys' block's, one factor for the
-// eight columns of a tile.  The weights are 2^(x - m + kLift), rounded to fp16 (11
-// digits down to 2^-28 of the largest), and sums of a tile's eight tokens share their
-// values' scale s, so that the weight times s / v_ref goes into the product, v_ref
-// being the largest scale of the warp's tokens so far, which takes the sums back at
-// the item's end.
-//
-// ldmatrix moves 16-bit pairs, here two neighbouring dimensions.  Keys: a lane gets
-// dimensions 4 tig .. 4 tig + 3 of sixteen, so the queries' fragments are loaded in that
-// order.  Values, transposed: the pairs of two tokens; the bytes are taken apart, and a
-// product of 16 dimensions is one of the even and one of the odd ones.
-constexpr float kLift = 14.f;
-
-__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32"
-        " {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
-    const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ float f16x2_sum(uint32_t v) {
-    const float2 f = f16x2_to_f32(v);
-    return f.x + f.y;
-}
-
-// Byte offset of a row's 16-byte chunk in a tile, as the tensor map swizzles it.
 template <int D>
-__device__ __forceinline__ uint32_t e8_chunk(int row, int chunk) {
-    return row * D + ((chunk ^ (D == 128 ? row & 7 : row >> 1 & 3)) << 4);
-}
-
-// Two query rows (heads h0 and h1 of the call; a row that is none is zero) as A
-// fragments, and the factors that their logits take.
-template <int D>
-__device__ __forceinline__ void load_queries_f16(const DecodeArgs& a, size_t h0, size_t h1, bool v0, bool v1,
-                                                 int tig, uint32_t (&qa)[D / 16][4], float& c0, float& c1) {
-    uint32_t most[2] = {0u, 0u};
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const uint2* row = reinterpret_cast<const uint2*>(a.q + (r ? h1 : h0) * D) + tig;
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-            const uint2 x = (r ? v1 : v0) ? row[kk * 4] : make_uint2(0u, 0u);
-            qa[kk][r] = x.x;
-            qa[kk][2 + r] = x.y;
-            // (sizes of bf16 order as their bits)
-            most[r] = max(most[r], max(max(x.x << 16, x.x) & 0x7fffffffu, max(x.y << 16, x.y) & 0x7fffffffu));
-        }
-    }
-    float* c[2] = {&c0, &c1};
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        uint32_t m = most[r];
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        const int k = max((int)(m >> 23) - 127, -100) - 14;
-        *c[r] = a.scale_log2 * power_of_two(k);
-        const float f = power_of_two(-k);
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)
-#pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-                const uint32_t x = qa[kk][e + r];
-                qa[kk][e + r] = pack_f16x2(__uint_as_float(x << 16) * f, __uint_as_float(x & 0xffff0000u) * f);
-            }
-    }
-}
-
-// One stage's 16 tokens of a warp.  True: some rows of V were zeroed in shared memory.
-template <int D>
-__device__ __forceinline__ bool e8_stage(const uint32_t (&qa)[D / 16][4], float (&o)[D / 8][4], uint32_t kb,
-                                         uint32_t vb, uint8_t* vgen, const float* sc_s, uint32_t vm, int tbase,
-                                         int n_tok, int lim0, int lim1, int w4, int lane, float c0, float c1,
-                                         float& m0, float& m1, float& l0, float& l1, float& v_ref) {
-    const int tig = lane & 3, mi = lane >> 3, rr = lane & 7;
-    // rows past the sequence's last and rows that their page's fill hides; a block
-    // without any other has no scale worth reading
-    const uint32_t live = vm & ((1u << min(max(n_tok - tbase, 0), 16)) - 1u);
-    float sk[2], sv[2];
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-        const bool some = (live >> (8 * nt)) & 0xffu;
-        sk[nt] = some ? sc_s[w4 * 2 + nt] : 0.f;
-        sv[nt] = some ? sc_s[kStageTokens / kScaleRows + w4 * 2 + nt] : 0.f;
-    }
-    // S = Q K^T over 16 tokens (two n8 tiles, even and odd steps apart)
-    float s4[2][2][4] = {};
-    {
-        const int t = w4 * 16 + (mi >> 1) * 8 + rr;
-#pragma unroll
-        for (int k2 = 0; k2 < D / 32; ++k2) {
-            uint32_t b[4];
-            ldsm_x4(kb + e8_chunk<D>(t, 2 * k2 + (mi & 1)), b[0], b[1], b[2], b[3]);
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-                mma_f16(s4[x >> 1][x & 1], qa[2 * k2 + (x & 1)], e4m3_to_f16x2(b[x]), e4m3_to_f16x2(b[x] >> 16));
-        }
-    }
-    float x[2][4];
-    float mx0 = -INFINITY, mx1 = -INFINITY;
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-        const float f0 = c0 * sk[nt], f1 = c1 * sk[nt];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int tk = tbase + nt * 8 + tig * 2 + e;
-            const bool rv = (vm >> (nt * 8 + tig * 2 + e)) & 1u;
-            x[nt][e] = tk < lim0 && rv ? (s4[nt][0][e] + s4[nt][1][e]) * f0 : -INFINITY;
-            x[nt][2 + e] = tk < lim1 && rv ? (s4[nt][0][2 + e] + s4[nt][1][2 + e]) * f1 : -INFINITY;
-            mx0 = fmaxf(mx0, x[nt][e]);
-            mx1 = fmaxf(mx1, x[nt][2 + e]);
-        }
-    }
-    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 1));
-    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 1));
-    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 2));
-    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 2));
-    const float mn0 = fmaxf(m0, mx0), mn1 = fmaxf(m1, mx1);
-    const float ms0 = mn0 == -INFINITY ? 0.f : mn0, ms1 = mn1 == -INFINITY ? 0.f : mn1;
-    float al0 = exp2f(m0 - ms0), al1 = exp2f(m1 - ms1);
-    m0 = mn0;
-    m1 = mn1;
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            x[nt][e] = exp2f(x[nt][e] - (ms0 - kLift));
-            x[nt][2 + e] = exp2f(x[nt][2 + e] - (ms1 - kLift));
-        }
-    // the normaliser sums the rounded weights
-    uint32_t pa[4];
-    pa[0] = pack_f16x2(x[0][0], x[0][1]);
-    pa[1] = pack_f16x2(x[0][2], x[0][3]);
-    pa[2] = pack_f16x2(x[1][0], x[1][1]);
-    pa[3] = pack_f16x2(x[1][2], x[1][3]);
-    l0 = l0 * al0 + (f16x2_sum(pa[0]) + f16x2_sum(pa[2]));
-    l1 = l1 * al1 + (f16x2_sum(pa[1]) + f16x2_sum(pa[3]));
-    const float sv_most = fmaxf(sv[0], sv[1]);
-    if (sv_most > v_ref) {  // (warp-uniform)
-        const float f = v_ref / sv_most;
-        al0 *= f;
-        al1 *= f;
-        v_ref = sv_most;
-    }
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-        const float f = sv[nt] / v_ref;
-        const uint32_t f2 = pack_f16x2(f, f);
-        pa[2 * nt] = mul_f16x2(pa[2 * nt], f2);
-        pa[2 * nt + 1] = mul_f16x2(pa[2 * nt + 1], f2);
-    }
-    if (__any_sync(0xffffffffu, al0 != 1.f || al1 != 1.f)) {
-#pragma unroll
-        for (int nd = 0; nd < D / 8; ++nd) {
-            o[nd][0] *= al0;
-            o[nd][1] *= al0;
-            o[nd][2] *= al1;
-            o[nd][3] *= al1;
-        }
-    }
-    // V rows that hold none of the sequence's may hold anything: zero them, so that
-    // 0 * V stays 0
-    const bool tail = live != 0xffffu;
-    if (tail) {
-        constexpr int per_row = D / 16;  // 16-byte chunks
-        for (int idx = lane; idx < 16 * per_row; idx += 32) {
-            const int r = idx / per_row;
-            if (!((live >> r) & 1u))
-                *reinterpret_cast<uint4*>(vgen + (w4 * 16 + r) * D + idx % per_row * 16) = make_uint4(0, 0, 0, 0);
-        }
-        __syncwarp();
-    }
-    // O += P V: of 16 dimensions the even ones, then the odd ones
-    {
-        const int t = w4 * 16 + (mi & 1) * 8 + rr;
-#pragma unroll
-        for (int j2 = 0; j2 < D / 32; ++j2) {
-            uint32_t b[4];
-            ldsm_x4_trans(vb + e8_chunk<D>(t, 2 * j2 + (mi >> 1)), b[0], b[1], b[2], b[3]);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) b[x] = __byte_perm(b[x], 0u, 0x3120);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int j = 2 * j2 + h;
-                mma_f16(o[2 * j], pa, e4m3_to_f16x2(b[2 * h]), e4m3_to_f16x2(b[2 * h + 1]));
-                mma_f16(o[2 * j + 1], pa, e4m3_to_f16x2(b[2 * h] >> 16), e4m3_to_f16x2(b[2 * h + 1] >> 16));
-            }
-        }
-    }
-    return tail;
-}
-
-template <int D, bool kE8>
 __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, uint8_t* smem,
                         uint64_t* all_bars, volatile int* abort_flag, int warp, int lane) {
-    using C = DecCfg<D, kE8>;
+    using C = DecCfg<D, false>;
     const int gid = lane >> 2, tig = lane & 3;
     const int r0 = gid, r1 = gid + 8;
     const int mi = lane >> 3, rr = lane & 7;
@@ -630,8 +427,6 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
     float* red_o = reinterpret_cast<float*>(smem + C::kOffOut);     // [8][8][D], out_pos
     uint32_t n_pass = 0;  // item-end passes so far
     uint8_t* ring = smem + group * C::kStages * C::kStageBytes;  // the group's slots
-    const float* scales =
-        reinterpret_cast<const float*>(smem + C::kOffScales) + group * C::kStages * C::kStageScales;
     int slot = 0;
     uint32_t phase = 0;
     int skip = group;   // stages to the group's next one
@@ -646,13 +441,7 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
         const int n_tok = seg->n_tok;
 
         uint32_t qa[C::kKS][4];
-        // (8 bits) a row's scale of the logits; the largest scale of the values so far
-        float c0 = a.scale_log2, c1 = a.scale_log2, v_ref = power_of_two(kLeastScale);
-        if constexpr (kE8) {
-            load_queries_f16<D>(a, v0 ? (size_t)item.seq0 * a.Hq + item.head * G + r0 % G : 0,
-                                v1 ? (size_t)item.seq1 * a.Hq + item.head * G + r1 % G : 0, v0, v1, tig, qa, c0,
-                                c1);
-        } else {
+        {
             const __nv_bfloat16* q0 =
                 a.q + ((size_t)(v0 ? item.seq0 : 0) * a.Hq + item.head * G + r0 % G) * D;
             const __nv_bfloat16* q1 =
@@ -715,12 +504,6 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
                 const uint32_t vb = kb + C::kTileBytes;
                 const int tbase = s * kStageTokens + w4 * 16;  // segment-relative
 
-                bool tail;
-                if constexpr (kE8) {
-                    tail = e8_stage<D>(qa, o, kb, vb, ring + slot * C::kStageBytes + C::kTileBytes,
-                                       scales + slot * C::kStageScales, vm, tbase, n_tok, lim0, lim1, w4, lane,
-                                       c0, c1, m0, m1, l0, l1, v_ref);
-                } else {
                 // S = Q K^T over this warp's 16 tokens (two n8 tiles)
                 float sc[2][4];
 #pragma unroll
@@ -793,7 +576,7 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
                 // Rows past the last valid token hold stale or never-written
                 // shared memory, and rows that their page's fill hides may hold
                 // anything: zero this warp's such V rows so 0 * V stays 0.
-                tail = tbase + 16 > n_tok || vm != 0xffffu;
+                const bool tail = tbase + 16 > n_tok || vm != 0xffffu;
                 if (tail) {
                     const uint32_t live = vm & ((1u << min(max(n_tok - tbase, 0), 16)) - 1u);
                     constexpr int per_row = C::kColBlocks * 8;  // 16-byte chunks per row
@@ -821,7 +604,6 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
                         mma_bf16(o[2 * nd2], pa, b0, b1);
                         mma_bf16(o[2 * nd2 + 1], pa, b2, b3);
                     }
-                }
                 }
                 if (tail) fence_proxy_async_smem();  // generic writes before the next TMA fill
                 __syncwarp();
@@ -856,33 +638,22 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
             if (dead && !last) continue;
             const int r = rb + gid;  // this lane's row of the pass: r0, then r1
             if (tig == 0) {
-                // (8 bits: the weights are 2^kLift times as large)
-                red_m[warp * kRowsPerTile + r] = (rb ? m1 : m0) - (kE8 ? kLift : 0.f);
+                red_m[warp * kRowsPerTile + r] = rb ? m1 : m0;
                 red_l[warp * kRowsPerTile + r] = rb ? l1 : l0;
             }
             if (r < rows) {
                 float* wo = red_o + warp * C::kPassRows * D;
-                if constexpr (kE8) {
 #pragma unroll
-                    for (int j = 0; j < C::kKS; ++j) {
-                        const float(&x)[4] = o[2 * j], (&y)[4] = o[2 * j + 1];
-                        *reinterpret_cast<float4*>(wo + out_pos<D>(gid, j * 16 + tig * 4)) =
-                            rb ? make_float4(x[2] * v_ref, y[2] * v_ref, x[3] * v_ref, y[3] * v_ref)
-                               : make_float4(x[0] * v_ref, y[0] * v_ref, x[1] * v_ref, y[1] * v_ref);
-                    }
-                } else {
-#pragma unroll
-                    for (int nd = 0; nd < C::kNT; ++nd)
-                        *reinterpret_cast<float2*>(wo + out_pos<D>(gid, nd * 8 + tig * 2)) =
-                            rb ? make_float2(o[nd][2], o[nd][3]) : make_float2(o[nd][0], o[nd][1]);
-                }
+                for (int nd = 0; nd < C::kNT; ++nd)
+                    *reinterpret_cast<float2*>(wo + out_pos<D>(gid, nd * 8 + tig * 2)) =
+                        rb ? make_float2(o[nd][2], o[nd][3]) : make_float2(o[nd][0], o[nd][1]);
             }
             if (last) {
                 // nothing is left to stream: the consumers add the rows themselves
                 // (every warp gets here, also after a wait ran out)
                 const int sole = a.items[it].sole;
                 named_bar_sync(1, C::kConsumers);
-                close_rows<D, kE8>(a, a.items + it, seg, item.head, sole, rows, rb, smem, threadIdx.x,
+                close_rows<D, false>(a, a.items + it, seg, item.head, sole, rows, rb, smem, threadIdx.x,
                               C::kConsumers);
                 if (rb + C::kPassRows < rows) {
                     named_bar_sync(1, C::kConsumers);
@@ -892,6 +663,446 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
             __syncwarp();
             if (lane == 0 && !dead) mbar_arrive(smem_addr(&all_bars[C::kBarOut]));
         }
+    }
+}
+
+// ---- rows in 8 bits -------------------------------------------------------------
+// The products take fp16: an e4m3 code is exact in it, and one conversion makes two.
+// A power of two for each query row takes it from bf16 into fp16's range, the largest
+// element to 2^14 .. 2^15 (elements below 2^-32 of it lose digits); the logits are
+// taken back with the softmax's scale and their block's, one factor for the eight keys
+// of a block.
+//
+// The keys are the rows of the first product, S^T = K Q^T, and the values' dimensions
+// those of the second, O^T = V^T P^T, so that the query rows are the columns, eight to a
+// product: with one sequence of 4 or 8 heads a group none is wasted, and a warp has the
+// registers to take two stages at a time, whose chains of products, exponentials and
+// conversions overlap (kStages2).  ldmatrix moves 16-bit pairs, here two neighbouring
+// dimensions.  Keys: a lane gets dimensions 4 tig .. 4 tig + 3 of sixteen, so the
+// queries' fragments are loaded in that order.  Values, transposed: the pairs of two
+// tokens; the bytes are taken apart, the even dimensions being the first eight rows of
+// a product and the odd ones the others.  P is transposed by movmatrix.
+//
+// Weights are 2^(x - m), rounded to fp16, m a reference that is raised only where some
+// weight passes 2^kMost, to the largest logit less kLift: 11 digits down to 2^-21 of
+// the largest's, an error of 2^-32 of it below.  The normaliser sums the rounded
+// weights.  A block's values have their scale s, so its weights take s / v_ref into the
+// product, v_ref being the largest scale of the warp's values so far, which the sums
+// get back at the item's end.
+constexpr float kLift = 7.f, kMost = 15.f;
+constexpr float kNoKeys = -1e30f;   // m of a row that has seen no key
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32"
+        " {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+// lo += the low half of w, hi += its high half.
+__device__ __forceinline__ void add_f16x2(uint32_t w, float& lo, float& hi) {
+    asm("{\n\t.reg .b16 l16, h16;\n\tmov.b32 {l16, h16}, %2;\n\t"
+        "add.rn.f32.f16 %0, l16, %0;\n\tadd.rn.f32.f16 %1, h16, %1;\n\t}"
+        : "+f"(lo), "+f"(hi)
+        : "r"(w));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t w) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(w));
+    return r;
+}
+
+// a / b of two scales, a at most b (what is below 2^-40 is nothing to fp16).
+__device__ __forceinline__ float scale_ratio(float a, float b) {
+    return __int_as_float(max(__float_as_int(a) - __float_as_int(b) + 0x3f800000, 87 << 23));
+}
+
+// Byte offset of a row's 16-byte chunk in a tile, as the tensor map swizzles it.
+template <int D>
+__device__ __forceinline__ uint32_t e8_chunk(int row, int chunk) {
+    return row * D + ((chunk ^ (D == 128 ? row & 7 : row >> 1 & 3)) << 4);
+}
+
+// A query row (head h of the call; one that is none is zero) as B fragments, and the
+// factor that its logits take: row gid of a column tile.
+template <int D>
+__device__ __forceinline__ float load_query_f16(const DecodeArgs& a, size_t h, bool on, int tig,
+                                                uint32_t (&qb)[D / 16][2]) {
+    uint32_t most = 0;
+    const uint2* row = reinterpret_cast<const uint2*>(a.q + h * D) + tig;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+        const uint2 x = on ? row[kk * 4] : make_uint2(0u, 0u);
+        qb[kk][0] = x.x;
+        qb[kk][1] = x.y;
+        // (sizes of bf16 order as their bits)
+        most = max(max(most, x.x << 16 & 0x7fffffffu), x.x & 0x7fff0000u);
+        most = max(max(most, x.y << 16 & 0x7fffffffu), x.y & 0x7fff0000u);
+    }
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    const int k = max((int)(most >> 23) - 127, -100) - 14;
+    const float f = power_of_two(-k);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t x = qb[kk][e];
+            qb[kk][e] = pack_f16x2(__uint_as_float(x << 16) * f, __uint_as_float(x & 0xffff0000u) * f);
+        }
+    return a.scale_log2 * power_of_two(k);
+}
+
+// Which of the 16 tokens of a stage that are a warp's hold rows of their pages, as in
+// consume(), and are the segment's.
+__device__ __forceinline__ uint32_t e8_live(const DecodeArgs& a, const DecodeSeg* seg, int n_tok, int tbase) {
+    uint32_t vm = 0xffffu;
+    if (a.page_fill) {
+        const int P = a.P, pq = tbase >> (__ffs(P) - 1);
+        const int f0 = pq < seg->n_pages ? __ldg(&a.page_fill[seg->page_off + pq]) : 0;
+        auto rows = [](int f, int from, int most) {
+            auto up_to = [&](int x) { return (1u << min(max(x - from, 0), most)) - 1u; };
+            return (up_to(f & kFillMask) & ~up_to(f >> kFillFirstBit & kFillMask)) | up_to(f >> kFillSinkBit);
+        };
+        if (P >= 16) {
+            vm = rows(f0, tbase & (P - 1), 16);
+        } else {
+            const int f1 = pq + 1 < seg->n_pages ? __ldg(&a.page_fill[seg->page_off + pq + 1]) : 0;
+            vm = rows(f0, 0, 8) | rows(f1, 0, 8) << 8;
+        }
+    }
+    return vm & ((1u << min(max(n_tok - tbase, 0), 16)) - 1u);
+}
+
+// What a consumer warp carries through an item: NR column tiles of eight query rows.
+template <int D, int NR>
+struct E8State {
+    uint32_t qb[NR][D / 16][2];
+    float o[D / 16][NR][4];   // dimensions 16 j + 2 gid (+ 1), rows 2 tig, 2 tig + 1
+    float c[NR][2], m[NR][2], l[NR][2];
+    float v_ref;
+};
+
+// N stages' 16 tokens each of a warp: slots `slot[n]` of the group's ring.  kAll: every
+// row sees every token; else row (r, e) those of bits see[n][r][e], and live[n] says
+// which tokens are the segment's.
+template <int D, int NR, int N, bool kAll>
+__device__ __forceinline__ void e8_stages(E8State<D, NR>& st, uint8_t* ring, const float* scales, const int (&slot)[N],
+                                          const uint32_t (&live)[N], const uint32_t (&see)[N][NR][2], int w4,
+                                          int lane) {
+    using C = DecCfg<D, true>;
+    const int gid = lane >> 2, mi = lane >> 3, rr = lane & 7;
+    // (this lane's row of a matrix; the swizzle's turn and the matrix's half of a step)
+    const int t = w4 * 16 + (mi & 1) * 8 + rr;
+    const uint32_t at = t * D, turn = (mi >> 1) ^ (D == 128 ? t & 7 : t >> 1 & 3);
+    auto chunk = [&](int n, int k2) {
+        return smem_addr(ring) + slot[n] * C::kStageBytes + at + ((turn ^ (2 * k2)) << 4);
+    };
+    float2 sk[N], sv[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const float* s = scales + slot[n] * C::kStageScales + w4 * 2;
+        sk[n] = *reinterpret_cast<const float2*>(s);
+        sv[n] = *reinterpret_cast<const float2*>(s + C::kStageScales / 2);
+        if (!kAll) {
+            // a block without rows of the segment has no scale worth reading
+            if (!(live[n] & 0xffu)) sk[n].x = 0.f, sv[n].x = power_of_two(kLeastScale);
+            if (!(live[n] >> 8)) sk[n].y = 0.f, sv[n].y = power_of_two(kLeastScale);
+        }
+    }
+    // weights' exponents x - m
+    float x[N][NR][4];
+    {
+        float acc[N][NR][2][4] = {};   // (even and odd steps apart)
+#pragma unroll
+        for (int k2 = 0; k2 < D / 32; ++k2)
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                // tokens 0 .. 7 and 8 .. 15 of an even step, then of the odd one
+                uint32_t b[4];
+                ldsm_x4(chunk(n, k2), b[0], b[1], b[2], b[3]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t f[4] = {e4m3_to_f16x2(b[2 * h]), e4m3_to_f16x2(b[2 * h + 1]),
+                                           e4m3_to_f16x2(b[2 * h] >> 16), e4m3_to_f16x2(b[2 * h + 1] >> 16)};
+#pragma unroll
+                    for (int r = 0; r < NR; ++r)
+                        mma_f16(acc[n][r][N * NR > 1 ? 0 : h], f, st.qb[r][2 * k2 + h][0], st.qb[r][2 * k2 + h][1]);
+                }
+            }
+        bool over = false;
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float most = -INFINITY;
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    const float f0 = st.c[r][e] * sk[n].x, f1 = st.c[r][e] * sk[n].y;
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        float s = acc[n][r][0][2 * b + e];
+                        if (N * NR == 1) s += acc[n][r][1][2 * b + e];
+                        float y = s * (b ? f1 : f0);
+                        if (!kAll && !(see[n][r][e] >> (gid + 8 * b) & 1u)) y = -INFINITY;
+                        x[n][r][2 * b + e] = y;
+                        most = fmaxf(most, y);
+                    }
+                }
+                over |= most - st.m[r][e] > kMost;
+            }
+        if (__any_sync(0xffffffffu, over)) {
+            // references from the largest logits
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int n = 0; n < N; ++n) mx = fmaxf(mx, fmaxf(x[n][r][e], x[n][r][2 + e]));
+#pragma unroll
+                    for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+                    mx = fmaxf(st.m[r][e], mx - kLift);
+                    const float al = exp2f(st.m[r][e] - mx);
+                    st.m[r][e] = mx;
+                    st.l[r][e] *= al;
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) {
+                        st.o[j][r][e] *= al;
+                        st.o[j][r][2 + e] *= al;
+                    }
+                }
+        }
+    }
+    float sv_most = st.v_ref;
+#pragma unroll
+    for (int n = 0; n < N; ++n) sv_most = fmaxf(sv_most, fmaxf(sv[n].x, sv[n].y));
+    if (sv_most > st.v_ref) {  // (warp-uniform)
+        const float f = scale_ratio(st.v_ref, sv_most);
+        st.v_ref = sv_most;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) st.o[j][r][i] *= f;
+    }
+    uint32_t pb[N][NR][2];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const float f = scale_ratio(b ? sv[n].y : sv[n].x, st.v_ref);
+            const uint32_t f2 = pack_f16x2(f, f);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const uint32_t h = pack_f16x2(exp2f(x[n][r][2 * b] - st.m[r][0]), exp2f(x[n][r][2 * b + 1] - st.m[r][1]));
+                add_f16x2(h, st.l[r][0], st.l[r][1]);
+                pb[n][r][b] = transpose_8x8(mul_f16x2(h, f2));
+            }
+        }
+    if (!kAll) {
+        // V rows that hold none of the segment's may hold anything: zero them, so that
+        // 0 * V stays 0
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            uint8_t* v = ring + slot[n] * C::kStageBytes + C::kTileBytes + w4 * 16 * D;
+            for (int i = lane; i < D; i += 32)   // 16-byte chunks of 16 rows
+                if (!((live[n] >> (i / (D / 16))) & 1u))
+                    *reinterpret_cast<uint4*>(v + i * 16) = make_uint4(0, 0, 0, 0);
+        }
+        __syncwarp();
+    }
+#pragma unroll
+    for (int j2 = 0; j2 < D / 32; ++j2)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            // tokens 0 .. 7 and 8 .. 15 of sixteen dimensions, then of the next
+            uint32_t b[4];
+            ldsm_x4_trans(chunk(n, j2) + C::kTileBytes, b[0], b[1], b[2], b[3]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t y = b[2 * h], z = b[2 * h + 1];
+                const uint32_t f[4] = {
+                    e4m3_to_f16x2(__byte_perm(y, 0u, 0x4420)), e4m3_to_f16x2(__byte_perm(y, 0u, 0x4431)),
+                    e4m3_to_f16x2(__byte_perm(z, 0u, 0x4420)), e4m3_to_f16x2(__byte_perm(z, 0u, 0x4431))};
+#pragma unroll
+                for (int r = 0; r < NR; ++r) mma_f16(st.o[2 * j2 + h][r], f, pb[n][r][0], pb[n][r][1]);
+            }
+        }
+    if (!kAll) fence_proxy_async_smem();  // generic writes before the next TMA fill
+}
+
+// A consumer's place in its group's ring, and its waits.
+struct E8Ring {
+    uint8_t* slots;
+    const float* scales;
+    uint64_t* bars;
+    int* err;
+    volatile int* abort_flag;
+    int slot;
+    uint32_t phase;
+    bool dead;  // warp-uniform: a wait ran out or the CTA aborted
+    uint32_t n_pass;
+    __device__ __forceinline__ void wait(uint64_t* bar, uint32_t parity, int lane) {
+        if (dead) return;
+        const bool ok = mbar_wait(smem_addr(bar), parity, abort_flag);
+        if (__all_sync(0xffffffffu, ok)) return;
+        if (lane == 0 && !*abort_flag) set_error(err, kErrTimeout);
+        *abort_flag = 1;
+        dead = true;
+    }
+};
+
+// One item of a consumer warp, from stage s on; returns the stage that comes after.
+// (Its end: see consume().)
+template <int D, int NR>
+__device__ __forceinline__ int e8_item(const DecodeArgs& a, const ItemHead& item, int it, bool last, int s,
+                                       E8Ring& rg, uint8_t* smem, uint64_t* all_bars, int warp, int lane) {
+    using C = DecCfg<D, true>;
+    constexpr int kStages2 = NR == 1 ? 2 : 1;
+    const int gid = lane >> 2, tig = lane & 3, w4 = warp & 3, G = a.G;
+    const DecodeSeg* seg = a.segs + item.seg;
+    const int n_tok = seg->n_tok, rows = item.n_grp * G;
+    E8State<D, NR> st;
+    int lim[NR][2];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        const int row = r * 8 + gid;
+        const bool on = row < rows;
+        const float c = load_query_f16<D>(
+            a, on ? (size_t)(r ? item.seq1 : item.seq0) * a.Hq + item.head * G + row % G : 0, on, tig, st.qb[r]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            st.c[r][e] = __shfl_sync(0xffffffffu, c, (2 * tig + e) * 4);
+            const int j = (r * 8 + 2 * tig + e) / G;
+            lim[r][e] = j < item.n_grp ? seg->grp_lim[j] : 0;
+            st.m[r][e] = kNoKeys;
+            st.l[r][e] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) st.o[j][r][0] = st.o[j][r][1] = st.o[j][r][2] = st.o[j][r][3] = 0.f;
+    }
+    st.v_ref = power_of_two(kLeastScale);
+    // tokens that every row sees, where pages have no slots without rows (rows that are
+    // none see what they like)
+    int all = a.page_fill ? 0 : n_tok;
+    for (int j = 0; j < item.n_grp; ++j) all = min(all, seg->grp_lim[j]);
+    auto step = [&](auto count) {
+        constexpr int N = decltype(count)::value;
+        int slot[N];
+        uint32_t phase[N];
+        const bool whole = N > 1 || (s + 1) * kStageTokens <= all;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            slot[n] = rg.slot;
+            phase[n] = rg.phase;
+            if (++rg.slot == C::kStages) {
+                rg.slot = 0;
+                rg.phase ^= 1;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) rg.wait(&rg.bars[slot[n]], phase[n], lane);
+        if (!rg.dead) {
+            uint32_t live[N] = {}, see[N][NR][2] = {};
+            if constexpr (N > 1) {
+                e8_stages<D, NR, N, true>(st, rg.slots, rg.scales, slot, live, see, w4, lane);
+            } else if (whole) {
+                e8_stages<D, NR, N, true>(st, rg.slots, rg.scales, slot, live, see, w4, lane);
+            } else {
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    const int tbase = (s + n * kDecodeGroups) * kStageTokens + w4 * 16;
+                    live[n] = e8_live(a, seg, n_tok, tbase);
+#pragma unroll
+                    for (int r = 0; r < NR; ++r)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            see[n][r][e] = live[n] & ((1u << min(max(lim[r][e] - tbase, 0), 16)) - 1u);
+                }
+                e8_stages<D, NR, N, false>(st, rg.slots, rg.scales, slot, live, see, w4, lane);
+            }
+            __syncwarp();
+            if (lane == 0)
+#pragma unroll
+                for (int n = 0; n < N; ++n) mbar_arrive(smem_addr(&rg.bars[C::kStages + slot[n]]));
+        }
+        s += N * kDecodeGroups;
+    };
+    while (kStages2 > 1 && (s + kDecodeGroups + 1) * kStageTokens <= all && s + kDecodeGroups < item.s1)
+        step(std::integral_constant<int, kStages2>());
+    while (s < item.s1) step(std::integral_constant<int, 1>());
+
+    // the rows, eight at a time, to the closing warps
+    float* red_m = reinterpret_cast<float*>(smem + C::kOffRed);
+    float* red_l = red_m + kDecodeConsumerWarps * kRowsPerTile;
+    float* wo = reinterpret_cast<float*>(smem + C::kOffOut) + warp * C::kPassRows * D;
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        const int rb = r * 8;
+        if (rb >= rows) break;
+        // the previous pass's rows have been read
+        if (rg.n_pass > 0 && !(last && rb > 0)) rg.wait(&all_bars[C::kBarOutFree], (rg.n_pass - 1) & 1, lane);
+        ++rg.n_pass;
+        if (rg.dead && !last) continue;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float l = st.l[r][e];
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+            const int at = 2 * tig + e;
+            if (gid == 0) {
+                red_m[warp * kRowsPerTile + rb + at] = st.m[r][e] == kNoKeys ? -INFINITY : st.m[r][e];
+                red_l[warp * kRowsPerTile + rb + at] = l;
+            }
+            if (rb + at < rows) {
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j)
+                    *reinterpret_cast<float2*>(wo + out_pos<D>(at, j * 16 + gid * 2)) =
+                        make_float2(st.o[j][r][e] * st.v_ref, st.o[j][r][2 + e] * st.v_ref);
+            }
+        }
+        if (last) {
+            const int sole = a.items[it].sole;
+            named_bar_sync(1, C::kConsumers);
+            close_rows<D, true>(a, a.items + it, seg, item.head, sole, rows, rb, smem, threadIdx.x, C::kConsumers);
+            if (rb + C::kPassRows < rows) {
+                named_bar_sync(1, C::kConsumers);
+                continue;
+            }
+        }
+        __syncwarp();
+        if (lane == 0 && !rg.dead) mbar_arrive(smem_addr(&all_bars[C::kBarOut]));
+    }
+    return s;
+}
+
+template <int D>
+__device__ void consume_e8(const DecodeArgs& a, int it0, int it1, ItemHead next, uint8_t* smem, uint64_t* all_bars,
+                           volatile int* abort_flag, int warp, int lane) {
+    using C = DecCfg<D, true>;
+    const int gid = lane >> 2, group = warp >> 2;
+    E8Ring rg = {smem + group * C::kStages * C::kStageBytes,
+                 reinterpret_cast<const float*>(smem + C::kOffScales) + group * C::kStages * C::kStageScales,
+                 all_bars + group * 2 * C::kStages, a.err, abort_flag, 0, 0, false, 0};
+    int skip = group;  // stages to the group's next one
+    for (int it = it0; it < it1; ++it) {
+        const ItemHead item = next;
+        if (it + 1 < it1) next.read(a, it + 1, gid / a.G, (gid + 8) / a.G);
+        const bool last = it + 1 == it1;
+        const int s = item.n_grp * a.G <= 8
+                          ? e8_item<D, 1>(a, item, it, last, item.s0 + skip, rg, smem, all_bars, warp, lane)
+                          : e8_item<D, 2>(a, item, it, last, item.s0 + skip, rg, smem, all_bars, warp, lane);
+        skip = s - item.s1;
     }
 }
 
@@ -1225,7 +1436,8 @@ __global__ void __launch_bounds__(DecCfg<D, kE8>::kThreads, 1)
                        threadIdx.x - C::kConsumers - kDecodeGroups * 32);
         return;
     }
-    consume<D, kE8>(a, it0, it1, head, smem, bars, abort_flag, warp, lane);
+    if constexpr (kE8) consume_e8<D>(a, it0, it1, head, smem, bars, abort_flag, warp, lane);
+    else consume<D>(a, it0, it1, head, smem, bars, abort_flag, warp, lane);
     merge_last_runs<D, kE8>(a, smem, bars, abort_flag, lane);
 }
 
