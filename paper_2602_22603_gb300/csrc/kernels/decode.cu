@@ -76,6 +76,8 @@ namespace {
 using namespace dev;
 
 // kE8: rows in 8 bits (see kv8.hpp).
+template <bool kE8>
+using ArgsOf = std::conditional_t<kE8, DecodeKv8Args, DecodeArgs>;
 template <int D, bool kE8>
 struct DecCfg {
     static constexpr int kColBlocks = kE8 ? 1 : D / 64;          // column blocks of a row
@@ -131,16 +133,13 @@ __device__ __forceinline__ float bf16x2_sum(uint32_t v) {
 // the current one waits for its slot.  Whole-page stages (P >= 64) are issued by
 // lane 0; with smaller pages each lane issues one box (page, column block, K or
 // V).
-template <bool kE8>
-using ArgsOf = std::conditional_t<kE8, DecodeKv8Args, DecodeArgs>;
-template <int D, bool kE8>
+template <int D>
 struct Producer {
-    using C = DecCfg<D, kE8>;
+    using C = DecCfg<D, false>;
     const CUtensorMap* tmap;
-    const ArgsOf<kE8>& a;
+    const DecodeArgs& a;
     uint8_t* ring;      // the group's slots
     uint64_t* bars;     // the group's barriers: full [kStages], empty [kStages]
-    float* scales;      // (8 bits) the group's slots
     volatile int* abort_flag;
     int group, lane;
     // this lane's box within a stage of small pages
@@ -156,7 +155,7 @@ struct Producer {
     __device__ void init() {
         box_cb = lane % C::kColBlocks;
         box_kv = (lane / C::kColBlocks) % 2;
-        box_page = kE8 || a.P < kStageTokens ? lane / (2 * C::kColBlocks) : 0;
+        box_page = a.P < kStageTokens ? lane / (2 * C::kColBlocks) : 0;
         it = a.cta_begin[blockIdx.x];
         it1 = a.cta_begin[blockIdx.x + 1];
         slot = 0;
@@ -187,13 +186,6 @@ struct Producer {
             open_item();
             s += over;
         }
-        if constexpr (kE8) {
-            // a lane to the scale of a block (number box_page) of keys or of values;
-            // those whose block begins a box load it too
-            const int at = (s * kStageTokens + box_page * kScaleRows) / a.P;
-            pid = lane < C::kStageScales && at < n_pages ? a.page_ids[page_off + at] : -1;
-            return;
-        }
         const int pi = s * kStageTokens / a.P + box_page;
         const int per = a.P < kStageTokens ? kStageTokens / a.P : 1;
         pid = box_page < per && pi < n_pages ? a.page_ids[page_off + pi] : -1;
@@ -211,40 +203,11 @@ struct Producer {
         s += kDecodeGroups;
         settle();
     }
-    __device__ bool box_lane() const {
-        return kE8 ? lane < C::kStageScales && box_page * kScaleRows % min(a.P, kStageTokens) == 0
-                   : a.P < kStageTokens || lane < 2 * C::kColBlocks;
-    }
     // Issues the current stage into its (free) slot.
     __device__ void issue() {
         const uint32_t full = smem_addr(&bars[slot]);
         const uint32_t dst = smem_addr(ring) + slot * C::kStageBytes;
-        if constexpr (kE8) {
-            const bool valid = pid >= 0 && pid < a.num_pages;
-            if (pid < -1 || pid >= a.num_pages) set_error(a.err, kErrBounds);
-            const bool box = valid && box_lane();
-            const uint32_t n = __popc(__ballot_sync(0xffffffffu, box));
-            if (lane == 0) {
-                if (n) mbar_arrive_expect_tx(full, n * min(a.P, kStageTokens) * C::kRowBytes);
-                else mbar_arrive(full);
-            }
-            __syncwarp();
-            if (box)
-                tma_load_4d(dst + box_kv * C::kTileBytes + box_page * kScaleRows * C::kRowBytes, tmap, full, 0,
-                            row(box_kv), pid, a.layer);
-            if (lane < C::kStageScales) {
-                if (valid) {
-                    const int64_t plane = (((int64_t)a.layer * a.num_pages + pid) * 2 + box_kv) * a.Hkv + head;
-                    const int at = (s * kStageTokens + box_page * kScaleRows) & (a.P - 1);
-                    const float* src = a.scales + (plane * a.P + at) / kScaleRows;
-                    const uint32_t to = smem_addr(scales + slot * C::kStageScales +
-                                                  box_kv * (C::kStageScales / 2) + box_page);
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(src) : "memory");
-                }
-                // (arrives when this lane's copy has landed)
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full) : "memory");
-            }
-        } else if (a.P >= kStageTokens) {
+        if (a.P >= kStageTokens) {
             if (lane == 0) {
                 if ((uint32_t)pid < (uint32_t)a.num_pages) {
                     mbar_arrive_expect_tx(full, C::kStageBytes);
@@ -295,7 +258,7 @@ struct Producer {
         // (the walk goes on from here after the wait: look ahead on a copy)
         Producer ahead = *this;
         for (; n < kPrefetchStages && ahead.more(); ++n) {
-            if (ahead.pid >= 0 && ahead.pid < a.num_pages && box_lane())
+            if (ahead.pid >= 0 && ahead.pid < a.num_pages && (a.P < kStageTokens || lane < 2 * C::kColBlocks))
                 tma_prefetch_l2_4d(tmap, box_cb * 64, ahead.row(box_kv), ahead.pid, a.layer);
             ahead.advance();
         }
@@ -319,6 +282,175 @@ struct Producer {
             for (int sl = 0; sl < C::kStages; ++sl)
                 if ((issued >> sl) & 1u)
                     mbar_wait(smem_addr(&bars[sl]), (issued_phase >> sl) & 1u);
+        }
+        __syncwarp();
+    }
+};
+
+// The same for rows in 8 bits, whose stages pass twice as fast: a page's id, read from
+// the plan when the walk got to its stage, then held the stage up (1,470 of 1,690 cycles
+// a stage, with the consumers waiting 600 of theirs).  So kWalks walks take turns, each
+// kWalks stages of the group apart, and a stage's id is read that many stages ahead.  A
+// lane has the scale of a block of keys or of values, copied beside its stage; those
+// whose block begins a box load it too.
+template <int D>
+struct ProducerE8 {
+    using C = DecCfg<D, true>;
+    static constexpr int kWalks = 4;
+    struct Walk {
+        int it, s, s1, head, page_off, n_pages;  // stage s of item it
+        int32_t pid;                             // this lane's page, -1: none
+    };
+    const CUtensorMap* tmap;
+    const DecodeKv8Args& a;
+    uint8_t* ring;      // the group's slots
+    float* scales;      // ... and their scales
+    uint64_t* bars;     // ... and barriers: full [kStages], empty [kStages]
+    volatile int* abort_flag;
+    int group, lane;
+    int kv, block;      // the lane's plane and block of a stage
+    bool box;           // a box begins at its block
+    int it1;
+    int64_t page_scales;  // scales of a page, all planes
+    Walk w[kWalks];
+    int slot;
+    uint32_t phase;
+    uint32_t issued, issued_phase;  // per-slot bits of the last issue
+    bool first;         // the CTA's first stage has not gone out yet
+
+    __device__ void init() {
+        kv = lane & 1;
+        block = lane >> 1;
+        box = lane < C::kStageScales && block * kScaleRows % min(a.P, kStageTokens) == 0;
+        page_scales = (int64_t)2 * a.Hkv * (a.P / kScaleRows);
+        it1 = a.cta_begin[blockIdx.x + 1];
+        slot = 0;
+        phase = 0;
+        issued = issued_phase = 0;
+        first = group == 0;
+        Walk x;
+        x.it = a.cta_begin[blockIdx.x];
+        if (x.it < it1) open(x);
+#pragma unroll
+        for (int i = 0; i < kWalks; ++i) {
+            w[i] = x;
+            if (x.it >= it1) continue;
+            w[i].s += group + i * kDecodeGroups;
+            settle(w[i]);
+        }
+    }
+    __device__ void open(Walk& x) const {
+        const DecodeItem* item = a.items + x.it;
+        const DecodeSeg* seg = a.segs + item->seg;
+        x.s = item->s0;
+        x.s1 = item->s1;
+        x.head = item->head;
+        x.page_off = seg->page_off;
+        x.n_pages = seg->n_pages;
+    }
+    // Carries a stage past the item's end into the items that follow.
+    __device__ __forceinline__ void settle(Walk& x) const {
+        while (x.s >= x.s1) {
+            const int over = x.s - x.s1;
+            if (++x.it >= it1) return;
+            open(x);
+            x.s += over;
+        }
+        const int at = (x.s * kStageTokens + block * kScaleRows) / a.P;
+        x.pid = lane < C::kStageScales && at < x.n_pages ? a.page_ids[x.page_off + at] : -1;
+    }
+    __device__ __forceinline__ int row(const Walk& x) const {
+        return (kv * a.Hkv + x.head) * a.P + (a.P > kStageTokens ? (x.s * kStageTokens) & (a.P - 1) : 0);
+    }
+    // Issues a walk's stage into the (free) slot.
+    __device__ __forceinline__ void issue(const Walk& x) {
+        const uint32_t full = smem_addr(&bars[slot]);
+        const bool valid = x.pid >= 0 && x.pid < a.num_pages;
+        if (x.pid < -1 || x.pid >= a.num_pages) set_error(a.err, kErrBounds);
+        const uint32_t n = __popc(__ballot_sync(0xffffffffu, box && valid));
+        if (lane == 0) {
+            if (n) mbar_arrive_expect_tx(full, n * min(a.P, kStageTokens) * C::kRowBytes);
+            else mbar_arrive(full);
+        }
+        __syncwarp();
+        if (box && valid)
+            tma_load_4d(smem_addr(ring) + slot * C::kStageBytes + kv * C::kTileBytes +
+                            block * kScaleRows * C::kRowBytes,
+                        tmap, full, 0, row(x), x.pid, a.layer);
+        if (lane < C::kStageScales) {
+            if (valid) {
+                const int at = (x.s * kStageTokens + block * kScaleRows) & (a.P - 1);
+                const float* src = a.scales + ((int64_t)a.layer * a.num_pages + x.pid) * page_scales +
+                                   ((kv * a.Hkv + x.head) * a.P + at) / kScaleRows;
+                const uint32_t to =
+                    smem_addr(scales + slot * C::kStageScales + kv * (C::kStageScales / 2) + block);
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(src) : "memory");
+            }
+            // (arrives when this lane's copy has landed)
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full) : "memory");
+        }
+        issued |= 1u << slot;
+        issued_phase = (issued_phase & ~(1u << slot)) | (phase << slot);
+    }
+    __device__ __forceinline__ void next_slot() {
+        first = false;
+        if (++slot == C::kStages) {
+            slot = 0;
+            phase ^= 1;
+        }
+    }
+    // Before the grid-dependency wait (see Producer): of the first kWalks stages those in
+    // pages that no running work writes; the others are prefetched into L2.  Returns
+    // the stages issued.
+    __device__ int early() {
+        static_assert(kWalks <= C::kStages, "slots that are free at the start");
+        if ((int)blockIdx.x == a.debug_drop_cta) return 0;
+        int n = 0;
+        bool go = a.kv_early && a.P >= kStageTokens;
+#pragma unroll
+        for (int i = 0; i < kWalks; ++i) {
+            if (w[i].it >= it1) break;
+            bool unsafe = false;
+            for (int u = lane; u < a.n_unsafe; u += 32) unsafe |= a.unsafe[u] == w[i].pid;
+            go = go && !__any_sync(0xffffffffu, unsafe);
+            if (go) {
+                issue(w[i]);
+                next_slot();
+                ++n;
+            } else if (box && w[i].pid >= 0 && w[i].pid < a.num_pages) {
+                tma_prefetch_l2_4d(tmap, 0, row(w[i]), w[i].pid, a.layer);
+            }
+        }
+        return n;
+    }
+    // n: stages that went out early.
+    __device__ void run(int n) {
+        bool ok = true, more = true;
+        while (more) {
+#pragma unroll
+            for (int i = 0; i < kWalks; ++i) {
+                more = more && w[i].it < it1;
+                if (!more) continue;
+                if (n > 0) {
+                    --n;
+                } else {
+                    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&bars[C::kStages + slot]), phase ^ 1, abort_flag));
+                    more = ok;
+                    if (!ok) continue;
+                    // (test hook: see Producer)
+                    if (!(first && (int)blockIdx.x == a.debug_drop_cta)) issue(w[i]);
+                    next_slot();
+                }
+                w[i].s += kWalks * kDecodeGroups;
+                settle(w[i]);
+            }
+        }
+        if (!ok && lane == 0) {
+            if (!*abort_flag) set_error(a.err, kErrTimeout);
+            *abort_flag = 1;
+            // Leave only after every copy already issued has landed (bounded).
+            for (int sl = 0; sl < C::kStages; ++sl)
+                if ((issued >> sl) & 1u) mbar_wait(smem_addr(&bars[sl]), (issued_phase >> sl) & 1u);
         }
         __syncwarp();
     }
@@ -675,9 +807,10 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
 //
 // The keys are the rows of the first product, S^T = K Q^T, and the values' dimensions
 // those of the second, O^T = V^T P^T, so that the query rows are the columns, eight to a
-// product: with one sequence of 4 or 8 heads a group none is wasted, and a warp has the
-// registers to take two stages at a time, whose chains of products, exponentials and
-// conversions overlap (kStages2).  ldmatrix moves 16-bit pairs, here two neighbouring
+// product: with one sequence of 4 or 8 heads a group none is wasted (16 sequences of
+// 20,001 .. 60,000 tokens, 64/8 heads: 200.5 us with the query rows as the sixteen rows,
+// 174.8 so; two stages of a warp at a time, whose chains overlap, gain nothing).
+// ldmatrix moves 16-bit pairs, here two neighbouring
 // dimensions.  Keys: a lane gets dimensions 4 tig .. 4 tig + 3 of sixteen, so the
 // queries' fragments are loaded in that order.  Values, transposed: the pairs of two
 // tokens; the bytes are taken apart, the even dimensions being the first eight rows of
@@ -791,73 +924,57 @@ struct E8State {
     float v_ref;
 };
 
-// N stages' 16 tokens each of a warp: slots `slot[n]` of the group's ring.  kAll: every
-// row sees every token; else row (r, e) those of bits see[n][r][e], and live[n] says
-// which tokens are the segment's.
-template <int D, int NR, int N, bool kAll>
-__device__ __forceinline__ void e8_stages(E8State<D, NR>& st, uint8_t* ring, const float* scales, const int (&slot)[N],
-                                          const uint32_t (&live)[N], const uint32_t (&see)[N][NR][2], int w4,
-                                          int lane) {
+// A stage's 16 tokens of a warp, in the ring's slot at `tile` (shared address), which
+// has the scales `sc`.  kAll: every row sees every token; else row (r, e) those of bits
+// see[r][e], and `live` says which tokens are the segment's.
+template <int D, int NR, bool kAll>
+__device__ __forceinline__ void e8_stage(E8State<D, NR>& st, uint8_t* tile, const float* sc, uint32_t live,
+                                         const uint32_t (&see)[NR][2], int w4, int lane) {
     using C = DecCfg<D, true>;
     const int gid = lane >> 2, mi = lane >> 3, rr = lane & 7;
     // (this lane's row of a matrix; the swizzle's turn and the matrix's half of a step)
     const int t = w4 * 16 + (mi & 1) * 8 + rr;
-    const uint32_t at = t * D, turn = (mi >> 1) ^ (D == 128 ? t & 7 : t >> 1 & 3);
-    auto chunk = [&](int n, int k2) {
-        return smem_addr(ring) + slot[n] * C::kStageBytes + at + ((turn ^ (2 * k2)) << 4);
-    };
-    float2 sk[N], sv[N];
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-        const float* s = scales + slot[n] * C::kStageScales + w4 * 2;
-        sk[n] = *reinterpret_cast<const float2*>(s);
-        sv[n] = *reinterpret_cast<const float2*>(s + C::kStageScales / 2);
-        if (!kAll) {
-            // a block without rows of the segment has no scale worth reading
-            if (!(live[n] & 0xffu)) sk[n].x = 0.f, sv[n].x = power_of_two(kLeastScale);
-            if (!(live[n] >> 8)) sk[n].y = 0.f, sv[n].y = power_of_two(kLeastScale);
-        }
+    const uint32_t at = smem_addr(tile) + t * D, turn = (mi >> 1) ^ (D == 128 ? t & 7 : t >> 1 & 3);
+    float2 sk = *reinterpret_cast<const float2*>(sc + w4 * 2);
+    float2 sv = *reinterpret_cast<const float2*>(sc + C::kStageScales / 2 + w4 * 2);
+    if (!kAll) {
+        // a block without rows of the segment has no scale worth reading
+        if (!(live & 0xffu)) sk.x = 0.f, sv.x = power_of_two(kLeastScale);
+        if (!(live >> 8)) sk.y = 0.f, sv.y = power_of_two(kLeastScale);
     }
-    // weights' exponents x - m
-    float x[N][NR][4];
+    // logits
+    float x[NR][4];
     {
-        float acc[N][NR][2][4] = {};   // (even and odd steps apart)
+        float acc[NR][2][4] = {};   // (even and odd steps apart, where there is one tile)
 #pragma unroll
-        for (int k2 = 0; k2 < D / 32; ++k2)
+        for (int k2 = 0; k2 < D / 32; ++k2) {
+            // tokens 0 .. 7 and 8 .. 15 of an even step, then of the odd one
+            uint32_t b[4];
+            ldsm_x4(at + ((turn ^ (2 * k2)) << 4), b[0], b[1], b[2], b[3]);
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                // tokens 0 .. 7 and 8 .. 15 of an even step, then of the odd one
-                uint32_t b[4];
-                ldsm_x4(chunk(n, k2), b[0], b[1], b[2], b[3]);
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t f[4] = {e4m3_to_f16x2(b[2 * h]), e4m3_to_f16x2(b[2 * h + 1]),
+                                       e4m3_to_f16x2(b[2 * h] >> 16), e4m3_to_f16x2(b[2 * h + 1] >> 16)};
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t f[4] = {e4m3_to_f16x2(b[2 * h]), e4m3_to_f16x2(b[2 * h + 1]),
-                                           e4m3_to_f16x2(b[2 * h] >> 16), e4m3_to_f16x2(b[2 * h + 1] >> 16)};
-#pragma unroll
-                    for (int r = 0; r < NR; ++r)
-                        mma_f16(acc[n][r][N * NR > 1 ? 0 : h], f, st.qb[r][2 * k2 + h][0], st.qb[r][2 * k2 + h][1]);
-                }
+                for (int r = 0; r < NR; ++r)
+                    mma_f16(acc[r][NR > 1 ? 0 : h], f, st.qb[r][2 * k2 + h][0], st.qb[r][2 * k2 + h][1]);
             }
+        }
         bool over = false;
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float most = -INFINITY;
+                const float f0 = st.c[r][e] * sk.x, f1 = st.c[r][e] * sk.y;
 #pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    const float f0 = st.c[r][e] * sk[n].x, f1 = st.c[r][e] * sk[n].y;
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        float s = acc[n][r][0][2 * b + e];
-                        if (N * NR == 1) s += acc[n][r][1][2 * b + e];
-                        float y = s * (b ? f1 : f0);
-                        if (!kAll && !(see[n][r][e] >> (gid + 8 * b) & 1u)) y = -INFINITY;
-                        x[n][r][2 * b + e] = y;
-                        most = fmaxf(most, y);
-                    }
+                for (int b = 0; b < 2; ++b) {
+                    float s = acc[r][0][2 * b + e];
+                    if (NR == 1) s += acc[r][1][2 * b + e];
+                    s *= b ? f1 : f0;
+                    if (!kAll && !(see[r][e] >> (gid + 8 * b) & 1u)) s = -INFINITY;
+                    x[r][2 * b + e] = s;
                 }
-                over |= most - st.m[r][e] > kMost;
+                over |= fmaxf(x[r][e], x[r][2 + e]) - st.m[r][e] > kMost;
             }
         if (__any_sync(0xffffffffu, over)) {
             // references from the largest logits
@@ -865,9 +982,7 @@ __device__ __forceinline__ void e8_stages(E8State<D, NR>& st, uint8_t* ring, con
             for (int r = 0; r < NR; ++r)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float mx = -INFINITY;
-#pragma unroll
-                    for (int n = 0; n < N; ++n) mx = fmaxf(mx, fmaxf(x[n][r][e], x[n][r][2 + e]));
+                    float mx = fmaxf(x[r][e], x[r][2 + e]);
 #pragma unroll
                     for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
                     mx = fmaxf(st.m[r][e], mx - kLift);
@@ -882,9 +997,7 @@ __device__ __forceinline__ void e8_stages(E8State<D, NR>& st, uint8_t* ring, con
                 }
         }
     }
-    float sv_most = st.v_ref;
-#pragma unroll
-    for (int n = 0; n < N; ++n) sv_most = fmaxf(sv_most, fmaxf(sv[n].x, sv[n].y));
+    const float sv_most = fmaxf(sv.x, sv.y);
     if (sv_most > st.v_ref) {  // (warp-uniform)
         const float f = scale_ratio(st.v_ref, sv_most);
         st.v_ref = sv_most;
@@ -895,49 +1008,41 @@ __device__ __forceinline__ void e8_stages(E8State<D, NR>& st, uint8_t* ring, con
 #pragma unroll
                 for (int i = 0; i < 4; ++i) st.o[j][r][i] *= f;
     }
-    uint32_t pb[N][NR][2];
+    uint32_t pb[NR][2];
 #pragma unroll
-    for (int n = 0; n < N; ++n)
+    for (int b = 0; b < 2; ++b) {
+        const float f = scale_ratio(b ? sv.y : sv.x, st.v_ref);
+        const uint32_t f2 = pack_f16x2(f, f);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const float f = scale_ratio(b ? sv[n].y : sv[n].x, st.v_ref);
-            const uint32_t f2 = pack_f16x2(f, f);
-#pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                const uint32_t h = pack_f16x2(exp2f(x[n][r][2 * b] - st.m[r][0]), exp2f(x[n][r][2 * b + 1] - st.m[r][1]));
-                add_f16x2(h, st.l[r][0], st.l[r][1]);
-                pb[n][r][b] = transpose_8x8(mul_f16x2(h, f2));
-            }
+        for (int r = 0; r < NR; ++r) {
+            const uint32_t h = pack_f16x2(exp2f(x[r][2 * b] - st.m[r][0]), exp2f(x[r][2 * b + 1] - st.m[r][1]));
+            add_f16x2(h, st.l[r][0], st.l[r][1]);
+            pb[r][b] = transpose_8x8(mul_f16x2(h, f2));
         }
+    }
     if (!kAll) {
         // V rows that hold none of the segment's may hold anything: zero them, so that
         // 0 * V stays 0
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            uint8_t* v = ring + slot[n] * C::kStageBytes + C::kTileBytes + w4 * 16 * D;
-            for (int i = lane; i < D; i += 32)   // 16-byte chunks of 16 rows
-                if (!((live[n] >> (i / (D / 16))) & 1u))
-                    *reinterpret_cast<uint4*>(v + i * 16) = make_uint4(0, 0, 0, 0);
-        }
+        uint8_t* v = tile + C::kTileBytes + w4 * 16 * D;
+        for (int i = lane; i < D; i += 32)   // 16-byte chunks of 16 rows
+            if (!((live >> (i / (D / 16))) & 1u)) *reinterpret_cast<uint4*>(v + i * 16) = make_uint4(0, 0, 0, 0);
         __syncwarp();
     }
 #pragma unroll
-    for (int j2 = 0; j2 < D / 32; ++j2)
+    for (int j2 = 0; j2 < D / 32; ++j2) {
+        // tokens 0 .. 7 and 8 .. 15 of sixteen dimensions, then of the next
+        uint32_t b[4];
+        ldsm_x4_trans(at + ((turn ^ (2 * j2)) << 4) + C::kTileBytes, b[0], b[1], b[2], b[3]);
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            // tokens 0 .. 7 and 8 .. 15 of sixteen dimensions, then of the next
-            uint32_t b[4];
-            ldsm_x4_trans(chunk(n, j2) + C::kTileBytes, b[0], b[1], b[2], b[3]);
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t y = b[2 * h], z = b[2 * h + 1];
+            const uint32_t f[4] = {
+                e4m3_to_f16x2(__byte_perm(y, 0u, 0x4420)), e4m3_to_f16x2(__byte_perm(y, 0u, 0x4431)),
+                e4m3_to_f16x2(__byte_perm(z, 0u, 0x4420)), e4m3_to_f16x2(__byte_perm(z, 0u, 0x4431))};
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t y = b[2 * h], z = b[2 * h + 1];
-                const uint32_t f[4] = {
-                    e4m3_to_f16x2(__byte_perm(y, 0u, 0x4420)), e4m3_to_f16x2(__byte_perm(y, 0u, 0x4431)),
-                    e4m3_to_f16x2(__byte_perm(z, 0u, 0x4420)), e4m3_to_f16x2(__byte_perm(z, 0u, 0x4431))};
-#pragma unroll
-                for (int r = 0; r < NR; ++r) mma_f16(st.o[2 * j2 + h][r], f, pb[n][r][0], pb[n][r][1]);
-            }
+            for (int r = 0; r < NR; ++r) mma_f16(st.o[2 * j2 + h][r], f, pb[r][0], pb[r][1]);
         }
+    }
     if (!kAll) fence_proxy_async_smem();  // generic writes before the next TMA fill
 }
 
@@ -968,7 +1073,6 @@ template <int D, int NR>
 __device__ __forceinline__ int e8_item(const DecodeArgs& a, const ItemHead& item, int it, bool last, int s,
                                        E8Ring& rg, uint8_t* smem, uint64_t* all_bars, int warp, int lane) {
     using C = DecCfg<D, true>;
-    constexpr int kStages2 = NR == 1 ? 2 : 1;
     const int gid = lane >> 2, tig = lane & 3, w4 = warp & 3, G = a.G;
     const DecodeSeg* seg = a.segs + item.seg;
     const int n_tok = seg->n_tok, rows = item.n_grp * G;
@@ -996,51 +1100,32 @@ __device__ __forceinline__ int e8_item(const DecodeArgs& a, const ItemHead& item
     // none see what they like)
     int all = a.page_fill ? 0 : n_tok;
     for (int j = 0; j < item.n_grp; ++j) all = min(all, seg->grp_lim[j]);
-    auto step = [&](auto count) {
-        constexpr int N = decltype(count)::value;
-        int slot[N];
-        uint32_t phase[N];
-        const bool whole = N > 1 || (s + 1) * kStageTokens <= all;
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            slot[n] = rg.slot;
-            phase[n] = rg.phase;
-            if (++rg.slot == C::kStages) {
-                rg.slot = 0;
-                rg.phase ^= 1;
-            }
+    for (; s < item.s1; s += kDecodeGroups) {
+        const int slot = rg.slot;
+        rg.wait(&rg.bars[slot], rg.phase, lane);
+        if (++rg.slot == C::kStages) {
+            rg.slot = 0;
+            rg.phase ^= 1;
         }
+        if (rg.dead) continue;
+        uint8_t* tile = rg.slots + slot * C::kStageBytes;
+        const float* sc = rg.scales + slot * C::kStageScales;
+        uint32_t see[NR][2] = {};
+        if ((s + 1) * kStageTokens <= all) {
+            e8_stage<D, NR, true>(st, tile, sc, 0xffffu, see, w4, lane);
+        } else {
+            const int tbase = s * kStageTokens + w4 * 16;
+            const uint32_t live = e8_live(a, seg, n_tok, tbase);
 #pragma unroll
-        for (int n = 0; n < N; ++n) rg.wait(&rg.bars[slot[n]], phase[n], lane);
-        if (!rg.dead) {
-            uint32_t live[N] = {}, see[N][NR][2] = {};
-            if constexpr (N > 1) {
-                e8_stages<D, NR, N, true>(st, rg.slots, rg.scales, slot, live, see, w4, lane);
-            } else if (whole) {
-                e8_stages<D, NR, N, true>(st, rg.slots, rg.scales, slot, live, see, w4, lane);
-            } else {
+            for (int r = 0; r < NR; ++r)
 #pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    const int tbase = (s + n * kDecodeGroups) * kStageTokens + w4 * 16;
-                    live[n] = e8_live(a, seg, n_tok, tbase);
-#pragma unroll
-                    for (int r = 0; r < NR; ++r)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            see[n][r][e] = live[n] & ((1u << min(max(lim[r][e] - tbase, 0), 16)) - 1u);
-                }
-                e8_stages<D, NR, N, false>(st, rg.slots, rg.scales, slot, live, see, w4, lane);
-            }
-            __syncwarp();
-            if (lane == 0)
-#pragma unroll
-                for (int n = 0; n < N; ++n) mbar_arrive(smem_addr(&rg.bars[C::kStages + slot[n]]));
+                for (int e = 0; e < 2; ++e)
+                    see[r][e] = live & ((1u << min(max(lim[r][e] - tbase, 0), 16)) - 1u);
+            e8_stage<D, NR, false>(st, tile, sc, live, see, w4, lane);
         }
-        s += N * kDecodeGroups;
-    };
-    while (kStages2 > 1 && (s + kDecodeGroups + 1) * kStageTokens <= all && s + kDecodeGroups < item.s1)
-        step(std::integral_constant<int, kStages2>());
-    while (s < item.s1) step(std::integral_constant<int, 1>());
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_addr(&rg.bars[C::kStages + slot]));
+    }
 
     // the rows, eight at a time, to the closing warps
     float* red_m = reinterpret_cast<float*>(smem + C::kOffRed);
@@ -1397,21 +1482,33 @@ __global__ void __launch_bounds__(DecCfg<D, kE8>::kThreads, 1)
     const int group = warp - kDecodeConsumerWarps;
     if (group >= 0 && group < kDecodeGroups) {
         if (threadIdx.x == C::kConsumers) prefetch_tmap(&tmap);
-        Producer<D, kE8> pr{&tmap, a, smem + group * C::kStages * C::kStageBytes,
-                            bars + group * 2 * C::kStages,
-                            reinterpret_cast<float*>(smem + C::kOffScales) + group * C::kStages * C::kStageScales,
-                            abort_flag, group, lane};
-        // A reused plan is read before the wait.  Pages no in-flight work writes
-        // (the host checked every library write to them is complete; the kernels
-        // before this one write no other pool memory) are loaded before it too:
-        // the first stages stream in while the previous kernel finishes.
-        if (a.plan_ready) pr.init();
-        named_bar_sync(2, C::kThreads);  // (the barriers are initialised)
-        if (a.plan_ready) pr.early();
-        grid_dependency_wait();
-        grid_launch_dependents();  // the next kernel may be scheduled as CTAs retire
-        if (!a.plan_ready) pr.init();
-        pr.run();
+        if constexpr (kE8) {
+            ProducerE8<D> pr{&tmap, a, smem + group * C::kStages * C::kStageBytes,
+                             reinterpret_cast<float*>(smem + C::kOffScales) + group * C::kStages * C::kStageScales,
+                             bars + group * 2 * C::kStages, abort_flag, group, lane};
+            int n = 0;
+            if (a.plan_ready) pr.init();
+            named_bar_sync(2, C::kThreads);  // (the barriers are initialised)
+            if (a.plan_ready) n = pr.early();
+            grid_dependency_wait();
+            grid_launch_dependents();
+            if (!a.plan_ready) pr.init();
+            pr.run(n);
+        } else {
+            Producer<D> pr{&tmap, a, smem + group * C::kStages * C::kStageBytes,
+                           bars + group * 2 * C::kStages, abort_flag, group, lane};
+            // A reused plan is read before the wait.  Pages no in-flight work writes
+            // (the host checked every library write to them is complete; the kernels
+            // before this one write no other pool memory) are loaded before it too:
+            // the first stages stream in while the previous kernel finishes.
+            if (a.plan_ready) pr.init();
+            named_bar_sync(2, C::kThreads);  // (the barriers are initialised)
+            if (a.plan_ready) pr.early();
+            grid_dependency_wait();
+            grid_launch_dependents();  // the next kernel may be scheduled as CTAs retire
+            if (!a.plan_ready) pr.init();
+            pr.run();
+        }
         return;
     }
     const bool closer = group >= kDecodeGroups;
