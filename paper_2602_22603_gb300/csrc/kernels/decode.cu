@@ -118,6 +118,13 @@ struct DecCfg {
     static_assert(kOffScales % 16 == 0 && kOffRed % 16 == 0, "alignment");
 };
 
+// One thread of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t on;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
+    return on != 0;
+}
+
 __device__ __forceinline__ uint32_t ld_u32(const __nv_bfloat16* p) {
     return *reinterpret_cast<const uint32_t*>(p);
 }
@@ -287,129 +294,164 @@ struct Producer {
     }
 };
 
-// The same for rows in 8 bits, whose stages pass twice as fast: a page's id, read from
-// the plan when the walk got to its stage, then held the stage up (1,470 of 1,690 cycles
-// a stage, with the consumers waiting 600 of theirs).  So kWalks walks take turns, each
-// kWalks stages of the group apart, and a stage's id is read that many stages ahead.  A
-// lane has the scale of a block of keys or of values, copied beside its stage; those
-// whose block begins a box load it too.
-template <int D>
+// The same for rows in 8 bits, whose stages pass twice as fast: what the producer did
+// for each held them up (1,470 of 1,690 cycles a stage, with the consumers waiting 600 of
+// theirs), first of all its reads of the plan when the walk got there.  So a stage's
+// page id is read kAhead stages ahead, an item's record two items ahead and its
+// segment's one item.
+//
+// kWhole (pages of 64 tokens or more): a stage is one box of keys, one of values and 32
+// bytes of either's scales, all issued by one elected thread.  Else a lane stands for a
+// block of keys or of values; those whose block begins a box load it, and every lane
+// copies its block's scale by cp.async (a bulk copy takes no less than 16 bytes).
+template <int D, bool kWhole>
 struct ProducerE8 {
     using C = DecCfg<D, true>;
-    static constexpr int kWalks = 4;
-    struct Walk {
-        int it, s, s1, head, page_off, n_pages;  // stage s of item it
-        int32_t pid;                             // this lane's page, -1: none
+    static constexpr int kAhead = 4;
+    static constexpr int kHalf = C::kStageScales / 2;
+    // A stage to come: the first row of its head's box of keys in its page, and the
+    // (lane's) page, -1: none.
+    struct Stage {
+        int row;
+        int32_t pid;
+        bool on;        // there is such a stage
+    };
+    struct Item {
+        int s0, s1, head, seg, page_off, n_pages;
     };
     const CUtensorMap* tmap;
     const DecodeKv8Args& a;
-    uint8_t* ring;      // the group's slots
-    float* scales;      // ... and their scales
-    uint64_t* bars;     // ... and barriers: full [kStages], empty [kStages]
+    uint32_t ring;      // the group's slots (shared address)
+    uint32_t scales;    // ... and their scales
+    uint32_t bars;      // ... and barriers: full [kStages], empty [kStages]
     volatile int* abort_flag;
     int group, lane;
-    int kv, block;      // the lane's plane and block of a stage
-    bool box;           // a box begins at its block
-    int it1;
-    int64_t page_scales;  // scales of a page, all planes
-    Walk w[kWalks];
+    int kv, block;      // (not kWhole) the lane's plane and block of a stage
+    bool box;           // ... a box begins at its block
+    int it, it1, s, log_p;       // the walk: stage s of item `it`
+    Item cur, nx, n2;            // the item, the next one, and the one after without its segment
+    int64_t page_scales;         // scales of a page, all planes
+    const float* layer_scales;
+    Stage w[kAhead];
     int slot;
-    uint32_t phase;
-    uint32_t issued, issued_phase;  // per-slot bits of the last issue
-    bool first;         // the CTA's first stage has not gone out yet
+    uint32_t phase, issued;
+    bool first;                  // the CTA's first stage has not gone out yet
 
-    __device__ void init() {
+    __device__ __forceinline__ void init() {
         kv = lane & 1;
         block = lane >> 1;
         box = lane < C::kStageScales && block * kScaleRows % min(a.P, kStageTokens) == 0;
+        log_p = __ffs(a.P) - 1;
         page_scales = (int64_t)2 * a.Hkv * (a.P / kScaleRows);
+        layer_scales = a.scales + (int64_t)a.layer * a.num_pages * page_scales;
+        it = a.cta_begin[blockIdx.x];
         it1 = a.cta_begin[blockIdx.x + 1];
         slot = 0;
-        phase = 0;
-        issued = issued_phase = 0;
+        phase = issued = 0;
         first = group == 0;
-        Walk x;
-        x.it = a.cta_begin[blockIdx.x];
-        if (x.it < it1) open(x);
+        read_item(it, cur);
+        read_item(it + 1, nx);
+        read_item(it + 2, n2);
+        read_segment(cur);
+        read_segment(nx);
+        s = cur.s0 + group;
+        settle();
 #pragma unroll
-        for (int i = 0; i < kWalks; ++i) {
-            w[i] = x;
-            if (x.it >= it1) continue;
-            w[i].s += group + i * kDecodeGroups;
-            settle(w[i]);
-        }
+        for (int i = 0; i < kAhead; ++i) w[i] = next();
     }
-    __device__ void open(Walk& x) const {
-        const DecodeItem* item = a.items + x.it;
-        const DecodeSeg* seg = a.segs + item->seg;
-        x.s = item->s0;
+    __device__ __forceinline__ void read_item(int i, Item& x) const {
+        const DecodeItem* item = a.items + (i < it1 ? i : 0);
+        x.s0 = item->s0;
         x.s1 = item->s1;
         x.head = item->head;
-        x.page_off = seg->page_off;
-        x.n_pages = seg->n_pages;
+        x.seg = item->seg;
     }
-    // Carries a stage past the item's end into the items that follow.
-    __device__ __forceinline__ void settle(Walk& x) const {
-        while (x.s >= x.s1) {
-            const int over = x.s - x.s1;
-            if (++x.it >= it1) return;
-            open(x);
-            x.s += over;
+    __device__ __forceinline__ void read_segment(Item& x) const {
+        x.page_off = a.segs[x.seg].page_off;
+        x.n_pages = a.segs[x.seg].n_pages;
+    }
+    // Carries the walk past an item's end into the items that follow.
+    __device__ __forceinline__ void settle() {
+        while (it < it1 && s >= cur.s1) {
+            s += nx.s0 - cur.s1;
+            ++it;
+            cur = nx;
+            nx = n2;
+            read_segment(nx);
+            read_item(it + 2, n2);
         }
-        const int at = (x.s * kStageTokens + block * kScaleRows) / a.P;
-        x.pid = lane < C::kStageScales && at < x.n_pages ? a.page_ids[x.page_off + at] : -1;
     }
-    __device__ __forceinline__ int row(const Walk& x) const {
-        return (kv * a.Hkv + x.head) * a.P + (a.P > kStageTokens ? (x.s * kStageTokens) & (a.P - 1) : 0);
+    // The walk's stage, and on to the group's next.
+    __device__ __forceinline__ Stage next() {
+        Stage x;
+        x.on = it < it1;
+        x.row = cur.head * a.P + (kWhole ? (s * kStageTokens) & (a.P - 1) : 0);
+        const int at = (s * kStageTokens + (kWhole ? 0 : block * kScaleRows)) >> log_p;
+        x.pid = x.on && (kWhole || lane < C::kStageScales) && at < cur.n_pages ? a.page_ids[cur.page_off + at] : -1;
+        s += kDecodeGroups;
+        settle();
+        return x;
     }
-    // Issues a walk's stage into the (free) slot.
-    __device__ __forceinline__ void issue(const Walk& x) {
-        const uint32_t full = smem_addr(&bars[slot]);
+    // Issues a stage into the (free) slot.
+    __device__ __forceinline__ void issue(const Stage& x) {
+        const uint32_t full = bars + 8 * slot, dst = ring + slot * C::kStageBytes;
+        const uint32_t sdst = scales + slot * C::kStageScales * 4;
         const bool valid = x.pid >= 0 && x.pid < a.num_pages;
         if (x.pid < -1 || x.pid >= a.num_pages) set_error(a.err, kErrBounds);
-        const uint32_t n = __popc(__ballot_sync(0xffffffffu, box && valid));
-        if (lane == 0) {
-            if (n) mbar_arrive_expect_tx(full, n * min(a.P, kStageTokens) * C::kRowBytes);
-            else mbar_arrive(full);
-        }
-        __syncwarp();
-        if (box && valid)
-            tma_load_4d(smem_addr(ring) + slot * C::kStageBytes + kv * C::kTileBytes +
-                            block * kScaleRows * C::kRowBytes,
-                        tmap, full, 0, row(x), x.pid, a.layer);
-        if (lane < C::kStageScales) {
-            if (valid) {
-                const int at = (x.s * kStageTokens + block * kScaleRows) & (a.P - 1);
-                const float* src = a.scales + ((int64_t)a.layer * a.num_pages + x.pid) * page_scales +
-                                   ((kv * a.Hkv + x.head) * a.P + at) / kScaleRows;
-                const uint32_t to =
-                    smem_addr(scales + slot * C::kStageScales + kv * (C::kStageScales / 2) + block);
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(src) : "memory");
+        if constexpr (kWhole) {
+            const int rk = x.row, rv = rk + a.Hkv * a.P;
+            const float* src = layer_scales + x.pid * page_scales;
+            if (elect_one()) {
+                if (valid) {
+                    mbar_arrive_expect_tx(full, C::kStageBytes + C::kStageScales * 4);
+                    tma_load_4d(dst, tmap, full, 0, rk, x.pid, a.layer);
+                    tma_load_4d(dst + C::kTileBytes, tmap, full, 0, rv, x.pid, a.layer);
+                    bulk_load(sdst, src + rk / kScaleRows, kHalf * 4, full);
+                    bulk_load(sdst + kHalf * 4, src + rv / kScaleRows, kHalf * 4, full);
+                } else {
+                    mbar_arrive(full);
+                }
             }
-            // (arrives when this lane's copy has landed)
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full) : "memory");
+        } else {
+            const uint32_t n = __popc(__ballot_sync(0xffffffffu, box && valid));
+            if (lane == 0) {
+                if (n) mbar_arrive_expect_tx(full, n * a.P * C::kRowBytes);
+                else mbar_arrive(full);
+            }
+            __syncwarp();
+            if (box && valid)
+                tma_load_4d(dst + kv * C::kTileBytes + block * kScaleRows * C::kRowBytes, tmap, full, 0,
+                            x.row + kv * a.Hkv * a.P, x.pid, a.layer);
+            if (lane < C::kStageScales) {
+                if (valid)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(sdst + (kv * kHalf + block) * 4),
+                                 "l"(layer_scales + x.pid * page_scales +
+                                     (x.row + kv * a.Hkv * a.P + (block * kScaleRows & (a.P - 1))) / kScaleRows)
+                                 : "memory");
+                // (arrives when this lane's copy has landed)
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full) : "memory");
+            }
         }
-        issued |= 1u << slot;
-        issued_phase = (issued_phase & ~(1u << slot)) | (phase << slot);
     }
     __device__ __forceinline__ void next_slot() {
         first = false;
+        ++issued;
         if (++slot == C::kStages) {
             slot = 0;
             phase ^= 1;
         }
     }
-    // Before the grid-dependency wait (see Producer): of the first kWalks stages those in
+    // Before the grid-dependency wait (see Producer): of the first kAhead stages those in
     // pages that no running work writes; the others are prefetched into L2.  Returns
     // the stages issued.
-    __device__ int early() {
-        static_assert(kWalks <= C::kStages, "slots that are free at the start");
+    __device__ __forceinline__ int early() {
+        static_assert(kAhead <= C::kStages, "slots that are free at the start");
         if ((int)blockIdx.x == a.debug_drop_cta) return 0;
         int n = 0;
-        bool go = a.kv_early && a.P >= kStageTokens;
+        bool go = kWhole && a.kv_early;
 #pragma unroll
-        for (int i = 0; i < kWalks; ++i) {
-            if (w[i].it >= it1) break;
+        for (int i = 0; i < kAhead; ++i) {
+            if (!w[i].on) break;
             bool unsafe = false;
             for (int u = lane; u < a.n_unsafe; u += 32) unsafe |= a.unsafe[u] == w[i].pid;
             go = go && !__any_sync(0xffffffffu, unsafe);
@@ -417,42 +459,53 @@ struct ProducerE8 {
                 issue(w[i]);
                 next_slot();
                 ++n;
-            } else if (box && w[i].pid >= 0 && w[i].pid < a.num_pages) {
-                tma_prefetch_l2_4d(tmap, 0, row(w[i]), w[i].pid, a.layer);
+            } else if ((kWhole ? lane < 2 : box) && w[i].pid >= 0 && w[i].pid < a.num_pages) {
+                tma_prefetch_l2_4d(tmap, 0, w[i].row + kv * a.Hkv * a.P, w[i].pid, a.layer);
             }
         }
         return n;
     }
     // n: stages that went out early.
-    __device__ void run(int n) {
+    __device__ __forceinline__ void run(int n) {
         bool ok = true, more = true;
         while (more) {
 #pragma unroll
-            for (int i = 0; i < kWalks; ++i) {
-                more = more && w[i].it < it1;
+            for (int i = 0; i < kAhead; ++i) {
+                more = more && w[i].on;
                 if (!more) continue;
                 if (n > 0) {
                     --n;
                 } else {
-                    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&bars[C::kStages + slot]), phase ^ 1, abort_flag));
+                    ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (C::kStages + slot), phase ^ 1, abort_flag));
                     more = ok;
                     if (!ok) continue;
-                    // (test hook: see Producer)
+                    // test hook: leave this stage unsignalled (see Producer)
                     if (!(first && (int)blockIdx.x == a.debug_drop_cta)) issue(w[i]);
                     next_slot();
                 }
-                w[i].s += kWalks * kDecodeGroups;
-                settle(w[i]);
+                w[i] = next();
             }
         }
         if (!ok && lane == 0) {
             if (!*abort_flag) set_error(a.err, kErrTimeout);
             *abort_flag = 1;
-            // Leave only after every copy already issued has landed (bounded).
-            for (int sl = 0; sl < C::kStages; ++sl)
-                if ((issued >> sl) & 1u) mbar_wait(smem_addr(&bars[sl]), (issued_phase >> sl) & 1u);
+            // Leave only after every copy already issued has landed (bounded; a stage that
+            // the test hook left out is waited for in vain).
+            for (uint32_t u = issued > C::kStages ? issued - C::kStages : 0; u < issued; ++u)
+                mbar_wait(bars + 8 * (u % C::kStages), (u / C::kStages) & 1);
         }
         __syncwarp();
+    }
+    // The producer warp's whole life.
+    __device__ __forceinline__ void live() {
+        int n = 0;
+        if (a.plan_ready) init();
+        named_bar_sync(2, C::kThreads);  // (the barriers are initialised)
+        if (a.plan_ready) n = early();
+        grid_dependency_wait();
+        grid_launch_dependents();
+        if (!a.plan_ready) init();
+        run(n);
     }
 };
 
@@ -1471,7 +1524,8 @@ __global__ void __launch_bounds__(DecCfg<D, kE8>::kThreads, 1)
         // per group: full [kStages], empty [kStages]
         for (int s = 0; s < kDecodeGroups * 2 * C::kStages; ++s)
             mbar_init(smem_addr(&bars[s]),
-                      s / C::kStages % 2 ? kDecodeConsumerWarps / kDecodeGroups : 1 + C::kStageScales);
+                      s / C::kStages % 2 ? kDecodeConsumerWarps / kDecodeGroups
+                                         : kE8 && a.P < kStageTokens ? 1 + C::kStageScales : 1);
         mbar_init(smem_addr(&bars[C::kBarOut]), kDecodeConsumerWarps);
         mbar_init(smem_addr(&bars[C::kBarOutFree]), C::kClosers / 32);
         mbar_init(smem_addr(&bars[C::kBarRuns]), 1);
@@ -1483,17 +1537,11 @@ __global__ void __launch_bounds__(DecCfg<D, kE8>::kThreads, 1)
     if (group >= 0 && group < kDecodeGroups) {
         if (threadIdx.x == C::kConsumers) prefetch_tmap(&tmap);
         if constexpr (kE8) {
-            ProducerE8<D> pr{&tmap, a, smem + group * C::kStages * C::kStageBytes,
-                             reinterpret_cast<float*>(smem + C::kOffScales) + group * C::kStages * C::kStageScales,
-                             bars + group * 2 * C::kStages, abort_flag, group, lane};
-            int n = 0;
-            if (a.plan_ready) pr.init();
-            named_bar_sync(2, C::kThreads);  // (the barriers are initialised)
-            if (a.plan_ready) n = pr.early();
-            grid_dependency_wait();
-            grid_launch_dependents();
-            if (!a.plan_ready) pr.init();
-            pr.run(n);
+            const uint32_t slots = smem_addr(smem) + group * C::kStages * C::kStageBytes;
+            const uint32_t scales = smem_addr(smem) + C::kOffScales + group * C::kStages * C::kStageScales * 4;
+            const uint32_t own = smem_addr(bars + group * 2 * C::kStages);
+            if (a.P >= kStageTokens) ProducerE8<D, true>{&tmap, a, slots, scales, own, abort_flag, group, lane}.live();
+            else ProducerE8<D, false>{&tmap, a, slots, scales, own, abort_flag, group, lane}.live();
         } else {
             Producer<D> pr{&tmap, a, smem + group * C::kStages * C::kStageBytes,
                            bars + group * 2 * C::kStages, abort_flag, group, lane};
