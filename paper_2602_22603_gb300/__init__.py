@@ -657,9 +657,15 @@ class Cache:
         n = self._counted(seqs, n_new, n, "qk_norm_rope_store")
         k, ks, _ = _rows(k, hkv, d, "k", n)
         v, vs, _ = _rows(v, hkv, d, "v", n)
-        sq_qk_norm_rope_store(self.handle, seqs, n_new, layer, q, qs, k, ks, v, vs,
-                              _flat(positions, _INT, n, "positions"), params,
-                              _flat(q_out, _BF16, n * hq * d, "q_out"), stream)
+        positions = _flat(positions, _INT, n, "positions")
+        q_out = _flat(q_out, _BF16, n * hq * d, "q_out")
+        # (the C call at once: sq_qk_norm_rope_store takes the arguments apart again)
+        arr, _keep = _ints(seqs)
+        cnt, _keep2 = _ints(n_new)
+        rc = lib().sq_qk_norm_rope_store(self.handle, arr, len(seqs), cnt, layer, q, qs, k, ks, v, vs, positions,
+                                         ctypes.addressof(params), q_out, _stream(stream))
+        if rc != SQ_OK:
+            raise SqError(rc, "sq_qk_norm_rope_store")
 
     def qk_norm_rope(self, q, k, positions, params, q_out, k_out, stream=None):
         """Norms and rotation of q [tokens, Hq, D] and k [tokens, Hkv, D] into tensors."""
@@ -726,8 +732,12 @@ class Cache:
         if _BF16 is None:
             _types()
         size = self._counted(seqs, counts, None, "read_kv") * self.Hkv * self.D
-        sq_read_kv(self.handle, seqs, counts, layer, _flat(k, _BF16, size, "k"), _flat(v, _BF16, size, "v"),
-                   stream)
+        k, v = _flat(k, _BF16, size, "k"), _flat(v, _BF16, size, "v")
+        arr, _keep = _ints(seqs)
+        cnt, _keep2 = _ints(counts)
+        rc = lib().sq_read_kv(self.handle, arr, len(seqs), cnt, layer, k, v, _stream(stream))
+        if rc != SQ_OK:
+            raise SqError(rc, "sq_read_kv")
 
     accept_draft = (lambda self, seq, n_draft, path, stream=None:
                     sq_accept_draft(self.handle, seq, n_draft, path, stream))

@@ -13,14 +13,14 @@ static int append_8bit(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const in
             const Geometry& g = c->g;
             cudaStream_t st = as_stream(stream);
             std::vector<RowRun> runs;
-            list_runs(c, seqs, n_seqs, n_new, kScaleRows, &runs, &pages);
+            list_runs(c, seqs, n_seqs, n_new, &runs, &pages);
             Kv8StoreInlineArgs a = {};
             a.k = bf16(k);
             a.v = bf16(v);
             a.k_stride = a.v_stride = (int64_t)g.Hkv * g.D;
             a.layer_stride = n * a.k_stride;
             a.pool = kv8_pool(c);
-            a.n_runs = (int32_t)runs.size();
+            set_runs(runs, &a);
             a.Hkv = g.Hkv;
             a.n_layers = g.L;
             a.plain = 1;
@@ -58,8 +58,7 @@ int read_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* co
     if (any_overlap({{c->pool, c->pool_bytes}}, {{k, rows_bytes(n, w, w)}, {v, rows_bytes(n, w, w)}}))
         return SQ_ERR_INVALID_ARG;
     std::vector<RowRun> runs;
-    // (64 rows at most, so that a long page is several CTAs' as well)
-    list_runs(c, seqs, n_seqs, counts, std::min(g.P, 64), &runs, nullptr);
+    list_runs(c, seqs, n_seqs, counts, &runs, nullptr);
     cudaStream_t st = as_stream(stream);
     Kv8ReadInlineArgs a;
     a.pool = {nullptr, nullptr, g.num_pages, g.Hkv, g.P};

@@ -301,11 +301,10 @@ void list_places(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t*
     }
 }
 
-// The newest n_new[i] rows of each sequence as runs of consecutive slots, none over a
-// border of `most` slots (a power of two, at most a page), and their pages.
-void list_runs(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new, int32_t most,
-               std::vector<RowRun>* runs, std::vector<int32_t>* pages) {
-    const int32_t P = c->g.P;
+// The newest n_new[i] rows of each sequence as runs, and their pages.
+void list_runs(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new, std::vector<RowRun>* runs,
+               std::vector<int32_t>* pages) {
+    const int32_t P = c->g.P, most = std::min(P, kRunRows);
     int32_t first = 0;
     for (int32_t i = 0; i < n_seqs; ++i) {
         const Seq* s = c->host->seq(seqs[i]);
@@ -325,6 +324,17 @@ void list_runs(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n
             left -= std::min(left, s->fill[p - 1]);
         }
         first += m;
+    }
+}
+
+// What a store's launch is told of its runs.
+void set_runs(const std::vector<RowRun>& runs, Kv8StoreArgs* a) {
+    a->n_runs = (int32_t)runs.size();
+    a->blocks = a->most = 0;
+    for (const RowRun& r : runs) {
+        const int32_t s0 = r.row % kScaleRows, blocks = (s0 + r.n + kScaleRows - 1) / kScaleRows;
+        a->blocks = std::max(a->blocks, blocks);
+        a->most = std::max(a->most, blocks > 2 ? kScaleRows : blocks == 1 ? r.n : std::max(kScaleRows - s0, s0 + r.n - kScaleRows));
     }
 }
 
@@ -354,7 +364,7 @@ int store_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n
     std::vector<RowPlace> places;
     std::vector<RowRun> runs;
     std::vector<int32_t> pages;
-    if (c->kv8) list_runs(c, seqs, n_seqs, n_new, kScaleRows, &runs, &pages);
+    if (c->kv8) list_runs(c, seqs, n_seqs, n_new, &runs, &pages);
     const bool upload_places = c->kv8 ? runs.size() > (size_t)kRunsInline : n > kNormInline;
     const bool captured = upload_places && capturing(as_stream(stream));
     StorePlanEntry* hit = nullptr;
@@ -384,9 +394,7 @@ int store_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n
             a.runs = reinterpret_cast<const RowRun*>(uploaded);
             a.q_out = bf16(q_out);
             a.pool = kv8_pool(c);
-            a.n_runs = (int32_t)runs.size();
-            a.most = 0;
-            for (const RowRun& r : runs) a.most = std::max(a.most, r.n);
+            set_runs(runs, &a);
             a.layer = layer;
             a.n_layers = 1;
             a.plain = 0;

@@ -678,6 +678,15 @@ static int create_impl(const sq_config* cfg, bool kv8, sq_cache** out) {
     int rc = geometry_from(cfg, &g);
     if (rc != SQ_OK) return rc;
     if (cfg->decode_ctas < 0) return SQ_ERR_INVALID_ARG;
+    if (kv8 && g.D == 128) {
+        // Stages of half the bytes pass in half the time, and a unit's start does not:
+        // 48 sequences of 200 .. 60,000 tokens, 32/8 heads, 170 us at the costs of bf16
+        // rows, 158 at twice and 161 at three times those.  (At 64 dimensions the warps'
+        // work on a stage takes as long as before: windows of 2,048 tokens of 64
+        // sequences 19.8, 21.8 and 23.1.)
+        g.unit_cost *= 2;
+        g.short_unit_cost *= 2;
+    }
     if (cfg->kv_pool && (reinterpret_cast<uintptr_t>(cfg->kv_pool) & 255)) return SQ_ERR_INVALID_ARG;
     std::unique_ptr<sq_cache> c(new (std::nothrow) sq_cache());
     if (!c) return SQ_ERR_NO_MEMORY;

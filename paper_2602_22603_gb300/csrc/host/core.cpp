@@ -563,7 +563,7 @@ static int deal_decode_stages(const Geometry& g, int32_t n_seqs, int32_t n_ctas,
     int64_t total = 0, stages = 0;
     for (size_t v = 0; v < unit_seg.size(); ++v) {
         const int32_t n = ceil_div(out->segs[unit_seg[v]].n_tok, kStageTokens) - first_stage(unit_seg[v]);
-        total += n <= kShortUnitStages ? kDecodeShortUnitCost : kDecodeUnitCost;
+        total += n <= kShortUnitStages ? g.short_unit_cost : g.unit_cost;
         unit_start.push_back(total);
         total += n;
         stages += n;

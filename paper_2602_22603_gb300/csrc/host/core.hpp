@@ -49,6 +49,8 @@ enum Status : int {
 struct Geometry {
     int32_t L = 0, Hq = 0, Hkv = 0, D = 0, P = 0;
     int32_t num_pages = 0, max_seqs = 0, max_pages_per_seq = 0;
+    // what decode's planner takes the start of a unit for, in stages (see plan.hpp)
+    int32_t unit_cost = kDecodeUnitCost, short_unit_cost = kDecodeShortUnitCost;
     int32_t G() const { return Hq / Hkv; }
     // K+V bytes of one token of one layer
     int64_t token_layer_bytes() const { return 2LL * Hkv * D * 2; }

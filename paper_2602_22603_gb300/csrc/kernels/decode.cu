@@ -118,13 +118,6 @@ struct DecCfg {
     static_assert(kOffScales % 16 == 0 && kOffRed % 16 == 0, "alignment");
 };
 
-// One thread of a converged warp.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t on;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
-    return on != 0;
-}
-
 __device__ __forceinline__ uint32_t ld_u32(const __nv_bfloat16* p) {
     return *reinterpret_cast<const uint32_t*>(p);
 }

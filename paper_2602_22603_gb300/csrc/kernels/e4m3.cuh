@@ -9,6 +9,13 @@
 namespace sq {
 namespace dev {
 
+// One thread of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t on;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
+    return on != 0;
+}
+
 // Two codes (the low 16 bits) as fp16, exact: the first in the low half.
 __device__ __forceinline__ uint32_t e4m3_to_f16x2(uint32_t two) {
     uint32_t r;

@@ -36,8 +36,8 @@ __device__ __forceinline__ float4 unpack4(uint2 v) {
                        __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
 }
 
-// Tasks of a run: its keys' and its values' heads, then the query heads of `most`
-// rows.
+// Tasks of a block of a run: its keys' and its values' heads, then the query heads of
+// `most` rows.
 template <int D>
 struct StoreTasks {
     int q, total;
@@ -60,10 +60,20 @@ __global__ void __launch_bounds__(kStoreThreads)
     const int lane = threadIdx.x & 31;
     const StoreTasks<D> per(a.Hq, a.Hkv, a.most);
     const unsigned task = blockIdx.x * (kStoreThreads / 32) + (threadIdx.x >> 5);
-    const unsigned r = task / (unsigned)per.total;
+    const unsigned x = task / (unsigned)per.total, r = x / (unsigned)a.blocks;
     if (r >= (unsigned)a.n_runs) return;
-    int part = (int)(task - r * per.total);
-    const RowRun run = a.runs ? a.runs[r] : a.inline_run[r];
+    int part = (int)(task - x * per.total);
+    RowRun run = a.runs ? a.runs[r] : a.inline_run[r];
+    {
+        // the block's rows of it
+        const int b0 = (run.row & ~(kScaleRows - 1)) + (int)(x - r * a.blocks) * kScaleRows;
+        const int from = max(run.row, b0), skip = from - run.row;
+        run.n = min(run.row + run.n, b0 + kScaleRows) - from;
+        if (run.n <= 0) return;
+        run.row = from;
+        run.first += skip;
+        run.pos += skip;
+    }
     const int sub = lane / C::kLanes, l = lane % C::kLanes;
     Lane ln;
     if (part >= 2 * a.Hkv) {
@@ -463,7 +473,7 @@ cudaError_t launch_after(void (*kernel)(P...), dim3 grid, unsigned block, int sm
 
 template <int D>
 cudaError_t store(const Kv8StoreInlineArgs& a, cudaStream_t st) {
-    const int64_t warps = (int64_t)a.n_runs * StoreTasks<D>(a.Hq, a.Hkv, a.most).total;
+    const int64_t warps = (int64_t)a.n_runs * a.blocks * StoreTasks<D>(a.Hq, a.Hkv, a.most).total;
     constexpr int per = kStoreThreads / 32;
     const dim3 grid((unsigned)((warps + per - 1) / per), (unsigned)a.n_layers);
     return launch_after(a.interleaved ? sq_kv8_store_kernel<D, true> : sq_kv8_store_kernel<D, false>, grid,

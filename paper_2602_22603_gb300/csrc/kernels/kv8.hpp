@@ -17,13 +17,14 @@ constexpr int kScaleRows = 8;
 constexpr int kLeastScale = -100;
 constexpr int kMostScale = 120;  // of elements up to 2^128
 
-// Rows in consecutive slots of one page (row: page * P + slot of the first), the
-// call's from `first` on; pos: the first one's position.
+// Rows in consecutive slots of one page, none over a border of kRunRows (row: page * P +
+// slot of the first), the call's from `first` on; pos: the first one's position.
 struct RowRun {
     int32_t row, first, n, pos;
 };
+constexpr int kRunRows = 64;
 // Runs that go with the launch; more are uploaded.
-constexpr int kRunsInline = 200;
+constexpr int kRunsInline = 236;
 
 struct Kv8Pool {
     uint8_t* codes;
@@ -36,12 +37,12 @@ struct Kv8StoreArgs {
     int64_t q_stride, k_stride, v_stride;    // elements between tokens
     int64_t layer_stride;                    // ... between layers (k and v)
     const int32_t* positions;                // [n] or null: the runs'
-    const RowRun* runs;                      // each within one block; null: inline_run
+    const RowRun* runs;                      // or null: inline_run
     __nv_bfloat16* q_out;                    // [n][Hq][D]
     Kv8Pool pool;
     const void *q_weight, *k_weight;         // [D] or null (ones)
     const float2* rope;                      // [max_pos][rot / 2] (cos, sin)
-    int32_t n_runs, most;                    // most: rows of any run
+    int32_t n_runs, blocks, most;            // most blocks of any run, most rows in any block
     int32_t Hq, Hkv, layer, n_layers;        // Hq 0: no queries
     int32_t plain;                           // 1: keys as they are, like values
     int32_t rot, interleaved, max_pos, weight_f32;

@@ -123,7 +123,8 @@ constexpr int s_buffers = D == 64 && (M & ~kE8) == (kBlocks | kOneTile | kTwoPro
 // read each (MMA warp and eight softmax warps).
 constexpr int kItemSlots = 4;
 constexpr int kItemReaders = 9;
-constexpr int kConverters = 8;  // warps that widen tiles (kE8), a warp to 16 rows
+// Warps that widen tiles (kE8): two groups that take alternate tiles, a warp to 32 rows.
+constexpr int kConvertGroups = 2, kConverters = 4 * kConvertGroups;
 constexpr int kProducer2 = 10;  // query blocks: the warp of their odd loads
 
 template <int D, int M>
@@ -171,7 +172,7 @@ struct PreCfg {
     static constexpr int kOffRows = kOffScales + kSlots * kTileScales * 4;
     static constexpr int kSmemBytes = kOffRows + (e8<M> ? kSlots * 4 : 0) + 1024;  // + alignment slack
     // registers of a thread (8 bits; see the kernel): softmax warps, converters, others
-    static constexpr int kSoftmaxRegs = 152, kConvertRegs = 48, kOtherRegs = 72;
+    static constexpr int kSoftmaxRegs = 144, kConvertRegs = 56, kOtherRegs = 80;
     static constexpr int kAllRegs = 256 * kSoftmaxRegs + 32 * kConverters * kConvertRegs + 128 * kOtherRegs;
     static_assert(!e8<M> || kThreads * 96 >= kAllRegs, "register split");
     static constexpr uint32_t kTmemCols = 512;
@@ -719,6 +720,70 @@ __device__ void prefill_produce(const CUtensorMap* pool_map, const CUtensorMap* 
     }
 }
 
+// Load b of a batch (see block_produce, whose lanes hold a box each) for rows in 8 bits:
+// its boxes of codes, with their scales, and for the converters the rows of V that the
+// sequence has.  Pages of 64 tokens or more: two boxes with 32 bytes of scales each,
+// issued by one elected thread.  (Every lane with a box issuing its own, and a scale
+// by cp.async for each lane, took 1,400 cycles a load.)  Else a lane to each box and to
+// the scale of each eight rows: a box has less of them than a bulk copy takes.
+template <int D, int M, typename Args>
+__device__ __forceinline__ void issue_codes(const CUtensorMap* pool_map, const Args& a, const Smem& sm, uint32_t bar,
+                                            uint32_t slot, int b, int per, int mine, int piece, int32_t page, int row,
+                                            int rows, uint32_t bytes, int kv, int lane) {
+    using C = PreCfg<D, M>;
+    const uint32_t codes = sm.base + C::kOffCodes + slot * C::kCodeStride;
+    const uint32_t scales = sm.base + C::kOffScales + slot * C::kTileScales * 4;
+    volatile int* n_rows = reinterpret_cast<volatile int*>(sm.ptr + C::kOffRows + 4 * slot);
+    const int64_t page_rows = (int64_t)2 * a.Hkv * a.P, layer_row = (int64_t)a.layer * a.num_pages * page_rows;
+    constexpr uint32_t kBoxScales = 64 / kScaleRows * 4;  // bytes
+    if (per == 2) {
+        const int from = 2 * b;
+        const int32_t p0 = __shfl_sync(0xffffffffu, page, from), p1 = __shfl_sync(0xffffffffu, page, from + 1);
+        const int w0 = __shfl_sync(0xffffffffu, row, from), w1 = __shfl_sync(0xffffffffu, row, from + 1);
+        const int limit = kv == 1 ? rows : 64;
+        const int r = __shfl_sync(0xffffffffu, limit, from) + __shfl_sync(0xffffffffu, limit, from + 1);
+        if (elect_one()) {
+            *n_rows = r;
+            const uint32_t n = (p0 >= 0 ? 1 : 0) + (p1 >= 0 ? 1 : 0);
+            mbar_arrive_expect_tx(bar, n * (64 * D + kBoxScales));
+            if (p0 >= 0) {
+                tma_load_4d(codes, pool_map, bar, 0, w0, p0, a.layer);
+                bulk_load(scales, a.scales + (layer_row + p0 * page_rows + w0) / kScaleRows, kBoxScales, bar);
+            }
+            if (p1 >= 0) {
+                tma_load_4d(codes + 64 * D, pool_map, bar, 0, w1, p1, a.layer);
+                bulk_load(scales + kBoxScales, a.scales + (layer_row + p1 * page_rows + w1) / kScaleRows, kBoxScales,
+                          bar);
+            }
+        }
+        __syncwarp();
+        return;
+    }
+    const int br = 128 / per;
+    const int r = __reduce_add_sync(0xffffffffu, mine == b ? rows : 0);
+    // the lane's eight rows lie in lane `from`'s box
+    const int from = b * per + lane * kScaleRows / br;
+    const int32_t spage = __shfl_sync(0xffffffffu, page, from & 31);
+    const int srow = __shfl_sync(0xffffffffu, row, from & 31) + lane * kScaleRows % br;
+    if (mine == b) {
+        if (piece == 0) {
+            *n_rows = kv == 1 ? r : kPrefillKeys;
+            mbar_arrive_expect_tx(bar, bytes);
+        }
+        __syncwarp((uint32_t)((1ull << per) - 1) << (b * per));
+        if (page >= 0) tma_load_4d(codes + piece * br * D, pool_map, bar, 0, row, page, a.layer);
+    }
+    __syncwarp();
+    if (lane < C::kTileScales) {
+        if (spage >= 0)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(scales + lane * 4),
+                         "l"(a.scales + (layer_row + spage * page_rows + srow) / kScaleRows)
+                         : "memory");
+        // (arrives when this lane's copy has landed)
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+    }
+}
+
 // The producer warps of block items.  A lane holds what one box of the next loads
 // needs (BlockBatch), so that a load costs a warp a wait, an expected byte count and
 // the boxes' copies.  Pages of 64 tokens or more are one warp's loads (one-tile blocks
@@ -862,41 +927,17 @@ __device__ void block_produce(const CUtensorMap* pool_map, const CUtensorMap* qm
                     const uint32_t bar = e8<M> ? sm.bar<D, M>(C::kBarRaw + slot)
                                          : fix ? sm.bar<D, M>(C::kBarVfix)
                                                : sm.bar<D, M>(C::kBarFull + slot);
-                    if constexpr (e8<M>) {
-                        // (the converters zero the rows of V that the bf16 instances' fix does)
-                        const int r0 = __reduce_add_sync(0xffffffffu, mine == b ? rows : 0);
-                        if (mine == b && piece == 0)
-                            *reinterpret_cast<volatile int*>(sm.ptr + C::kOffRows + 4 * slot) =
-                                kv == 1 ? r0 : kPrefillKeys;
-                        // a lane to the scale of eight rows, whose box is lane `from`'s
-                        const int from = b * per + lane * kScaleRows / br;
-                        const int32_t spage = __shfl_sync(0xffffffffu, page, from & 31);
-                        const int skey = __shfl_sync(0xffffffffu, cur.key, from & 31);
-                        const int skv = __shfl_sync(0xffffffffu, kv, from & 31);
-                        if (lane < C::kTileScales) {
-                            if (spage >= 0) {
-                                const int at = (skey & (a.P - 1)) + lane * kScaleRows % br;
-                                const int64_t plane =
-                                    (((int64_t)a.layer * a.num_pages + spage) * 2 + skv) * a.Hkv + it.g;
-                                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(
-                                                 sm.base + C::kOffScales + (slot * C::kTileScales + lane) * 4),
-                                             "l"(a.scales + (plane * a.P + at) / kScaleRows)
-                                             : "memory");
-                            }
-                            // (arrives when this lane's copy has landed)
-                            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar)
-                                         : "memory");
-                        }
-                    }
-                    if (mine == b) {
+                    if constexpr (e8<M>)
+                        issue_codes<D, M>(pool_map, a, sm, bar, slot, b, per, mine, piece, page, row, rows, bytes, kv,
+                                          lane);
+                    if (!e8<M> && mine == b) {
                         if (piece == 0) mbar_arrive_expect_tx(bar, bytes);
                         __syncwarp(group << (b * per));
                         if (box) {
                             const uint32_t dst =
-                                e8<M> ? sm.base + C::kOffCodes + slot * C::kCodeStride + piece * br * D
-                                      : sm.base + C::kOffRing + slot * C::kSlotBytes + piece * br * 128;
+                                sm.base + C::kOffRing + slot * C::kSlotBytes + piece * br * 128;
 #pragma unroll
-                            for (int cb = 0; cb < (e8<M> ? 1 : C::kColBlocks); ++cb)
+                            for (int cb = 0; cb < C::kColBlocks; ++cb)
                                 tma_load_4d(dst + cb * C::kBlockBytes, pool_map, bar, cb * 64, row, page,
                                             a.layer);
                         }
@@ -972,15 +1013,55 @@ __device__ __forceinline__ void take_registers() {
 
 // Rows in 8 bits: the converters widen a tile's codes to bf16 where the products read
 // them: code times scale, exact, so that everything behind is as for bf16 rows.  A
-// thread takes half a row (a warp whole rows, which it has read before it writes).  V
-// rows past the sequence's end are zeroed, as the bf16 instances' producer does.
+// thread takes a row, half of it at a time (of 128 codes: what it writes lies over its
+// own row's codes alone, which it has read by then).  V rows past the sequence's end are
+// zeroed, as the bf16 instances' producer does.  (Eight warps on one tile, half a row a
+// thread: 1,600 cycles a tile, most of them the chain of loads, conversions, stores and
+// fence, which two groups on a tile each overlap: 107.3 us for 8 trees of 16, 93.0 so.)
+//
+// A code's conversion makes an fp16 number of it, and one mixed-precision fused
+// multiply-add the fp32 product with the scale, where that is an fp16 number.
+__device__ __forceinline__ uint32_t widen_pair(uint32_t f16x2, uint16_t scale) {
+    float lo, hi;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\t"
+        "fma.rn.f32.f16 %0, l, %3, %4;\n\tfma.rn.f32.f16 %1, h, %3, %4;\n\t}"
+        : "=f"(lo), "=f"(hi)
+        : "r"(f16x2), "h"(scale), "f"(-0.f));
+    return pack_bf16x2(lo, hi);
+}
+// 64 codes of a row as bf16 into its 128 bytes of a column block.
+template <bool kNarrow>
+__device__ __forceinline__ void widen_half(const uint4 (&c)[4], float s, uint8_t* out, int row) {
+    const uint16_t s16 = __half_as_ushort(__float2half_rn(s));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t cw[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t o[4];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t w = cw[2 * h + k];
+                if (kNarrow) {
+                    o[2 * k] = widen_pair(e4m3_to_f16x2(w), s16);
+                    o[2 * k + 1] = widen_pair(e4m3_to_f16x2(w >> 16), s16);
+                } else {
+                    const float4 v = e4m3_values(w, s);
+                    o[2 * k] = pack_bf16x2(v.x, v.y);
+                    o[2 * k + 1] = pack_bf16x2(v.z, v.w);
+                }
+            }
+            *reinterpret_cast<uint4*>(out + (((2 * i + h) ^ (row & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+    }
+}
+
 template <int D, int M>
 __device__ void convert_tiles(const Smem& sm, int* err, volatile int* abort_flag, int w, int lane) {
     using C = PreCfg<D, M>;
-    constexpr int kVecs = D / 32;  // 16 codes each
-    const int row = w * 16 + (lane & 15), half = lane >> 4;
+    const int row = (w & 3) * 32 + lane, group = w >> 2;
     const int turn = D == 128 ? row & 7 : row >> 1 & 3;  // (the tensor map's swizzle)
-    uint32_t slot = 0, phase = 0;
+    uint32_t slot = group, phase = 0;                    // of the group's next tile
     bool ok = true;
     for (uint32_t k = 0; ok; ++k) {
         ok = __all_sync(0xffffffffu, item_wait<D, M>(sm, k, abort_flag));
@@ -989,38 +1070,37 @@ __device__ void convert_tiles(const Smem& sm, int* err, volatile int* abort_flag
         __syncwarp();
         if (lane == 0) item_free<D, M>(sm, k);
         if (T < 0) break;
-        for (int x = 0; x < 2 * T; ++x) {
+        // (an item's loads are an even number)
+        static_assert(kConvertGroups == 2, "a load of either kind of an item's pairs");
+        for (int x = 0; x < T; ++x) {
             ok = __all_sync(0xffffffffu, mbar_wait(sm.bar<D, M>(C::kBarRaw + slot), phase, abort_flag));
             if (!ok) break;
             const uint8_t* src = sm.ptr + C::kOffCodes + slot * C::kCodeStride + row * D;
-            uint4 c[kVecs];
-#pragma unroll
-            for (int i = 0; i < kVecs; ++i)
-                c[i] = *reinterpret_cast<const uint4*>(src + (((half * kVecs + i) ^ turn) << 4));
+            uint8_t* to = sm.ptr + C::kOffRing + slot * C::kSlotBytes + row * 128;
             const float s =
                 reinterpret_cast<const float*>(sm.ptr + C::kOffScales)[slot * C::kTileScales + row / kScaleRows];
             const bool on = row < *reinterpret_cast<const volatile int*>(sm.ptr + C::kOffRows + 4 * slot);
-            __syncwarp();
-            uint8_t* to = sm.ptr + C::kOffRing + slot * C::kSlotBytes + row * 128 +
-                          (D == 128 ? half * C::kBlockBytes : 0);
+            // (scales are powers of two: most are fp16 numbers too)
+            const bool narrow = __all_sync(0xffffffffu, s >= 0x1p-24f && s <= 0x1p15f);
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i) {
-                const uint32_t cw[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+            for (int cb = 0; cb < D / 64; ++cb) {
+                uint4 c[4];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float4 a = e4m3_values(cw[2 * h], s), b = e4m3_values(cw[2 * h + 1], s);
-                    const int chunk = (D == 128 ? 0 : 4 * half) + 2 * i + h;
-                    *reinterpret_cast<uint4*>(to + ((chunk ^ (row & 7)) << 4)) =
-                        on ? make_uint4(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w), pack_bf16x2(b.x, b.y),
-                                        pack_bf16x2(b.z, b.w))
-                           : make_uint4(0, 0, 0, 0);
-                }
+                for (int i = 0; i < 4; ++i)
+                    c[i] = *reinterpret_cast<const uint4*>(src + (((cb * 4 + i) ^ turn) << 4));
+                uint8_t* out = to + cb * C::kBlockBytes;
+                if (narrow) widen_half<true>(c, s, out, row);
+                else widen_half<false>(c, s, out, row);
             }
+            if (!__all_sync(0xffffffffu, on) && !on)
+                for (int x = 0; x < 8 * C::kColBlocks; ++x)
+                    *reinterpret_cast<uint4*>(to + (x >> 3) * C::kBlockBytes + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(sm.bar<D, M>(C::kBarFull + slot));
-            if (++slot == C::kSlots) {
-                slot = 0;
+            slot += kConvertGroups;
+            if (slot >= C::kSlots) {
+                slot -= C::kSlots;
                 phase ^= 1;
             }
         }
@@ -2153,8 +2233,8 @@ __global__ void __launch_bounds__(PreCfg<D, ModeOf<Args>::value>::kThreads, 1)
     if (role == 0 && lane == 0) {
         mbar_init(sm.bar<D, M>(C::kBarQ), 1);
         for (int s = 0; s < C::kSlots; ++s) {
-            mbar_init(sm.bar<D, M>(C::kBarFull + s), e8<M> ? kConverters : 1);
-            if (e8<M>) mbar_init(sm.bar<D, M>(C::kBarRaw + s), 1 + C::kTileScales);
+            mbar_init(sm.bar<D, M>(C::kBarFull + s), e8<M> ? kConverters / kConvertGroups : 1);
+            if (e8<M>) mbar_init(sm.bar<D, M>(C::kBarRaw + s), a.n_pieces > 2 ? 1 + C::kTileScales : 1);
             mbar_init(sm.bar<D, M>(C::kBarEmpty + s), 1);
         }
         for (int b = 0; b < C::kBufs; ++b) {

@@ -25,21 +25,30 @@ cudaError_t launch_kv8_store(const Kv8StoreInlineArgs& a, int D, cudaStream_t st
     const Clock& c = tick(st);
     if (a.runs) use(st, c, a.runs, false);
     for (int r = 0; r < a.n_runs; ++r) {
-        const RowRun run = a.runs ? a.runs[r] : a.inline_run[r];
-        const int page = run.row / a.pool.P, slot = run.row % a.pool.P, s0 = slot % kScaleRows;
-        if (run.n < 1 || run.n > a.most || s0 + run.n > kScaleRows || page < 0 || page >= a.pool.num_pages)
-            if (!a.plain || run.n < 1 || s0 + run.n > kScaleRows) ++g_bad;
-        for (int l = 0; l < a.n_layers; ++l)
-            for (int kv = 0; kv < 2; ++kv)
-                for (int h = 0; h < a.Hkv; ++h) {
-                    const int64_t row = plane8(a.pool, a.layer + l, page, kv, h) + slot;
-                    const __nv_bfloat16* src = (kv ? a.v : a.k) + l * a.layer_stride;
-                    for (int i = 0; i < run.n; ++i)
-                        for (int e = 0; e < D; ++e)
-                            a.pool.codes[(row + i) * D + e] = *reinterpret_cast<const uint8_t*>(
-                                src + (run.first + i) * (kv ? a.v_stride : a.k_stride) + h * D + e);
-                    a.pool.scales[row / kScaleRows] = (float)(s0 + run.n);
-                }
+        const RowRun all = a.runs ? a.runs[r] : a.inline_run[r];
+        const int page = all.row / a.pool.P;
+        if (all.n < 1 || all.n > kRunRows || page < 0 || page >= a.pool.num_pages ||
+            all.row / std::min(a.pool.P, kRunRows) != (all.row + all.n - 1) / std::min(a.pool.P, kRunRows))
+            ++g_bad;
+        for (int b = 0; b < a.blocks; ++b) {
+            const int b0 = all.row / kScaleRows * kScaleRows + b * kScaleRows;
+            const int from = std::max(all.row, b0), end = std::min(all.row + all.n, b0 + kScaleRows);
+            if (end - from > a.most) ++g_bad;
+            if (b + 1 == a.blocks && end < all.row + all.n) ++g_bad;
+            if (end <= from) continue;
+            const int first = all.first + from - all.row, slot = from % a.pool.P;
+            for (int l = 0; l < a.n_layers; ++l)
+                for (int kv = 0; kv < 2; ++kv)
+                    for (int h = 0; h < a.Hkv; ++h) {
+                        const int64_t row = plane8(a.pool, a.layer + l, page, kv, h) + slot;
+                        const __nv_bfloat16* src = (kv ? a.v : a.k) + l * a.layer_stride;
+                        for (int i = 0; i < end - from; ++i)
+                            for (int e = 0; e < D; ++e)
+                                a.pool.codes[(row + i) * D + e] = *reinterpret_cast<const uint8_t*>(
+                                    src + (first + i) * (kv ? a.v_stride : a.k_stride) + h * D + e);
+                        a.pool.scales[row / kScaleRows] = (float)(slot % kScaleRows + end - from);
+                    }
+        }
     }
     return cudaSuccess;
 }
