@@ -36,15 +36,17 @@ __device__ __forceinline__ float4 e4m3_values(uint32_t four, float scale) {
 __device__ __forceinline__ float e4m3_input(float x, float most) {
     return fabsf(x) <= 3.4028234e38f ? fminf(fmaxf(x, -most), most) : NAN;
 }
-// Two values as codes, to nearest even: a's in the low byte.
-__device__ __forceinline__ uint32_t to_e4m3x2(float a, float b, float most) {
-    a = e4m3_input(a, most);
-    b = e4m3_input(b, most);
+// Two values of at most 448 or NaN as codes, to nearest even: a's in the low byte.
+__device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {
     uint32_t r;
     asm("{\n\t.reg .b16 t;\n\tcvt.rn.satfinite.e4m3x2.f32 t, %2, %1;\n\tcvt.u32.u16 %0, t;\n\t}"
         : "=r"(r)
         : "f"(a), "f"(b));
     return r;
+}
+// Any two.
+__device__ __forceinline__ uint32_t to_e4m3x2(float a, float b, float most) {
+    return to_e4m3x2(e4m3_input(a, most), e4m3_input(b, most));
 }
 __device__ __forceinline__ uint32_t to_e4m3(const float4& v, int e) {
     const float inv = __int_as_float((127 - e) << 23), most = e < kMostScale ? 448.f : 240.f;

@@ -30,12 +30,6 @@ __device__ __forceinline__ int64_t plane_row(const Kv8Pool& p, int layer, int64_
     return (((layer * p.num_pages + page) * 2 + kv) * p.Hkv + head) * p.P;
 }
 
-// Four elements of an input row.
-__device__ __forceinline__ float4 unpack4(uint2 v) {
-    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u),
-                       __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
-}
-
 // Tasks of a block of a run: its keys' and its values' heads, then the query heads of
 // `most` rows.
 template <int D>
@@ -60,13 +54,13 @@ __global__ void __launch_bounds__(kStoreThreads)
     const int lane = threadIdx.x & 31;
     const StoreTasks<D> per(a.Hq, a.Hkv, a.most);
     const unsigned task = blockIdx.x * (kStoreThreads / 32) + (threadIdx.x >> 5);
-    const unsigned x = task / (unsigned)per.total, r = x / (unsigned)a.blocks;
+    const unsigned at = task / (unsigned)per.total, r = at / (unsigned)a.blocks;
     if (r >= (unsigned)a.n_runs) return;
-    int part = (int)(task - x * per.total);
+    int part = (int)(task - at * per.total);
     RowRun run = a.runs ? a.runs[r] : a.inline_run[r];
     {
         // the block's rows of it
-        const int b0 = (run.row & ~(kScaleRows - 1)) + (int)(x - r * a.blocks) * kScaleRows;
+        const int b0 = (run.row & ~(kScaleRows - 1)) + (int)(at - r * a.blocks) * kScaleRows;
         const int from = max(run.row, b0), skip = from - run.row;
         run.n = min(run.row + run.n, b0 + kScaleRows) - from;
         if (run.n <= 0) return;
@@ -164,54 +158,80 @@ __global__ void __launch_bounds__(kStoreThreads)
     const float old = s0 > 0 ? *scale : 0.f;
     Eight w;
     if (norm) load_weights(a.k_weight, a.weight_f32, ln, w);
-    float4 xf[kPass], xg[kPass];
-    float size = 0.f;
+    // (rows that are none are zeros)
+    Eight x[kPass];
 #pragma unroll
     for (int u = 0; u < kPass; ++u) {
         const int i = u * C::kGroups + sub;
-        const bool fresh = i >= s0 && i < s1;
+        x[u].set(rf[u], rg[u]);
         if (norm) {
             // (every lane: the sums are the warp's)
             Turn tn;
             int pos = 0;
-            if (fresh) {
+            if (i >= s0 && i < s1) {
                 pos = a.positions ? __ldg(&a.positions[run.first + i - s0]) : run.pos + i - s0;
                 if (a.rot > 0) pos = checked_pos(pos, a.max_pos, a.err);
             }
             load_turn<kPairs>(tn, a.rope, pos, a.rot, ln);
-            Eight x;
-            x.set(rf[u], rg[u]);
-            f32x2 ss = mul2(x.v[0], x.v[0]);
+            f32x2 ss = mul2(x[u].v[0], x[u].v[0]);
 #pragma unroll
-            for (int k = 1; k < 4; ++k) ss = fma2(x.v[k], x.v[k], ss);
+            for (int k = 1; k < 4; ++k) ss = fma2(x[u].v[k], x[u].v[k], ss);
             const float rs = rsqrtf(row_sum<D>(ss) * (1.f / D) + a.eps);
             const f32x2 rr = f2(rs, rs);
-            float2 o[4];
+            Eight y;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                o[k] = un2(mul2(fma2(x.v[k], mul2(w.v[k], tn.c[k]),
-                                     ln.turned(mul2(x.other<kPairs>(k), mul2(w.other<kPairs>(k), tn.s[k])))),
-                                rr));
-            xf[u] = make_float4(o[0].x, o[0].y, o[1].x, o[1].y);
-            xg[u] = make_float4(o[2].x, o[2].y, o[3].x, o[3].y);
-        } else {
-            xf[u] = unpack4(rf[u]);
-            xg[u] = unpack4(rg[u]);
+                y.v[k] = mul2(fma2(x[u].v[k], mul2(w.v[k], tn.c[k]),
+                                   ln.turned(mul2(x[u].other<kPairs>(k), mul2(w.other<kPairs>(k), tn.s[k])))),
+                              rr);
+            x[u] = y;
         }
         if (i < s0) {
-            xf[u] = e4m3_values(rf[u].x, old);
-            xg[u] = e4m3_values(rg[u].x, old);
+            const float4 f = e4m3_values(rf[u].x, old), g = e4m3_values(rg[u].x, old);
+            x[u].v[0] = f2(f.x, f.y);
+            x[u].v[1] = f2(f.z, f.w);
+            x[u].v[2] = f2(g.x, g.y);
+            x[u].v[3] = f2(g.z, g.w);
         }
-        if (i < s1) size = fmaxf(size, fmaxf(finite_size(xf[u]), finite_size(xg[u])));
+        if (i >= s1) x[u].v[0] = x[u].v[1] = x[u].v[2] = x[u].v[3] = 0;
     }
-    const int e = scale_exponent(warp_size(size));
+    // the largest size (NaN is none; an infinity, seldom, is left out the second time)
+    float size = 0.f;
+#pragma unroll
+    for (int u = 0; u < kPass; ++u)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 v = un2(x[u].v[k]);
+            size = fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), size);
+        }
+    size = warp_size(size);
+    const bool odd = !(size < 0x1.fp127f);   // (and sizes that round to infinities)
+    if (odd) {
+        size = 0.f;
+#pragma unroll
+        for (int u = 0; u < kPass; ++u)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float2 v = un2(x[u].v[k]);
+                size = fmaxf(fmaxf(finite_size(v.x), finite_size(v.y)), size);
+            }
+        size = warp_size(size);
+    }
+    const int e = scale_exponent(size);
     const float s = power_of_two(e);
+    const f32x2 inv = f2(power_of_two(-e), power_of_two(-e));
 #pragma unroll
     for (int u = 0; u < kPass; ++u) {
         const int i = u * C::kGroups + sub;
         if (i >= s1 || (i < s0 && s == old)) continue;
-        *reinterpret_cast<uint32_t*>(codes + i * D + ln.f) = to_e4m3(xf[u], e);
-        *reinterpret_cast<uint32_t*>(codes + i * D + ln.g) = to_e4m3(xg[u], e);
+        uint32_t c[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 v = un2(mul2(x[u].v[k], inv));
+            c[k] = odd ? to_e4m3x2(v.x, v.y, e < kMostScale ? 448.f : 240.f) : to_e4m3x2(v.x, v.y);
+        }
+        *reinterpret_cast<uint32_t*>(codes + i * D + ln.f) = c[0] | c[1] << 16;
+        *reinterpret_cast<uint32_t*>(codes + i * D + ln.g) = c[2] | c[3] << 16;
     }
     if (lane == 0) *scale = s;
 }
