@@ -186,6 +186,7 @@ struct sq_cache {
     bool own_pool = false;
     size_t pool_bytes = 0;
     CUtensorMap tmap;
+    CUtensorMap pair_map;  // (8-bit caches) a page's keys and values of a head in one box
     void* encode_fn = nullptr;  // cuTensorMapEncodeTiled
     int* d_err = nullptr;
     // prefill split-K partials, reused by every call (grown on demand)
@@ -310,6 +311,23 @@ int make_pool_map(const sq_cache* c, void* pool, int elem, int cols, int32_t pag
     return r == CUDA_SUCCESS ? SQ_OK : SQ_ERR_UNSUPPORTED;
 }
 
+// The codes again, with dims head dim, slot, KV head, K or V, page of a layer: a box has
+// the rows of a page of a head, keys and then values.
+int make_pair_map(sq_cache* c) {
+    auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(c->encode_fn);
+    const Geometry& g = c->g;
+    const cuuint64_t head = (cuuint64_t)g.P * g.D;
+    cuuint64_t dims[5] = {(cuuint64_t)g.D, (cuuint64_t)g.P, (cuuint64_t)g.Hkv, 2, (cuuint64_t)g.num_pages * g.L};
+    cuuint64_t strides[4] = {(cuuint64_t)g.D, head, g.Hkv * head, 2 * g.Hkv * head};
+    cuuint32_t box[5] = {(cuuint32_t)g.D, (cuuint32_t)std::min(g.P, kStageTokens), 1, 2, 1};
+    cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    CUresult r = encode(&c->pair_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, c->pool, dims, strides, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        g.D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SQ_OK : SQ_ERR_UNSUPPORTED;
+}
+
 int make_tensor_map(sq_cache* c) {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult q;
@@ -318,7 +336,8 @@ int make_tensor_map(sq_cache* c) {
         q != cudaDriverEntryPointSuccess || !fn)
         return SQ_ERR_CUDA;
     c->encode_fn = fn;
-    return make_pool_map(c, c->pool, c->kv8 ? 1 : 2, c->kv8 ? c->g.D : 64, c->g.num_pages, c->g.L, &c->tmap);
+    const int rc = make_pool_map(c, c->pool, c->kv8 ? 1 : 2, c->kv8 ? c->g.D : 64, c->g.num_pages, c->g.L, &c->tmap);
+    return rc == SQ_OK && c->kv8 ? make_pair_map(c) : rc;
 }
 
 // Queries {D, Hq, n_q}: one box is the G heads of a KV head x BP positions.
@@ -678,6 +697,8 @@ static int create_impl(const sq_config* cfg, bool kv8, sq_cache** out) {
     int rc = geometry_from(cfg, &g);
     if (rc != SQ_OK) return rc;
     if (cfg->decode_ctas < 0) return SQ_ERR_INVALID_ARG;
+    // (a row's place in a layer is 32 bits)
+    if (kv8 && (int64_t)g.num_pages * g.P > 0x7fffffff) return SQ_ERR_UNSUPPORTED;
     if (kv8 && g.D == 128) {
         // Stages of half the bytes pass in half the time, and a unit's start does not:
         // 48 sequences of 200 .. 60,000 tokens, 32/8 heads, 170 us at the costs of bf16
@@ -1282,7 +1303,7 @@ static int decode_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, int32_t 
     c->debug_flags &= ~SQ_DEBUG_DROP_DECODE_STAGE;
     a.err = c->d_err;
     a.scales = c->kv8 ? kv8_pool(c).scales : nullptr;
-    e = c->kv8 ? launch_decode_kv8(c->tmap, a, L.n_ctas, g.D, st) : launch_decode(c->tmap, a, L.n_ctas, g.D, st);
+    e = c->kv8 ? launch_decode_kv8(c->pair_map, a, L.n_ctas, g.D, st) : launch_decode(c->tmap, a, L.n_ctas, g.D, st);
     if (e != cudaSuccess) return drop_plan(*hit, st, cuda_status(e));
     if (!captured) {
         e = cudaEventRecord(hit->ev, st);
@@ -1900,7 +1921,7 @@ int sq_decode_attention_noalloc(sq_cache* c, const sq_seq* seqs, int32_t n_seqs,
     c->debug_flags &= ~SQ_DEBUG_DROP_DECODE_STAGE;
     a.err = c->d_err;
     a.scales = c->kv8 ? kv8_pool(c).scales : nullptr;
-    e = c->kv8 ? launch_decode_kv8(c->tmap, a, L.n_ctas, g.D, st) : launch_decode(c->tmap, a, L.n_ctas, g.D, st);
+    e = c->kv8 ? launch_decode_kv8(c->pair_map, a, L.n_ctas, g.D, st) : launch_decode(c->tmap, a, L.n_ctas, g.D, st);
     if (e != cudaSuccess) return cuda_status(e);
     for (int32_t i = 0; i < n_seqs; ++i) c->host->seq_mut(seqs[i])->last_stream = stream;
     c->stats.decode_calls += 1;

@@ -293,19 +293,22 @@ struct Producer {
 // page id is read kAhead stages ahead, an item's record two items ahead and its
 // segment's one item.
 //
-// kWhole (pages of 64 tokens or more): a stage is one box of keys, one of values and 32
-// bytes of either's scales, all issued by one elected thread.  Else a lane stands for a
-// block of keys or of values; those whose block begins a box load it, and every lane
-// copies its block's scale by cp.async (a bulk copy takes no less than 16 bytes).
+// A box has the rows of a page (64 at most) of keys and of values, one after the other,
+// since every box costs its thread about 100 cycles (windows of 2,048 tokens of 64
+// sequences on pages of 16: 18.9 -> 17.1 us).  kWhole (pages of 64 tokens or more): a
+// stage is one box and 32 bytes of either plane's scales, all issued by one elected
+// thread.  Else a lane stands for a block of keys or of values; of those that begin a
+// page the keys' load it, and every lane copies its block's scale by cp.async (a bulk
+// copy takes no less than 16 bytes).
 template <int D, bool kWhole>
 struct ProducerE8 {
     using C = DecCfg<D, true>;
     static constexpr int kAhead = 4;
     static constexpr int kHalf = C::kStageScales / 2;
-    // A stage to come: the first row of its head's box of keys in its page, and the
-    // (lane's) page, -1: none.
+    // A stage to come: its KV head, its first row in its page, and the (lane's) page, -1:
+    // none.
     struct Stage {
-        int row;
+        int head, row;
         int32_t pid;
         bool on;        // there is such a stage
     };
@@ -320,7 +323,7 @@ struct ProducerE8 {
     volatile int* abort_flag;
     int group, lane;
     int kv, block;      // (not kWhole) the lane's plane and block of a stage
-    bool box;           // ... a box begins at its block
+    bool box;           // ... it issues the box that begins there
     int it, it1, s, log_p;       // the walk: stage s of item `it`
     Item cur, nx, n2;            // the item, the next one, and the one after without its segment
     int64_t page_scales;         // scales of a page, all planes
@@ -333,7 +336,7 @@ struct ProducerE8 {
     __device__ __forceinline__ void init() {
         kv = lane & 1;
         block = lane >> 1;
-        box = lane < C::kStageScales && block * kScaleRows % min(a.P, kStageTokens) == 0;
+        box = lane < C::kStageScales && kv == 0 && block * kScaleRows % min(a.P, kStageTokens) == 0;
         log_p = __ffs(a.P) - 1;
         page_scales = (int64_t)2 * a.Hkv * (a.P / kScaleRows);
         layer_scales = a.scales + (int64_t)a.layer * a.num_pages * page_scales;
@@ -378,7 +381,8 @@ struct ProducerE8 {
     __device__ __forceinline__ Stage next() {
         Stage x;
         x.on = it < it1;
-        x.row = cur.head * a.P + (kWhole ? (s * kStageTokens) & (a.P - 1) : 0);
+        x.head = cur.head;
+        x.row = kWhole ? (s * kStageTokens) & (a.P - 1) : 0;
         const int at = (s * kStageTokens + (kWhole ? 0 : block * kScaleRows)) >> log_p;
         x.pid = x.on && (kWhole || lane < C::kStageScales) && at < cur.n_pages ? a.page_ids[cur.page_off + at] : -1;
         s += kDecodeGroups;
@@ -391,16 +395,16 @@ struct ProducerE8 {
         const uint32_t sdst = scales + slot * C::kStageScales * 4;
         const bool valid = x.pid >= 0 && x.pid < a.num_pages;
         if (x.pid < -1 || x.pid >= a.num_pages) set_error(a.err, kErrBounds);
+        const float* src = layer_scales + x.pid * page_scales +
+                           ((kWhole ? 0 : kv * a.Hkv) + x.head) * (a.P / kScaleRows);
         if constexpr (kWhole) {
-            const int rk = x.row, rv = rk + a.Hkv * a.P;
-            const float* src = layer_scales + x.pid * page_scales;
+            src += x.row / kScaleRows;
             if (elect_one()) {
                 if (valid) {
                     mbar_arrive_expect_tx(full, C::kStageBytes + C::kStageScales * 4);
-                    tma_load_4d(dst, tmap, full, 0, rk, x.pid, a.layer);
-                    tma_load_4d(dst + C::kTileBytes, tmap, full, 0, rv, x.pid, a.layer);
-                    bulk_load(sdst, src + rk / kScaleRows, kHalf * 4, full);
-                    bulk_load(sdst + kHalf * 4, src + rv / kScaleRows, kHalf * 4, full);
+                    load_pair(dst, full, x);
+                    bulk_load(sdst, src, kHalf * 4, full);
+                    bulk_load(sdst + kHalf * 4, src + page_scales / 2, kHalf * 4, full);
                 } else {
                     mbar_arrive(full);
                 }
@@ -408,23 +412,28 @@ struct ProducerE8 {
         } else {
             const uint32_t n = __popc(__ballot_sync(0xffffffffu, box && valid));
             if (lane == 0) {
-                if (n) mbar_arrive_expect_tx(full, n * a.P * C::kRowBytes);
+                if (n) mbar_arrive_expect_tx(full, n * a.P * 2 * C::kRowBytes);
                 else mbar_arrive(full);
             }
             __syncwarp();
-            if (box && valid)
-                tma_load_4d(dst + kv * C::kTileBytes + block * kScaleRows * C::kRowBytes, tmap, full, 0,
-                            x.row + kv * a.Hkv * a.P, x.pid, a.layer);
+            if (box && valid) load_pair(dst + block * kScaleRows * 2 * C::kRowBytes, full, x);
             if (lane < C::kStageScales) {
                 if (valid)
                     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(sdst + (kv * kHalf + block) * 4),
-                                 "l"(layer_scales + x.pid * page_scales +
-                                     (x.row + kv * a.Hkv * a.P + (block * kScaleRows & (a.P - 1))) / kScaleRows)
+                                 "l"(src + (block * kScaleRows & (a.P - 1)) / kScaleRows)
                                  : "memory");
                 // (arrives when this lane's copy has landed)
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full) : "memory");
             }
         }
+    }
+    // A page's box of keys and of values.
+    __device__ __forceinline__ void load_pair(uint32_t dst, uint32_t full, const Stage& x) const {
+        asm volatile(
+            "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+            " [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
+            "l"(tmap), "r"(full), "r"(0), "r"(x.row), "r"(x.head), "r"(0), "r"(a.layer * a.num_pages + x.pid)
+            : "memory");
     }
     __device__ __forceinline__ void next_slot() {
         first = false;
@@ -452,8 +461,11 @@ struct ProducerE8 {
                 issue(w[i]);
                 next_slot();
                 ++n;
-            } else if ((kWhole ? lane < 2 : box) && w[i].pid >= 0 && w[i].pid < a.num_pages) {
-                tma_prefetch_l2_4d(tmap, 0, w[i].row + kv * a.Hkv * a.P, w[i].pid, a.layer);
+            } else if ((kWhole ? lane == 0 : box) && w[i].pid >= 0 && w[i].pid < a.num_pages) {
+                asm volatile("cp.async.bulk.prefetch.tensor.5d.L2.global.tile [%0, {%1, %2, %3, %4, %5}];" ::"l"(tmap),
+                             "r"(0), "r"(w[i].row), "r"(w[i].head), "r"(0),
+                             "r"(a.layer * a.num_pages + w[i].pid)
+                             : "memory");
             }
         }
         return n;
@@ -940,25 +952,22 @@ __device__ __forceinline__ float load_query_f16(const DecodeArgs& a, size_t h, b
     return a.scale_log2 * power_of_two(k);
 }
 
-// Which of the 16 tokens of a stage that are a warp's hold rows of their pages, as in
-// consume(), and are the segment's.
-__device__ __forceinline__ uint32_t e8_live(const DecodeArgs& a, const DecodeSeg* seg, int n_tok, int tbase) {
-    uint32_t vm = 0xffffu;
-    if (a.page_fill) {
-        const int P = a.P, pq = tbase >> (__ffs(P) - 1);
-        const int f0 = pq < seg->n_pages ? __ldg(&a.page_fill[seg->page_off + pq]) : 0;
-        auto rows = [](int f, int from, int most) {
-            auto up_to = [&](int x) { return (1u << min(max(x - from, 0), most)) - 1u; };
-            return (up_to(f & kFillMask) & ~up_to(f >> kFillFirstBit & kFillMask)) | up_to(f >> kFillSinkBit);
-        };
-        if (P >= 16) {
-            vm = rows(f0, tbase & (P - 1), 16);
-        } else {
-            const int f1 = pq + 1 < seg->n_pages ? __ldg(&a.page_fill[seg->page_off + pq + 1]) : 0;
-            vm = rows(f0, 0, 8) | rows(f1, 0, 8) << 8;
-        }
-    }
-    return vm & ((1u << min(max(n_tok - tbase, 0), 16)) - 1u);
+// The plan's entries of the pages that a warp's 16 tokens of a stage lie in (two where
+// pages have 8), and which of the tokens hold rows of their pages, as in consume().
+__device__ __forceinline__ int2 e8_fills(const DecodeArgs& a, int page_off, int n_pages, int tbase) {
+    const int pq = tbase >> (__ffs(a.P) - 1);
+    int2 f = make_int2(0, 0);
+    if (pq < n_pages) f.x = __ldg(&a.page_fill[page_off + pq]);
+    if (a.P == 8 && pq + 1 < n_pages) f.y = __ldg(&a.page_fill[page_off + pq + 1]);
+    return f;
+}
+__device__ __forceinline__ uint32_t e8_rows(int f, int from, int most) {
+    // the first rows up to x, of `most` from row `from` on
+    auto up_to = [&](int x) { return (1u << min(max(x - from, 0), most)) - 1u; };
+    return (up_to(f & kFillMask) & ~up_to(f >> kFillFirstBit & kFillMask)) | up_to(f >> kFillSinkBit);
+}
+__device__ __forceinline__ uint32_t e8_filled(int2 fills, int P, int tbase) {
+    return P >= 16 ? e8_rows(fills.x, tbase & (P - 1), 16) : e8_rows(fills.x, 0, 8) | e8_rows(fills.y, 0, 8) << 8;
 }
 
 // What a consumer warp carries through an item: NR column tiles of eight query rows.
@@ -975,12 +984,14 @@ struct E8State {
 // see[r][e], and `live` says which tokens are the segment's.
 template <int D, int NR, bool kAll>
 __device__ __forceinline__ void e8_stage(E8State<D, NR>& st, uint8_t* tile, const float* sc, uint32_t live,
-                                         const uint32_t (&see)[NR][2], int w4, int lane) {
+                                         const uint32_t (&see)[NR][2], int box_rows, int w4, int lane) {
     using C = DecCfg<D, true>;
     const int gid = lane >> 2, mi = lane >> 3, rr = lane & 7;
-    // (this lane's row of a matrix; the swizzle's turn and the matrix's half of a step)
+    // (this lane's row of a matrix, in a box's keys or, `box_rows` further, values; the
+    // swizzle's turn and the matrix's half of a step)
     const int t = w4 * 16 + (mi & 1) * 8 + rr;
-    const uint32_t at = smem_addr(tile) + t * D, turn = (mi >> 1) ^ (D == 128 ? t & 7 : t >> 1 & 3);
+    auto key_row = [&](int row) { return 2 * row - (row & (box_rows - 1)); };
+    const uint32_t at = smem_addr(tile) + key_row(t) * D, turn = (mi >> 1) ^ (D == 128 ? t & 7 : t >> 1 & 3);
     float2 sk = *reinterpret_cast<const float2*>(sc + w4 * 2);
     float2 sv = *reinterpret_cast<const float2*>(sc + C::kStageScales / 2 + w4 * 2);
     if (!kAll) {
@@ -1069,16 +1080,19 @@ __device__ __forceinline__ void e8_stage(E8State<D, NR>& st, uint8_t* tile, cons
     if (!kAll) {
         // V rows that hold none of the segment's may hold anything: zero them, so that
         // 0 * V stays 0
-        uint8_t* v = tile + C::kTileBytes + w4 * 16 * D;
-        for (int i = lane; i < D; i += 32)   // 16-byte chunks of 16 rows
-            if (!((live >> (i / (D / 16))) & 1u)) *reinterpret_cast<uint4*>(v + i * 16) = make_uint4(0, 0, 0, 0);
+        for (int i = lane; i < D; i += 32) {   // 16-byte chunks of 16 rows
+            const int r = i / (D / 16);
+            if (!((live >> r) & 1u))
+                *reinterpret_cast<uint4*>(tile + (key_row(w4 * 16 + r) + box_rows) * D + i % (D / 16) * 16) =
+                    make_uint4(0, 0, 0, 0);
+        }
         __syncwarp();
     }
 #pragma unroll
     for (int j2 = 0; j2 < D / 32; ++j2) {
         // tokens 0 .. 7 and 8 .. 15 of sixteen dimensions, then of the next
         uint32_t b[4];
-        ldsm_x4_trans(at + ((turn ^ (2 * j2)) << 4) + C::kTileBytes, b[0], b[1], b[2], b[3]);
+        ldsm_x4_trans(at + ((turn ^ (2 * j2)) << 4) + box_rows * D, b[0], b[1], b[2], b[3]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const uint32_t y = b[2 * h], z = b[2 * h + 1];
@@ -1114,8 +1128,8 @@ struct E8Ring {
 };
 
 // One item of a consumer warp, from stage s on; returns the stage that comes after.
-// (Its end: see consume().)
-template <int D, int NR>
+// (Its end: see consume().)  kFills: the plan has page fills.
+template <int D, int NR, bool kFills>
 __device__ __forceinline__ int e8_item(const DecodeArgs& a, const ItemHead& item, int it, bool last, int s,
                                        E8Ring& rg, uint8_t* smem, uint64_t* all_bars, int warp, int lane) {
     using C = DecCfg<D, true>;
@@ -1142,12 +1156,29 @@ __device__ __forceinline__ int e8_item(const DecodeArgs& a, const ItemHead& item
         for (int j = 0; j < D / 16; ++j) st.o[j][r][0] = st.o[j][r][1] = st.o[j][r][2] = st.o[j][r][3] = 0.f;
     }
     st.v_ref = power_of_two(kLeastScale);
-    // tokens that every row sees, where pages have no slots without rows (rows that are
+    // tokens that every row sees, where their pages have rows for them (rows that are
     // none see what they like)
-    int all = a.page_fill ? 0 : n_tok;
+    int all = n_tok;
     for (int j = 0; j < item.n_grp; ++j) all = min(all, seg->grp_lim[j]);
+    const int box_rows = min(a.P, kStageTokens);
+    int page_off = 0, n_pages = 0;
+    int2 next_fills = make_int2(0, 0);  // (read a stage ahead)
+    if (kFills) {
+        page_off = seg->page_off;
+        n_pages = seg->n_pages;
+        if (s < item.s1) next_fills = e8_fills(a, page_off, n_pages, s * kStageTokens + w4 * 16);
+    }
     for (; s < item.s1; s += kDecodeGroups) {
-        const int slot = rg.slot;
+        const int slot = rg.slot, tbase = s * kStageTokens + w4 * 16;
+        const bool whole = tbase + 16 <= all;
+        uint32_t live = 0xffffu;
+        if (kFills) {
+            const int2 fills = next_fills;
+            if (s + kDecodeGroups < item.s1)
+                next_fills = e8_fills(a, page_off, n_pages, tbase + kDecodeGroups * kStageTokens);
+            live = e8_filled(fills, a.P, tbase);
+        }
+        if (!whole) live &= (1u << min(max(n_tok - tbase, 0), 16)) - 1u;
         rg.wait(&rg.bars[slot], rg.phase, lane);
         if (++rg.slot == C::kStages) {
             rg.slot = 0;
@@ -1157,17 +1188,15 @@ __device__ __forceinline__ int e8_item(const DecodeArgs& a, const ItemHead& item
         uint8_t* tile = rg.slots + slot * C::kStageBytes;
         const float* sc = rg.scales + slot * C::kStageScales;
         uint32_t see[NR][2] = {};
-        if ((s + 1) * kStageTokens <= all) {
-            e8_stage<D, NR, true>(st, tile, sc, 0xffffu, see, w4, lane);
+        if (live == 0xffffu && whole) {
+            e8_stage<D, NR, true>(st, tile, sc, live, see, box_rows, w4, lane);
         } else {
-            const int tbase = s * kStageTokens + w4 * 16;
-            const uint32_t live = e8_live(a, seg, n_tok, tbase);
 #pragma unroll
             for (int r = 0; r < NR; ++r)
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
                     see[r][e] = live & ((1u << min(max(lim[r][e] - tbase, 0), 16)) - 1u);
-            e8_stage<D, NR, false>(st, tile, sc, live, see, w4, lane);
+            e8_stage<D, NR, false>(st, tile, sc, live, see, box_rows, w4, lane);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_addr(&rg.bars[C::kStages + slot]));
@@ -1217,7 +1246,7 @@ __device__ __forceinline__ int e8_item(const DecodeArgs& a, const ItemHead& item
     return s;
 }
 
-template <int D>
+template <int D, bool kFills>
 __device__ void consume_e8(const DecodeArgs& a, int it0, int it1, ItemHead next, uint8_t* smem, uint64_t* all_bars,
                            volatile int* abort_flag, int warp, int lane) {
     using C = DecCfg<D, true>;
@@ -1231,8 +1260,8 @@ __device__ void consume_e8(const DecodeArgs& a, int it0, int it1, ItemHead next,
         if (it + 1 < it1) next.read(a, it + 1, gid / a.G, (gid + 8) / a.G);
         const bool last = it + 1 == it1;
         const int s = item.n_grp * a.G <= 8
-                          ? e8_item<D, 1>(a, item, it, last, item.s0 + skip, rg, smem, all_bars, warp, lane)
-                          : e8_item<D, 2>(a, item, it, last, item.s0 + skip, rg, smem, all_bars, warp, lane);
+                          ? e8_item<D, 1, kFills>(a, item, it, last, item.s0 + skip, rg, smem, all_bars, warp, lane)
+                          : e8_item<D, 2, kFills>(a, item, it, last, item.s0 + skip, rg, smem, all_bars, warp, lane);
         skip = s - item.s1;
     }
 }
@@ -1574,8 +1603,10 @@ __global__ void __launch_bounds__(DecCfg<D, kE8>::kThreads, 1)
                        threadIdx.x - C::kConsumers - kDecodeGroups * 32);
         return;
     }
-    if constexpr (kE8) consume_e8<D>(a, it0, it1, head, smem, bars, abort_flag, warp, lane);
-    else consume<D>(a, it0, it1, head, smem, bars, abort_flag, warp, lane);
+    if constexpr (kE8) {
+        if (a.page_fill) consume_e8<D, true>(a, it0, it1, head, smem, bars, abort_flag, warp, lane);
+        else consume_e8<D, false>(a, it0, it1, head, smem, bars, abort_flag, warp, lane);
+    } else consume<D>(a, it0, it1, head, smem, bars, abort_flag, warp, lane);
     merge_last_runs<D, kE8>(a, smem, bars, abort_flag, lane);
 }
 

@@ -94,7 +94,8 @@ struct Kv8EvictArgs {
     int* err;
 };
 
-// Single tokens over such rows (tmap: the codes', a box of whole rows).
+// Single tokens over such rows (tmap: the codes', 5-D: head dim, slot, KV head, K or V,
+// page of a layer; a box has min(P, kStageTokens) rows of both).
 struct DecodeKv8Args : DecodeArgs {
     const float* scales;
 };
