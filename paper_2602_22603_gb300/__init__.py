@@ -713,8 +713,13 @@ class Cache:
         """Attention of the newest n_q[i] tokens (None: one) of each sequence, each
         seeing its last `window` tokens and the first n_sink."""
         q, out, lse, _ = self._attention(seqs, n_q, q, out, out_dtype, lse, "window_attention")
-        sq_window_attention(self.handle, seqs, n_q, layer, q, out, window, n_sink, out_dtype, lse,
-                            sm_scale, stream)
+        # (the C call at once: sq_window_attention takes the arguments apart again)
+        arr, _keep = _ints(seqs)
+        cnt, _keep2 = _ints(n_q)
+        rc = lib().sq_window_attention(self.handle, arr, len(seqs), cnt, layer, q, out, out_dtype, lse, sm_scale,
+                                       window, n_sink, _stream(stream))
+        if rc != SQ_OK:
+            raise SqError(rc, "sq_window_attention")
 
     def tree_attention(self, seqs, n_draft, parents, layer, q, out, window=0, n_sink=0,
                        out_dtype=SQ_OUT_BF16, lse=None, sm_scale=1.0, stream=None):
