@@ -364,6 +364,32 @@ def test_eviction(hq, hkv, d, page, ragged):
     assert c.sync_status() == sq.SQ_OK
 
 
+@pytest.mark.parametrize("d,page", [(128, 64), (64, 16)])
+def test_eviction_joins_rows_of_very_different_scales(d, page):
+    """Blocks of sizes from 2^-90 to 2^90, packed together."""
+    c = sq.Cache(1, 4, 2, d, page, 100, bits=8)
+    h = c.seq_new()
+    g = gen(31)
+    n = 640
+    x = torch.randn(n, 2, d, generator=g, device="cuda")
+    size = torch.randint(-90, 90, (n // 8, 2), generator=g, device="cuda")
+    size[::3] = torch.randint(-20, 20, (len(size[::3]), 2), generator=g, device="cuda")
+    x = (x * torch.exp2(size.float()).repeat_interleave(8, 0)[..., None]).bfloat16()
+    x[17, 0, 5], x[100, 1, 7] = math.nan, math.inf
+    append(c, h, x[None], x[None])
+    before = read(c, h)
+    spans = [(i, i + 5) for i in range(2, n - 10, 13)]
+    keep = torch.ones(n, dtype=torch.bool, device="cuda")
+    for a, b in spans:
+        keep[a:b] = False
+    c.evict_spans(h, spans)
+    for p in range(2):
+        want, _ = ref.held(before[p][keep], blocks(c, h))
+        same(read(c, h)[p], want)
+        same_scales(scales_of(c, h)[p], want, blocks(c, h))
+    assert c.sync_status() == sq.SQ_OK
+
+
 def test_drafted_step():
     """Extension, store, tree, acceptance, then single tokens: the calls of a decode
     step together, in two layers."""
