@@ -657,15 +657,9 @@ class Cache:
         n = self._counted(seqs, n_new, n, "qk_norm_rope_store")
         k, ks, _ = _rows(k, hkv, d, "k", n)
         v, vs, _ = _rows(v, hkv, d, "v", n)
-        positions = _flat(positions, _INT, n, "positions")
-        q_out = _flat(q_out, _BF16, n * hq * d, "q_out")
-        # (the C call at once: sq_qk_norm_rope_store takes the arguments apart again)
-        arr, _keep = _ints(seqs)
-        cnt, _keep2 = _ints(n_new)
-        rc = lib().sq_qk_norm_rope_store(self.handle, arr, len(seqs), cnt, layer, q, qs, k, ks, v, vs, positions,
-                                         ctypes.addressof(params), q_out, _stream(stream))
-        if rc != SQ_OK:
-            raise SqError(rc, "sq_qk_norm_rope_store")
+        sq_qk_norm_rope_store(self.handle, seqs, n_new, layer, q, qs, k, ks, v, vs,
+                              _flat(positions, _INT, n, "positions"), params,
+                              _flat(q_out, _BF16, n * hq * d, "q_out"), stream)
 
     def qk_norm_rope(self, q, k, positions, params, q_out, k_out, stream=None):
         """Norms and rotation of q [tokens, Hq, D] and k [tokens, Hkv, D] into tensors."""
@@ -713,13 +707,8 @@ class Cache:
         """Attention of the newest n_q[i] tokens (None: one) of each sequence, each
         seeing its last `window` tokens and the first n_sink."""
         q, out, lse, _ = self._attention(seqs, n_q, q, out, out_dtype, lse, "window_attention")
-        # (the C call at once: sq_window_attention takes the arguments apart again)
-        arr, _keep = _ints(seqs)
-        cnt, _keep2 = _ints(n_q)
-        rc = lib().sq_window_attention(self.handle, arr, len(seqs), cnt, layer, q, out, out_dtype, lse, sm_scale,
-                                       window, n_sink, _stream(stream))
-        if rc != SQ_OK:
-            raise SqError(rc, "sq_window_attention")
+        sq_window_attention(self.handle, seqs, n_q, layer, q, out, window, n_sink, out_dtype, lse,
+                            sm_scale, stream)
 
     def tree_attention(self, seqs, n_draft, parents, layer, q, out, window=0, n_sink=0,
                        out_dtype=SQ_OUT_BF16, lse=None, sm_scale=1.0, stream=None):
@@ -738,11 +727,7 @@ class Cache:
             _types()
         size = self._counted(seqs, counts, None, "read_kv") * self.Hkv * self.D
         k, v = _flat(k, _BF16, size, "k"), _flat(v, _BF16, size, "v")
-        arr, _keep = _ints(seqs)
-        cnt, _keep2 = _ints(counts)
-        rc = lib().sq_read_kv(self.handle, arr, len(seqs), cnt, layer, k, v, _stream(stream))
-        if rc != SQ_OK:
-            raise SqError(rc, "sq_read_kv")
+        sq_read_kv(self.handle, seqs, counts, layer, k, v, stream)
 
     accept_draft = (lambda self, seq, n_draft, path, stream=None:
                     sq_accept_draft(self.handle, seq, n_draft, path, stream))
