@@ -541,8 +541,8 @@ SQ_API int sq_accept_draft(sq_cache *cache, sq_seq seq, int32_t n_draft, const i
  * their scales.  sq_evict_spans and sq_evict_spans_ragged pack codes, a block's scale
  * made anew.  A caller that writes rows itself writes scales of the form above.
  * What is said above of a store of more than 240 rows holds here for one of more than
- * 236 runs (rows of up to 64 slots of a page each); an append or sq_read_kv of as many
- * cannot be captured (UNSUPPORTED).
+ * 236 runs (rows of up to 64 slots of a page each); an sq_read_kv of as many, and any
+ * append, cannot be captured (UNSUPPORTED).
  *
  * Attention takes the values as they are: logits are fp32 sums of exact products of the
  * bf16 queries (elements below 2^-32 of their row's largest lose digits) and the

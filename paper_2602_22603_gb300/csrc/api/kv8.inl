@@ -6,6 +6,7 @@
 static int append_8bit(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new, const void* k,
                        const void* v, void* stream) {
     return guarded([&] {
+        if (capturing(as_stream(stream))) return (int)SQ_ERR_UNSUPPORTED;
         int64_t n = 0;
         for (int32_t i = 0; i < n_seqs; ++i) n += n_new ? n_new[i] : 1;
         std::vector<int32_t> pages;
@@ -25,19 +26,20 @@ static int append_8bit(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const in
             a.n_layers = g.L;
             a.plain = 1;
             a.err = c->d_err;
+            int rc;
             if (runs.size() <= (size_t)kRunsInline) {
                 std::copy(runs.begin(), runs.end(), a.inline_run);
-                return cuda_status(launch_kv8_store(a, g.D, st));
+                rc = cuda_status(launch_kv8_store(a, g.D, st));
+            } else {
+                rc = with_upload(c, runs.data(), runs.size() * sizeof(RowRun), stream, [&](const uint8_t* d) {
+                    a.runs = reinterpret_cast<const RowRun*>(d);
+                    return launch_kv8_store(a, g.D, st);
+                });
             }
-            if (capturing(st)) return SQ_ERR_UNSUPPORTED;
-            return with_upload(c, runs.data(), runs.size() * sizeof(RowRun), stream, [&](const uint8_t* d) {
-                a.runs = reinterpret_cast<const RowRun*>(d);
-                return launch_kv8_store(a, g.D, st);
-            });
+            if (rc == SQ_OK) note_writes(c, pages.data(), pages.size(), stream);
+            return rc;
         };
-        const int rc = extend_impl(c, seqs, n_seqs, n_new, stream, store);
-        if (rc == SQ_OK) note_writes(c, pages.data(), pages.size(), stream);
-        return rc;
+        return extend_impl(c, seqs, n_seqs, n_new, stream, store);
     });
 }
 

@@ -173,10 +173,11 @@ void note_store(sq_cache* c, std::vector<int32_t>&& pages, void* stream) {
     c->store_ticket = c->write_seq;
 }
 
-// `then` is enqueued after the copies, with the rows counted; where it fails they are
-// taken back.
-template <typename Then>
-int extend_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new, void* stream, Then then) {
+// `rows`, where there is one, is enqueued after the copies, with the rows counted, and
+// notes its writes; where it fails they are taken back.
+template <typename Rows>
+int extend_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new, void* stream, Rows rows) {
+    constexpr bool kLater = std::is_same<Rows, std::nullptr_t>::value;  // (their rows come later)
     int rc = check_handles(c, seqs, n_seqs);
     if (rc != SQ_OK) return rc;
     int64_t total = 0;
@@ -191,7 +192,7 @@ int extend_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
     std::vector<uint64_t> old_versions(n_seqs);
     std::vector<std::vector<LenUpdate>> ups(n_seqs);
     std::vector<char> passed(n_seqs, 0);
-    std::vector<int32_t> taken, copied;
+    std::vector<int32_t> taken, copied, left;
     std::vector<CowCopy> copies;
     // takes back what was planned, unless everything is enqueued
     struct Undo {
@@ -213,6 +214,9 @@ int extend_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
         if (p.cow) {
             copies.push_back({p.cow_old, p.cow_new, p.cow_rows});
             copied.push_back(p.cow_new);
+            if (c->kv8) left.push_back(p.cow_old);
+        } else if (c->kv8 && p.last_fill0 > 0 && !p.pages.empty()) {
+            taken.push_back(p.pages[0]);   // (its rows may change their scale)
         }
     }
     // cached decode plans that the longer sequences leave valid: their row limits
@@ -260,13 +264,16 @@ int extend_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
         if (e != cudaSuccess) return cuda_status(e);
         a.lens.n = 0;
     }
-    rc = then();
-    if (rc != SQ_OK) return rc;
+    if constexpr (!kLater) {
+        rc = rows();
+        if (rc != SQ_OK) return rc;
+    }
     undo.planned = 0;
     note_writes(c, copied.data(), copied.size(), stream);
+    rc = record_freed(c, left, stream);
     for (int32_t i = 0; i < n_seqs; ++i) {
         if (plans[i].n_new == 0) continue;
-        c->host->seq_mut(seqs[i])->extended = true;
+        if (kLater) c->host->seq_mut(seqs[i])->extended = true;
         const uint64_t nv = c->host->seq(seqs[i])->version;
         if (passed[i])
             for (const LenUpdate& u : ups[i]) plan_len_apply(c, u, nv, plans[i].n_new, plans[i].pages[0], st);
@@ -274,7 +281,7 @@ int extend_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
         if (plans[i].cow) c->stats.cow_pages += 1;
     }
     c->stats.appended_tokens += total;
-    return SQ_OK;
+    return rc;
 }
 
 // Where the newest n_new[i] rows of each sequence lie, sequence after sequence,
@@ -380,6 +387,13 @@ int store_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n
     for (int32_t p : pages)
         if (c->host->alloc().refcount(p) > 1) return SQ_ERR_INVALID_ARG;
     cudaStream_t st = as_stream(stream);
+    if (c->kv8) {
+        // (see record_freed; runs of a graph take turns by the caller's order)
+        bool marked = false;
+        for (int32_t p : pages) marked |= c->fenced[p] != 0;
+        if (marked && !capturing(st)) rc = fence_taken_pages(c, pages, stream);
+        if (rc != SQ_OK) return rc;
+    }
     auto launch = [&](const uint8_t* uploaded) {
         if (c->kv8) {
             Kv8StoreInlineArgs a;
@@ -868,7 +882,7 @@ extern "C" {
 int sq_extend(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new, void* stream) {
     TraceRange trace_("sq_extend");
     if (!c) return SQ_ERR_BAD_HANDLE;
-    return guarded([&] { return extend_impl(c, seqs, n_seqs, n_new, stream, [] { return SQ_OK; }); });
+    return guarded([&] { return extend_impl(c, seqs, n_seqs, n_new, stream, nullptr); });
 }
 
 int sq_qk_norm_rope_store(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* n_new,

@@ -376,9 +376,16 @@ int fence_taken_pages(sq_cache* c, const std::vector<int32_t>& taken, void* stre
     return SQ_OK;
 }
 
-// Marks pages freed by the work enqueued on `stream` so far.
+// Marks pages freed by the work enqueued on `stream` so far.  (8-bit caches) Also those
+// that a sequence gives up and others hold on to: the last holder left may take the rows
+// of a block to another scale, so what it writes waits for the sequences that read them.
 int record_freed(sq_cache* c, const std::vector<int32_t>& freed, void* stream) {
     if (freed.empty()) return SQ_OK;
+    if (c->kv8) {
+        // (a page's mark is one stream's: that stream follows the earlier ones)
+        const int rc = fence_taken_pages(c, freed, stream);
+        if (rc != SQ_OK) return rc;
+    }
     auto it = c->free_event.find(stream);
     if (it == c->free_event.end()) {
         cudaEvent_t ev;
@@ -393,6 +400,16 @@ int record_freed(sq_cache* c, const std::vector<int32_t>& freed, void* stream) {
         c->fenced[p] = 1;
     }
     return SQ_OK;
+}
+
+// (8-bit caches) A sequence's pages that others hold too: see record_freed.  (That it may
+// still hold some of them costs a wait for its stream, which they then follow.)
+std::vector<int32_t> shared_pages(const sq_cache* c, sq_seq seq) {
+    std::vector<int32_t> pages;
+    if (c->kv8)
+        for (int32_t p : c->host->seq(seq)->pages)
+            if (c->host->alloc().refcount(p) > 1) pages.push_back(p);
+    return pages;
 }
 
 // Whether what is enqueued on a stream goes into a graph (to be run any number of
@@ -1374,6 +1391,7 @@ int evict_impl(sq_cache* c, sq_seq seq, const sq_span* spans, int32_t n_spans, v
         b[i] = spans[i].end;
     }
     EvictPlan plan;
+    std::vector<int32_t> left = shared_pages(c, seq);
     int rc = c->host->evict(seq, a.data(), b.data(), n_spans, &plan, ragged);
     if (rc != SQ_OK) return rc;
     const Geometry& g = c->g;
@@ -1385,6 +1403,10 @@ int evict_impl(sq_cache* c, sq_seq seq, const sq_span* spans, int32_t n_spans, v
     rc = fence_taken_pages(c, plan.cow_pages, stream);
     if (rc != SQ_OK) return undo(rc);
     if (!plan.moves.empty() && c->kv8) {
+        std::vector<int32_t> written;
+        for (const EvictMove& m : plan.moves) written.push_back(m.dst_page);
+        rc = fence_taken_pages(c, written, stream);
+        if (rc != SQ_OK) return undo(rc);
         rc = launch_evict_8bit(c, plan, stream);
         if (rc != SQ_OK) return undo(rc);
     } else if (!plan.moves.empty()) {
@@ -1448,6 +1470,7 @@ int evict_impl(sq_cache* c, sq_seq seq, const sq_span* spans, int32_t n_spans, v
             if (written.empty() || written.back() != m.dst_page) written.push_back(m.dst_page);
         note_writes(c, written.data(), written.size(), stream);
     }
+    if (c->kv8) plan.freed.insert(plan.freed.end(), left.begin(), left.end());
     rc = record_freed(c, plan.freed, stream);
     if (rc != SQ_OK) return rc;
     c->host->seq_mut(seq)->last_stream = stream;
@@ -1722,7 +1745,7 @@ int sq_release(sq_cache* c, sq_seq seq, void* stream) {
         cudaEventDestroy(ev);
         if (e != cudaSuccess) return cuda_status(e);
     }
-    std::vector<int32_t> freed;
+    std::vector<int32_t> freed = shared_pages(c, seq);
     int rc = c->host->release(seq, &freed);
     if (rc != SQ_OK) return rc;
     return record_freed(c, freed, stream);

@@ -1,7 +1,13 @@
 // fake_operators.cpp with stand-ins for the launchers of 8-bit rows: a code is the low
 // byte of the element that it is given, a block's scale the rows that the block held
 // when it was written; moves, copies and reads take both along.
+#define cudaEventQuery event_query
+#define cudaStreamIsCapturing stream_capturing
 #include "fake_operators.cpp"
+#undef cudaEventQuery
+#undef cudaStreamIsCapturing
+
+#include <algorithm>
 
 #include "../paper_2602_22603_gb300/csrc/kernels/kv8.hpp"
 
@@ -15,6 +21,18 @@ static bool fails8(int kind) {
     g_fail8 = -1;
     return true;
 }
+// Uses of the pool's pages, as of other memory (see fake_device.cpp).
+static std::map<int, std::vector<Use>> g_pages;
+static int64_t g_page_races = 0;
+static void use_page(cudaStream_t st, const Clock& c, int page, bool write) {
+    for (const Use& u : g_pages[page]) {
+        auto known = c.find(u.stream);
+        if ((u.write || write) && (known == c.end() || known->second < u.seq)) ++g_page_races;
+    }
+    g_pages[page].push_back({st, c.at(st), write});
+}
+static std::vector<int> g_early;   // pages that the last launch of single tokens was to leave to its wait
+static int g_early_on = 0;
 static int64_t plane8(const Kv8Pool& p, int layer, int page, int kv, int head) {
     return (((layer * p.num_pages + page) * 2 + kv) * p.Hkv + head) * (int64_t)p.P;
 }
@@ -30,6 +48,7 @@ cudaError_t launch_kv8_store(const Kv8StoreInlineArgs& a, int D, cudaStream_t st
         if (all.n < 1 || all.n > kRunRows || page < 0 || page >= a.pool.num_pages ||
             all.row / std::min(a.pool.P, kRunRows) != (all.row + all.n - 1) / std::min(a.pool.P, kRunRows))
             ++g_bad;
+        use_page(st, c, page, true);
         for (int b = 0; b < a.blocks; ++b) {
             const int b0 = all.row / kScaleRows * kScaleRows + b * kScaleRows;
             const int from = std::max(all.row, b0), end = std::min(all.row + all.n, b0 + kScaleRows);
@@ -54,7 +73,12 @@ cudaError_t launch_kv8_store(const Kv8StoreInlineArgs& a, int D, cudaStream_t st
 }
 cudaError_t launch_kv8_copy(const Kv8CopyArgs& a, int D, cudaStream_t st) {
     if (fails8(kCopy8)) return cudaErrorLaunchFailure;
-    tick(st);
+    const Clock& c = tick(st);
+    for (int i = 0; i < a.lens.n; ++i) *a.lens.ptr[i] = a.lens.val[i];
+    for (int i = 0; i < a.n_cow; ++i) {
+        use_page(st, c, a.cow[i].src_page, false);
+        use_page(st, c, a.cow[i].dst_page, true);
+    }
     for (int i = 0; i < a.n_cow; ++i)
         for (int l = 0; l < a.L; ++l)
             for (int x = 0; x < 2 * a.pool.Hkv; ++x) {
@@ -113,6 +137,7 @@ cudaError_t launch_kv8_evict(const Kv8EvictArgs& a, int D, cudaStream_t st) {
         for (int x = 0; x < 2 * p.Hkv; ++x)
             for (int t = 0; t < a.n_tiles; ++t) {
                 const EvictTile tile = a.tiles[t];
+                if (l + x == 0) use_page(st, c, tile.dst_page, true);
                 const int end = t + 1 < a.n_tiles ? a.tiles[t + 1].piece_begin : a.n_pieces;
                 std::vector<uint8_t> rows((size_t)tile.n_rows * D, 0);
                 for (int k = tile.piece_begin; k < end; ++k)
@@ -125,9 +150,20 @@ cudaError_t launch_kv8_evict(const Kv8EvictArgs& a, int D, cudaStream_t st) {
             }
     return cudaSuccess;
 }
+static int g_rows = 0;   // rows of its longest segment
 cudaError_t launch_decode_kv8(const CUtensorMap& m, const DecodeKv8Args& a, int n, int D, cudaStream_t st) {
     if (!a.scales) ++g_bad;
-    return launch_decode(m, a, n, D, st);
+    const cudaError_t e = launch_decode(m, a, n, D, st);
+    if (e != cudaSuccess) return e;
+    g_early.assign(a.unsafe, a.unsafe + (a.kv_early ? a.n_unsafe : 0));
+    g_early_on = a.kv_early;
+    g_rows = 0;
+    for (int i = 0; i < a.cta_begin[n]; ++i) {
+        const DecodeSeg& s = a.segs[a.items[i].seg];
+        g_rows = std::max(g_rows, (int)s.n_tok);
+        for (int p = 0; p < s.n_pages; ++p) use_page(st, g_streams[st], a.page_ids[s.page_off + p], false);
+    }
+    return e;
 }
 
 }  // namespace sq
@@ -135,3 +171,17 @@ cudaError_t launch_decode_kv8(const CUtensorMap& m, const DecodeKv8Args& a, int 
 EXPORT void fake_fail8(int kind) { sq::g_fail8 = kind; }
 EXPORT int64_t fake_bad() { return sq::g_bad; }
 EXPORT int fake_wide() { return sq::g_wide; }
+EXPORT int64_t fake_page_races() { return sq::g_page_races; }
+EXPORT void fake_new_pages() { sq::g_pages.clear(), sq::g_page_races = 0; }
+// Whether the last launch of single tokens was to load a page before its wait.
+EXPORT int fake_early(int page) {
+    return sq::g_early_on && std::find(sq::g_early.begin(), sq::g_early.end(), page) == sq::g_early.end();
+}
+EXPORT int fake_rows() { return sq::g_rows; }
+static bool g_done = false, g_graph = false;
+EXPORT void fake_done(int done) { g_done = done; }       // what events answer
+EXPORT void fake_graph(int graph) { g_graph = graph; }   // streams are captured
+extern "C" cudaError_t cudaEventQuery(cudaEvent_t) { return g_done ? cudaSuccess : cudaErrorNotReady; }
+extern "C" cudaError_t cudaStreamIsCapturing(cudaStream_t, cudaStreamCaptureStatus* s) {
+    return *s = g_graph ? cudaStreamCaptureStatusActive : cudaStreamCaptureStatusNone, cudaSuccess;
+}

@@ -39,7 +39,7 @@ def lib():
         for name, (res, args) in sq._SIGS.items():
             f = getattr(L, name)
             f.restype, f.argtypes = res, args
-        L.fake_count.restype = L.fake_races.restype = L.fake_bad.restype = ctypes.c_int64
+        L.fake_count.restype = L.fake_races.restype = L.fake_bad.restype = L.fake_page_races.restype = ctypes.c_int64
         L.fake_malloc_limit.argtypes = [ctypes.c_int64]
         _lib = L
     return _lib
@@ -50,6 +50,7 @@ def L(monkeypatch):
     monkeypatch.setattr(sq, "_lib", lib())
     lib().fake_reset()
     lib().fake_fail8(-1)
+    lib().fake_new_pages()
     yield lib()
     assert lib().fake_bad() == 0
 
@@ -263,4 +264,122 @@ def test_rows_of_a_bf16_cache_are_read_as_they_are(L):
     out = np.zeros((50, HKV, D), np.uint16), np.zeros((50, HKV, D), np.uint16)
     sq.sq_read_kv(c.handle, [a], [50], 1, out[0].ctypes.data, out[1].ctypes.data, 1)
     assert (out[0] == k[1]).all() and (out[1] == k[1]).all()
+    c.close()
+
+
+def decode(c, hs, stream=1):
+    sq.sq_decode_attention(c.handle, hs, 0, Q, OUT, sm_scale=0.1, stream=stream)
+
+
+def test_rows_that_an_append_writes_are_not_read_ahead_of_it(L):
+    """The next token's call on a kept plan, its last page written by an append alone."""
+    c = sq.Cache(2, HQ, HKV, D, 64, PAGES, bits=8)
+    a = c.seq_new()
+    append(c, a, 100, 1)
+    first, last = c.page_table(a)
+    L.fake_done(1)
+    decode(c, [a])
+    decode(c, [a])
+    assert L.fake_early(first) and L.fake_early(last)
+    L.fake_done(0)
+    plans = c.stats()["decode_plans_built"]
+    for m in (1, 2):
+        append(c, a, m, 2)
+        decode(c, [a])
+        assert c.stats()["decode_plans_built"] == plans
+        assert L.fake_early(first) and not L.fake_early(last)
+    c.extend([a], [1], 1)
+    store(c, [a], [1], 0, 3)
+    decode(c, [a])
+    assert not L.fake_early(last)
+    c.close()
+
+
+def test_failed_appends_leave_no_plan_with_their_rows(L):
+    c = sq.Cache(2, HQ, HKV, D, 64, PAGES, bits=8)
+    a = c.seq_new()
+    append(c, a, 100, 1)
+    for kind in (STORE8, COPY8):
+        decode(c, [a])
+        decode(c, [a])
+        L.fake_fail8(kind)
+        with pytest.raises(sq.SqError):
+            append(c, a, 1, 2)
+        decode(c, [a])
+        assert L.fake_rows() == 100
+    append(c, a, 1, 2)
+    decode(c, [a])
+    assert L.fake_rows() == 101
+    c.close()
+
+
+def test_captured_calls_of_many_rows_are_refused(L, cache):
+    a = cache.seq_new()
+    append(cache, a, 20, 1)
+    f = cache.fork_aux(a)
+    before = [cache.page_table(h) for h in (a, f)], cache.free_pages(), cache.next_pos(a)
+    L.fake_graph(1)
+    try:
+        x = np.zeros((2, 3, HKV, D), np.uint16)
+        for call in (lambda: append(cache, a, 3, 5),
+                     lambda: cache.append_kv_batch([a, f], x.ctypes.data, x.ctypes.data, 1)):
+            with pytest.raises(sq.SqError) as e:
+                call()
+            assert e.value.code == sq.SQ_ERR_UNSUPPORTED
+    finally:
+        L.fake_graph(0)
+    assert ([cache.page_table(h) for h in (a, f)], cache.free_pages(), cache.next_pos(a)) == before
+    n = 237 * min(cache.P, 64)
+    if n > PAGES * cache.P // 2:
+        return
+    b = cache.seq_new()
+    append(cache, b, n, 1)
+    L.fake_graph(1)
+    try:
+        with pytest.raises(sq.SqError) as e:
+            read(cache, b)
+        assert e.value.code == sq.SQ_ERR_UNSUPPORTED
+    finally:
+        L.fake_graph(0)
+
+
+@pytest.mark.parametrize("end", ["release", "append", "extend", "evict", "evict_copy", "two"])
+@pytest.mark.parametrize("write", ["append", "store", "evict"])
+def test_a_block_of_rows_changes_scale_after_its_readers(L, end, write):
+    """A fork on another stream reads a page and gives it up; what its parent then writes
+    there, rows of the fork's among those that may be scaled anew, waits for that."""
+    c = sq.Cache(2, HQ, HKV, D, 64, PAGES, bits=8)
+    a = c.seq_new()
+    append(c, a, 100, 1)
+    page = c.page_table(a)[1]
+    f = c.fork_aux(a)
+    g = c.fork_aux(a) if end == "two" else None
+    L.fake_new_pages()
+    decode(c, [f], 2)
+    if end == "release":
+        c.release(f, 2)
+    elif end == "append":
+        append(c, f, 1, 2, 2)
+    elif end == "extend":
+        c.extend([f], [1], 2)
+    elif end == "evict":
+        c.evict_spans(f, [(60, 100)], 2)
+    elif end == "evict_copy":
+        c.evict_spans_ragged(f, [(80, 90)], 2)
+    else:
+        decode(c, [g], 3)
+        c.release(g, 3)
+        c.release(f, 2)
+    if write == "append":
+        append(c, a, 1, 2, 1)
+    elif write == "store":
+        c.extend([a], [1], 4)
+        L.fake_new_pages()
+        f = c.fork_aux(a)
+        decode(c, [f], 2)
+        c.release(f, 2)
+        store(c, [a], [1], 0, 3, 1)
+    else:
+        c.evict_spans_ragged(a, [(70, 71)], 1)
+    assert c.page_table(a)[1] == page and L.fake_page_races() == 0
     c.close()
