@@ -518,3 +518,119 @@ def test_noalloc_tokens():
     sq.sq_decode_attention_noalloc(c.handle, hs, 0, q, outs[1], sq.SQ_OUT_F32, 0.1)
     assert torch.equal(*outs)
     assert c.sync_status() == sq.SQ_OK
+
+
+@pytest.mark.parametrize("hq,hkv,d,page", [(8, 2, 128, 64), (16, 4, 64, 16), (8, 1, 64, 8), (32, 2, 128, 32)])
+def test_tokens_of_forks(hq, hkv, d, page):
+    """Sequences that share pages, more of them than a tile's columns, each grown by rows
+    of its own: a block that a fork copies and scales anew leaves the others' as it was."""
+    c = sq.Cache(1, hq, hkv, d, page, 3000 // page + 400, bits=8)
+    hs = fill_sequences(c, [1500 + page // 2 + 3, 70], 30)
+    g = gen(31)
+    for i in range(7):
+        hs.append(c.fork_aux(hs[0]))
+    before = read(c, hs[0])
+    for i, h in enumerate(hs):
+        if i % 3 != 2:
+            k, v = (rows(g, 1 + 3 * i, hkv, d, 1.0)[None] * 2.0 ** (i - 4) for _ in range(2))
+            append(c, h, k, v)
+    same(read(c, hs[2])[0], before[0])   # (shared, and not grown)
+    same(read(c, hs[2])[1], before[1])
+    q = rows(gen(32), len(hs), hq, d, 0.5)
+    out = torch.empty(len(hs), hq, d, device="cuda")
+    for _ in range(2):
+        out.fill_(3.0)
+        c.decode_attention(hs, 0, q, out, sq.SQ_OUT_F32, d ** -0.5)
+    for i, h in enumerate(hs):
+        want, weighted, logits = ref.attention(q[i:i + 1], *read(c, h), d ** -0.5)
+        assert ((out[i:i + 1].double() - want).abs() <= ref.token_budget(want, weighted, logits, d)).all()
+    assert c.sync_status() == sq.SQ_OK
+
+
+@pytest.mark.parametrize("hq,hkv,d,page", [(8, 2, 128, 8), (4, 4, 64, 256), (16, 1, 64, 64)])
+def test_tokens_of_long_contexts(hq, hkv, d, page):
+    """Many pieces to a row; one token more at a time on a kept plan."""
+    n = 20011
+    c = sq.Cache(1, hq, hkv, d, page, n // page + 60, bits=8)
+    h = fill_sequences(c, [n], 33)[0]
+    g = gen(34)
+    for i in range(4):
+        q = rows(g, 1, hq, d, 0.5)
+        out = torch.empty(1, hq, d, device="cuda")
+        c.decode_attention([h], 0, q, out, sq.SQ_OUT_F32, d ** -0.5)
+        want, weighted, logits = ref.attention(q, *read(c, h), d ** -0.5)
+        assert ((out.double() - want).abs() <= ref.token_budget(want, weighted, logits, d)).all()
+        k, v = (rows(g, 1, hkv, d)[None] * 4.0 ** i for _ in range(2))
+        append(c, h, k, v)
+    assert c.sync_status() == sq.SQ_OK
+
+
+@pytest.mark.parametrize("d,page", [(128, 64), (64, 16), (128, 8)])
+def test_rows_of_nan(d, page):
+    """A row of NaN and of infinities counts for the queries that see it, and for no other."""
+    hq, hkv, n, bad = 8, 2, 400, 333
+    c = sq.Cache(1, hq, hkv, d, page, n // page + 8, bits=8)
+    h = c.seq_new()
+    g = gen(35)
+    k, v = (rows(g, n, hkv, d, 0.5) for _ in range(2))
+    v[bad, 0, 3], v[bad, 1, 5] = math.nan, math.inf
+    append(c, h, k[None], v[None])
+    q = rows(g, n, hq, d, 0.5)
+    kk, vv = read(c, h)
+    assert vv[bad].isnan().sum() == 2
+    for m, window, sinks in ((n, 50, 0), (80, 30, 7), (20, 40, 0)):
+        out = torch.empty(m, hq, d, dtype=torch.bfloat16, device="cuda")
+        c.window_attention([h], [m], 0, q[:m], out, window, sinks, sm_scale=d ** -0.5)
+        i, j = torch.arange(n - m, n, device="cuda")[:, None], torch.arange(n, device="cuda")[None]
+        keep = (j <= i) & ((j > i - window) | (j < sinks))
+        want, weighted, logits = ref.attention(q[:m], kk, torch.nan_to_num(vv, nan=0.0), d ** -0.5, keep)
+        sees = keep[:, bad]
+        assert out[sees][:, :4, 3].isnan().all() and out[sees][:, 4:, 5].isnan().all()
+        off = (out.double() - want).abs()
+        fits = off <= (weighted * 2.0 ** -7 + want.abs() * 2.0 ** -8 +
+                       weighted * (2.0 * (d + 8) * 2.0 ** -24 * logits)[..., None])
+        fits[sees, :4, 3] = fits[sees, 4:, 5] = True
+        assert fits.all()
+    one = torch.empty(1, hq, d, device="cuda")
+    for window, sinks, seen in ((n - bad, 0, True), (n - bad - 1, 0, False), (3, bad + 1, True), (3, bad, False)):
+        c.window_attention([h], None, 0, q[:1], one, window, sinks, out_dtype=sq.SQ_OUT_F32, sm_scale=d ** -0.5)
+        assert one[0, :4, 3].isnan().all() == seen and one[0, 4:, 5].isnan().all() == seen
+        one[0, :4, 3] = one[0, 4:, 5] = 0.0
+        assert one.isfinite().all()
+    assert c.sync_status() == sq.SQ_OK
+
+
+def test_calls_of_no_rows():
+    c = sq.Cache(1, 8, 2, 64, 16, 20, bits=8)
+    hs = fill_sequences(c, [20, 5], 36)
+    before = [read(c, h)[0] for h in hs]
+    none = torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    c.read_kv(hs, [0, 0], 0, none, none)
+    c.append_kv(hs[0], 0, none, none)
+    c.extend(hs, [0, 0])
+    out = torch.full((2, 2, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    c.read_kv(hs, [0, 1], 0, out[:1], out[1:])
+    same(out[0].double(), before[1][-1])
+    assert c.sync_status() == sq.SQ_OK
+
+
+@pytest.mark.parametrize("d,page", [(128, 64), (64, 16)])
+def test_an_unsignalled_stage_runs_out(d, page):
+    """A bounded wait that runs out is reported, and the cache works on."""
+    c = sq.Cache(1, 8, 2, d, page, 4000 // page, bits=8)
+    h = fill_sequences(c, [3000], 37)[0]
+    q = rows(gen(38), 1, 8, d, 0.5)
+    outs = [torch.empty(1, 8, d, device="cuda") for _ in range(2)]
+    c.decode_attention([h], 0, q, outs[0], sq.SQ_OUT_F32, 0.1)
+    assert c.sync_status() == sq.SQ_OK
+    sq.sq_debug_set(c.handle, sq.SQ_DEBUG_DROP_DECODE_STAGE)
+    c.decode_attention([h], 0, q, outs[1], sq.SQ_OUT_F32, 0.1)
+    assert c.sync_status() == sq.SQ_ERR_DEVICE_TIMEOUT
+    for _ in range(2):
+        outs[1].fill_(3.0)
+        c.decode_attention([h], 0, q, outs[1], sq.SQ_OUT_F32, 0.1)
+        assert torch.equal(*outs)
+    k, v = (rows(gen(39), 5, 2, d)[None] for _ in range(2))
+    append(c, h, k, v)
+    c.evict_spans(h, [(10, 500)])
+    assert read(c, h)[0].isfinite().all() and c.sync_status() == sq.SQ_OK
