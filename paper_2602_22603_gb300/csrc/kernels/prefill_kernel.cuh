@@ -1621,7 +1621,7 @@ struct RowMask<kE8 | kBlocks | kOneTile | kTwoProducers> : BlockRowMask {};
 
 // A key that a row does not see has the weight 0 in the row's tile product, and
 // 0 times an infinity or NaN in that key's V row is NaN.  Besides, a row's weights may
-// sum to 2^40 and more (its maximum starts at 0), and times large values they pass
+// sum to 2^80 (its maximum starts at 0), and times large values they pass
 // what fp32 holds where their average is finite.  So where a block's row has an output
 // that is not finite though its normaliser is, and some key that its tiles hide has
 // such a V row, or no key of the item has one (then the sums overflowed), it is taken
@@ -1926,13 +1926,17 @@ __device__ bool prefill_softmax(const Args& a, const Smem& sm, uint32_t tmem, in
     //
     // A block of queries has few key tiles, often the sinks' few keys first, whose
     // maxima the window's raise: there a row starts at a maximum of 0 and a tile's
-    // weights are accepted while its sum stays below 2^40 (and above 2^-40 where
+    // weights are accepted while its sum stays below 2^80 (and above 2^-40 where
     // they are the row's first), since a weight rounded to bf16 keeps its 8 bits at
     // any size and sums are fp32 (those that overflow: rows_again).  16,384 queries at
     // a window of 1,024 with 4 sinks: 367 -> 254 us, half of it the maxima of first
-    // tiles.
+    // tiles.  To raise a maximum holds a CTA up for about 5 us, many more than its
+    // instructions take: they are seldom run and come from memory.  With 2^40, which
+    // each of 32 rows passes at a tile of its own where logits are large (deviations
+    // of 10 and more), 8 trees of 16 over 8,001 .. 32,000 tokens took 113 us (now 94),
+    // a prompt of 8,191 queries 430 (370).
     constexpr float kLeast = 0x1p-40f;
-    const float accept = of_blocks<M> ? 0x1p40f : __all_sync(0xffffffffu, valid) ? 65536.f : 256.f;
+    const float accept = of_blocks<M> ? 0x1p80f : __all_sync(0xffffffffu, valid) ? 65536.f : 256.f;
     float m_run = of_blocks<M> ? 0.f : -INFINITY, l = 0.f;
     // {first keys, flags} of the next key tile; its visibility bits are read
     // only where a tile is masked (they would hold eight registers of the loop)
