@@ -289,28 +289,30 @@ struct Producer {
 
 // The same for rows in 8 bits, whose stages pass twice as fast: what the producer did
 // for each held them up (1,470 of 1,690 cycles a stage, with the consumers waiting 600 of
-// theirs), first of all its reads of the plan when the walk got there.  So a stage's
-// page id is read kAhead stages ahead, an item's record two items ahead and its
-// segment's one item.
+// theirs).  So it walks the plan a batch of an item's stages at a time, a lane to each
+// stage's page (each of its pages, where it has several), and reads an item's record two
+// items ahead and its segment's one item: 48 sequences of 200 .. 60,000 tokens take 158
+// us of 156 for their bytes at 128 dimensions, and at 64 on pages of 16 116 (stage by
+// stage, page ids read four stages ahead, 194).  With a second batch's page ids read in
+// advance they take 121: the walk past an item's end waits for its loads sooner.
 //
 // A box has the rows of a page (64 at most) of keys and of values, one after the other,
 // since every box costs its thread about 100 cycles (windows of 2,048 tokens of 64
-// sequences on pages of 16: 18.9 -> 17.1 us).  kWhole (pages of 64 tokens or more): a
-// stage is one box and 32 bytes of either plane's scales, all issued by one elected
-// thread.  Else a lane stands for a block of keys or of values; of those that begin a
-// page the keys' load it, and every lane copies its block's scale by cp.async (a bulk
-// copy takes no less than 16 bytes).
+// sequences on pages of 16: 18.9 -> 17.1 us).  The lane that issues it also copies the
+// page's scales: in bulk (kWhole, pages of 64 tokens or more: 32 bytes of either plane),
+// else by cp.async (a bulk copy takes no less than 16 bytes).
 template <int D, bool kWhole>
 struct ProducerE8 {
     using C = DecCfg<D, true>;
-    static constexpr int kAhead = 4;
     static constexpr int kHalf = C::kStageScales / 2;
-    // A stage to come: its KV head, its first row in its page, and the (lane's) page, -1:
-    // none.
-    struct Stage {
-        int head, row;
+    static constexpr int kMost = D == 128 ? 4 : 8;   // stages of a batch
+    static constexpr int kEarly = 4;                 // stages that may go out before the wait
+    static_assert(kMost <= C::kStages && kEarly <= C::kStages, "slots that are free at the start");
+    // The next stages of one item: their KV head, and of the lane's the first row in its
+    // page and the page, -1: none.
+    struct Batch {
+        int n, head, row;
         int32_t pid;
-        bool on;        // there is such a stage
     };
     struct Item {
         int s0, s1, head, seg, page_off, n_pages;
@@ -322,22 +324,23 @@ struct ProducerE8 {
     uint32_t bars;      // ... and barriers: full [kStages], empty [kStages]
     volatile int* abort_flag;
     int group, lane;
-    int kv, block;      // (not kWhole) the lane's plane and block of a stage
-    bool box;           // ... it issues the box that begins there
+    int log_q, stage, part;      // (pages of a stage: 1 << log_q) the lane's of a batch
+    int most;                    // stages of a batch
     int it, it1, s, log_p;       // the walk: stage s of item `it`
     Item cur, nx, n2;            // the item, the next one, and the one after without its segment
     int64_t page_scales;         // scales of a page, all planes
     const float* layer_scales;
-    Stage w[kAhead];
+    Batch w;
     int slot;
     uint32_t phase, issued;
     bool first;                  // the CTA's first stage has not gone out yet
 
     __device__ __forceinline__ void init() {
-        kv = lane & 1;
-        block = lane >> 1;
-        box = lane < C::kStageScales && kv == 0 && block * kScaleRows % min(a.P, kStageTokens) == 0;
         log_p = __ffs(a.P) - 1;
+        log_q = kWhole ? 0 : __ffs(kStageTokens) - 1 - log_p;
+        stage = lane >> log_q;
+        part = lane & ((1 << log_q) - 1);
+        most = min(kMost, 32 >> log_q);
         page_scales = (int64_t)2 * a.Hkv * (a.P / kScaleRows);
         layer_scales = a.scales + (int64_t)a.layer * a.num_pages * page_scales;
         it = a.cta_begin[blockIdx.x];
@@ -351,9 +354,7 @@ struct ProducerE8 {
         read_segment(cur);
         read_segment(nx);
         s = cur.s0 + group;
-        settle();
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) w[i] = next();
+        next();
     }
     __device__ __forceinline__ void read_item(int i, Item& x) const {
         const DecodeItem* item = a.items + (i < it1 ? i : 0);
@@ -377,62 +378,67 @@ struct ProducerE8 {
             read_item(it + 2, n2);
         }
     }
-    // The walk's stage, and on to the group's next.
-    __device__ __forceinline__ Stage next() {
-        Stage x;
-        x.on = it < it1;
-        x.head = cur.head;
-        x.row = kWhole ? (s * kStageTokens) & (a.P - 1) : 0;
-        const int at = (s * kStageTokens + (kWhole ? 0 : block * kScaleRows)) >> log_p;
-        x.pid = x.on && (kWhole || lane < C::kStageScales) && at < cur.n_pages ? a.page_ids[cur.page_off + at] : -1;
-        s += kDecodeGroups;
+    // The walk's next stages of its item, and on behind them.
+    __device__ __forceinline__ void next() {
+        static_assert(kDecodeGroups == 2, "a group's stages are every other one");
         settle();
-        return x;
+        w.n = it < it1 ? min(most, (cur.s1 - s + 1) >> 1) : 0;
+        w.head = cur.head;
+        const int st = s + 2 * stage;
+        w.row = kWhole ? (st * kStageTokens) & (a.P - 1) : 0;
+        const int at = ((st * kStageTokens) >> log_p) + part;
+        w.pid = stage < w.n && at < cur.n_pages ? a.page_ids[cur.page_off + at] : -1;
+        s += 2 * w.n;
     }
-    // Issues a stage into the (free) slot.
-    __device__ __forceinline__ void issue(const Stage& x) {
-        const uint32_t full = bars + 8 * slot, dst = ring + slot * C::kStageBytes;
-        const uint32_t sdst = scales + slot * C::kStageScales * 4;
-        const bool valid = x.pid >= 0 && x.pid < a.num_pages;
-        if (x.pid < -1 || x.pid >= a.num_pages) set_error(a.err, kErrBounds);
-        const float* src = layer_scales + x.pid * page_scales +
-                           ((kWhole ? 0 : kv * a.Hkv) + x.head) * (a.P / kScaleRows);
-        if constexpr (kWhole) {
-            src += x.row / kScaleRows;
-            if (elect_one()) {
+    // Issues the batch's stage j into the (free) slot.
+    __device__ __forceinline__ void issue(int j) {
+        if (stage == j) {
+            const uint32_t full = bars + 8 * slot;
+            const uint32_t dst = ring + slot * C::kStageBytes, sdst = scales + slot * C::kStageScales * 4;
+            const bool valid = w.pid >= 0 && w.pid < a.num_pages;
+            if (w.pid < -1 || w.pid >= a.num_pages) set_error(a.err, kErrBounds);
+            const float* src = layer_scales + w.pid * page_scales + w.head * (a.P / kScaleRows);
+            if constexpr (kWhole) {
                 if (valid) {
+                    src += w.row / kScaleRows;
                     mbar_arrive_expect_tx(full, C::kStageBytes + C::kStageScales * 4);
-                    load_pair(dst, full, x);
+                    load_pair(dst, full);
                     bulk_load(sdst, src, kHalf * 4, full);
                     bulk_load(sdst + kHalf * 4, src + page_scales / 2, kHalf * 4, full);
                 } else {
                     mbar_arrive(full);
                 }
-            }
-        } else {
-            const uint32_t n = __popc(__ballot_sync(0xffffffffu, box && valid));
-            if (lane == 0) {
-                if (n) mbar_arrive_expect_tx(full, n * a.P * 2 * C::kRowBytes);
-                else mbar_arrive(full);
-            }
-            __syncwarp();
-            if (box && valid) load_pair(dst + block * kScaleRows * 2 * C::kRowBytes, full, x);
-            if (lane < C::kStageScales) {
-                if (valid)
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(sdst + (kv * kHalf + block) * 4),
-                                 "l"(src + (block * kScaleRows & (a.P - 1)) / kScaleRows)
-                                 : "memory");
-                // (arrives when this lane's copy has landed)
+            } else {
+                if (valid) {
+                    mbar_arrive_expect_tx(full, a.P * 2 * C::kRowBytes);
+                    load_pair(dst + part * a.P * 2 * C::kRowBytes, full);
+                    const uint32_t to = sdst + part * (a.P / kScaleRows) * 4;
+                    copy_scales(to, src);
+                    copy_scales(to + kHalf * 4, src + page_scales / 2);
+                } else {
+                    mbar_arrive(full);
+                }
+                // (arrives when this lane's copies have landed)
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full) : "memory");
             }
         }
+        __syncwarp();
+    }
+    // A page's scales of one plane and head: 1, 2 or 4.
+    __device__ __forceinline__ void copy_scales(uint32_t dst, const float* src) const {
+        if (a.P == 8)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+        else if (a.P == 16)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+        else
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
     }
     // A page's box of keys and of values.
-    __device__ __forceinline__ void load_pair(uint32_t dst, uint32_t full, const Stage& x) const {
+    __device__ __forceinline__ void load_pair(uint32_t dst, uint32_t full) const {
         asm volatile(
             "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
             " [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
-            "l"(tmap), "r"(full), "r"(0), "r"(x.row), "r"(x.head), "r"(0), "r"(a.layer * a.num_pages + x.pid)
+            "l"(tmap), "r"(full), "r"(0), "r"(w.row), "r"(w.head), "r"(0), "r"(a.layer * a.num_pages + w.pid)
             : "memory");
     }
     __device__ __forceinline__ void next_slot() {
@@ -443,53 +449,44 @@ struct ProducerE8 {
             phase ^= 1;
         }
     }
-    // Before the grid-dependency wait (see Producer): of the first kAhead stages those in
-    // pages that no running work writes; the others are prefetched into L2.  Returns
-    // the stages issued.
+    // Before the grid-dependency wait (see Producer): of the first batch's first kEarly
+    // stages those in pages that no running work writes; the others are prefetched into
+    // L2.  Returns the stages issued.
     __device__ __forceinline__ int early() {
-        static_assert(kAhead <= C::kStages, "slots that are free at the start");
         if ((int)blockIdx.x == a.debug_drop_cta) return 0;
         int n = 0;
         bool go = kWhole && a.kv_early;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (!w[i].on) break;
+        for (int j = 0; j < min(w.n, kEarly); ++j) {
+            const int32_t pid = __shfl_sync(0xffffffffu, w.pid, j);
             bool unsafe = false;
-            for (int u = lane; u < a.n_unsafe; u += 32) unsafe |= a.unsafe[u] == w[i].pid;
+            for (int u = lane; u < a.n_unsafe; u += 32) unsafe |= a.unsafe[u] == pid;
             go = go && !__any_sync(0xffffffffu, unsafe);
             if (go) {
-                issue(w[i]);
+                issue(j);
                 next_slot();
                 ++n;
-            } else if ((kWhole ? lane == 0 : box) && w[i].pid >= 0 && w[i].pid < a.num_pages) {
+            } else if (stage == j && w.pid >= 0 && w.pid < a.num_pages) {
                 asm volatile("cp.async.bulk.prefetch.tensor.5d.L2.global.tile [%0, {%1, %2, %3, %4, %5}];" ::"l"(tmap),
-                             "r"(0), "r"(w[i].row), "r"(w[i].head), "r"(0),
-                             "r"(a.layer * a.num_pages + w[i].pid)
+                             "r"(0), "r"(w.row), "r"(w.head), "r"(0), "r"(a.layer * a.num_pages + w.pid)
                              : "memory");
             }
         }
         return n;
     }
-    // n: stages that went out early.
+    // n: stages of the first batch that went out early.
     __device__ __forceinline__ void run(int n) {
-        bool ok = true, more = true;
-        while (more) {
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                more = more && w[i].on;
-                if (!more) continue;
-                if (n > 0) {
-                    --n;
-                } else {
-                    ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (C::kStages + slot), phase ^ 1, abort_flag));
-                    more = ok;
-                    if (!ok) continue;
-                    // test hook: leave this stage unsignalled (see Producer)
-                    if (!(first && (int)blockIdx.x == a.debug_drop_cta)) issue(w[i]);
-                    next_slot();
-                }
-                w[i] = next();
+        bool ok = true;
+        while (ok && w.n > 0) {
+            for (int j = 0; j < w.n; ++j) {
+                if (j < n) continue;
+                ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (C::kStages + slot), phase ^ 1, abort_flag));
+                if (!ok) break;
+                // test hook: leave this stage unsignalled (see Producer)
+                if (!(first && (int)blockIdx.x == a.debug_drop_cta)) issue(j);
+                next_slot();
             }
+            n = 0;
+            next();
         }
         if (!ok && lane == 0) {
             if (!*abort_flag) set_error(a.err, kErrTimeout);
@@ -1542,12 +1539,15 @@ __global__ void __launch_bounds__(DecCfg<D, kE8>::kThreads, 1)
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kOffBars);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + C::kBarRuns + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // per group: full [kStages], empty [kStages]
+    if (threadIdx.x < kDecodeGroups * 2 * C::kStages) {
+        // (8 bits, several pages to a stage: two arrivals for each page)
+        const int filled = kE8 && a.P < kStageTokens ? 2 * kStageTokens >> (__ffs(a.P) - 1) : 1;
+        mbar_init(smem_addr(&bars[threadIdx.x]),
+                  threadIdx.x / C::kStages % 2 ? kDecodeConsumerWarps / kDecodeGroups : filled);
+        fence_mbar_init();
+    }
     if (threadIdx.x == 0) {
-        // per group: full [kStages], empty [kStages]
-        for (int s = 0; s < kDecodeGroups * 2 * C::kStages; ++s)
-            mbar_init(smem_addr(&bars[s]),
-                      s / C::kStages % 2 ? kDecodeConsumerWarps / kDecodeGroups
-                                         : kE8 && a.P < kStageTokens ? 1 + C::kStageScales : 1);
         mbar_init(smem_addr(&bars[C::kBarOut]), kDecodeConsumerWarps);
         mbar_init(smem_addr(&bars[C::kBarOutFree]), C::kClosers / 32);
         mbar_init(smem_addr(&bars[C::kBarRuns]), 1);
