@@ -569,8 +569,8 @@ int norm_backward_impl(sq_cache* c, int32_t n_tokens, const void* q, int64_t q_s
 // The pages of a plan as bf16, in the order of its list, as a pool of one layer.  Blocks
 // of two query tiles are the tensor cores' bound, and every page serves many of them:
 // it is widened once, before them (with the kernel's own converters, as one-tile blocks
-// have them, 512 queries over 60,001 tokens, 32/8 heads of 128, take 555 us against 419,
-// a prompt of 8,191 525 against 370).
+// have them, 512 queries over 60,001 tokens, 32/8 heads of 128, take 555 us against 420,
+// a prompt of 8,191 525 against 373).
 int widen_pages(sq_cache* c, const BlockPlanEntry& plan, int32_t layer, cudaStream_t st, bool captured,
                 CUtensorMap* map) {
     const Geometry& g = c->g;

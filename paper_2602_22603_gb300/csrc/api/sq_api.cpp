@@ -720,8 +720,8 @@ static int create_impl(const sq_config* cfg, bool kv8, sq_cache** out) {
         // Stages of half the bytes pass in half the time, and a unit's start does not:
         // 48 sequences of 200 .. 60,000 tokens, 32/8 heads, 170 us at the costs of bf16
         // rows, 158 at twice and 161 at three times those.  (At 64 dimensions the warps'
-        // work on a stage takes as long as before: windows of 2,048 tokens of 64
-        // sequences 19.8, 21.8 and 23.1.)
+        // work on a stage takes as long as before: 150 sequences of up to 400 tokens 14.7
+        // us and 15.6 at twice, windows of 4,096 of 64 sequences 19.7 and 20.9.)
         g.unit_cost *= 2;
         g.short_unit_cost *= 2;
     }

@@ -864,7 +864,9 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
 // those of the second, O^T = V^T P^T, so that the query rows are the columns, eight to a
 // product: with one sequence of 4 or 8 heads a group none is wasted (16 sequences of
 // 20,001 .. 60,000 tokens, 64/8 heads: 200.5 us with the query rows as the sixteen rows,
-// 174.8 so; two stages of a warp at a time, whose chains overlap, gain nothing).
+// 174.8 so; two stages of a warp at a time, whose chains overlap, gain nothing, nor do
+// they at 64 dimensions: 114.9 and 112.9 us over 48 long contexts, 15.8 and 17.1 over 64
+// windows of 2,048).
 // ldmatrix moves 16-bit pairs, here two neighbouring
 // dimensions.  Keys: a lane gets dimensions 4 tig .. 4 tig + 3 of sixteen, so the
 // queries' fragments are loaded in that order.  Values, transposed: the pairs of two
