@@ -634,3 +634,100 @@ def test_an_unsignalled_stage_runs_out(d, page):
     append(c, h, k, v)
     c.evict_spans(h, [(10, 500)])
     assert read(c, h)[0].isfinite().all() and c.sync_status() == sq.SQ_OK
+
+
+def all_calls(c, h, seed):
+    """Every call of a step over a sequence of 500 rows; what they give."""
+    g = gen(seed)
+    hq, hkv, d = c.Hq, c.Hkv, c.D
+    k, v = (torch.stack([rows(g, 500, hkv, d, 0.7) for _ in range(c.L)]) for _ in range(2))
+    append(c, h, k, v)
+    layer, outs = c.L - 1, []
+    c.extend([h], [9])
+    q, k, v = rows(g, 9, hq + 2 * hkv, d).split([hq, hkv, hkv], 1)
+    q_out = torch.empty(9, hq, d, dtype=torch.bfloat16, device="cuda")
+    c.qk_norm_rope_store([h], [9], layer, q, k, v, None, sq.norm_rope(sq.rope_table(600, d), d, 1e-6), q_out)
+    outs.append(q_out)
+    f = c.fork_aux(h)
+    append(c, f, *(rows(g, c.L * 3, hkv, d).view(c.L, 3, hkv, d) for _ in range(2)))
+    for x in (h, f):
+        for m in (1, 9, 400):
+            q = rows(g, m, hq, d, 0.5)
+            outs.append(torch.empty_like(q))
+            c.window_attention([x], [m], layer, q, outs[-1], 0, sm_scale=d ** -0.5)
+    c.release(f)
+    c.evict_spans(h, [(13, 77), (300, 301)])
+    outs.append(torch.empty(9, hq, d, dtype=torch.bfloat16, device="cuda"))
+    c.tree_attention([h], [9], [max(-1, j - 2) for j in range(9)], layer, q_out, outs[-1], sm_scale=d ** -0.5)
+    c.accept_draft(h, 9, [0, 2, 4])
+    outs += [x.clone() for x in read(c, h, layer=layer)]
+    assert c.sync_status() == sq.SQ_OK
+    return outs
+
+
+@pytest.mark.parametrize("hq,hkv,d,page", [(32, 8, 128, 64), (16, 4, 64, 16)])
+def test_pages_far_into_a_pool(hq, hkv, d, page):
+    """Offsets past 32 bits: the same bits as at a small pool's start."""
+    per = 2 * hkv * page * d
+    pages = (5 << 30) // (2 * per)
+    big, small = (sq.Cache(2, hq, hkv, d, page, n, bits=8) for n in (pages, 900 // page + 60))
+    filler = big.seq_new()
+    big.extend([filler], [(pages - 900 // page - 60) * page])
+    want, got = (all_calls(c, c.seq_new(), 40) for c in (small, big))
+    assert all(torch.equal(x, y) for x, y in zip(want, got))
+
+
+def test_a_pool_of_the_callers():
+    hq, hkv, d, page, pages = 8, 2, 128, 64, 30
+    cfg = sq.make_config(2, hq, hkv, d, page, pages)
+    pool = torch.full((sq.sq_pool_bytes_8bit(cfg),), 0x7f, dtype=torch.uint8, device="cuda")
+    given, own = sq.Cache(2, hq, hkv, d, page, pages, kv_pool=pool, bits=8), sq.Cache(2, hq, hkv, d, page, pages, bits=8)
+    assert sq.sq_pool_ptr(given.handle) == pool.data_ptr()
+    hs = [c.seq_new() for c in (given, own)]
+    want, got = (all_calls(c, h, 41) for c, h in zip((own, given), hs))
+    assert all(torch.equal(x, y) for x, y in zip(want, got))
+    # rows that the caller writes: the other cache's
+    given.pool_view().view(torch.uint8).copy_(own.pool_view().view(torch.uint8))
+    given.scale_view().copy_(own.scale_view())
+    for x, y in zip(read(given, hs[0]), read(own, hs[1])):
+        same(x, y)
+    with pytest.raises(sq.SqError):
+        sq.Cache(2, hq, hkv, d, page, pages, kv_pool=pool[1:], bits=8)
+
+
+def test_captured_blocks_of_two_tiles():
+    """Graphs of calls that widen pages share the cache's workspace: run in any order,
+    also after it has grown, they give what the calls give."""
+    hq, hkv, d, page = 8, 2, 64, 32
+    c = sq.Cache(1, hq, hkv, d, page, 300, bits=8)
+    hs = fill_sequences(c, [900, 300, 5000], 42)
+    q = rows(gen(43), 300, hq, d, 0.5)
+    outs = [torch.empty(300, hq, d, dtype=torch.bfloat16, device="cuda") for _ in hs]
+    s = torch.cuda.Stream()
+
+    def call(i, m=300):
+        c.window_attention([hs[i]], [m], 0, q[:m], outs[i][:m], 0, sm_scale=d ** -0.5)
+
+    graphs = []
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=s):
+            with pytest.raises(sq.SqError) as e:
+                call(0)
+            assert e.value.code == sq.SQ_ERR_UNSUPPORTED
+        for i in range(2):
+            call(i)
+            s.synchronize()
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=s):
+                call(i)
+        call(2)   # (more pages than the workspace had)
+        s.synchronize()
+        want = [x.clone() for x in outs]
+        for order in ((0, 1), (1, 0, 0, 1)):
+            for i in order:
+                outs[i].fill_(3.0)
+                graphs[i].replay()
+                call(2)
+            s.synchronize()
+            assert all(torch.equal(x, y) for x, y in zip(outs, want))
+    assert c.sync_status() == sq.SQ_OK
