@@ -549,10 +549,12 @@ SQ_API int sq_accept_draft(sq_cache *cache, sq_seq seq, int32_t n_draft, const i
  * values; single tokens round their softmax weights to 11 bits, and values of blocks
  * smaller than the largest one seen by 2^10 and more count with an error of up to
  * 2^-38 of that.  Query blocks (sq_window_attention of more than one token, and
- * sq_tree_attention) are those of a bf16 cache of the same values, bit for bit.  Where
- * a sequence has more queries than one tile holds (128 rows: 128 / (Hq / Hkv) of them),
- * the pages that the call reads are widened to bf16 first, in library memory of twice
- * their bytes, kept with the cache (a captured call needs an earlier one of as many). */
+ * sq_tree_attention) are those of a bf16 cache of the same values: bit for bit where no
+ * sequence has more queries than a tile holds (128 rows: 128 / (Hq / Hkv) of them) or
+ * some sequence more than three tiles do, else as exact, with sums in another order.  In
+ * calls of more than three tiles the pages that they read are widened to bf16 first, in
+ * library memory of twice their bytes, kept with the cache (a captured call needs an
+ * earlier one of as many). */
 #define SQ_SCALE_ROWS 8
 
 /* Bytes of the pool of an 8-bit cache (0 if the configuration is invalid). */

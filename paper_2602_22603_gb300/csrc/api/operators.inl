@@ -566,6 +566,15 @@ int norm_backward_impl(sq_cache* c, int32_t n_tokens, const void* q, int64_t q_s
     return e != cudaSuccess ? cuda_status(e) : rc;
 }
 
+// (8-bit caches) Query tiles of a sequence up to which each is a block of its own, whose
+// keys and values the kernel converts: up to three the conversions cost less than the
+// pages widened in memory, though every tile has its own.  32/8 heads of 128 dimensions,
+// two, three and four tiles over 60,000 tokens: 86, 122 and 156 us against 117, 161 and
+// 154; over 8,000 25, 31 and 36 against 24, 31 and 29; 8 sequences of 1 .. 96 queries over
+// 8,000 71 against 128.  64/8 heads of 64 over 60,000: 73, 104 and 135 against 83, 144 and
+// 123; over 8,000 22, 29 and 33 against 20, 26 and 26.
+constexpr int32_t kWideTiles = 3;
+
 // The pages of a plan as bf16, in the order of its list, as a pool of one layer.  Blocks
 // of two query tiles are the tensor cores' bound, and every page serves many of them:
 // it is widened once, before them (with the kernel's own converters, as one-tile blocks
@@ -662,11 +671,13 @@ int blocks_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
             at += in[i].n_q;
         }
         BlockPlanHost plan;
-        rc = plan_blocks(g, in, window, n_sink, c->num_sms, kPrefillPartLimit, &plan);
+        const int32_t most_one = c->kv8 ? kWideTiles : 1;
+        rc = plan_blocks(g, in, window, n_sink, c->num_sms, kPrefillPartLimit, &plan, most_one);
         if (rc == SQ_OK && plan.n_parts > 0) {
             rc = reserve_parts(c, (size_t)plan.n_parts * prefill_part_bytes(g.D));
             // no room for partial results: the plan without any
-            if (rc == SQ_ERR_NO_MEMORY) rc = plan_blocks(g, in, window, n_sink, c->num_sms, 0, &plan);
+            if (rc == SQ_ERR_NO_MEMORY)
+                rc = plan_blocks(g, in, window, n_sink, c->num_sms, 0, &plan, most_one);
         }
         if (rc != SQ_OK) return rc;
         std::vector<int32_t> read, wide;

@@ -223,9 +223,10 @@ inline void deal_units(const std::vector<Unit>& units, int32_t heads, int32_t ct
 
 // Plans one call (kPrefillPartLimit bytes of partial results, or `part_limit`).
 // The arguments have been checked but for the drafted rows' slots (kUnsupported)
-// and the plan's size (kCapacity).
+// and the plan's size (kCapacity).  A call whose sequences have at most `most_one` query
+// tiles each is planned a tile at a time, others by pairs of tiles.
 inline int plan_blocks(const Geometry& g, const std::vector<BlockSeq>& seqs, int32_t window, int32_t n_sink,
-                       int32_t ctas, int64_t part_limit, BlockPlanHost* out) {
+                       int32_t ctas, int64_t part_limit, BlockPlanHost* out, int32_t most_one = 1) {
     using namespace blocks_detail;
     *out = BlockPlanHost();
     const int32_t P = g.P, BP = kPrefillRows / g.G();
@@ -236,6 +237,7 @@ inline int plan_blocks(const Geometry& g, const std::vector<BlockSeq>& seqs, int
     int64_t queries = 0;
     for (const BlockSeq& q : seqs) {
         queries += q.n_q;
+        if (q.n_q > (int64_t)BP * most_one) out->one = false;
         if (q.n_q > 0) table |= q.parents || has_partial_pages(*q.s, P);
     }
     if (queries > 0x7fffffff / std::max(1, g.Hq)) return kCapacity;
@@ -300,9 +302,9 @@ inline int plan_blocks(const Geometry& g, const std::vector<BlockSeq>& seqs, int
                 out->rows[2 * (size_t)(q_row + i)] = low[i];
                 out->rows[2 * (size_t)(q_row + i) + 1] = top[i];
             }
-        const int32_t span = m <= BP ? BP : BP * kPrefillQTiles;
-        if (m > BP) out->one = false;
-        out->unit_rows = std::max(out->unit_rows, m <= BP ? m * g.G() : kPrefillQTiles * kPrefillRows);
+        const int32_t span = out->one || m <= BP ? BP : BP * kPrefillQTiles;
+        out->unit_rows =
+            std::max(out->unit_rows, span == BP ? std::min(m, BP) * g.G() : kPrefillQTiles * kPrefillRows);
         for (int32_t b = 0; b < m; b += span) {
             const int32_t e = std::min(m, b + span);
             int32_t lo = 0x7fffffff, hi = 0;

@@ -272,8 +272,8 @@ def wide_twin(c, pages):
 
 @pytest.mark.parametrize("hq,hkv,d,page", GEOMETRIES)
 def test_query_blocks_are_those_of_the_values(hq, hkv, d, page):
-    """Prompts, chunks and trees: bit for bit the bf16 cache's outputs over the same
-    values."""
+    """Prompts, chunks and trees of one tile a sequence or of more than three: bit for
+    bit the bf16 cache's outputs over the same values."""
     lengths = [300, 64, 9, 1500]
     pages = sum(-(-n // page) for n in lengths) + 8
     c = sq.Cache(2, hq, hkv, d, page, pages, bits=8)
@@ -288,7 +288,9 @@ def test_query_blocks_are_those_of_the_values(hq, hkv, d, page):
             left[i] -= n
     assert [c.page_table(h) for h in hs] == [twin.page_table(h) for h in other]
     scale = d ** -0.5
-    for counts, window, sinks in (([300, 64, 9, 1500], 0, 0), ([1, 3, 9, 130], 100, 5), ([0, 2, 1, 40], 0, 0)):
+    tile = 128 // (hq // hkv)
+    for counts, window, sinks in (([300, 64, 9, 1500], 0, 0), ([1, 3, 9, 3 * tile + 2], 100, 5),
+                                  ([0, 2, 1, min(40, tile)], 0, 0)):
         q = rows(gen(10), sum(counts), hq, d, 0.5)
         outs = [torch.empty_like(q) for _ in range(2)]
         lses = [torch.empty(q.shape[0], hq, device="cuda") for _ in range(2)]
@@ -297,7 +299,7 @@ def test_query_blocks_are_those_of_the_values(hq, hkv, d, page):
                 cache.window_attention(h, counts, 1, q, out, window, sinks, lse=lse, sm_scale=scale)
         assert torch.equal(*outs) and torch.equal(*lses)
         assert not outs[0].isnan().any()
-    counts = [17, 1, 5, 33]
+    counts = [min(17, tile), 1, 5, min(33, tile)]
     parents = [max(-1, j - 1 - j % 3) for m in counts for j in range(m)]
     q = rows(gen(11), sum(counts), hq, d, 0.5)
     outs = [torch.empty_like(q) for _ in range(2)]
@@ -730,4 +732,56 @@ def test_captured_blocks_of_two_tiles():
                 call(2)
             s.synchronize()
             assert all(torch.equal(x, y) for x, y in zip(outs, want))
+    assert c.sync_status() == sq.SQ_OK
+
+
+@pytest.mark.parametrize("hq,hkv,d,page", GEOMETRIES)
+@pytest.mark.parametrize("ragged", [False, True])
+def test_blocks_of_two_and_three_tiles(hq, hkv, d, page, ragged):
+    """Chunks and trees of up to three query tiles a sequence, beside shorter ones, over
+    whole and partial pages."""
+    tile = 128 // (hq // hkv)
+    lengths = [3 * tile + 300, 2 * tile + 70, tile + 1]
+    c = sq.Cache(1, hq, hkv, d, page, sum(-(-n // page) for n in lengths) + 40, bits=8)
+    hs = fill_sequences(c, lengths, 44)
+    if ragged:
+        c.evict_spans_ragged(hs[0], [(5, 40), (90, 91), (130, 133)])
+    ctx = [c.seq_info(h)[0] for h in hs]
+    scale = d ** -0.5
+
+    def check(out, q, i, keep):
+        want, weighted, logits = ref.attention(q, *read(c, hs[i]), scale, keep)
+        # weights and outputs in bf16 (2^-8 of each, the normaliser's as well), sums as
+        # in token_budget
+        off = (out.double() - want).abs()
+        assert (off <= weighted * 2.0 ** -7 + want.abs() * 2.0 ** -8 +
+                weighted * (2.0 * (d + 8) * 2.0 ** -24 * logits)[..., None]).all()
+
+    for counts, window, sinks in (([3 * tile, 2 * tile, 1], 0, 0), ([2 * tile + 1, 2 * tile - 1, tile + 1], 60, 3)):
+        q = rows(gen(45), sum(counts), hq, d, 0.5)
+        out = torch.full_like(q, 3.0)
+        for _ in range(2):
+            c.window_attention(hs, counts, 0, q, out, window, sinks, sm_scale=scale)
+        at = 0
+        for i, m in enumerate(counts):
+            p, j = torch.arange(ctx[i] - m, ctx[i], device="cuda")[:, None], torch.arange(ctx[i], device="cuda")[None]
+            keep = (j <= p) & ((j > p - window) | (j < sinks)) if window else j <= p
+            check(out[at:at + m], q[at:at + m], i, keep)
+            at += m
+    counts = [min(256, 3 * tile), min(256, 2 * tile), 1]
+    parents = [max(-1, j - 1 - j % 3) for m in counts for j in range(m)]
+    q = rows(gen(46), sum(counts), hq, d, 0.5)
+    out = torch.full_like(q, 3.0)
+    c.tree_attention(hs, counts, parents, 0, q, out, sm_scale=scale)
+    at = 0
+    for i, m in enumerate(counts):
+        keep = torch.ones(m, ctx[i], dtype=torch.bool)
+        own = torch.zeros(m, m, dtype=torch.bool)
+        for j in range(m):
+            if parents[at + j] >= 0:
+                own[j] = own[parents[at + j]]
+            own[j, j] = True
+        keep[:, ctx[i] - m:] = own
+        check(out[at:at + m], q[at:at + m], i, keep.cuda())
+        at += m
     assert c.sync_status() == sq.SQ_OK

@@ -172,22 +172,23 @@ def test_failed_appends_leave_nothing(L, cache):
     with pytest.raises(sq.SqError):
         cache.evict_spans(a, [(0, 1)], 1)
     assert ([cache.page_table(h) for h in (a, f)], cache.free_pages(), cache.next_pos(a)) == before
-    append(cache, a, 80, 1)
-    for m, fail in ((3, lambda: L.fake_fail(BLOCKS)), (90, lambda: L.fake_fail(BLOCKS)),
-                    (90, lambda: L.fake_fail8(WIDEN8))):
+    append(cache, a, 90, 1)
+    for m, fail in ((3, lambda: L.fake_fail(BLOCKS)), (100, lambda: L.fake_fail(BLOCKS)),
+                    (100, lambda: L.fake_fail8(WIDEN8))):
         fail()
         with pytest.raises(sq.SqError):
             sq.sq_window_attention(cache.handle, [a], [m], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
         sq.sq_window_attention(cache.handle, [a], [m], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
 
 
-def test_blocks_of_two_tiles_widen_the_pages_that_they_see(L, cache):
+def test_blocks_of_many_tiles_widen_the_pages_that_they_see(L, cache):
     a, b = cache.seq_new(), cache.seq_new()
     append(cache, a, 1000, 1)
     append(cache, b, 40, 2)
-    rows = 128 // (HQ // HKV)   # queries of a tile
-    sq.sq_window_attention(cache.handle, [a, b], [rows, 3], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
-    assert L.fake_wide() == 0
+    rows = 3 * 128 // (HQ // HKV)   # queries of three tiles
+    for n in (rows // 3, rows // 3 + 1, rows):
+        sq.sq_window_attention(cache.handle, [a, b], [n, 3], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
+        assert L.fake_wide() == 0
     sq.sq_window_attention(cache.handle, [a, b], [rows + 1, 3], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
     assert L.fake_wide() == sum(cache.seq_info(h)[1] for h in (a, b))
     # (whole 64-row boxes of the window's, and the sinks')
@@ -202,7 +203,7 @@ def test_query_blocks_take_turns_over_streams(L, cache):
     append(cache, b, 900, 2)
     for s in (1, 2, 3, 1, 2):
         for h in (a, b):
-            sq.sq_window_attention(cache.handle, [h], [90], 0, Q, OUT, 0, sm_scale=0.1, stream=s)
+            sq.sq_window_attention(cache.handle, [h], [100], 0, Q, OUT, 0, sm_scale=0.1, stream=s)
         sq.sq_tree_attention(cache.handle, [a, b], [2, 2], [-1, 0, -1, 0], 0, Q, OUT, sm_scale=0.1, stream=s)
     assert L.fake_races() == 0
 
@@ -214,11 +215,11 @@ def test_no_room_for_widened_pages(L):
     c.append_kv(a, 5000, k.ctypes.data, k.ctypes.data, 1)
     L.fake_malloc_limit(1 << 20)
     with pytest.raises(sq.SqError) as e:
-        sq.sq_window_attention(c.handle, [a], [90], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
+        sq.sq_window_attention(c.handle, [a], [100], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
     assert e.value.code == sq.SQ_ERR_NO_MEMORY
     sq.sq_decode_attention(c.handle, [a], 0, Q, OUT, sm_scale=0.1, stream=1)
     L.fake_malloc_limit(-1)
-    sq.sq_window_attention(c.handle, [a], [90], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
+    sq.sq_window_attention(c.handle, [a], [100], 0, Q, OUT, 0, sm_scale=0.1, stream=1)
     c.close()
 
 
