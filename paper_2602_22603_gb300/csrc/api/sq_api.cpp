@@ -730,6 +730,8 @@ static int create_impl(const sq_config* cfg, bool kv8, sq_cache** out) {
     if (!c) return SQ_ERR_NO_MEMORY;
     c->g = g;
     c->kv8 = kv8;
+    // (small pages' rows in 8 bits are never read ahead: their writes need no tickets)
+    if (kv8 && g.P < kStageTokens) c->early_ok = false;
     if (kv8 && !kv8_prepare) return SQ_ERR_UNSUPPORTED;
     c->host.reset(new (std::nothrow) HostCache(g));
     if (!c->host) return SQ_ERR_NO_MEMORY;
