@@ -164,10 +164,28 @@ int used_buffer(TurnBuffer& b, cudaStream_t st, bool captured) {
 // pages of the newest store one by one.
 void note_store(sq_cache* c, std::vector<int32_t>&& pages, void* stream) {
     if (!c->early_ok) return;
+    const bool again = pages == c->store_pages;
+    if (again && stream == c->store_stream && !c->write_pending.empty() &&
+        c->write_pending.back().first == c->store_ticket && !capturing(as_stream(stream))) {
+        // The store before was the last write, to the same pages (the next layer's): its
+        // event moves on, since nothing may read them ahead of this one either.  (With
+        // events of its own for every store, looked after 32 at a time, one of a single
+        // token took 10.5 us instead of 8.8.)
+        const uint64_t t = ++c->write_seq;
+        if (cudaEventRecord(c->write_pending.back().second, as_stream(stream)) != cudaSuccess) {
+            cudaGetLastError();
+            c->early_ok = false;
+            return;
+        }
+        for (int32_t p : pages) c->page_ticket[p] = t;
+        c->write_pending.back().first = c->store_ticket = t;
+        return;
+    }
     // (stores may go on without an attention call, which would look after them)
     if (c->write_pending.size() >= 32 && !capturing(as_stream(stream))) poll_writes(c);
     note_writes(c, pages.data(), pages.size(), stream);
-    if (pages != c->store_pages) {
+    c->store_stream = stream;
+    if (!again) {
         c->store_rest = c->store_ticket;
         c->store_pages = std::move(pages);
     }

@@ -243,6 +243,7 @@ struct sq_cache {
     // stores before it to other pages
     std::vector<int32_t> store_pages;
     uint64_t store_ticket = 0, store_rest = 0;
+    void* store_stream = nullptr;
     std::vector<uint64_t> page_ticket;
     std::deque<std::pair<uint64_t, cudaEvent_t>> write_pending;
     std::vector<cudaEvent_t> write_events;  // recycled

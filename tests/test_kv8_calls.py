@@ -384,3 +384,37 @@ def test_a_block_of_rows_changes_scale_after_its_readers(L, end, write):
         c.evict_spans_ragged(a, [(70, 71)], 1)
     assert c.page_table(a)[1] == page and L.fake_page_races() == 0
     c.close()
+
+
+def test_stores_of_the_same_rows_share_an_event(L):
+    """Layer after layer: nothing reads their pages ahead until the last store is done,
+    other pages stay readable, and other writes between have events of their own."""
+    c = sq.Cache(2, HQ, HKV, D, 64, PAGES, bits=8)
+    a, b = c.seq_new(), c.seq_new()
+    append(c, a, 100, 1)
+    append(c, b, 10, 1)
+    first, last = c.page_table(a)
+    L.fake_done(1)
+    c.extend([a], [1], 1)
+    store(c, [a], [1], 0, 3)
+    decode(c, [a])
+    decode(c, [a])
+    assert L.fake_early(first) and L.fake_early(last)
+    L.fake_done(0)
+    for i in range(5):
+        store(c, [a], [1], i % 2, 3)
+        decode(c, [a])
+        assert L.fake_early(first) and not L.fake_early(last)
+    store(c, [a], [1], 0, 3, stream=2)
+    append(c, b, 1, 4)
+    store(c, [a], [1], 1, 3)
+    decode(c, [a])
+    assert L.fake_early(first) and not L.fake_early(last)
+    store(c, [b], [1], 0, 3)   # (the stores before it are not listed page by page)
+    decode(c, [a])
+    assert not L.fake_early(first) and not L.fake_early(last)
+    L.fake_done(1)
+    decode(c, [a])
+    assert L.fake_early(first) and L.fake_early(last)
+    L.fake_done(0)
+    c.close()
