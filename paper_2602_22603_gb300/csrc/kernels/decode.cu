@@ -878,8 +878,11 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
 // the largest's, an error of 2^-32 of it below.  The normaliser sums the rounded
 // weights.  A block's values have their scale s, so its weights take s / v_ref into the
 // product, v_ref being the largest scale of the warp's values so far, which the sums
-// get back at the item's end.
+// get back at the item's end, and 2^-kMost with it (the normaliser too), so that they are
+// of weights of at most 1: with weights of 2^kMost they pass what fp32 holds where values
+// are large.
 constexpr float kLift = 7.f, kMost = 15.f;
+static_assert(kMost == 15.f, "0x1p-15f at an item's end");
 constexpr float kNoKeys = -1e30f;   // m of a row that has seen no key
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -1221,13 +1224,14 @@ __device__ __forceinline__ int e8_item(const DecodeArgs& a, const ItemHead& item
             const int at = 2 * tig + e;
             if (gid == 0) {
                 red_m[warp * kRowsPerTile + rb + at] = st.m[r][e] == kNoKeys ? -INFINITY : st.m[r][e];
-                red_l[warp * kRowsPerTile + rb + at] = l;
+                red_l[warp * kRowsPerTile + rb + at] = l * 0x1p-15f;
             }
             if (rb + at < rows) {
+                const float v = st.v_ref * 0x1p-15f;
 #pragma unroll
                 for (int j = 0; j < D / 16; ++j)
                     *reinterpret_cast<float2*>(wo + out_pos<D>(at, j * 16 + gid * 2)) =
-                        make_float2(st.o[j][r][e] * st.v_ref, st.o[j][r][2 + e] * st.v_ref);
+                        make_float2(st.o[j][r][e] * v, st.o[j][r][2 + e] * v);
             }
         }
         if (last) {

@@ -1,0 +1,60 @@
+"""Single tokens over rows of 8 bits at the ends of what queries, keys and values may be:
+the results are those of the values that the cache holds."""
+
+import pytest
+import torch
+
+import paper_2602_22603_gb300 as sq
+from tests import kv8_reference as ref
+from tests.test_gpu_kv8 import append, gen, read, rows
+
+pytestmark = pytest.mark.gpu
+LARGEST = 240 * 2.0 ** 120   # that a block holds
+
+
+def cache_of(hq, hkv, d, page, k, v, ctas=0):
+    """A cache with one sequence of these rows, and the rows as they are held.  (ctas:
+    of a call; of one its warps have many stages.)"""
+    n = k.shape[0]
+    c = sq.Cache(1, hq, hkv, d, page, -(-n // page) + 4, bits=8, decode_ctas=ctas)
+    h = c.seq_new()
+    append(c, h, k.bfloat16()[None], v.bfloat16()[None])
+    return c, h, *read(c, h)
+
+
+def single(c, hs, q, scale):
+    out = torch.empty(len(hs), c.Hq, c.D, device="cuda")
+    c.decode_attention(hs, 0, q, out, sq.SQ_OUT_F32, scale)
+    assert c.sync_status() == sq.SQ_OK
+    return out.double()
+
+
+def rising(g, n, hkv, d, step):
+    """Keys whose first dimension rises from -n step / 2 by about `step` a row (held with
+    4 significant bits, so that it stays for some rows), the others small."""
+    k = torch.randn(n, hkv, d, generator=g, device="cuda") * 0.05
+    k[..., 0] = ((torch.arange(n, device="cuda") - n / 2) * step)[:, None]
+    return k
+
+
+@pytest.mark.parametrize("hq,hkv,d,page", [(4, 1, 128, 64), (16, 2, 64, 8), (32, 2, 64, 64), (6, 2, 128, 256)])
+@pytest.mark.parametrize("n,size", [(1, 1e36), (1, 1e37), (1, LARGEST), (7, 1e37), (100, 1e36), (300, 1e36)])
+@pytest.mark.parametrize("step", [0.0, 0.3, 1.5, 6.0])
+@pytest.mark.parametrize("ctas", [0, 1])
+def test_values_of_any_size(hq, hkv, d, page, n, size, step, ctas):
+    """Values up to the largest that are held, one sign a dimension (so that sums are as
+    large as they can be), at logits that rise and bring weights above 1."""
+    g = gen(1)
+    v = (0.5 + 0.5 * torch.rand(n, hkv, d, generator=g, device="cuda")) * size
+    v[:, :, ::2] = size
+    v *= torch.where(torch.arange(d, device="cuda") % 3 == 0, -1.0, 1.0)
+    c, h, k, v = cache_of(hq, hkv, d, page, rising(g, n, hkv, d, step), v, ctas)
+    assert n > 1 or size < LARGEST or (v.abs().amax() == LARGEST)
+    q = rows(g, 1, hq, d, 0.0) * 0.1
+    q[..., 0] = 1.0
+    # (in units of the largest: 64 bits have room, the budget's least term has not)
+    got = single(c, [h], q, 1.0) / size
+    want, weighted, logits = ref.attention(q, k, v / size, 1.0)
+    assert torch.isfinite(got).all()
+    assert ((got - want).abs() <= ref.token_budget(want, weighted, logits, d)).all()
+    c.close()
