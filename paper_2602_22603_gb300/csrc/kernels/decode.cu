@@ -883,7 +883,7 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
 // are large.
 constexpr float kLift = 7.f, kMost = 15.f;
 static_assert(kMost == 15.f, "0x1p-15f at an item's end");
-constexpr float kNoKeys = -1e30f;   // m of a row that has seen no key
+constexpr float kNoKeys = -3.4028234e38f;   // m at a row's start: no logit is below
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -1223,7 +1223,8 @@ __device__ __forceinline__ int e8_item(const DecodeArgs& a, const ItemHead& item
             for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
             const int at = 2 * tig + e;
             if (gid == 0) {
-                red_m[warp * kRowsPerTile + rb + at] = st.m[r][e] == kNoKeys ? -INFINITY : st.m[r][e];
+                // (without a weight either it has seen no key)
+                red_m[warp * kRowsPerTile + rb + at] = st.m[r][e] == kNoKeys && l == 0.f ? -INFINITY : st.m[r][e];
                 red_l[warp * kRowsPerTile + rb + at] = l * 0x1p-15f;
             }
             if (rb + at < rows) {

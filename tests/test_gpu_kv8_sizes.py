@@ -58,3 +58,27 @@ def test_values_of_any_size(hq, hkv, d, page, n, size, step, ctas):
     assert torch.isfinite(got).all()
     assert ((got - want).abs() <= ref.token_budget(want, weighted, logits, d)).all()
     c.close()
+
+
+@pytest.mark.parametrize("hq,hkv,d,page", [(4, 1, 128, 64), (32, 2, 64, 8)])
+@pytest.mark.parametrize("n", [1, 9, 700])
+@pytest.mark.parametrize("size", [2.0 ** 90, 1e30, 2.0 ** 101, 2.0 ** 120, 2.0 ** 126])
+def test_logits_far_below_zero(hq, hkv, d, page, n, size):
+    """All logits from -size on down: the key nearest to zero has all the weight.  (They
+    differ by a fifth and more of the nearest, and fp32 logits by 2^-16 at most.)"""
+    g = gen(2)
+    k = torch.zeros(n, hkv, d, device="cuda")
+    # 1, 1.25, 1.5 or 1.75 times a power of two: held exactly, in blocks that span 2^8
+    k[..., 0] = -torch.randint(5, 7 * 64, (n, hkv), generator=g, device="cuda").float()
+    k[..., 0] = torch.round(k[..., 0] / 64) * 64 - 64
+    best = int(torch.randint(0, n, (1,), generator=g, device="cuda"))
+    k[best, :, 0] = -40.0
+    v = rows(g, n, hkv, d).float()
+    c, h, k, v = cache_of(hq, hkv, d, page, k * 2.0 ** 20, v)
+    q = torch.zeros(1, hq, d, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 2.0 ** 60
+    got = single(c, [h], q, size / 2.0 ** 60 / (40 * 2.0 ** 20))
+    want = v[best].repeat_interleave(hq // hkv, 0)[None]
+    # (its weight is a power of two that fp16 holds: one fp32 division and product)
+    assert ((got - want).abs() <= want.abs() * 2.0 ** -20).all()
+    c.close()
