@@ -858,7 +858,8 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
 // A power of two for each query row takes it from bf16 into fp16's range, the largest
 // element to 2^14 .. 2^15 (elements below 2^-32 of it lose digits); the logits are
 // taken back with the softmax's scale and their block's, one factor for the eight keys
-// of a block.
+// of a block, and, where that might be an infinity (and make NaN of a key of zeros), a
+// power of two as the softmax takes them.
 //
 // The keys are the rows of the first product, S^T = K Q^T, and the values' dimensions
 // those of the second, O^T = V^T P^T, so that the query rows are the columns, eight to a
@@ -913,6 +914,9 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t w) {
     return r;
 }
 
+// Exponent of the power of two at or below a positive number (0: -127).
+__device__ __forceinline__ int exponent_of(float x) { return (__float_as_int(x) >> 23) - 127; }
+
 // a / b of two scales, a at most b (what is below 2^-40 is nothing to fp16).
 __device__ __forceinline__ float scale_ratio(float a, float b) {
     return __int_as_float(max(__float_as_int(a) - __float_as_int(b) + 0x3f800000, 87 << 23));
@@ -925,9 +929,9 @@ __device__ __forceinline__ uint32_t e8_chunk(int row, int chunk) {
 }
 
 // A query row (head h of the call; one that is none is zero) as B fragments, and the
-// factor that its logits take: row gid of a column tile.
+// two factors that its logits take: row gid of a column tile.
 template <int D>
-__device__ __forceinline__ float load_query_f16(const DecodeArgs& a, size_t h, bool on, int tig,
+__device__ __forceinline__ float2 load_query_f16(const DecodeArgs& a, size_t h, bool on, int tig,
                                                 uint32_t (&qb)[D / 16][2]) {
     uint32_t most = 0;
     const uint2* row = reinterpret_cast<const uint2*>(a.q + h * D) + tig;
@@ -951,7 +955,10 @@ __device__ __forceinline__ float load_query_f16(const DecodeArgs& a, size_t h, b
             const uint32_t x = qb[kk][e];
             qb[kk][e] = pack_f16x2(__uint_as_float(x << 16) * f, __uint_as_float(x & 0xffff0000u) * f);
         }
-    return a.scale_log2 * power_of_two(k);
+    // (a product that passes fp32: one key has all the weight with any such factor)
+    const float c = fminf(a.scale_log2 * power_of_two(k), 3.4028234e38f);
+    const int up = min(max(exponent_of(c), 0), 126);
+    return make_float2(c * power_of_two(-up), power_of_two(up));
 }
 
 // The plan's entries of the pages that a warp's 16 tokens of a stage lie in (two where
@@ -977,7 +984,8 @@ template <int D, int NR>
 struct E8State {
     uint32_t qb[NR][D / 16][2];
     float o[D / 16][NR][4];   // dimensions 16 j + 2 gid (+ 1), rows 2 tig, 2 tig + 1
-    float c[NR][2], m[NR][2], l[NR][2];
+    float c[NR][2], up[NR][2];   // what logits take: below 4, and a power of two, 1 or more
+    float m[NR][2], l[NR][2];
     float v_ref;
 };
 
@@ -1033,7 +1041,7 @@ __device__ __forceinline__ void e8_stage(E8State<D, NR>& st, uint8_t* tile, cons
                     if (!kAll && !(see[r][e] >> (gid + 8 * b) & 1u)) s = -INFINITY;
                     x[r][2 * b + e] = s;
                 }
-                over |= fmaxf(x[r][e], x[r][2 + e]) - st.m[r][e] > kMost;
+                over |= fmaf(fmaxf(x[r][e], x[r][2 + e]), st.up[r][e], -st.m[r][e]) > kMost;
             }
         if (__any_sync(0xffffffffu, over)) {
             // references from the largest logits
@@ -1044,7 +1052,7 @@ __device__ __forceinline__ void e8_stage(E8State<D, NR>& st, uint8_t* tile, cons
                     float mx = fmaxf(x[r][e], x[r][2 + e]);
 #pragma unroll
                     for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-                    mx = fmaxf(st.m[r][e], mx - kLift);
+                    mx = fmaxf(st.m[r][e], mx * st.up[r][e] - kLift);
                     const float al = exp2f(st.m[r][e] - mx);
                     st.m[r][e] = mx;
                     st.l[r][e] *= al;
@@ -1074,7 +1082,8 @@ __device__ __forceinline__ void e8_stage(E8State<D, NR>& st, uint8_t* tile, cons
         const uint32_t f2 = pack_f16x2(f, f);
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            const uint32_t h = pack_f16x2(exp2f(x[r][2 * b] - st.m[r][0]), exp2f(x[r][2 * b + 1] - st.m[r][1]));
+            const uint32_t h = pack_f16x2(exp2f(fmaf(x[r][2 * b], st.up[r][0], -st.m[r][0])),
+                                          exp2f(fmaf(x[r][2 * b + 1], st.up[r][1], -st.m[r][1])));
             add_f16x2(h, st.l[r][0], st.l[r][1]);
             pb[r][b] = transpose_8x8(mul_f16x2(h, f2));
         }
@@ -1144,11 +1153,12 @@ __device__ __forceinline__ int e8_item(const DecodeArgs& a, const ItemHead& item
     for (int r = 0; r < NR; ++r) {
         const int row = r * 8 + gid;
         const bool on = row < rows;
-        const float c = load_query_f16<D>(
+        const float2 c = load_query_f16<D>(
             a, on ? (size_t)(r ? item.seq1 : item.seq0) * a.Hq + item.head * G + row % G : 0, on, tig, st.qb[r]);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            st.c[r][e] = __shfl_sync(0xffffffffu, c, (2 * tig + e) * 4);
+            st.c[r][e] = __shfl_sync(0xffffffffu, c.x, (2 * tig + e) * 4);
+            st.up[r][e] = __shfl_sync(0xffffffffu, c.y, (2 * tig + e) * 4);
             const int j = (r * 8 + 2 * tig + e) / G;
             lim[r][e] = j < item.n_grp ? seg->grp_lim[j] : 0;
             st.m[r][e] = kNoKeys;

@@ -1,5 +1,6 @@
 """Single tokens over rows of 8 bits at the ends of what queries, keys and values may be:
 the results are those of the values that the cache holds."""
+import math
 
 import pytest
 import torch
@@ -81,4 +82,58 @@ def test_logits_far_below_zero(hq, hkv, d, page, n, size):
     want = v[best].repeat_interleave(hq // hkv, 0)[None]
     # (its weight is a power of two that fp16 holds: one fp32 division and product)
     assert ((got - want).abs() <= want.abs() * 2.0 ** -20).all()
+    c.close()
+
+
+@pytest.mark.parametrize("hq,hkv,d,page", [(4, 1, 128, 64), (16, 2, 64, 16), (32, 2, 64, 64)])
+@pytest.mark.parametrize("big,scale", [(2.0 ** 100, 1.0), (2.0 ** 126, 1.0), (2.0 ** 120, 1e30), (1.0, 3e38)])
+def test_keys_of_zeros_beside_large_ones(hq, hkv, d, page, big, scale):
+    """Queries and keys whose sizes' product passes fp32, in other dimensions: every logit
+    is 0."""
+    g = gen(3)
+    n = 90
+    k = torch.zeros(n, hkv, d, device="cuda")
+    k[::3, :, d // 2:] = torch.randn(n // 3, hkv, d // 2, generator=g, device="cuda") * 1e37
+    c, h, k, v = cache_of(hq, hkv, d, page, k, rows(g, n, hkv, d).float())
+    q = torch.zeros(1, hq, d, dtype=torch.bfloat16, device="cuda")
+    q[..., :d // 2] = rows(g, 1, hq, d // 2, 0.0) * big
+    got = single(c, [h], q, scale)
+    want, weighted, logits = ref.attention(torch.zeros_like(q), k, v, 1.0)
+    assert ((got - want).abs() <= ref.token_budget(want, weighted, logits, d)).all()
+    c.close()
+
+
+def test_large_queries():
+    """Logits of ordinary size from large queries and small keys, and the other way."""
+    g = gen(4)
+    hq, hkv, d, n = 16, 2, 64, 200
+    v = rows(g, n, hkv, d).float()
+    for e in (-90, -60, -20, 20, 60, 100):
+        c, h, k, vv = cache_of(hq, hkv, d, 16, torch.randn(n, hkv, d, generator=g, device="cuda") * 2.0 ** e, v)
+        q = torch.randn(1, hq, d, generator=g, device="cuda").bfloat16() * 2.0 ** -e
+        got = single(c, [h], q, d ** -0.5)
+        want, weighted, logits = ref.attention(q, k, vv, d ** -0.5)
+        assert ((got - want).abs() <= ref.token_budget(want, weighted, logits, d)).all()
+        c.close()
+
+
+@pytest.mark.parametrize("size,scale", [(2.0 ** 100, 2.0 ** 100), (2.0 ** 126, 2.0 ** 120), (1.0, 2.0 ** 127),
+                                        (2.0 ** -80, 2.0 ** 126)])
+def test_large_scales(size, scale):
+    """Factors that pass fp32 where logits do not: the largest logit has all the weight
+    (and all the same where the keys are too small for a cache to hold)."""
+    g = gen(5)
+    hq, hkv, d, n = 8, 2, 128, 150
+    k = torch.randint(1, 8, (n, hkv, d), generator=g, device="cuda") * (torch.arange(d, device="cuda") == 3)
+    k[77, :, 3] = 14
+    e = 100 - math.log2(size) - math.log2(scale)   # logits of 2^100 and more
+    c, h, k, v = cache_of(hq, hkv, d, 64, k.double() * 2.0 ** e, rows(g, n, hkv, d).float())
+    q = torch.full((1, hq, d), size, dtype=torch.bfloat16, device="cuda")
+    got = single(c, [h], q, scale)
+    if k.any():
+        want = v[77].repeat_interleave(hq // hkv, 0)[None]
+        assert ((got - want).abs() <= want.abs() * 2.0 ** -20).all()
+    else:
+        want, weighted, logits = ref.attention(q, k, v, 1.0)
+        assert ((got - want).abs() <= ref.token_budget(want, weighted, logits, d)).all()
     c.close()
