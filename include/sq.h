@@ -546,9 +546,9 @@ SQ_API int sq_accept_draft(sq_cache *cache, sq_seq seq, int32_t n_draft, const i
  *
  * Attention takes the values as they are: logits are fp32 sums of exact products of the
  * bf16 queries (elements below 2^-32 of their row's largest lose digits) and the
- * values; single tokens round their softmax weights to 11 bits, and values of blocks
- * smaller than the largest one seen by 2^10 and more count with an error of up to
- * 2^-38 of that.  Query blocks (sq_window_attention of more than one token, and
+ * values; single tokens round what each key adds to 11 bits, or to 2^-31 of the most that
+ * one key may add (its weight times the largest value of its block), whichever is more.
+ * Query blocks (sq_window_attention of more than one token, and
  * sq_tree_attention) are those of a bf16 cache of the same values: bit for bit where no
  * sequence has more queries than a tile holds (128 rows: 128 / (Hq / Hkv) of them) or
  * some sequence more than three tiles do, else as exact, with sums in another order.  In

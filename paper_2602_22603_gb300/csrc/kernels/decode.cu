@@ -874,16 +874,19 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
 // tokens; the bytes are taken apart, the even dimensions being the first eight rows of
 // a product and the odd ones the others.  P is transposed by movmatrix.
 //
-// Weights are 2^(x - m), rounded to fp16, m a reference that is raised only where some
-// weight passes 2^kMost, to the largest logit less kLift: 11 digits down to 2^-21 of
-// the largest's, an error of 2^-32 of it below.  The normaliser sums the rounded
-// weights.  A block's values have their scale s, so its weights take s / v_ref into the
-// product, v_ref being the largest scale of the warp's values so far, which the sums
-// get back at the item's end, and 2^-kMost with it (the normaliser too), so that they are
-// of weights of at most 1: with weights of 2^kMost they pass what fp32 holds where values
-// are large.
+// Weights are w = 2^(x - m), m a reference that is raised only where some weight passes
+// 2^kMost, to the largest logit less kLift.  The normaliser sums them rounded to fp16: 11
+// digits down to 2^-14, an error of 2^-25 below, which is 2^-32 of the largest weight's.
+// A block's values have their scale s, so what goes into the product is w s / v, v being
+// a power of two of the row's own that is raised where some w s passes 2^kMost v, to at
+// most 2^-kLift of it, and comes down as m goes up; rounded once, so that what a key adds
+// is off by 2^-12 of itself, or by 2^-32 of what the row's largest w s stands for.  (One
+// reference for all rows of a warp, the largest scale met, lost every value 2^25 below an
+// outlier's, whatever the outlier's weight.)  The sums get v back at the item's end, and
+// 2^-kMost with it (the normaliser too), so that they are of weights of at most 1: with
+// weights of 2^kMost they pass what fp32 holds where values are large.
 constexpr float kLift = 7.f, kMost = 15.f;
-static_assert(kMost == 15.f, "0x1p-15f at an item's end");
+static_assert(kMost == 15.f, "0x7800 of a stage, 0x1p-15f at an item's end");
 constexpr float kNoKeys = -3.4028234e38f;   // m at a row's start: no logit is below
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -897,9 +900,24 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
-    const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+__device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
+    const __half2 v = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
     return *reinterpret_cast<const uint32_t*>(&v);
+}
+// a *= x, b *= y.
+__device__ __forceinline__ void scale_pair(float& a, float& b, float x, float y) {
+    asm("{\n\t.reg .b64 u, v;\n\tmov.b64 u, {%0, %1};\n\tmov.b64 v, {%2, %3};\n\t"
+        "mul.rn.f32x2 u, u, v;\n\tmov.b64 {%0, %1}, u;\n\t}"
+        : "+f"(a), "+f"(b)
+        : "f"(x), "f"(y));
+}
+// Whether either half of a is above b's.
+__device__ __forceinline__ bool above_f16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("{\n\t.reg .pred p, q;\n\tsetp.gt.f16x2 p|q, %1, %2;\n\tor.pred p, p, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r)
+        : "r"(a), "r"(b));
+    return r != 0;
 }
 // lo += the low half of w, hi += its high half.
 __device__ __forceinline__ void add_f16x2(uint32_t w, float& lo, float& hi) {
@@ -916,11 +934,6 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t w) {
 
 // Exponent of the power of two at or below a positive number (0: -127).
 __device__ __forceinline__ int exponent_of(float x) { return (__float_as_int(x) >> 23) - 127; }
-
-// a / b of two scales, a at most b (what is below 2^-40 is nothing to fp16).
-__device__ __forceinline__ float scale_ratio(float a, float b) {
-    return __int_as_float(max(__float_as_int(a) - __float_as_int(b) + 0x3f800000, 87 << 23));
-}
 
 // Byte offset of a row's 16-byte chunk in a tile, as the tensor map swizzles it.
 template <int D>
@@ -986,7 +999,7 @@ struct E8State {
     float o[D / 16][NR][4];   // dimensions 16 j + 2 gid (+ 1), rows 2 tig, 2 tig + 1
     float c[NR][2], up[NR][2];   // what logits take: below 4, and a power of two, 1 or more
     float m[NR][2], l[NR][2];
-    float v_ref;
+    float iv[NR][2];          // 1 / v
 };
 
 // A stage's 16 tokens of a warp, in the ring's slot at `tile` (shared address), which
@@ -1027,7 +1040,6 @@ __device__ __forceinline__ void e8_stage(E8State<D, NR>& st, uint8_t* tile, cons
                     mma_f16(acc[r][NR > 1 ? 0 : h], f, st.qb[r][2 * k2 + h][0], st.qb[r][2 * k2 + h][1]);
             }
         }
-        bool over = false;
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
@@ -1041,53 +1053,67 @@ __device__ __forceinline__ void e8_stage(E8State<D, NR>& st, uint8_t* tile, cons
                     if (!kAll && !(see[r][e] >> (gid + 8 * b) & 1u)) s = -INFINITY;
                     x[r][2 * b + e] = s;
                 }
-                over |= fmaf(fmaxf(x[r][e], x[r][2 + e]), st.up[r][e], -st.m[r][e]) > kMost;
             }
-        if (__any_sync(0xffffffffu, over)) {
-            // references from the largest logits
-#pragma unroll
-            for (int r = 0; r < NR; ++r)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float mx = fmaxf(x[r][e], x[r][2 + e]);
-#pragma unroll
-                    for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-                    mx = fmaxf(st.m[r][e], mx * st.up[r][e] - kLift);
-                    const float al = exp2f(st.m[r][e] - mx);
-                    st.m[r][e] = mx;
-                    st.l[r][e] *= al;
-#pragma unroll
-                    for (int j = 0; j < D / 16; ++j) {
-                        st.o[j][r][e] *= al;
-                        st.o[j][r][2 + e] *= al;
-                    }
-                }
-        }
     }
-    const float sv_most = fmaxf(sv.x, sv.y);
-    if (sv_most > st.v_ref) {  // (warp-uniform)
-        const float f = scale_ratio(st.v_ref, sv_most);
-        st.v_ref = sv_most;
+    // weights, and what goes into the second product (w s first: it passes fp32's range
+    // only where some reference has to be raised)
+    uint32_t h[NR][2], p[NR][2], pb[NR][2];
+    auto weigh = [&] {
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j)
+        for (int r = 0; r < NR; ++r)
 #pragma unroll
-            for (int r = 0; r < NR; ++r)
+            for (int b = 0; b < 2; ++b) {
+                const float w0 = exp2f(fmaf(x[r][2 * b], st.up[r][0], -st.m[r][0]));
+                const float w1 = exp2f(fmaf(x[r][2 * b + 1], st.up[r][1], -st.m[r][1])), s = b ? sv.y : sv.x;
+                h[r][b] = pack_f16x2(w0, w1);
+                p[r][b] = pack_f16x2(w0 * s * st.iv[r][0], w1 * s * st.iv[r][1]);
+            }
+    };
+    weigh();
+    uint32_t most = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) st.o[j][r][i] *= f;
-    }
-    uint32_t pb[NR][2];
+    for (int r = 0; r < NR; ++r)
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const float f = scale_ratio(b ? sv.y : sv.x, st.v_ref);
-        const uint32_t f2 = pack_f16x2(f, f);
+        for (int b = 0; b < 2; ++b) most = max_f16x2(most, max_f16x2(h[r][b], p[r][b]));
+    if (__any_sync(0xffffffffu, above_f16x2(most, 0x78007800u))) {  // (2^kMost)
+        // references from the largest logits, and from the largest w s
+        auto largest = [](float y) {
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, off));
+            return y;
+        };
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            const uint32_t h = pack_f16x2(exp2f(fmaf(x[r][2 * b], st.up[r][0], -st.m[r][0])),
-                                          exp2f(fmaf(x[r][2 * b + 1], st.up[r][1], -st.m[r][1])));
-            add_f16x2(h, st.l[r][0], st.l[r][1]);
-            pb[r][b] = transpose_8x8(mul_f16x2(h, f2));
+            float f[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                // (of either block: its largest w s is its largest logit's)
+                const float x0 = largest(x[r][e]) * st.up[r][e], x1 = largest(x[r][2 + e]) * st.up[r][e];
+                const float m = fmaxf(st.m[r][e], fmaxf(x0, x1) - kLift);
+                const float al = exp2f(st.m[r][e] - m);
+                st.m[r][e] = m;
+                st.l[r][e] *= al;
+                const float ws = fmaxf(exp2f(x0 - m) * sv.x, exp2f(x1 - m) * sv.y);
+                const int v0 = -exponent_of(st.iv[r][e]);
+                const int v = min(max(max(v0 + exponent_of(al), exponent_of(ws) - (int)kLift), -126), 126);
+                st.iv[r][e] = power_of_two(-v);
+                f[e] = al * power_of_two(max(v0 - v, -126));
+            }
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) {
+                scale_pair(st.o[j][r][0], st.o[j][r][1], f[0], f[1]);
+                scale_pair(st.o[j][r][2], st.o[j][r][3], f[0], f[1]);
+            }
         }
+        weigh();
     }
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            pb[r][b] = transpose_8x8(p[r][b]);
+            add_f16x2(h[r][b], st.l[r][0], st.l[r][1]);
+        }
     if (!kAll) {
         // V rows that hold none of the segment's may hold anything: zero them, so that
         // 0 * V stays 0
@@ -1163,11 +1189,11 @@ __device__ __forceinline__ int e8_item(const DecodeArgs& a, const ItemHead& item
             lim[r][e] = j < item.n_grp ? seg->grp_lim[j] : 0;
             st.m[r][e] = kNoKeys;
             st.l[r][e] = 0.f;
+            st.iv[r][e] = 0x1p126f;
         }
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) st.o[j][r][0] = st.o[j][r][1] = st.o[j][r][2] = st.o[j][r][3] = 0.f;
     }
-    st.v_ref = power_of_two(kLeastScale);
     // tokens that every row sees, where their pages have rows for them (rows that are
     // none see what they like)
     int all = n_tok;
@@ -1238,7 +1264,8 @@ __device__ __forceinline__ int e8_item(const DecodeArgs& a, const ItemHead& item
                 red_l[warp * kRowsPerTile + rb + at] = l * 0x1p-15f;
             }
             if (rb + at < rows) {
-                const float v = st.v_ref * 0x1p-15f;
+                // (v is 2^-126 where there is no key, else 2^-107 and more)
+                const float v = power_of_two(max(-exponent_of(st.iv[r][e]) - (int)kMost, -126));
 #pragma unroll
                 for (int j = 0; j < D / 16; ++j)
                     *reinterpret_cast<float2*>(wo + out_pos<D>(at, j * 16 + gid * 2)) =

@@ -137,3 +137,76 @@ def test_large_scales(size, scale):
         want, weighted, logits = ref.attention(q, k, v, 1.0)
         assert ((got - want).abs() <= ref.token_budget(want, weighted, logits, d)).all()
     c.close()
+
+
+def share_budget(q, k, v, scale, blocks):
+    """What a key may be off by beside its own rounding, for each of n keys: fp16's least
+    step is 2^-24, where the row's largest product of a weight and a block's scale is 2^7
+    or more.  Half a step of a code of at most 448, and a block's largest value is 224
+    scales or more: 2^-31 of the largest product of a weight and such a value (and of the
+    normaliser 2^-32 of the largest weight, as much of the output)."""
+    m, hq, d = q.shape
+    g = hq // k.shape[1]
+    most = torch.empty(v.shape[:2], dtype=torch.float64, device=v.device)
+    for a, b in blocks:
+        most[a:b] = v[a:b].abs().amax((0, 2))
+    s = torch.einsum("mhd,nhd->mhn", q.double(), k.repeat_interleave(g, 1)) * scale
+    w = torch.softmax(s, -1)
+    return k.shape[0] * 2.0 ** -31 * (w * most.repeat_interleave(g, 1).T[None]).amax(-1)[..., None]
+
+
+@pytest.mark.parametrize("hq,hkv,d,page", [(4, 1, 128, 64), (16, 2, 64, 8), (32, 2, 64, 64), (16, 1, 128, 16)])
+@pytest.mark.parametrize("gap", [12, 20, 26, 38, 60, 110])
+@pytest.mark.parametrize("far", [0.0, 0.5, 1.0, 1.2, 2.0, math.inf])
+@pytest.mark.parametrize("ctas", [0, 1])
+def test_blocks_of_values_beside_much_larger_ones(hq, hkv, d, page, gap, far, ctas):
+    """Blocks whose values are 2^gap of the others', before, between and after those in
+    every warp's share, at weights of 2^-(far gap) of theirs: negligible ones (a weight of
+    0 too) take nothing from the others, whatever their size."""
+    g = gen(int(100 * min(far, 9)) + gap)
+    n = 1100
+    q = torch.zeros(1, hq, d, dtype=torch.bfloat16, device="cuda")
+    q[..., :] = 0.1 * rows(g, 1, hq, d, 0.0)
+    q[..., 0] = 1.0
+    k = torch.randn(n, hkv, d, generator=g, device="cuda")
+    v = torch.randn(n, hkv, d, generator=g, device="cuda") * 2.0 ** -(gap // 2)
+    block = torch.arange(n, device="cuda") // 8
+    large = (block % 11 == 3) | (block < 2) & (block % 2 == 0)
+    k[..., 0] = torch.where(large, -min(far * gap, 3000.0) * math.log(2.0), 0.0)[:, None]
+    v = torch.where(large[:, None, None], v * 2.0 ** gap, v)
+    c, h, k, v = cache_of(hq, hkv, d, page, k, v, ctas)
+    blocks = ref.blocks_of(c.page_fills(h), page)
+    for scale in (1.0, 0.25):
+        got = single(c, [h], q, scale)
+        want, weighted, logits = ref.attention(q, k, v, scale)
+        assert ((got - want).abs() <= ref.token_budget(want, weighted, logits, d) +
+                share_budget(q, k, v, scale, blocks)).all()
+    c.close()
+
+
+@pytest.mark.parametrize("d,page", [(128, 64), (64, 16)])
+@pytest.mark.parametrize("ctas", [0, 1])
+def test_rows_of_a_pass_keep_their_own_references(d, page, ctas):
+    """Query heads of one KV head, and of forks that share pages: some attend to large
+    values, some to small ones alone, in turns along the context."""
+    hq, hkv, n = 8, 1, 900
+    g = gen(7)
+    k = torch.randn(n, hkv, d, generator=g, device="cuda") * 0.3
+    v = torch.randn(n, hkv, d, generator=g, device="cuda")
+    part = torch.arange(n, device="cuda") // 40 % 3
+    v *= torch.exp2(torch.tensor([-30.0, 0.0, 30.0], device="cuda")[part])[:, None, None]
+    for i in range(3):
+        k[:, 0, i] = torch.where(part == i, 0.0, -120.0)
+    c, h, k, v = cache_of(hq, hkv, d, page, k, v, ctas)
+    f = c.fork_aux(h)
+    q = 0.1 * rows(g, 2, hq, d, 0.0)
+    q[..., :3] = 0
+    for i in range(2):
+        for j in range(hq):
+            q[i, j, (i + j) % 3] = 1.0
+    got = single(c, [h, f], q, 1.0)
+    blocks = ref.blocks_of(c.page_fills(h), page)
+    want, weighted, logits = ref.attention(q, k, v, 1.0)
+    assert ((got - want).abs() <= ref.token_budget(want, weighted, logits, d) +
+            share_budget(q, k, v, 1.0, blocks)).all()
+    c.close()
