@@ -213,16 +213,24 @@ int extend_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
     std::vector<char> passed(n_seqs, 0);
     std::vector<int32_t> taken, copied, left;
     std::vector<CowCopy> copies;
-    // takes back what was planned, unless everything is enqueued
+    // takes back what was planned, unless everything is enqueued.  What is under way then
+    // (copies into pages that are free again, words of plans that other calls may
+    // replace) is waited for; in a captured call it does not run.
     struct Undo {
         HostCache* host;
         const sq_seq* seqs;
         const std::vector<AppendPlan>* plans;
         int32_t planned;
+        bool enqueued;
+        cudaStream_t st;
         ~Undo() {
+            if (planned > 0 && enqueued && !capturing(st)) {
+                cudaStreamSynchronize(st);
+                cudaGetLastError();
+            }
             for (int32_t j = planned - 1; j >= 0; --j) host->undo_append(seqs[j], (*plans)[j]);
         }
-    } undo = {c->host.get(), seqs, &plans, 0};
+    } undo = {c->host.get(), seqs, &plans, 0, false, st};
     for (int32_t i = 0; i < n_seqs; ++i) {
         old_versions[i] = c->host->seq(seqs[i])->version;
         rc = c->host->append(seqs[i], n_new ? n_new[i] : 1, &plans[i]);
@@ -281,6 +289,7 @@ int extend_impl(sq_cache* c, const sq_seq* seqs, int32_t n_seqs, const int32_t* 
             e = launch_append_batch(a, st);
         }
         if (e != cudaSuccess) return cuda_status(e);
+        undo.enqueued = true;
         a.lens.n = 0;
     }
     if constexpr (!kLater) {
