@@ -935,12 +935,6 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t w) {
 // Exponent of the power of two at or below a positive number (0: -127).
 __device__ __forceinline__ int exponent_of(float x) { return (__float_as_int(x) >> 23) - 127; }
 
-// Byte offset of a row's 16-byte chunk in a tile, as the tensor map swizzles it.
-template <int D>
-__device__ __forceinline__ uint32_t e8_chunk(int row, int chunk) {
-    return row * D + ((chunk ^ (D == 128 ? row & 7 : row >> 1 & 3)) << 4);
-}
-
 // A query row (head h of the call; one that is none is zero) as B fragments, and the
 // two factors that its logits take: row gid of a column tile.
 template <int D>

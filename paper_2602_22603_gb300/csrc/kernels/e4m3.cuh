@@ -59,9 +59,6 @@ __device__ __forceinline__ float finite_size(float x) {
     const float a = fabsf(x);
     return a <= 3.4028234e38f ? a : 0.f;
 }
-__device__ __forceinline__ float finite_size(const float4& v) {
-    return fmaxf(fmaxf(finite_size(v.x), finite_size(v.y)), fmaxf(finite_size(v.z), finite_size(v.w)));
-}
 // 16 codes as fp16, and the largest size of them (before their scale; NaN is none).
 __device__ __forceinline__ void codes_f16(const uint4& c, __half2 (&h)[8]) {
     const uint32_t w[4] = {c.x, c.y, c.z, c.w};
