@@ -472,8 +472,9 @@ SQ_API int sq_qk_norm_rope_backward(sq_cache *cache, int32_t n_tokens, const voi
  * infinity or NaN there does not reach its output (it costs time: such a query is
  * taken once more, 40 to 130 us a head for 1,000 keys).  NaN in a query, or in a
  * key or value that it sees, is NaN in its output.  Values may have any finite
- * size: a query whose weighted sums pass 32 bits on the way (values of 1e26 and
- * more, weights being relative to 1) is taken once more too.
+ * size: a query whose weighted sums pass 32 bits on the way is taken once more too
+ * (weights are relative to 1, and those of a run of keys may sum to 2^80 before they
+ * are scaled down: values of 1e14 and more where logits are large).
  * Single tokens without lse run as sq_decode_attention does (values up to 3e38
  * over the number of keys seen).
  * Weights and normaliser are rounded as in sq_prefill_attention, whose limits on
@@ -520,11 +521,13 @@ SQ_API int sq_accept_draft(sq_cache *cache, sq_seq seq, int32_t n_draft, const i
  * for each block: SQ_SCALE_ROWS consecutive slots of one page, plane and KV head.  An
  * element's value is its code times its block's scale.  The scale is a power of two,
  * the least one from 2^-100 on with which the largest finite element of the block's
- * rows, before it is rounded, is at most 448; codes are rounded once, to nearest even.  A value then has 4
- * significant bits down to 2^-13 of its block's largest, and steps of 2^-16 of it
- * (or finer) below.  A block's rows may be taken from one scale to another (when a
- * larger row joins them, or rows of several blocks are packed into one): that changes
- * only values in those last steps.  An element that is an infinity or NaN is held as
+ * rows is at most 448: of rows that come before they are rounded, of rows that the block
+ * holds already as they are held (so where the largest was rounded down to 224 times
+ * the scale, the next row that joins may halve it).  Codes are rounded once, to nearest
+ * even.  A value then has 4 significant bits down to 2^-13 of its block's largest, and
+ * steps of 2^-16 of it (or finer) below.  A block's rows may be taken from one scale to
+ * another (when a row joins them, or rows of several blocks are packed into one): that
+ * changes only values in those last steps.  An element that is an infinity or NaN is held as
  * NaN, and counts for no scale; finite ones above 240 * 2^120 are held as that.
  *
  * Pool: codes [num_layers][num_pages][2][num_kv_heads][page_size][head_dim], a byte
@@ -551,10 +554,12 @@ SQ_API int sq_accept_draft(sq_cache *cache, sq_seq seq, int32_t n_draft, const i
  * Query blocks (sq_window_attention of more than one token, and
  * sq_tree_attention) are those of a bf16 cache of the same values: bit for bit where no
  * sequence has more queries than a tile holds (128 rows: 128 / (Hq / Hkv) of them) or
- * some sequence more than three tiles do, else as exact, with sums in another order.  In
- * calls of more than three tiles the pages that they read are widened to bf16 first, in
- * library memory of twice their bytes, kept with the cache (a captured call needs an
- * earlier one of as many). */
+ * some sequence more than three tiles do, else as exact, with sums in another order.  Where
+ * some sequence of a call has queries of more than three tiles, all pages that the call
+ * reads, the other sequences' too, are widened to bf16 first, in library memory of twice
+ * their bytes (and up to a quarter more), kept with the cache (a captured call needs an
+ * earlier one of as many); NO_MEMORY where there is none.  So long chunks are best called
+ * apart from single tokens over long contexts. */
 #define SQ_SCALE_ROWS 8
 
 /* Bytes of the pool of an 8-bit cache (0 if the configuration is invalid). */

@@ -10,7 +10,8 @@ namespace sq {
 // fp32 scales [L][num_pages][2][Hkv][P / kScaleRows].  A row's value is its code
 // times the scale of its block, kScaleRows slots of one page, plane and head.  A
 // scale is the least power of two, from 2^kLeastScale on, with which the largest
-// finite element of the block's rows is at most 448: codes of any scale then share
+// finite element of the block's rows (new ones before they are rounded, others as
+// they are held) is at most 448: codes of any scale then share
 // one grid but for the smallest (below 2^-6), so that taking a row to another scale
 // changes nothing but what falls below that.
 constexpr int kScaleRows = 8;
