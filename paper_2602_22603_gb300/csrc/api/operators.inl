@@ -600,7 +600,8 @@ int norm_backward_impl(sq_cache* c, int32_t n_tokens, const void* q, int64_t q_s
 // two, three and four tiles over 60,000 tokens: 86, 122 and 156 us against 117, 161 and
 // 154; over 8,000 25, 31 and 36 against 24, 31 and 29; 8 sequences of 1 .. 96 queries over
 // 8,000 71 against 128.  64/8 heads of 64 over 60,000: 73, 104 and 135 against 83, 144 and
-// 123; over 8,000 22, 29 and 33 against 20, 26 and 26.
+// 123; over 8,000 22, 29 and 33 against 20, 26 and 26.  (The rule takes no account of the
+// context: at 8,000 tokens two tiles, and of 64 dimensions two and three, lose 1 to 3 us.)
 constexpr int32_t kWideTiles = 3;
 
 // The pages of a plan as bf16, in the order of its list, as a pool of one layer.  Blocks

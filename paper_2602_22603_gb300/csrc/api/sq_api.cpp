@@ -719,10 +719,11 @@ static int create_impl(const sq_config* cfg, bool kv8, sq_cache** out) {
     if (kv8 && (int64_t)g.num_pages * g.P > 0x7fffffff) return SQ_ERR_UNSUPPORTED;
     if (kv8 && g.D == 128) {
         // Stages of half the bytes pass in half the time, and a unit's start does not:
-        // 48 sequences of 200 .. 60,000 tokens, 32/8 heads, 170 us at the costs of bf16
-        // rows, 158 at twice and 161 at three times those.  (At 64 dimensions the warps'
-        // work on a stage takes as long as before: 150 sequences of up to 400 tokens 14.7
-        // us and 15.6 at twice, windows of 4,096 of 64 sequences 19.7 and 20.9.)
+        // 48 sequences of 200 .. 60,000 tokens, 32/8 heads, 174 us at the costs of bf16
+        // rows, 160 at twice and 162 at three times those.  (At 64 dimensions the warps'
+        // work on a stage takes as long as before: 150 sequences of up to 400 tokens 15.6
+        // us and 17.0 at twice, 16/4 heads, 26.4 and 30.4, 64/8.  Long contexts gain
+        // there too, 64/8 heads over 200 .. 60,000 tokens 118 us and 108.)
         g.unit_cost *= 2;
         g.short_unit_cost *= 2;
     }

@@ -291,10 +291,10 @@ struct Producer {
 // for each held them up (1,470 of 1,690 cycles a stage, with the consumers waiting 600 of
 // theirs).  So it walks the plan a batch of an item's stages at a time, a lane to each
 // stage's page (each of its pages, where it has several), and reads an item's record two
-// items ahead and its segment's one item: 48 sequences of 200 .. 60,000 tokens take 158
-// us of 156 for their bytes at 128 dimensions, and at 64 on pages of 16 116 (stage by
-// stage, page ids read four stages ahead, 194).  With a second batch's page ids read in
-// advance they take 121: the walk past an item's end waits for its loads sooner.
+// items ahead and its segment's one item: 48 sequences of 200 .. 60,000 tokens take 160
+// us of 156 for their bytes at 128 dimensions, and at 64 on pages of 16 120 (then 116;
+// stage by stage, page ids read four stages ahead, 194).  With a second batch's page ids
+// read in advance they took 121: the walk past an item's end waits for its loads sooner.
 //
 // A box has the rows of a page (64 at most) of keys and of values, one after the other,
 // since every box costs its thread about 100 cycles (windows of 2,048 tokens of 64
@@ -863,11 +863,11 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
 //
 // The keys are the rows of the first product, S^T = K Q^T, and the values' dimensions
 // those of the second, O^T = V^T P^T, so that the query rows are the columns, eight to a
-// product: with one sequence of 4 or 8 heads a group none is wasted (16 sequences of
-// 20,001 .. 60,000 tokens, 64/8 heads: 200.5 us with the query rows as the sixteen rows,
-// 174.8 so; two stages of a warp at a time, whose chains overlap, gain nothing, nor do
-// they at 64 dimensions: 114.9 and 112.9 us over 48 long contexts, 15.8 and 17.1 over 64
-// windows of 2,048).
+// product: with one sequence of 4 or 8 heads a group none is wasted (when this was
+// chosen, 16 sequences of 20,001 .. 60,000 tokens, 64/8 heads: 200.5 us with the query rows
+// as the sixteen rows, 174.8 so, now 143; two stages of a warp at a time, whose chains
+// overlap, gain nothing, nor do they at 64 dimensions: 114.9 and 112.9 us over 48 long
+// contexts, 15.8 and 17.1 over 64 windows of 2,048, now 118.5 and 16.7).
 // ldmatrix moves 16-bit pairs, here two neighbouring
 // dimensions.  Keys: a lane gets dimensions 4 tig .. 4 tig + 3 of sixteen, so the
 // queries' fragments are loaded in that order.  Values, transposed: the pairs of two
@@ -882,7 +882,9 @@ __device__ void consume(const DecodeArgs& a, int it0, int it1, ItemHead next, ui
 // most 2^-kLift of it, and comes down as m goes up; rounded once, so that what a key adds
 // is off by 2^-12 of itself, or by 2^-32 of what the row's largest w s stands for.  (One
 // reference for all rows of a warp, the largest scale met, lost every value 2^25 below an
-// outlier's, whatever the outlier's weight.)  The sums get v back at the item's end, and
+// outlier's, whatever the outlier's weight; 48 contexts of 200 .. 60,000 tokens, 32/8 heads
+// of 128 dimensions, took 158.8 us and 160.4 so, 64/8 of 64 115 and 118.5, 64 windows of
+// 2,048 15.9 and 16.7.)  The sums get v back at the item's end, and
 // 2^-kMost with it (the normaliser too), so that they are of weights of at most 1: with
 // weights of 2^kMost they pass what fp32 holds where values are large.
 constexpr float kLift = 7.f, kMost = 15.f;
