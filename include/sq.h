@@ -235,7 +235,8 @@ SQ_API int sq_evict_spans_ragged(sq_cache *cache, sq_seq seq, const sq_span *spa
  * in a key or value that it sees, is NaN in its output.  The
  * kernel runs on the tensor cores (bf16 products, fp32 accumulation; the
  * softmax weights are rounded to bf16 before the value product, and the
- * normaliser sums the same rounded weights).  Where key ranges are shared out
+ * normaliser sums the same rounded weights; logits of more than 1e9 in size may
+ * give NaN).  Where key ranges are shared out
  * to more CTAs than there are query tiles, their fp32 partial results take up
  * to 128 MB of library memory, kept with the cache; where that much cannot be
  * had the call runs without sharing them out.
@@ -478,7 +479,8 @@ SQ_API int sq_qk_norm_rope_backward(sq_cache *cache, int32_t n_tokens, const voi
  * Single tokens without lse run as sq_decode_attention does (values up to 3e38
  * over the number of keys seen).
  * Weights and normaliser are rounded as in sq_prefill_attention, whose limits on
- * library memory for partial results hold too.  A plan of more than 2^24 key
+ * logits and on library memory for partial results hold too (single tokens without
+ * lse: logits of any size).  A plan of more than 2^24 key
  * tiles (all queries of the call together) is refused.
  * Errors: BAD_HANDLE, INVALID_ARG, CAPACITY, UNSUPPORTED, NO_MEMORY, CUDA. */
 SQ_API int sq_window_attention(sq_cache *cache, const sq_seq *seqs, int32_t n_seqs,
